@@ -359,6 +359,98 @@ varrate_status varrate_anchor_residual(const varrate_config* cfg, const void* k,
                                        int32_t stride, int32_t c, const int32_t* idx, void* e_out,
                                        int32_t* dev_status, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Paged cache of tokens that are not coded yet. A serving program stores keys and values here while
+ * a prompt is prefilled and attends over them (varrate_paged_append, varrate_paged_attn), takes
+ * the finished prompt out for varrate_encode, and the newer tokens for the exact tail of the
+ * decode calls (varrate_paged_gather). The library keeps no state about it: pages are handed out by
+ * the caller. Limits: head_dim == 128, 1 <= group <= 8, page_size a power of two in [16, 256],
+ * n_pages * 2 * n_kv_heads * page_size < 2^31 (VARRATE_ERR_UNSUPPORTED otherwise). */
+
+/* The pages. Token u of a sequence is row u mod page_size of the page with the number
+ * page_table[u / page_size]; one page number stands for that page of every layer. */
+typedef struct {
+  void* pool;            /* [n_layers][n_pages][2][n_kv_heads][page_size][d] dtype; 0 is K, 1 is V */
+  int32_t n_layers;
+  int32_t n_pages;
+  int32_t n_kv_heads;    /* G */
+  int32_t page_size;
+  int32_t head_dim;      /* d (must be 128) */
+  int32_t dtype;         /* varrate_dtype */
+} varrate_pages;
+
+/* A batch of sequences with new tokens (device pointers). Sequence s brings n_s = row_start[s + 1] -
+ * row_start[s] >= 0 new tokens in rows row_start[s] .. row_start[s + 1] - 1; kv_len[s] counts its tokens, the
+ * new ones included, so the one in row row_start[s] + i has position kv_len[s] - n_s + i. Rows
+ * before row_start[0] and from row_start[n_seqs] on belong to no sequence (a batch padded to a captured
+ * size): nothing is read from them or written to them. Entries of page_table past a sequence's last
+ * page are not looked at.
+ * A sequence with row_start out of order or outside [0, n_rows], with kv_len[s] outside
+ * [n_s, max_pages * page_size], or with a page number outside [0, n_pages) among those that the call
+ * reads or writes raises VARRATE_ERR_CORRUPT in *dev_status; its results are not to be trusted (rows may
+ * stay unwritten), the other sequences' are, as long as their rows are not claimed twice. */
+typedef struct {
+  const int32_t* row_start;    /* [n_seqs + 1] */
+  const int32_t* kv_len;       /* [n_seqs] */
+  const int32_t* page_table;   /* [n_seqs][max_pages] */
+  int32_t n_seqs;              /* S >= 0 */
+  int32_t max_pages;           /* >= 1 */
+  int32_t n_rows;              /* T >= 0, rows of q, k, v and out */
+} varrate_seqs;
+
+/* Append: new tokens of one layer into their pages, with the norm of every query and key head (where
+ * the model has one) and the rotation to the token's position on the way. Per head x of a query or key:
+ *   y = x / sqrt(mean(x^2) + eps) * w     (only where a weight vector w is given; w as it is, no + 1)
+ *   z_i = y_i cos a_i - y_{i+h} sin a_i,  z_{i+h} = y_{i+h} cos a_i + y_i sin a_i,  i < h = rot_dim / 2,
+ *   z_j = y_j for j >= rot_dim;           a_i = position * freq[i]
+ * in fp32, rounded once to dtype; a_i is exact modulo a turn up to the rounding of freq[i] / 2 pi to double.
+ *   q, k, v   rows [H][d], [G][d], [G][d], one row q_stride, k_stride, v_stride elements after the other
+ *             (parts of one joint projection, say): each stride at least the row's length and a multiple
+ *             of 16 bytes. q may be NULL (keys and values only; q_out is not looked at).
+ *   q_norm    [d] dtype, or NULL: no norm of the queries;  k_norm the same for the keys
+ *   eps       >= 0, finite
+ *   freq      [rot_dim / 2] double; rot_dim a multiple of 16 in [0, d] (0: no rotation, freq may be NULL)
+ *   q_out     [T][H][d]: rotated queries. It may be q itself where q_stride == H * d; any other overlap
+ *             of an output with an input is not allowed.
+ * V goes to its page unchanged. Two tokens may not have the same place in the pages (pages that two
+ * sequences share are read, not written). One kernel, no workspace. */
+varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
+                                    int32_t group, const void* q, int64_t q_stride, const void* k,
+                                    int64_t k_stride, const void* v, int64_t v_stride,
+                                    const void* q_norm, const void* k_norm, double eps,
+                                    const double* freq, int32_t rot_dim, void* q_out,
+                                    int32_t* dev_status, void* stream);
+
+/* Attention of the new tokens over the pages of one layer (which hold the new tokens' keys and values
+ * already): per query head h of KV head g = h / group, for the token at position p of its sequence,
+ *   o = sum_{u <= p} alpha_u v_u,   alpha = softmax_{u <= p}(<q, k_u> / sqrt(d)).
+ * One new token of a sequence is a decode step, many are a chunk of its prompt; a batch may hold both.
+ * What stands in the pages at positions after p (unused slots, later tokens: NaN and infinities as
+ * well) has no part in the result. A row whose scores are all -infinity gives zeros.
+ *   q     [T][H][d];  out [T][H][d], not overlapping q
+ *   ws    at least varrate_paged_attn_ws_bytes(pages, seqs, group) bytes (which looks at no device
+ *         memory: n_seqs, n_rows and max_pages only), zero-filled before the first call that uses it.
+ *         It starts with a counter that a call leaves at zero again, the rest is written before it is read:
+ *         one workspace serves any number of calls that are ordered on one stream. Calls that
+ *         overlap on one workspace race; a call that finds the counter used raises VARRATE_ERR_CORRUPT.
+ * bf16: products on the tensor cores, weights rounded to bf16 before they meet the values, everything else in fp32.
+ * fp32: fp32 throughout. */
+size_t varrate_paged_attn_ws_bytes(const varrate_pages* pages, const varrate_seqs* seqs, int32_t group);
+varrate_status varrate_paged_attn(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
+                                  int32_t group, const void* q, void* out, int32_t* dev_status, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* Gather: tokens first[s] .. first[s] + n - 1 of every sequence out of the pages, for the layers
+ * layer .. layer + n_layers - 1, in the layout of varrate_encode's keys and values (all layers) and of the
+ * exact tail of the decode calls (one layer): k_out, v_out [S][n_layers][G][n][d] dtype. Uses kv_len and
+ * page_table of `seqs`, not row_start (which may be NULL).
+ *   first     [S] int32, or NULL: 0 for every sequence
+ * A sequence with first[s] < 0 or first[s] + n > kv_len[s] raises VARRATE_ERR_CORRUPT and its part of
+ * the outputs stays as it was; k_out or v_out may be NULL (not wanted). One kernel, no workspace. */
+varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
+                                    int32_t n_layers, const int32_t* first, int32_t n, void* k_out,
+                                    void* v_out, int32_t* dev_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "paged.h"
 
 using vr::Shape;
 
@@ -365,6 +366,94 @@ varrate_status varrate_anchor_residual(const varrate_config* cfg, const void* k,
   if (!vr::anchor_residual_supported(s, stride, c)) return VARRATE_ERR_UNSUPPORTED;
   if (vr::launch_anchor_residual(s, k, v, stride, c, idx, e_out, dev_status, num_sms(), (cudaStream_t)stream) < 0)
     return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+static varrate_status paged_check(const varrate_pages* pages, const varrate_seqs* seqs) {
+  if (pages == nullptr || seqs == nullptr) return VARRATE_ERR_ARG;
+  if (!valid_dtype(pages->dtype) || pages->n_layers < 1 || pages->n_pages < 1 || pages->n_kv_heads < 1 ||
+      pages->page_size < 1 || seqs->n_seqs < 0 || seqs->max_pages < 1 || seqs->n_rows < 0)
+    return VARRATE_ERR_ARG;
+  if (pages->head_dim != vr::kHeadDim) return VARRATE_ERR_UNSUPPORTED;
+  const int32_t ps = pages->page_size;
+  if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0) return VARRATE_ERR_UNSUPPORTED;
+  if ((double)pages->n_pages * 2.0 * pages->n_kv_heads * ps > (double)INT32_MAX) return VARRATE_ERR_UNSUPPORTED;
+  return VARRATE_OK;
+}
+
+static vr::Paged make_paged(const varrate_pages* pages, const varrate_seqs* seqs) {
+  vr::Paged p;
+  p.pool = static_cast<unsigned char*>(pages->pool);
+  p.layer_rows = (int64_t)pages->n_pages * 2 * pages->n_kv_heads * pages->page_size;
+  p.n_pages = pages->n_pages; p.G = pages->n_kv_heads; p.dtype = pages->dtype;
+  p.page_log2 = 0;
+  while ((1 << p.page_log2) < pages->page_size) ++p.page_log2;
+  p.row_start = seqs->row_start; p.kv_len = seqs->kv_len; p.table = seqs->page_table;
+  p.S = seqs->n_seqs; p.max_pages = seqs->max_pages; p.T = seqs->n_rows;
+  return p;
+}
+
+// A batch's device pointers (looked at only where there are sequences).
+static varrate_status paged_pointers(const varrate_pages* pages, const varrate_seqs* seqs, bool rows) {
+  if (!pages->pool || !seqs->kv_len || !seqs->page_table || (rows && !seqs->row_start)) return VARRATE_ERR_ARG;
+  return aligned16({pages->pool, seqs->kv_len, seqs->page_table, seqs->row_start}) ? VARRATE_OK : VARRATE_ERR_ARG;
+}
+
+varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
+                                    int32_t group, const void* q, int64_t q_stride, const void* k,
+                                    int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm,
+                                    const void* k_norm, double eps, const double* freq, int32_t rot_dim,
+                                    void* q_out, int32_t* dev_status, void* stream) {
+  varrate_status st = paged_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers || group < 1 || !(eps >= 0.0) || !isfinite(eps)) return VARRATE_ERR_ARG;
+  if (group > 8) return VARRATE_ERR_UNSUPPORTED;
+  if (rot_dim < 0 || rot_dim > vr::kHeadDim || (rot_dim % 16) != 0) return VARRATE_ERR_ARG;
+  if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
+  if ((st = paged_pointers(pages, seqs, true)) != VARRATE_OK) return st;
+  if (!k || !v || (q && !q_out) || (rot_dim > 0 && !freq)) return VARRATE_ERR_ARG;
+  if (!aligned16({q, k, v, q_norm, k_norm, freq, q_out, dev_status})) return VARRATE_ERR_ARG;
+  const int64_t vec = pages->dtype == VARRATE_F32 ? 4 : 8, kd = (int64_t)pages->n_kv_heads * vr::kHeadDim;
+  if (k_stride < kd || k_stride % vec != 0 || v_stride < kd || v_stride % vec != 0) return VARRATE_ERR_ARG;
+  if (q && (q_stride < kd * group || q_stride % vec != 0 || (q == q_out && q_stride != kd * group))) return VARRATE_ERR_ARG;
+  vr::launch_paged_append(make_paged(pages, seqs), layer, group, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm,
+                          (float)eps, freq, rot_dim, q_out, dev_status, num_sms(), (cudaStream_t)stream);
+  return launched();
+}
+
+size_t varrate_paged_attn_ws_bytes(const varrate_pages* pages, const varrate_seqs* seqs, int32_t group) {
+  if (paged_check(pages, seqs) != VARRATE_OK || group < 1 || group > 8) return 0;
+  return vr::paged_attn_ws_bytes(make_paged(pages, seqs), group, num_sms());
+}
+
+varrate_status varrate_paged_attn(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer, int32_t group,
+                                  const void* q, void* out, int32_t* dev_status, void* ws, size_t ws_bytes_,
+                                  void* stream) {
+  varrate_status st = paged_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers || group < 1) return VARRATE_ERR_ARG;
+  if (group > 8) return VARRATE_ERR_UNSUPPORTED;
+  if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
+  if ((st = paged_pointers(pages, seqs, true)) != VARRATE_OK) return st;
+  if (!q || !out || q == out || !aligned16({q, out, dev_status, ws})) return VARRATE_ERR_ARG;
+  const vr::Paged p = make_paged(pages, seqs);
+  const int sms = num_sms();
+  if (ws_bytes_ < vr::paged_attn_ws_bytes(p, group, sms) || ws == nullptr) return VARRATE_ERR_WORKSPACE;
+  if (vr::launch_paged_attn(p, layer, group, q, out, dev_status, ws, sms, (cudaStream_t)stream) < 0) return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
+                                    int32_t n_layers, const int32_t* first, int32_t n, void* k_out, void* v_out,
+                                    int32_t* dev_status, void* stream) {
+  varrate_status st = paged_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || n_layers < 1 || n_layers > pages->n_layers - layer || n < 0) return VARRATE_ERR_ARG;
+  if (seqs->n_seqs == 0 || n == 0 || (!k_out && !v_out)) return VARRATE_OK;
+  if ((st = paged_pointers(pages, seqs, false)) != VARRATE_OK) return st;
+  if (!aligned16({first, k_out, v_out, dev_status})) return VARRATE_ERR_ARG;
+  vr::launch_paged_gather(make_paged(pages, seqs), layer, n_layers, first, n, k_out, v_out, dev_status, num_sms(),
+                          (cudaStream_t)stream);
   return launched();
 }
 

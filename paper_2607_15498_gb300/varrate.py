@@ -61,6 +61,17 @@ class varrate_qpacked(ctypes.Structure):
                 ("bits", ctypes.c_int32), ("qcap_bytes", ctypes.c_int64)]
 
 
+class varrate_pages(ctypes.Structure):
+    _fields_ = [("pool", _c_void_p), ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class varrate_seqs(ctypes.Structure):
+    _fields_ = [("row_start", _c_void_p), ("kv_len", _c_void_p), ("page_table", _c_void_p),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32)]
+
+
 _lib = None
 
 _SIGS = {
@@ -112,6 +123,19 @@ _SIGS = {
     "varrate_anchor_residual": (ctypes.c_int32, [ctypes.POINTER(varrate_config), _c_void_p, _c_void_p,
                                                  ctypes.c_int32, ctypes.c_int32, _c_void_p, _c_void_p,
                                                  _c_void_p, _c_void_p]),
+    "varrate_paged_append": (ctypes.c_int32, [ctypes.POINTER(varrate_pages), ctypes.POINTER(varrate_seqs),
+                                              ctypes.c_int32, ctypes.c_int32, _c_void_p, ctypes.c_int64,
+                                              _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64,
+                                              _c_void_p, _c_void_p, ctypes.c_double, _c_void_p,
+                                              ctypes.c_int32, _c_void_p, _c_void_p, _c_void_p]),
+    "varrate_paged_attn_ws_bytes": (ctypes.c_size_t, [ctypes.POINTER(varrate_pages),
+                                                      ctypes.POINTER(varrate_seqs), ctypes.c_int32]),
+    "varrate_paged_attn": (ctypes.c_int32, [ctypes.POINTER(varrate_pages), ctypes.POINTER(varrate_seqs),
+                                            ctypes.c_int32, ctypes.c_int32, _c_void_p, _c_void_p,
+                                            _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+    "varrate_paged_gather": (ctypes.c_int32, [ctypes.POINTER(varrate_pages), ctypes.POINTER(varrate_seqs),
+                                              ctypes.c_int32, ctypes.c_int32, _c_void_p, ctypes.c_int32,
+                                              _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
 }
 
 EXPORTED = tuple(_SIGS)
@@ -279,6 +303,55 @@ def varrate_decode_attn_q(cfg, qpacked, basis_k, basis_v, q, layer, tail_k, tail
                                        _stream(stream))
 
 
+def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
+                         dev_status, stream=None) -> int:
+    """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
+    ERR_ARG where a tensor is not of the cache's type, shape or device."""
+    G, d, T = pages.c.n_kv_heads, pages.c.head_dim, seqs.c.n_rows
+    H = G if q is None else q.shape[1]
+    if H % G or not (pages.takes(k, (T, G, d), True) and pages.takes(v, (T, G, d), True)):
+        return ERR_ARG
+    if q is not None and not (pages.takes(q, (T, H, d), True) and pages.takes(q_out, (T, H, d))):
+        return ERR_ARG
+    for w in (q_norm, k_norm):
+        if w is not None and not pages.takes(w, (d,)):
+            return ERR_ARG
+    if rot_dim and not (freq.dtype == torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
+                        and freq.device == pages.pool.device):
+        return ERR_ARG
+    return lib().varrate_paged_append(pages.ref, seqs.ref, layer, H // G, _ptr(q), 0 if q is None else q.stride(0),
+                                      k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _ptr(q_norm),
+                                      _ptr(k_norm), eps, _ptr(freq), rot_dim, _ptr(q_out), _ptr(dev_status),
+                                      _stream(stream))
+
+
+def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
+    return lib().varrate_paged_attn_ws_bytes(pages.ref, seqs.ref, group)
+
+
+def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream=None) -> int:
+    """q and out [T][H][d], dense. ERR_ARG where a tensor is not of the cache's type, shape or device."""
+    shape = (seqs.c.n_rows, pages.c.n_kv_heads * group, pages.c.head_dim)
+    if not (pages.takes(q, shape) and pages.takes(out, shape)):
+        return ERR_ARG
+    return lib().varrate_paged_attn(pages.ref, seqs.ref, layer, group, q.data_ptr(), out.data_ptr(), _ptr(dev_status),
+                                    _ptr(ws), _nbytes(ws), _stream(stream))
+
+
+def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, dev_status, stream=None) -> int:
+    """k_out, v_out [S][n_layers][G][n][d], dense, or None. ERR_ARG where a tensor is not of the cache's
+    type, shape or device."""
+    shape = (seqs.c.n_seqs, n_layers, pages.c.n_kv_heads, n, pages.c.head_dim)
+    for t in (k_out, v_out):
+        if t is not None and not pages.takes(t, shape):
+            return ERR_ARG
+    if first is not None and not (first.dtype == torch.int32 and first.is_contiguous()
+                                  and first.shape == (seqs.c.n_seqs,) and first.device == pages.pool.device):
+        return ERR_ARG
+    return lib().varrate_paged_gather(pages.ref, seqs.ref, layer, n_layers, _ptr(first), n, _ptr(k_out), _ptr(v_out),
+                                      _ptr(dev_status), _stream(stream))
+
+
 # ------------------------------------------------------------- device-memory plumbing
 
 def make_config(n_layers, n_kv_heads, group, n_ctx, batch=1, budget_frac=0.2, r_min=16, window=32,
@@ -346,6 +419,66 @@ class QPackedCache:
         qbase = torch.zeros((B, L, d + 2), dtype=torch.int64, device=device)
         c = varrate_qpacked(data.data_ptr(), qbase.data_ptr(), source.bucket_count.data_ptr(), bits, cap)
         return QPackedCache(data, qbase, source, bits, cap, c)
+
+
+@dataclass
+class PagedCache:
+    """The pages of a paged cache: pool [n_layers][n_pages][2][G][page_size][d] (0 is K, 1 is V) plus the
+    C struct pointing at it. Which page belongs to which sequence is the caller's."""
+    pool: torch.Tensor
+    c: varrate_pages
+
+    @staticmethod
+    def of(pool: torch.Tensor) -> "PagedCache":
+        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in (
+                torch.bfloat16, torch.float32):
+            raise VarrateError(ERR_ARG, "PagedCache.of")
+        L, P, _, G, ps, d = pool.shape
+        c = varrate_pages(pool.data_ptr(), L, P, G, ps, d, BF16 if pool.dtype == torch.bfloat16 else F32)
+        return PagedCache(pool, c)
+
+    @staticmethod
+    def allocate(n_layers, n_pages, n_kv_heads, page_size, dtype=BF16, device="cuda") -> "PagedCache":
+        return PagedCache.of(torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size, 128), device=device,
+                                         dtype=torch.bfloat16 if dtype == BF16 else torch.float32))
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.c)
+
+    def takes(self, t: torch.Tensor, shape, rows_apart=False) -> bool:
+        """Whether t has this shape and the cache's type and device and is dense (or its rows are)."""
+        if t.shape != shape or t.dtype != self.pool.dtype or t.device != self.pool.device:
+            return False
+        return t.is_contiguous() or (rows_apart and t.stride()[1:] == (shape[2], 1))
+
+
+@dataclass
+class SeqBatch:
+    """A batch of sequences with new tokens: row_start [S + 1], kv_len [S] and page_table [S][max_pages],
+    int32 on the GPU, n_rows rows of queries, keys and values; plus the C struct. The tensors may be
+    refilled in place from step to step (the calls read them on the stream)."""
+    row_start: torch.Tensor
+    kv_len: torch.Tensor
+    page_table: torch.Tensor
+    c: varrate_seqs
+
+    @staticmethod
+    def of(row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int) -> "SeqBatch":
+        S = kv_len.numel()
+        for t, shape in ((row_start, (S + 1,)), (kv_len, (S,)), (page_table, (S, page_table.shape[-1]))):
+            if t is not None and (t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous()):
+                raise VarrateError(ERR_ARG, "SeqBatch.of")
+        c = varrate_seqs(_ptr(row_start), _ptr(kv_len), _ptr(page_table), S, page_table.shape[-1], n_rows)
+        return SeqBatch(row_start, kv_len, page_table, c)
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.c)
+
+
+def paged_attn_workspace(pages: PagedCache, seqs: SeqBatch, group: int) -> torch.Tensor:
+    """Device scratch of varrate_paged_attn for batches of this size, zero-filled as its first call wants it."""
+    n = varrate_paged_attn_ws_bytes(pages, seqs, group)
+    return torch.zeros(max(n, 256), dtype=torch.uint8, device=pages.pool.device)
 
 
 def workspace(cfg: varrate_config, which_call: int, device="cuda") -> torch.Tensor:
