@@ -36,6 +36,20 @@ __device__ __forceinline__ bool seq_range(const Paged& p, int s, SeqRange& r) {
   return a >= 0 && b >= a && b <= p.T && len >= r.n && len <= ((int64_t)p.max_pages << p.page_log2);
 }
 
+// Entries of a[0 .. n) that are <= t, a sorted; one warp. (Unsorted: some number in [0, n].)
+__device__ __forceinline__ int count_le(const int32_t* a, int n, int t, int lane) {
+  int lo = 0;
+  while (n > 32) {
+    const int step = (n + 31) >> 5, i = (lane + 1) * step - 1;   // last entry of the lane's part
+    const bool le = i < n && __ldg(a + lo + i) <= t;
+    const int k = __popc(__ballot_sync(0xffffffffu, le));
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  const bool le = lane < n && __ldg(a + lo + lane) <= t;
+  return lo + __popc(__ballot_sync(0xffffffffu, le));
+}
+
 int launch_paged_append(const Paged& p, int layer, int group, const void* q, int64_t q_stride, const void* k,
                         int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm,
                         float eps, const double* freq, int rot, void* q_out, int32_t* dev_status, int num_sms,
@@ -43,6 +57,9 @@ int launch_paged_append(const Paged& p, int layer, int group, const void* q, int
 int launch_paged_gather(const Paged& p, int layer, int n_layers, const int32_t* first, int n, void* k_out, void* v_out,
                         int32_t* dev_status, int num_sms, cudaStream_t st);
 size_t paged_attn_ws_bytes(const Paged& p, int group, int num_sms);
+size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms);
+int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
+                         int num_sms, cudaStream_t st);
 int launch_paged_attn(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
                       int num_sms, cudaStream_t st);
 

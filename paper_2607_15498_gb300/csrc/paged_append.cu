@@ -18,20 +18,6 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;                 // heads in flight per half-warp
 constexpr int kStep = 2 * kUnroll;         // heads per pass of a warp
 
-// Entries of a[0 .. n) that are <= t, a sorted; one warp. (Unsorted: some number in [0, n].)
-__device__ __forceinline__ int count_le(const int32_t* a, int n, int t, int lane) {
-  int lo = 0;
-  while (n > 32) {
-    const int step = (n + 31) >> 5, i = (lane + 1) * step - 1;   // last entry of the lane's part
-    const bool le = i < n && __ldg(a + lo + i) <= t;
-    const int k = __popc(__ballot_sync(0xffffffffu, le));
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
-  const bool le = lane < n && __ldg(a + lo + lane) <= t;
-  return lo + __popc(__ballot_sync(0xffffffffu, le));
-}
-
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
   const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
   x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;

@@ -194,13 +194,14 @@ int launch(const Paged& p, int layer, int group, const void* q, void* out, int32
 
 }  // namespace
 
-size_t paged_attn_ws_bytes(const Paged&, int, int) { return 256; }
+size_t paged_attn_ws_bytes(const Paged& p, int group, int num_sms) {
+  return p.dtype == VARRATE_F32 ? 256 : paged_attn_tc_ws_bytes(p, group, num_sms);
+}
 
 int launch_paged_attn(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
                       int num_sms, cudaStream_t st) {
-  (void)ws; (void)num_sms;
   return p.dtype == VARRATE_F32 ? launch<float>(p, layer, group, q, out, dev_status, st)
-                                : launch<__nv_bfloat16>(p, layer, group, q, out, dev_status, st);
+                                : launch_paged_attn_tc(p, layer, group, q, out, dev_status, ws, num_sms, st);
 }
 
 }  // namespace vr

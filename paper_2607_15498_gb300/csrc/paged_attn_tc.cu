@@ -1,0 +1,869 @@
+// Paged cache, attention of new tokens, bf16: tcgen05 products fed by TMA out of the pages.
+//
+// The rows of a query tile are (token, query head) pairs of one KV head, at most 128: tq = 128 / group tokens. Per tile
+// of 128 keys
+//   scores  S[row][key] = Q[row][.] K[key][.]     M = 128, N = 128, K = 128, both operands in shared memory
+//   values  O[row][.]  += P[row][key] V[key][.]   M = 128, N = 128, K = keys, P (bf16) from TMEM over the scores
+// A page holds a head's keys (and values) as rows of 256 bytes, so a tile is one TMA box of 64 columns per page and half
+// row; 128-byte swizzle; keys are the K-major B operand, values the MN-major one.
+// Two softmax warpgroups (thread = row) work in turn, so that the products of one run under the softmax of the other:
+//   a block of more than tq new tokens gives each warpgroup a query tile of its own, and both use every key tile;
+//   a smaller one (a decode step) gives both the same query tile and every second key tile, merged at the end.
+// The reference maximum of a row moves only when a score exceeds it by kSlack (log2 units); then its accumulator is
+// rescaled in TMEM.
+//
+// Work is cut into units (sequence, run of key tiles, block, KV head), taken in that order by one CTA per SM: the first by
+// its number, the others from a counter in the workspace. The length K of a run is the same for the whole batch:
+// every CTA weighs the same 32 values of it (make_plan). Blocks of one sequence are taken longest first, and blocks that read
+// the same keys stand next to each other, so that they meet in L2. Units of a block that is cut write maximum, sum and
+// unnormalised values; paged_attn_combine_kernel merges them.
+//
+// Values at positions that a row does not see have weight 0 in P, and 0 times an infinity is no number: in the tiles
+// where that can happen two warps zero every value past the block's last token, and values that are not finite and
+// that only a part of the block's tokens sees are zeroed too, remembered (kSpecial) and added to the rows that see them.
+//
+// Warps: 0-3, 4-7 softmax; 8 TMA producer; 9 issues the products; 10-11 values. Every wait is bounded; one that gives up
+// raises VARRATE_ERR_TIMEOUT, its CTA takes no further unit and ends after its copies and products in flight have.
+#include <math.h>
+#include <stddef.h>
+
+#include <atomic>
+
+#include <cudaTypedefs.h>
+
+#include "common.cuh"
+#include "decode_common.cuh"
+#include "paged.h"
+
+namespace vr {
+
+bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 10;
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
+constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
+constexpr float kSlack = 8.f;
+constexpr int kCand = 32;
+constexpr int kOverhead = 2;                                // of a unit, in key tiles (start, output)
+constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
+constexpr int kNone = 0x7fff;                               // kSpecial: no such value
+
+// Workspace: header, first partial of every sequence [S + 1], then the partials: values [rows][d], (max, sum) [rows].
+struct Header {
+  unsigned int taken;       // units taken from the counter; zero between calls
+  unsigned int gave_up;     // a CTA that timed out: not all units were taken
+  int run;                  // key tiles of a run
+  int units;
+};
+constexpr size_t kHeaderBytes = 256;
+
+struct Unit {
+  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from;
+  // g: KV head; row0: row of the block's first token; pos0: its position; key tiles t0 .. t1 - 1, of which the first
+  // warpgroup's query tile sees those before e0; both: one query tile for both; slot: partial, or -1; values_from: first
+  // tile whose values have to be looked at
+};
+
+struct Ctl {
+  uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, drain;
+  Unit unit[2];
+  union {
+    struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
+    struct { unsigned long long weight; int items, most, units[kCand], split[kCand], chunk[kCand]; } plan;
+  };
+  int16_t special[2][3][kHeadDim];                          // first position (from the first looked-at tile) of +inf, -inf, NaN
+  int any_special[2];
+  int err;
+  uint32_t tmem;
+};
+constexpr size_t kSmemBytes = 2 * kTileBytes + kRing * kTileBytes + sizeof(Ctl);
+static_assert(kSmemBytes <= 232448, "shared memory of a block");
+
+// Key tiles that hold the first `keys` keys (keys < 2^32).
+__device__ __forceinline__ int tiles_of(uint32_t keys) { return (int)((keys + (kKeys - 1)) / kKeys); }
+
+// Blocks, key tiles and cuts of one sequence.
+struct SeqPlan {
+  int row0, n, len, nb, tiles, cuts, chunk;
+};
+__device__ __forceinline__ SeqPlan seq_plan(const SeqRange& r, int bq, int run) {
+  SeqPlan q;
+  q.row0 = r.row0; q.n = r.n; q.len = r.len;
+  q.nb = (r.n + bq - 1) / bq;
+  q.tiles = tiles_of(r.len);
+  q.cuts = q.nb ? (q.tiles + run - 1) / run : 0;
+  q.chunk = q.nb ? (q.tiles + q.cuts - 1) / q.cuts : 0;
+  return q;
+}
+
+__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, kWaitTries));
+}
+
+// The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
+// j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
+// mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
+// not hold are left out. Same for every CTA. All threads.
+__device__ void make_plan(const Paged& p, Ctl& c, int bq, int C, int max_parts, int& run, int& units) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) { c.plan.weight = 0; c.plan.items = 0; c.plan.most = 0; }
+  if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
+  __syncthreads();
+  unsigned long long w = 0;
+  int most = 0;
+  for (int s = tid; s < p.S; s += kThreads) {
+    SeqRange r;
+    if (!seq_range(p, s, r) || r.n == 0) continue;
+    const int nb = (r.n + bq - 1) / bq;
+    const int last = tiles_of(r.len), first = tiles_of(r.len - r.n + min(bq, r.n));
+    w += (unsigned long long)p.G * nb * (unsigned long long)(first + last);
+    most = max(most, last);
+  }
+  if (w) { atomicAdd(&c.plan.weight, w); atomicMax(&c.plan.most, most); }
+  __syncthreads();
+  const unsigned long long W = (c.plan.weight + 1) / 2;
+  const int longest = c.plan.most;
+  // this lane's candidate
+  int cand = longest + 1;
+  if (lane < kCand - 1) {
+    const unsigned long long j = 1 + (lane >> 2), i = lane & 3, div = 16ull * j * (unsigned long long)C;
+    const unsigned long long k = (W * (16 + i) + div - 1) / div;
+    cand = k < 1 ? 1 : k < (unsigned long long)cand ? (int)k : cand;
+  }
+  int u = 0, split = 0, chunk = 0;
+  for (int s = warp; s < p.S; s += kThreads / 32) {
+    SeqRange r;
+    if (!seq_range(p, s, r)) continue;
+    const SeqPlan q = seq_plan(r, bq, cand);
+    const int n = p.G * q.nb * q.cuts;
+    u += n;
+    split += q.cuts > 1 ? n : 0;
+    chunk = max(chunk, q.chunk);
+  }
+  if (u) { atomicAdd(&c.plan.units[lane], u); atomicAdd(&c.plan.split[lane], split); atomicMax(&c.plan.chunk[lane], chunk); }
+  __syncthreads();
+  u = c.plan.units[lane];
+  float est = INFINITY;
+  if (c.plan.split[lane] <= max_parts) {
+    const float total = (float)W + (float)kOverhead * u, mean = total / fmaxf((float)u, 1.f);
+    est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, c.plan.chunk[lane] + kOverhead - mean));
+  }
+  int best = lane;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float e = __shfl_xor_sync(0xffffffffu, est, o);
+    const int b = __shfl_xor_sync(0xffffffffu, best, o);
+    if (e < est || (e == est && b < best)) { est = e; best = b; }
+  }
+  run = __shfl_sync(0xffffffffu, cand, best);
+  units = __shfl_sync(0xffffffffu, u, best);
+  __syncthreads();
+}
+
+// Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
+struct Walk {
+  int s0 = 0, before = 0, parts_before = 0;     // first sequence held; units and partials before it
+  int incl, parts_incl, total, parts;           // scans over the sequences held, and their sums
+  SeqPlan q;
+
+  __device__ __forceinline__ void load(const Paged& p, int bq, int run, int lane) {
+    SeqRange r;
+    r.n = 0; r.len = 0; r.row0 = 0;
+    if (s0 + lane < p.S && !seq_range(p, s0 + lane, r)) r.n = 0;
+    if (r.n == 0) r.len = 0;
+    q = seq_plan(r, bq, run);
+    incl = p.G * q.nb * q.cuts;
+    parts_incl = q.cuts > 1 ? incl : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o), z = __shfl_up_sync(0xffffffffu, parts_incl, o);
+      if (lane >= o) { incl += y; parts_incl += z; }
+    }
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    parts = __shfl_sync(0xffffffffu, parts_incl, 31);
+  }
+  __device__ __forceinline__ void next(const Paged& p, int bq, int run, int lane) {
+    before += total;
+    parts_before += parts;
+    s0 += 32;
+    load(p, bq, run, lane);
+  }
+  // unit u (at or after the last one asked for, below the number of units): its sequence and what it is
+  __device__ __forceinline__ int find(const Paged& p, int bq, int tq, int run, int u, int lane, Unit& x) {
+    while (u >= before + total && s0 < p.S) next(p, bq, run, lane);
+    const int l = __ffs(__ballot_sync(0xffffffffu, u < before + incl)) - 1;
+    if (l < 0) { x.valid = 0; x.t0 = 0; x.t1 = 0; return 0; }
+    SeqPlan f;
+    f.row0 = __shfl_sync(0xffffffffu, q.row0, l); f.n = __shfl_sync(0xffffffffu, q.n, l);
+    f.len = __shfl_sync(0xffffffffu, q.len, l); f.nb = __shfl_sync(0xffffffffu, q.nb, l);
+    f.cuts = __shfl_sync(0xffffffffu, q.cuts, l); f.chunk = __shfl_sync(0xffffffffu, q.chunk, l);
+    const int units = p.G * f.nb * f.cuts;
+    const int at = u - before - (__shfl_sync(0xffffffffu, incl, l) - units);
+    x.g = at % p.G;
+    const int b = f.nb - 1 - at / p.G % f.nb, j = at / p.G / f.nb;
+    x.ntok = min(bq, f.n - b * bq);
+    x.row0 = f.row0 + b * bq;
+    x.pos0 = f.len - f.n + b * bq;
+    const int end = x.pos0 + x.ntok, tiles = tiles_of(end);
+    x.t0 = j * f.chunk;
+    x.t1 = min(x.t0 + f.chunk, tiles);
+    x.both = x.ntok <= tq;
+    x.e0 = max(x.t0, min(x.t1, tiles_of((uint32_t)x.pos0 + tq)));
+    x.slot = f.cuts > 1 ? parts_before + __shfl_sync(0xffffffffu, parts_incl, l) - units + at : -1;
+    x.values_from = max(x.t0, x.ntok > 1 ? (x.pos0 + 1) / kKeys : end / kKeys);
+    x.valid = 1;
+    return s0 + l;
+  }
+};
+
+// D[tmem] (+)= A[tmem] * B[smem]^T (A: bf16 pairs, row = lane, 8 columns per K = 16), issued by the lane with `issue` set.
+__device__ __forceinline__ void tc_mma_bf16_ts_if(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc,
+                                                  uint32_t accumulate, uint32_t issue) {
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n tcgen05.wait::ld.sync.aligned;\n"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n"
+      ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
+__device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+
+// 32 fp32 columns of a row's values: to bf16 in the output, or as they are to a partial.
+__device__ __forceinline__ void put_out(__nv_bfloat16* dst, const float (&v)[32], float f) {
+#pragma unroll
+  for (int k = 0; k < 32; k += 8)
+    *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16(v[k] * f, v[k + 1] * f), pack_bf16(v[k + 2] * f, v[k + 3] * f),
+                                                    pack_bf16(v[k + 4] * f, v[k + 5] * f), pack_bf16(v[k + 6] * f, v[k + 7] * f));
+}
+__device__ __forceinline__ void put_part(float* dst, const float (&v)[32]) {
+#pragma unroll
+  for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __nv_bfloat16* __restrict__ q,
+                     __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
+                     int* __restrict__ first_part, float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Ctl& c = *reinterpret_cast<Ctl*>(smem + (2 + kRing) * kTileBytes);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tq = kRows / grp, bq = 2 * tq, H = p.G * grp, C = gridDim.x;
+  const uint32_t q_addr = smem_addr(smem), ring = q_addr + 2 * kTileBytes;
+
+  pdl_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&c.full[i], 1); mbar_init(&c.empty[i], 1); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
+      mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 2);
+    }
+    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.drain, 1);
+    c.err = 0;
+    fence_mbar_init();
+  }
+  pdl_wait();
+  int run, units;
+  make_plan(p, c, bq, C, max_parts, run, units);
+  if (blockIdx.x == 0) {
+    for (int s = tid; s < p.S; s += kThreads) {
+      SeqRange r;
+      if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+    }
+    if (tid == 0) { header->run = run; header->units = units; }
+    if (warp == kValues) {
+      Walk w;
+      w.load(p, bq, run, lane);
+      for (;;) {
+        const int mine = w.q.cuts > 1 ? p.G * w.q.nb * w.q.cuts : 0;
+        if (w.s0 + lane < p.S) first_part[w.s0 + lane] = w.parts_before + w.parts_incl - mine;
+        if (w.s0 + 32 >= p.S) break;
+        w.next(p, bq, run, lane);
+      }
+      if (lane == 0) first_part[p.S] = w.parts_before + w.parts;
+    }
+  }
+  if ((int)blockIdx.x >= units) return;
+  if (warp == kIssuer) tmem_alloc(&c.tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = c.tmem;
+
+  if (warp == kProducer) {
+    // ------------------------------------------------------------------ units, and their keys and values
+    Walk w;
+    w.load(p, bq, run, lane);
+    const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box
+    const int per_tile = kKeys / page_keys;
+    int u = blockIdx.x;
+    uint32_t n = 0;                                               // ring tiles so far
+    bool ok = true;
+    for (uint32_t un = 0; ok; ++un) {
+      Unit x;
+      int s = 0;
+      x.valid = 0;
+      while (u < units) {
+        s = w.find(p, bq, tq, run, u, lane, x);
+        if (x.t0 < x.t1) break;                                   // else: the block ends before this run
+        x.valid = 0;
+        if (lane == 0) u = C + (int)atomicAdd(&header->taken, 1u);
+        u = __shfl_sync(0xffffffffu, u, 0);
+      }
+      ok = wait_all(&c.u_empty[un & 1], ((un >> 1) & 1) ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        c.unit[un & 1] = x;
+        mbar_arrive(&c.u_full[un & 1]);
+      }
+      if (!x.valid) break;
+      int next = 0;
+      if (lane == 0) next = C + (int)atomicAdd(&header->taken, 1u);
+      const int32_t* table = p.table + (int64_t)s * p.max_pages;
+      const int end = x.pos0 + x.ntok;
+      const int piece = lane >> 1, half = lane & 1;               // this lane's box of a tile
+      auto page_at = [&](int t) {
+        const int key = t * kKeys + piece * page_keys;
+        return piece < per_tile && key < end ? __ldg(table + (key >> p.page_log2)) : 0;
+      };
+      int page = page_at(x.t0);
+      for (int t = x.t0; t < x.t1 && ok; ++t) {
+        const int key = t * kKeys + piece * page_keys;
+        const bool mine = piece < per_tile && key < end;
+        const int boxes = min(per_tile, (end - t * kKeys + page_keys - 1) / page_keys);
+        int pg = page;
+        if (mine && (pg < 0 || pg >= p.n_pages)) {
+          raise_status(dev_status, VARRATE_ERR_CORRUPT);
+          pg = 0;
+        }
+        const int row = (int)page_row(p, pg, 0, x.g, key & ((1 << p.page_log2) - 1));
+        const int row_v = row + (p.G << p.page_log2);
+        if (t + 1 < x.t1) page = page_at(t + 1);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          const uint32_t slot = n % kRing;
+          ok = ok && wait_all(&c.empty[slot], ((n / kRing) & 1) ^ 1);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(&c.full[slot], (uint32_t)boxes * page_keys * 256);
+          __syncwarp();
+          if (mine)
+            tma_load_2d(ring + slot * kTileBytes + half * (kKeys * 128) + piece * page_keys * 128, &tmap, half * 64,
+                        kv ? row_v : row, &c.full[slot]);
+          if (kv && t >= x.values_from && lane == 0) mbar_arrive(&c.look[slot]);
+        }
+      }
+      u = __shfl_sync(0xffffffffu, next, 0);
+    }
+    if (!ok) {
+      c.err = 1;
+      const uint32_t oldest = n > kRing ? n - kRing : 0;          // no copy is in flight when the block ends
+      for (uint32_t i = oldest; i < n; ++i) wait_all(&c.full[i % kRing], (i / kRing) & 1);
+    }
+  } else if (warp == kIssuer) {
+    // ------------------------------------------------------------------ products: one lane issues
+    const uint32_t leader = lane == 0;
+    const uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
+    uint32_t n0 = 0, looked = 0;                                  // ring tiles of earlier units; parities by slot
+    uint32_t par_p = 0;                                           // parities of the warpgroups' weights
+    bool ok = true;
+    for (uint32_t un = 0; ok; ++un) {
+      ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
+      if (!ok) break;
+      const int valid = c.unit[un & 1].valid, t0 = c.unit[un & 1].t0, nt = c.unit[un & 1].t1 - t0;
+      const int n_first = c.unit[un & 1].e0 - t0, both = c.unit[un & 1].both, from = c.unit[un & 1].values_from - t0;
+      __syncwarp();
+      if (!valid) break;
+      if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
+      ok = wait_all(&c.q_full[0], un & 1) && wait_all(&c.q_full[1], un & 1);
+      if (!ok) break;
+      const int steps = both ? nt : 2 * nt;
+      uint32_t begun = 0;                                         // accumulators that hold products of this unit
+      auto tile_of = [&](int k) { return both ? k : k >> 1; };
+      auto skipped = [&](int k) { return !both && !(k & 1) && (k >> 1) >= n_first; };
+      auto scores = [&](int k) {
+        const int i = tile_of(k), e = k & 1;
+        const uint32_t n = n0 + 2 * i, slot = n % kRing;
+        if (!wait_all(&c.full[slot], (n / kRing) & 1)) return false;
+        tc_fence_after();
+        const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + slot * kTileBytes);
+#pragma unroll
+        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+          const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
+          tc_mma_bf16_if(tmem + 128 * e, a + o, b + o, idesc_s, ks != 0, leader);
+        }
+        if (leader) {
+          tc_commit(&c.s_full[e]);
+          if (both || e) tc_commit(&c.empty[slot]);
+        }
+        __syncwarp();
+        return true;
+      };
+      for (int k = 0; k < 2 && k < steps; ++k)
+        if (!skipped(k)) ok = ok && scores(k);
+      for (int k = 0; k < steps && ok; ++k) {
+        const int i = tile_of(k), e = k & 1;
+        if (!skipped(k)) {
+          const uint32_t n = n0 + 2 * i + 1, slot = n % kRing;
+          ok = wait_all(&c.full[slot], (n / kRing) & 1);
+          if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
+          ok = ok && wait_all(&c.p_full[e], (par_p >> e) & 1);
+          if (!ok) break;
+          par_p ^= 1u << e;
+          tc_fence_after();
+          const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
+#pragma unroll
+          for (int ks = 0; ks < kKeys / 16; ++ks)
+            tc_mma_bf16_ts_if(tmem + 256 + 128 * e, tmem + 128 * e + 8 * ks, b + ks * (2048 / 16), idesc_o,
+                              ((begun >> e) & 1) | (ks != 0), leader);
+          begun |= 1u << e;
+          if (leader) {
+            tc_commit(&c.o_full[e]);
+            if (both || e) tc_commit(&c.empty[slot]);
+          }
+          __syncwarp();
+          if (i >= from && (both || e)) looked ^= 1u << slot;
+        }
+        if (k + 2 < steps && !skipped(k + 2)) ok = scores(k + 2);
+      }
+      n0 += 2 * (uint32_t)nt;
+    }
+    if (!ok && lane == 0) {                                       // the products in flight end before TMEM is freed
+      c.err = 1;
+      tc_commit(&c.drain);
+      mbar_wait_bounded(&c.drain, 0, kWaitTries);
+    }
+    __syncwarp();
+  } else if (warp >= kValues) {
+    // ------------------------------------------------------------------ values that no row, or not every row, sees
+    const int panel = warp - kValues;                             // columns 64 panel + 2 lane, + 1
+    uint32_t n0 = 0, par = 0;
+    bool ok = true;
+    for (uint32_t un = 0; ok; ++un) {
+      ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
+      if (!ok) break;
+      const Unit x = c.unit[un & 1];
+      __syncwarp();
+      if (!x.valid) break;
+      int16_t first[2][3];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) first[i / 3][i % 3] = kNone;
+      bool any = false;
+      const int end = x.pos0 + x.ntok;
+      for (int t = x.values_from; t < x.t1; ++t) {
+        const uint32_t n = n0 + 2 * (t - x.t0) + 1, slot = n % kRing;
+        ok = wait_all(&c.look[slot], (par >> slot) & 1) && wait_all(&c.full[slot], (n / kRing) & 1);
+        if (!ok) break;
+        par ^= 1u << slot;
+        const int lo = min(kKeys, max(0, x.pos0 + 1 - t * kKeys)), hi = min(kKeys, end - t * kKeys);
+        unsigned char* v = smem + (2 + slot) * kTileBytes + panel * (kKeys * 128);
+        auto word = [&](int key) { return reinterpret_cast<uint32_t*>(v + key * 128 + (((lane >> 2) ^ (key & 7)) << 4) + (lane & 3) * 4); };
+#pragma unroll 4
+        for (int key = lo; key < hi; ++key) {
+          const uint32_t a = *word(key);
+          if ((a & 0x7f80u) == 0x7f80u || (a & 0x7f800000u) == 0x7f800000u) {   // infinity or NaN
+            any = true;
+            uint32_t b = a;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t h = (a >> (16 * i)) & 0xffffu;
+              if ((h & 0x7f80u) != 0x7f80u) continue;
+              b &= i ? 0x0000ffffu : 0xffff0000u;
+              const int16_t at = (int16_t)(t * kKeys + key - x.values_from * kKeys);
+              int16_t& f = first[i][(h & 0x7f) ? 2 : h >> 15];
+              f = min(f, at);
+            }
+            *word(key) = b;
+          }
+        }
+        for (int key = hi; key < kKeys; ++key) *word(key) = 0;
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.looked[slot]);
+      }
+      if (!ok) break;
+      any = __any_sync(0xffffffffu, any);
+      if (any) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) c.special[un & 1][i % 3][64 * panel + 2 * lane + i / 3] = first[i / 3][i % 3];
+      }
+      if (lane == 0) {
+        reinterpret_cast<int16_t*>(&c.any_special[un & 1])[panel] = any;
+        mbar_arrive(&c.u_looked[un & 1]);
+        mbar_arrive(&c.u_empty[un & 1]);
+      }
+      n0 += 2 * (uint32_t)(x.t1 - x.t0);
+    }
+    if (!ok) c.err = 1;
+  } else {
+    // ------------------------------------------------------------------ softmax: one row per thread
+    const int e = warp >> 2, r = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
+    uint32_t n_s = 0, n_o = 0, n_both = 0;                        // score tiles, value products, merged units so far
+    bool ok = true;
+    float m = -INFINITY, l = 0.f;                                 // reference maximum, sum
+    bool begun = false;                                           // the accumulator holds something of this unit
+    // Pass nu: the queries of unit nu, the output of unit nu - 1 (the first scores of nu run under it), the tiles of nu.
+    for (uint32_t nu = 0;; ++nu) {
+      ok = wait_all(&c.u_full[nu & 1], (nu >> 1) & 1);
+      if (!ok) break;
+      const bool valid = c.unit[nu & 1].valid;
+      if (valid) {
+        const Unit& x = c.unit[nu & 1];
+        const int tok0 = x.both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;   // at least one token
+        const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (r & 15) * 8;
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int row = (8 * b + i) * 8 + (r >> 4);
+            if (row < rows) v[i] = __ldg(reinterpret_cast<const uint4*>(src + ((int64_t)(row / grp) * H + row % grp) * kHeadDim));
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int row = (8 * b + i) * 8 + (r >> 4);
+            if (row < rows) *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(row, r & 15, kRows)) = v[i];
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.q_full[e]);
+      }
+      if (nu > 0) {
+        const uint32_t un = nu - 1;
+        const Unit& x = c.unit[un & 1];
+        const int tok0 = x.both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
+        const bool live = (warp & 3) * 32 < rows, mine = r < rows;
+        const int tok = tok0 + min(r, rows - 1) / grp, sees = x.pos0 + tok + 1;
+        ok = wait_all(&c.u_looked[un & 1], (un >> 1) & 1);
+        if (ok && begun) ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        float w0 = 1.f, w1 = 0.f;                                   // weights of the two warpgroups' values
+        bool second = false;
+        if (x.both) {
+          if (e) {
+            c.o1.m[r] = m;
+            c.o1.l[r] = l;
+            if (r == 0) c.o1.begun = begun;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.o1_full);
+            ok = wait_all(&c.o1_empty, n_both & 1);
+            if (!ok) break;
+          } else {
+            ok = wait_all(&c.o1_full, n_both & 1);
+            if (!ok) break;
+            tc_fence_after();
+            second = c.o1.begun;
+            if (second) {
+              const float m1 = c.o1.m[r], l1 = c.o1.l[r];
+              const float mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.f : mm;
+              w0 = fast_exp2((m - ref) * scale_log2);
+              w1 = fast_exp2((m1 - ref) * scale_log2);
+              l = l * w0 + l1 * w1;
+              m = mm;
+            }
+          }
+          ++n_both;
+        }
+        if (live && !(x.both && e)) {
+          const int special = c.any_special[un & 1];
+          const float f = l == 0.f ? 0.f : 1.f / l;
+          const int64_t row = x.slot < 0 ? ((int64_t)(x.row0 + tok) * H + x.g * grp + r % grp) : (int64_t)x.slot * part_rows + tok0 * grp + r;
+#pragma unroll 1
+          for (int cb = 0; cb < kHeadDim; cb += 32) {
+            float v[32];
+            __syncwarp();
+            if (begun) tmem_ld32(to + cb, v);
+            if (second) {
+              float v1[32];
+              tmem_ld32(tmem + 384 + lanes + cb, v1);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = fmaf(v[k], w0, v1[k] * w1);
+            }
+            if (special) {
+              const int at = sees - x.values_from * kKeys;          // positions below it are seen
+              for (int k = 0; k < 32; ++k) {
+                const int col = cb + k;
+                if (!((special >> (col < 64 ? 0 : 16)) & 1)) continue;
+                float y = 0.f;
+                if (c.special[un & 1][0][col] < at) y += INFINITY;
+                if (c.special[un & 1][1][col] < at) y -= INFINITY;
+                if (c.special[un & 1][2][col] < at) y = NAN;
+                add_at(v, k, y);
+              }
+            }
+            if (mine) {
+              if (x.slot < 0) put_out(out + row * kHeadDim + cb, v, f);
+              else if (begun) put_part(part + row * kHeadDim + cb, v);
+            }
+          }
+          if (mine && x.slot >= 0 && begun) {
+            float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
+            *reinterpret_cast<float2*>(ml + row * 2) = make_float2(m, l);
+          }
+          tc_fence_before();
+        }
+        if (x.both && !e) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c.o1_empty);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
+      }
+      if (!valid) break;
+      const Unit& x = c.unit[nu & 1];
+      const int both = x.both, tok0 = both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
+      const bool live = (warp & 3) * 32 < rows, mine = r < rows;
+      const int sees = x.pos0 + tok0 + min(r, rows - 1) / grp + 1;   // keys that this row sees
+      const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
+      float mc = 0.f;                                             // reference maximum times the scale
+      m = -INFINITY;
+      l = 0.f;
+      begun = false;
+      for (int t = x.t0 + (both ? e : 0); t < last; t += step) {
+        ok = wait_all(&c.s_full[e], n_s & 1);
+        if (!ok) break;
+        ++n_s;
+        tc_fence_after();
+        if (live) {
+          const int lim = sees - t * kKeys;
+          const bool cut = __any_sync(0xffffffffu, lim < kKeys);
+          auto load = [&](int cb, float (&s)[32]) {
+            tmem_ld32(ts + cb, s);
+            if (cut) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
+            }
+          };
+          auto most = [&](const float (&s)[32], float mx) {
+            float a = fmaxf(mx, s[0]), b = s[1];
+#pragma unroll
+            for (int k = 2; k < 32; k += 4) {
+              a = fmaxf(fmaxf(a, s[k]), s[k + 1]);
+              if (k + 2 < 32) b = fmaxf(fmaxf(b, s[k + 2]), s[k + 3]);
+            }
+            return fmaxf(a, b);
+          };
+          float pk[64], mx = -INFINITY;
+          float2 sum[2];
+          // Weights from the reference as it is, and the maximum on the way; if that shows that the reference has to
+          // move (or there is none yet), the maximum first, then the weights again.
+          bool known = begun;
+          for (;;) {
+            if (!known) {
+              if (!begun) {
+#pragma unroll 1
+                for (int cb = 0; cb < kKeys; cb += 32) {
+                  float s[32];
+                  load(cb, s);
+                  mx = most(s, mx);
+                }
+              }
+              float f = 1.f;
+              if (mine && mx > m && (mx - m) * scale_log2 > kSlack) {   // (m = -inf: any score)
+                f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
+                m = mx;
+                mc = mx * scale_log2;
+                l *= f;
+              }
+              if (begun) {                                        // the accumulator's last product has ended
+                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int cb = 0; cb < kHeadDim; cb += 8) {
+                  float v[8];
+                  tmem_ld8(to + cb, v);
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) v[k] *= f;
+                  tmem_st8(to + cb, v);
+                }
+              }
+            }
+            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            mx = -INFINITY;
+#pragma unroll
+            for (int cb = 0; cb < kKeys; cb += 32) {
+              float s[32];
+              load(cb, s);
+              mx = most(s, mx);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
+                const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
+                sum[k & 1] = add2(sum[k & 1], w);
+                pk[cb / 2 + k] = __uint_as_float(pack_bf16(w.x, w.y));
+              }
+            }
+            if (!known || !__any_sync(0xffffffffu, mine && mx > m && (mx - m) * scale_log2 > kSlack)) break;
+            known = false;
+          }
+          if (!ok) break;
+          tmem_st32(ts, *reinterpret_cast<float(*)[32]>(pk));
+          tmem_st32(ts + 32, *reinterpret_cast<float(*)[32]>(pk + 32));
+          const float2 total = add2(sum[0], sum[1]);
+          l += total.x + total.y;
+          tmem_wait_st();
+        }
+        begun = true;
+        ++n_o;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.p_full[e]);
+      }
+      if (!ok) break;
+    }
+    if (!ok) c.err = 1;
+  }
+  __syncthreads();
+  if (warp == kIssuer) tmem_dealloc(tmem, 512);
+  if (tid == 0 && c.err) {
+    raise_status(dev_status, VARRATE_ERR_TIMEOUT);
+    atomicExch(&header->gave_up, 1u);
+  }
+}
+
+// Merges the partials of blocks that were cut, a warp per (row, query head), and leaves the header as the next call wants
+// it. A run j of a block counts for a row only where the row's query tile reaches it.
+__global__ void __launch_bounds__(256)
+paged_attn_combine_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, Header* header,
+                          const int* __restrict__ first_part, const float* __restrict__ part, int part_rows, int max_parts,
+                          int grp, float scale_log2) {
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp, tq = kRows / grp, bq = 2 * tq;
+  const int run = header->run;
+  if (__ldcg(first_part + p.S) > 0) {
+    const float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + warp; i < (int64_t)p.T * H; i += (int64_t)gridDim.x * 8) {
+      const int t = (int)(i / H), h = (int)(i % H), g = h / grp;
+      const int s = count_le(p.row_start, p.S + 1, t, lane) - 1;
+      SeqRange r;
+      if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
+      const SeqPlan f = seq_plan(r, bq, run);
+      if (f.cuts < 2) continue;
+      const int tok = t - f.row0, b = tok / bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
+      // the row's query tile: its last token's position decides which runs it reaches
+      const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
+      const int tiles = tiles_of(f.len - f.n + b * bq + last);
+      const int runs = (tiles + f.chunk - 1) / f.chunk;
+      const int64_t row = (int64_t)(in * grp + h % grp);
+      auto part_row = [&](int j) {
+        return (int64_t)(__ldcg(first_part + s) + (j * f.nb + f.nb - 1 - b) * p.G + g) * part_rows + row;
+      };
+      float m = -INFINITY;
+      for (int j = lane; j < runs; j += 32) m = fmaxf(m, __ldcg(ml + part_row(j) * 2));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int j = 0; j < runs; ++j) {
+        const int64_t pr = part_row(j);
+        const float2 x = __ldcg(reinterpret_cast<const float2*>(ml) + pr);
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(part + pr * kHeadDim) + lane);
+        const float w = fast_exp2((x.x - ref) * scale_log2);
+        l = fmaf(x.y, w, l);
+        v.x = fmaf(y.x, w, v.x); v.y = fmaf(y.y, w, v.y); v.z = fmaf(y.z, w, v.z); v.w = fmaf(y.w, w, v.w);
+      }
+      const float f1 = l == 0.f ? 0.f : 1.f / l;
+      *reinterpret_cast<uint2*>(out + i * kHeadDim + lane * 4) = make_uint2(pack_bf16(v.x * f1, v.y * f1), pack_bf16(v.z * f1, v.w * f1));
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (header->taken != (unsigned)header->units && !header->gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+    header->taken = 0;
+    header->gave_up = 0;
+  }
+}
+
+int rows_of_part(const Paged& p, int group) {
+  const int64_t rows = (int64_t)p.T * group, most = 2 * (kRows / group) * group;
+  return (int)(rows < most ? rows : most);
+}
+size_t first_part_bytes(const Paged& p) { return (((size_t)p.S + 1) * sizeof(int) + 255) & ~size_t(255); }
+
+}  // namespace
+
+size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms) {
+  const size_t rows = (size_t)kPartsPerSm * num_sms * rows_of_part(p, group);
+  return kHeaderBytes + first_part_bytes(p) + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
+}
+
+int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
+                         int num_sms, cudaStream_t st) {
+  static std::atomic<int> smem_set[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || smem_set[dev].load(std::memory_order_acquire) == 0) {
+    if (cudaFuncSetAttribute(paged_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes) != cudaSuccess)
+      return -1;
+    if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
+  }
+  CUtensorMap tmap;
+  const int ps = 1 << p.page_log2;
+  if (!make_tmap_rows_bf16(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim * 2, (uint64_t)p.layer_rows, ps < kKeys ? ps : kKeys))
+    return -1;
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  Header* header = reinterpret_cast<Header*>(w);
+  int* first_part = reinterpret_cast<int*>(w + kHeaderBytes);
+  float* part = reinterpret_cast<float*>(w + kHeaderBytes + first_part_bytes(p));
+  const int max_parts = kPartsPerSm * num_sms, rows = rows_of_part(p, group);
+  const float scale_log2 = kLog2e / sqrtf((float)kHeadDim);
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(num_sms);
+  lc.blockDim = dim3(kThreads);
+  lc.dynamicSmemBytes = kSmemBytes;
+  lc.stream = st;
+  lc.attrs = pdl;
+  lc.numAttrs = 1;
+  if (cudaLaunchKernelEx(&lc, paged_attn_tc_kernel, tmap, p, (const __nv_bfloat16*)q, (__nv_bfloat16*)out, dev_status, header,
+                         first_part, part, rows, max_parts, group, scale_log2) != cudaSuccess)
+    return -1;
+  const int64_t warps = (int64_t)p.T * p.G * group;
+  lc.gridDim = dim3((unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4));
+  lc.blockDim = dim3(256);
+  lc.dynamicSmemBytes = 0;
+  if (cudaLaunchKernelEx(&lc, paged_attn_combine_kernel, p, (__nv_bfloat16*)out, dev_status, header, (const int*)first_part,
+                         (const float*)part, rows, max_parts, group, scale_log2) != cudaSuccess)
+    return -1;
+  return 2;
+}
+
+}  // namespace vr
