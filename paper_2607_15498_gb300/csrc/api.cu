@@ -416,8 +416,9 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
   const int64_t vec = pages->dtype == VARRATE_F32 ? 4 : 8, kd = (int64_t)pages->n_kv_heads * vr::kHeadDim;
   if (k_stride < kd || k_stride % vec != 0 || v_stride < kd || v_stride % vec != 0) return VARRATE_ERR_ARG;
   if (q && (q_stride < kd * group || q_stride % vec != 0 || (q == q_out && q_stride != kd * group))) return VARRATE_ERR_ARG;
-  vr::launch_paged_append(make_paged(pages, seqs), layer, group, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm,
-                          (float)eps, freq, rot_dim, q_out, dev_status, num_sms(), (cudaStream_t)stream);
+  if (vr::launch_paged_append(make_paged(pages, seqs), layer, group, q, q_stride, k, k_stride, v, v_stride, q_norm,
+                              k_norm, (float)eps, freq, rot_dim, q_out, dev_status, num_sms(), (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
   return launched();
 }
 
@@ -452,8 +453,9 @@ varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_se
   if (seqs->n_seqs == 0 || n == 0 || (!k_out && !v_out)) return VARRATE_OK;
   if ((st = paged_pointers(pages, seqs, false)) != VARRATE_OK) return st;
   if (!aligned16({first, k_out, v_out, dev_status})) return VARRATE_ERR_ARG;
-  vr::launch_paged_gather(make_paged(pages, seqs), layer, n_layers, first, n, k_out, v_out, dev_status, num_sms(),
-                          (cudaStream_t)stream);
+  if (vr::launch_paged_gather(make_paged(pages, seqs), layer, n_layers, first, n, k_out, v_out, dev_status, num_sms(),
+                              (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
   return launched();
 }
 

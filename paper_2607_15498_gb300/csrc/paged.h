@@ -50,6 +50,22 @@ __device__ __forceinline__ int count_le(const int32_t* a, int n, int t, int lane
   return lo + __popc(__ballot_sync(0xffffffffu, le));
 }
 
+// Launch with programmatic stream serialization: the kernel waits (pdl_wait) before it touches memory.
+template <typename... P, typename... A>
+inline bool launch_pdl(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  lc.attrs = pdl;
+  lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, kernel, P(args)...) == cudaSuccess;
+}
+
 int launch_paged_append(const Paged& p, int layer, int group, const void* q, int64_t q_stride, const void* k,
                         int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm,
                         float eps, const double* freq, int rot, void* q_out, int32_t* dev_status, int num_sms,

@@ -843,25 +843,13 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
   float* part = reinterpret_cast<float*>(w + kHeaderBytes + first_part_bytes(p));
   const int max_parts = kPartsPerSm * num_sms, rows = rows_of_part(p, group);
   const float scale_log2 = kLog2e / sqrtf((float)kHeadDim);
-  cudaLaunchAttribute pdl[1];
-  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  pdl[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(num_sms);
-  lc.blockDim = dim3(kThreads);
-  lc.dynamicSmemBytes = kSmemBytes;
-  lc.stream = st;
-  lc.attrs = pdl;
-  lc.numAttrs = 1;
-  if (cudaLaunchKernelEx(&lc, paged_attn_tc_kernel, tmap, p, (const __nv_bfloat16*)q, (__nv_bfloat16*)out, dev_status, header,
-                         first_part, part, rows, max_parts, group, scale_log2) != cudaSuccess)
+  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, p, (const __nv_bfloat16*)q,
+                  (__nv_bfloat16*)out, dev_status, header, first_part, part, rows, max_parts, group, scale_log2))
     return -1;
   const int64_t warps = (int64_t)p.T * p.G * group;
-  lc.gridDim = dim3((unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4));
-  lc.blockDim = dim3(256);
-  lc.dynamicSmemBytes = 0;
-  if (cudaLaunchKernelEx(&lc, paged_attn_combine_kernel, p, (__nv_bfloat16*)out, dev_status, header, (const int*)first_part,
-                         (const float*)part, rows, max_parts, group, scale_log2) != cudaSuccess)
+  const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
+  if (!launch_pdl(paged_attn_combine_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, header,
+                  (const int*)first_part, (const float*)part, rows, max_parts, group, scale_log2))
     return -1;
   return 2;
 }

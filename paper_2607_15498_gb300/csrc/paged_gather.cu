@@ -20,6 +20,8 @@ paged_gather_kernel(Paged p, int layer0, int n_layers, const int32_t* __restrict
   constexpr int kRows = kThreads / kPer, kTokens = kRows * kUnroll;
   const int tid = threadIdx.x, piece = tid % kPer, row = tid / kPer;
   const uint4* pool = reinterpret_cast<const uint4*>(p.pool);
+  pdl_trigger();
+  pdl_wait();
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     // (sequence, layer, K or V, head, chunk), the chunk fastest
     int64_t x = u / chunks;
@@ -67,13 +69,9 @@ int launch_paged_gather(const Paged& p, int layer, int n_layers, const int32_t* 
   const int chunks = (n + tokens - 1) / tokens;
   const int64_t units = (int64_t)p.S * n_layers * 2 * p.G * chunks;
   const int grid = (int)(units < (int64_t)num_sms * 8 ? units : (int64_t)num_sms * 8);
-  if (p.dtype == VARRATE_F32)
-    paged_gather_kernel<512><<<grid, kThreads, 0, st>>>(p, layer, n_layers, first, n, (uint4*)k_out, (uint4*)v_out,
-                                                        dev_status, units, chunks);
-  else
-    paged_gather_kernel<256><<<grid, kThreads, 0, st>>>(p, layer, n_layers, first, n, (uint4*)k_out, (uint4*)v_out,
-                                                        dev_status, units, chunks);
-  return 1;
+  return launch_pdl(p.dtype == VARRATE_F32 ? paged_gather_kernel<512> : paged_gather_kernel<256>, dim3(grid), kThreads, 0, st,
+                    p, layer, n_layers, first, n, (uint4*)k_out, (uint4*)v_out, dev_status, units, chunks)
+             ? 1 : -1;
 }
 
 }  // namespace vr
