@@ -104,7 +104,9 @@ __device__ __forceinline__ SeqPlan seq_plan(const SeqRange& r, int bq, int run) 
 }
 
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, kWaitTries));
+  for (uint32_t i = 0; i < kWaitTries; ++i)
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return false;
 }
 
 // The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
@@ -223,13 +225,17 @@ struct Walk {
   }
 };
 
-// D[tmem] (+)= A[tmem] * B[smem]^T (A: bf16 pairs, row = lane, 8 columns per K = 16), issued by the lane with `issue` set.
-__device__ __forceinline__ void tc_mma_bf16_ts_if(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc,
-                                                  uint32_t accumulate, uint32_t issue) {
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+// D[tmem] (+)= A[tmem] * B[smem]^T (A: bf16 pairs, row = lane, 8 columns per K = 16), issued by one thread.
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(issue) : "memory");
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
@@ -381,77 +387,86 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       for (uint32_t i = oldest; i < n; ++i) wait_all(&c.full[i % kRing], (i / kRing) & 1);
     }
   } else if (warp == kIssuer) {
-    // ------------------------------------------------------------------ products: one lane issues
-    const uint32_t leader = lane == 0;
-    const uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
-    uint32_t n0 = 0, looked = 0;                                  // ring tiles of earlier units; parities by slot
-    uint32_t par_p = 0;                                           // parities of the warpgroups' weights
+    // ------------------------------------------------------------------ products
+    // The warp stays together and its values are the same in every lane (broadcast from lane 0 where they come from
+    // memory), so that descriptors stay in uniform registers; one elected lane issues.
+    constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
+    auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
+    Ring start = {0, 0};                                          // first tile of the unit
+    uint32_t looked = 0, par_p = 0;                               // parities by slot, by warpgroup
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
       ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
       if (!ok) break;
-      const int valid = c.unit[un & 1].valid, t0 = c.unit[un & 1].t0, nt = c.unit[un & 1].t1 - t0;
-      const int n_first = c.unit[un & 1].e0 - t0, both = c.unit[un & 1].both, from = c.unit[un & 1].values_from - t0;
-      __syncwarp();
+      const Unit* x = &c.unit[un & 1];
+      const int valid = __shfl_sync(0xffffffffu, x->valid, 0), t0 = __shfl_sync(0xffffffffu, x->t0, 0);
+      const int nt = __shfl_sync(0xffffffffu, x->t1, 0) - t0, n_first = __shfl_sync(0xffffffffu, x->e0, 0) - t0;
+      const int both = __shfl_sync(0xffffffffu, x->both, 0), from = __shfl_sync(0xffffffffu, x->values_from, 0) - t0;
       if (!valid) break;
       if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
       ok = wait_all(&c.q_full[0], un & 1) && wait_all(&c.q_full[1], un & 1);
       if (!ok) break;
+      // Step k: weights times values, then the scores that take their place. Warpgroup k & 1, tile k (one query tile) or k / 2.
       const int steps = both ? nt : 2 * nt;
+      Ring key = start, value = start;
+      if (++value.slot == kRing) { value.slot = 0; value.phase ^= 1; }
       uint32_t begun = 0;                                         // accumulators that hold products of this unit
-      auto tile_of = [&](int k) { return both ? k : k >> 1; };
-      auto skipped = [&](int k) { return !both && !(k & 1) && (k >> 1) >= n_first; };
-      auto scores = [&](int k) {
-        const int i = tile_of(k), e = k & 1;
-        const uint32_t n = n0 + 2 * i, slot = n % kRing;
-        if (!wait_all(&c.full[slot], (n / kRing) & 1)) return false;
-        tc_fence_after();
-        const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + slot * kTileBytes);
+      for (int k = -2; k < steps && ok; ++k) {
+        const int e = k & 1;
+        if (k >= 0) {
+          const int i = both ? k : k >> 1;
+          if (both || e || i < n_first) {
+            ok = wait_all(&c.full[value.slot], value.phase);
+            if (ok && i >= from) ok = wait_all(&c.looked[value.slot], (looked >> value.slot) & 1);
+            ok = ok && wait_all(&c.p_full[e], (par_p >> e) & 1);
+            if (!ok) break;
+            par_p ^= 1u << e;
+            tc_fence_after();
+            const uint64_t b = sdesc_sw128_mn(ring + value.slot * kTileBytes, kKeys * 128);
+            const uint32_t accumulate = (begun >> e) & 1;
+            if (elect_one()) {
 #pragma unroll
-        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
-          const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
-          tc_mma_bf16_if(tmem + 128 * e, a + o, b + o, idesc_s, ks != 0, leader);
+              for (int ks = 0; ks < kKeys / 16; ++ks)
+                tc_mma_bf16_ts(tm + 256 + 128 * e, tm + 128 * e + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
+              tc_commit(&c.o_full[e]);
+              if (both || e) tc_commit(&c.empty[value.slot]);
+            }
+            __syncwarp();
+            begun |= 1u << e;
+          }
+          if (both || e) {
+            if (i >= from) looked ^= 1u << value.slot;
+            further(value);
+          }
         }
-        if (leader) {
-          tc_commit(&c.s_full[e]);
-          if (both || e) tc_commit(&c.empty[slot]);
-        }
-        __syncwarp();
-        return true;
-      };
-      for (int k = 0; k < 2 && k < steps; ++k)
-        if (!skipped(k)) ok = ok && scores(k);
-      for (int k = 0; k < steps && ok; ++k) {
-        const int i = tile_of(k), e = k & 1;
-        if (!skipped(k)) {
-          const uint32_t n = n0 + 2 * i + 1, slot = n % kRing;
-          ok = wait_all(&c.full[slot], (n / kRing) & 1);
-          if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
-          ok = ok && wait_all(&c.p_full[e], (par_p >> e) & 1);
+        const int i = both ? k + 2 : (k + 2) >> 1;
+        if (k + 2 < steps && (both || e || i < n_first)) {
+          ok = wait_all(&c.full[key.slot], key.phase);
           if (!ok) break;
-          par_p ^= 1u << e;
           tc_fence_after();
-          const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
+          const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
+          if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < kKeys / 16; ++ks)
-            tc_mma_bf16_ts_if(tmem + 256 + 128 * e, tmem + 128 * e + 8 * ks, b + ks * (2048 / 16), idesc_o,
-                              ((begun >> e) & 1) | (ks != 0), leader);
-          begun |= 1u << e;
-          if (leader) {
-            tc_commit(&c.o_full[e]);
-            if (both || e) tc_commit(&c.empty[slot]);
+            for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+              const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
+              tc_mma_bf16(tm + 128 * e, a + o, b + o, idesc_s, ks != 0);
+            }
+            tc_commit(&c.s_full[e]);
+            if (both || e) tc_commit(&c.empty[key.slot]);
           }
           __syncwarp();
-          if (i >= from && (both || e)) looked ^= 1u << slot;
         }
-        if (k + 2 < steps && !skipped(k + 2)) ok = scores(k + 2);
+        if (both || e) further(key);
       }
-      n0 += 2 * (uint32_t)nt;
+      start = value;                                              // value stands one behind the next unit's first tile
+      if (start.slot == 0) { start.slot = kRing - 1; start.phase ^= 1; } else --start.slot;
     }
-    if (!ok && lane == 0) {                                       // the products in flight end before TMEM is freed
+    if (!ok) {                                                    // the products in flight end before TMEM is freed
       c.err = 1;
-      tc_commit(&c.drain);
-      mbar_wait_bounded(&c.drain, 0, kWaitTries);
+      if (elect_one()) tc_commit(&c.drain);
+      wait_all(&c.drain, 0);
     }
     __syncwarp();
   } else if (warp >= kValues) {
