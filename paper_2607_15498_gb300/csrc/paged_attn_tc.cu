@@ -22,7 +22,8 @@
 // where that can happen two warps zero every value past the block's last token, and values that are not finite and
 // that only a part of the block's tokens sees are zeroed too, remembered (kSpecial) and added to the rows that see them.
 //
-// Warps: 0-3, 4-7 softmax; 8 TMA producer; 9 issues the products; 10-11 values. Every wait is bounded; one that gives up
+// Warps: 0-3, 4-7 softmax; 8 TMA producer; 9, 10 issue the products of one softmax warpgroup each (the tensor core takes
+// few products ahead, so that a single issuing warp's waits would stand in its way); 11 values. Every wait is bounded; one that gives up
 // raises VARRATE_ERR_TIMEOUT, its CTA takes no further unit and ends after its copies and products in flight have.
 #include <math.h>
 #include <stddef.h>
@@ -42,7 +43,7 @@ bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 10;
+constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kRows = 128, kKeys = 128;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
@@ -72,7 +73,7 @@ struct Unit {
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, drain;
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], o1_full, o1_empty;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
@@ -279,13 +280,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
-      mbar_init(&c.full[i], 1); mbar_init(&c.empty[i], 1); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 2);
+      mbar_init(&c.full[i], 1); mbar_init(&c.empty[i], 2); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
-      mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 2);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
-    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.drain, 1);
+    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4);
     c.err = 0;
     fence_mbar_init();
   }
@@ -386,16 +387,18 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const uint32_t oldest = n > kRing ? n - kRing : 0;          // no copy is in flight when the block ends
       for (uint32_t i = oldest; i < n; ++i) wait_all(&c.full[i % kRing], (i / kRing) & 1);
     }
-  } else if (warp == kIssuer) {
-    // ------------------------------------------------------------------ products
+  } else if (warp == kIssuer || warp == kIssuer + 1) {
+    // ------------------------------------------------------------------ products of warpgroup e
     // The warp stays together and its values are the same in every lane (broadcast from lane 0 where they come from
-    // memory), so that descriptors stay in uniform registers; one elected lane issues.
+    // memory), so that descriptors stay in uniform registers; one elected lane issues. Both issuers pass every tile of
+    // the ring in order, whether they use it or not.
+    const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
     constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + 128 * e, to = tm + 256 + 128 * e;
     struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
     auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
-    Ring start = {0, 0};                                          // first tile of the unit
-    uint32_t looked = 0, par_p = 0;                               // parities by slot, by warpgroup
+    Ring key = {0, 0}, value = {1, 0};
+    uint32_t looked = 0, par_p = 0;                               // parities
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
       ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
@@ -406,72 +409,72 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const int both = __shfl_sync(0xffffffffu, x->both, 0), from = __shfl_sync(0xffffffffu, x->values_from, 0) - t0;
       if (!valid) break;
       if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
-      ok = wait_all(&c.q_full[0], un & 1) && wait_all(&c.q_full[1], un & 1);
+      ok = wait_all(&c.q_full[e], un & 1);
       if (!ok) break;
-      // Step k: weights times values, then the scores that take their place. Warpgroup k & 1, tile k (one query tile) or k / 2.
-      const int steps = both ? nt : 2 * nt;
-      Ring key = start, value = start;
-      if (++value.slot == kRing) { value.slot = 0; value.phase ^= 1; }
-      uint32_t begun = 0;                                         // accumulators that hold products of this unit
-      for (int k = -2; k < steps && ok; ++k) {
-        const int e = k & 1;
-        if (k >= 0) {
-          const int i = both ? k : k >> 1;
-          if (both || e || i < n_first) {
-            ok = wait_all(&c.full[value.slot], value.phase);
-            if (ok && i >= from) ok = wait_all(&c.looked[value.slot], (looked >> value.slot) & 1);
-            ok = ok && wait_all(&c.p_full[e], (par_p >> e) & 1);
-            if (!ok) break;
-            par_p ^= 1u << e;
-            tc_fence_after();
-            const uint64_t b = sdesc_sw128_mn(ring + value.slot * kTileBytes, kKeys * 128);
-            const uint32_t accumulate = (begun >> e) & 1;
-            if (elect_one()) {
-#pragma unroll
-              for (int ks = 0; ks < kKeys / 16; ++ks)
-                tc_mma_bf16_ts(tm + 256 + 128 * e, tm + 128 * e + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
-              tc_commit(&c.o_full[e]);
-              if (both || e) tc_commit(&c.empty[value.slot]);
-            }
-            __syncwarp();
-            begun |= 1u << e;
-          }
-          if (both || e) {
-            if (i >= from) looked ^= 1u << value.slot;
-            further(value);
-          }
-        }
-        const int i = both ? k + 2 : (k + 2) >> 1;
-        if (k + 2 < steps && (both || e || i < n_first)) {
-          ok = wait_all(&c.full[key.slot], key.phase);
-          if (!ok) break;
+      auto mine = [&](int i) { return both ? (i & 1) == e : e || i < n_first; };
+      auto scores = [&](int i) {                                  // of tile i, or past it
+        if (!wait_all(&c.full[key.slot], key.phase)) return false;
+        if (mine(i)) {
           tc_fence_after();
           const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
           if (elect_one()) {
 #pragma unroll
             for (int ks = 0; ks < kHeadDim / 16; ++ks) {
               const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
-              tc_mma_bf16(tm + 128 * e, a + o, b + o, idesc_s, ks != 0);
+              tc_mma_bf16(ts, a + o, b + o, idesc_s, ks != 0);
             }
             tc_commit(&c.s_full[e]);
-            if (both || e) tc_commit(&c.empty[key.slot]);
+            tc_commit(&c.empty[key.slot]);
           }
-          __syncwarp();
+        } else if (elect_one()) {
+          mbar_arrive(&c.empty[key.slot]);
         }
-        if (both || e) further(key);
+        __syncwarp();
+        further(key);
+        return true;
+      };
+      // the keys of the first own tile, then of each tile: its values, and the keys of the own tile after it
+      const int step = both ? 2 : 1;
+      int ahead = 0;                                              // tiles whose keys are done
+      while (ok && ahead < nt && ahead < (both ? e : 0) + 1) ok = scores(ahead++);
+      uint32_t accumulate = 0;                                    // the accumulator holds products of this unit
+      for (int i = 0; i < nt && ok; ++i) {
+        ok = wait_all(&c.full[value.slot], value.phase);
+        if (!ok) break;
+        if (mine(i)) {
+          if (i >= from) ok = wait_all(&c.looked[value.slot], (looked >> value.slot) & 1);
+          ok = ok && wait_all(&c.p_full[e], par_p);
+          if (!ok) break;
+          par_p ^= 1;
+          tc_fence_after();
+          const uint64_t b = sdesc_sw128_mn(ring + value.slot * kTileBytes, kKeys * 128);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
+            tc_commit(&c.o_full[e]);
+            tc_commit(&c.empty[value.slot]);
+          }
+          accumulate = 1;
+        } else if (elect_one()) {
+          mbar_arrive(&c.empty[value.slot]);
+        }
+        __syncwarp();
+        if (i >= from) looked ^= 1u << value.slot;
+        further(value);
+        if (mine(i) || i >= n_first)                              // (a first warpgroup past its last tile goes on past the keys)
+          while (ok && ahead < nt && ahead <= i + step) ok = scores(ahead++);
       }
-      start = value;                                              // value stands one behind the next unit's first tile
-      if (start.slot == 0) { start.slot = kRing - 1; start.phase ^= 1; } else --start.slot;
     }
     if (!ok) {                                                    // the products in flight end before TMEM is freed
       c.err = 1;
-      if (elect_one()) tc_commit(&c.drain);
-      wait_all(&c.drain, 0);
+      if (elect_one()) tc_commit(&c.drain[e]);
+      wait_all(&c.drain[e], 0);
     }
     __syncwarp();
-  } else if (warp >= kValues) {
+  } else if (warp == kValues) {
     // ------------------------------------------------------------------ values that no row, or not every row, sees
-    const int panel = warp - kValues;                             // columns 64 panel + 2 lane, + 1
+    const int panel = lane >> 4, col = 4 * (lane & 15);           // this lane's columns: 64 panel + col .. + 3
     uint32_t n0 = 0, par = 0;
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
@@ -480,9 +483,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const Unit x = c.unit[un & 1];
       __syncwarp();
       if (!x.valid) break;
-      int16_t first[2][3];
+      int16_t first[4][3];
 #pragma unroll
-      for (int i = 0; i < 6; ++i) first[i / 3][i % 3] = kNone;
+      for (int i = 0; i < 12; ++i) first[i / 3][i % 3] = kNone;
       bool any = false;
       const int end = x.pos0 + x.ntok;
       for (int t = x.values_from; t < x.t1; ++t) {
@@ -492,26 +495,28 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         par ^= 1u << slot;
         const int lo = min(kKeys, max(0, x.pos0 + 1 - t * kKeys)), hi = min(kKeys, end - t * kKeys);
         unsigned char* v = smem + (2 + slot) * kTileBytes + panel * (kKeys * 128);
-        auto word = [&](int key) { return reinterpret_cast<uint32_t*>(v + key * 128 + (((lane >> 2) ^ (key & 7)) << 4) + (lane & 3) * 4); };
+        auto word = [&](int key) { return reinterpret_cast<uint2*>(v + key * 128 + (((col >> 3) ^ (key & 7)) << 4) + (col & 4) * 2); };
+        auto odd = [](uint32_t a) { return (a & 0x7f80u) == 0x7f80u || (a & 0x7f800000u) == 0x7f800000u; };   // infinity or NaN
 #pragma unroll 4
         for (int key = lo; key < hi; ++key) {
-          const uint32_t a = *word(key);
-          if ((a & 0x7f80u) == 0x7f80u || (a & 0x7f800000u) == 0x7f800000u) {   // infinity or NaN
+          const uint2 a = *word(key);
+          if (odd(a.x) || odd(a.y)) {
             any = true;
-            uint32_t b = a;
+            uint32_t b[2] = {a.x, a.y};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t h = (a >> (16 * i)) & 0xffffu;
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t h = ((i < 2 ? a.x : a.y) >> (16 * (i & 1))) & 0xffffu;
               if ((h & 0x7f80u) != 0x7f80u) continue;
-              b &= i ? 0x0000ffffu : 0xffff0000u;
+              b[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
               const int16_t at = (int16_t)(t * kKeys + key - x.values_from * kKeys);
-              int16_t& f = first[i][(h & 0x7f) ? 2 : h >> 15];
-              f = min(f, at);
+              if (h & 0x7f) first[i][2] = min(first[i][2], at);
+              else if (h >> 15) first[i][1] = min(first[i][1], at);
+              else first[i][0] = min(first[i][0], at);
             }
-            *word(key) = b;
+            *word(key) = make_uint2(b[0], b[1]);
           }
         }
-        for (int key = hi; key < kKeys; ++key) *word(key) = 0;
+        for (int key = hi; key < kKeys; ++key) *word(key) = make_uint2(0, 0);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&c.looked[slot]);
@@ -520,10 +525,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       any = __any_sync(0xffffffffu, any);
       if (any) {
 #pragma unroll
-        for (int i = 0; i < 6; ++i) c.special[un & 1][i % 3][64 * panel + 2 * lane + i / 3] = first[i / 3][i % 3];
+        for (int i = 0; i < 12; ++i) c.special[un & 1][i % 3][64 * panel + col + i / 3] = first[i / 3][i % 3];
       }
+      if (lane == 0) c.any_special[un & 1] = any;
+      __syncwarp();
       if (lane == 0) {
-        reinterpret_cast<int16_t*>(&c.any_special[un & 1])[panel] = any;
         mbar_arrive(&c.u_looked[un & 1]);
         mbar_arrive(&c.u_empty[un & 1]);
       }
@@ -623,8 +629,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               const int at = sees - x.values_from * kKeys;          // positions below it are seen
               for (int k = 0; k < 32; ++k) {
                 const int col = cb + k;
-                if (!((special >> (col < 64 ? 0 : 16)) & 1)) continue;
-                float y = 0.f;
+                  float y = 0.f;
                 if (c.special[un & 1][0][col] < at) y += INFINITY;
                 if (c.special[un & 1][1][col] < at) y -= INFINITY;
                 if (c.special[un & 1][2][col] < at) y = NAN;
