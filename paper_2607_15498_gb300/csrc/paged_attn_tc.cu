@@ -73,7 +73,7 @@ struct Unit {
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], o1_full, o1_empty;
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], p_half[2], turn[2], o1_full, o1_empty;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
@@ -238,6 +238,33 @@ __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem,
       " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// 32 fp32 columns of this warp's 32 TMEM lanes: begun here, there after tmem_ld32_end (which waits for every load begun).
+__device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld32_end(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+      : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+        "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+        "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+        "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+      :: "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      " tcgen05.wait::ld.sync.aligned;\n"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
@@ -284,7 +311,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
-      mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
     mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4);
     c.err = 0;
@@ -398,7 +425,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
     auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
     Ring key = {0, 0}, value = {1, 0};
-    uint32_t looked = 0, par_p = 0;                               // parities
+    uint32_t looked = 0, par_p = 0, turns = e ^ 1;                // parities; the first warpgroup begins
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
       ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
@@ -412,58 +439,86 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       ok = wait_all(&c.q_full[e], un & 1);
       if (!ok) break;
       auto mine = [&](int i) { return both ? (i & 1) == e : e || i < n_first; };
-      auto scores = [&](int i) {                                  // of tile i, or past it
-        if (!wait_all(&c.full[key.slot], key.phase)) return false;
-        if (mine(i)) {
-          tc_fence_after();
-          const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
-          if (elect_one()) {
+      auto scores = [&]() {                                       // issued by the elected lane
+        const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
 #pragma unroll
-            for (int ks = 0; ks < kHeadDim / 16; ++ks) {
-              const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
-              tc_mma_bf16(ts, a + o, b + o, idesc_s, ks != 0);
-            }
-            tc_commit(&c.s_full[e]);
-            tc_commit(&c.empty[key.slot]);
-          }
-        } else if (elect_one()) {
-          mbar_arrive(&c.empty[key.slot]);
+        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+          const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
+          tc_mma_bf16(ts, a + o, b + o, idesc_s, ks != 0);
         }
+        tc_commit(&c.s_full[e]);
+        tc_commit(&c.empty[key.slot]);
+      };
+      auto pass = [&](Ring& x) {                                  // a tile that the other issuer uses alone
+        if (!wait_all(&c.full[x.slot], x.phase)) return false;
+        if (elect_one()) mbar_arrive(&c.empty[x.slot]);
         __syncwarp();
-        further(key);
+        further(x);
         return true;
       };
-      // the keys of the first own tile, then of each tile: its values, and the keys of the own tile after it
+      // The keys of the first own tile; then per own tile, once its weights and the keys of the next one are there (the
+      // products are queued behind one another, a wait between them would hold them up): its values, those keys.
       const int step = both ? 2 : 1;
       int ahead = 0;                                              // tiles whose keys are done
-      while (ok && ahead < nt && ahead < (both ? e : 0) + 1) ok = scores(ahead++);
+      for (; ok && ahead < nt && ahead < step && !mine(ahead); ++ahead) ok = pass(key);
+      if (ok && ahead < nt && mine(ahead)) {
+        ok = wait_all(&c.full[key.slot], key.phase);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) scores();
+        __syncwarp();
+        further(key);
+        ++ahead;
+      }
       uint32_t accumulate = 0;                                    // the accumulator holds products of this unit
       for (int i = 0; i < nt && ok; ++i) {
-        ok = wait_all(&c.full[value.slot], value.phase);
+        for (; ok && ahead < nt && ahead <= i + step && !mine(ahead); ++ahead) ok = pass(key);
         if (!ok) break;
-        if (mine(i)) {
-          if (i >= from) ok = wait_all(&c.looked[value.slot], (looked >> value.slot) & 1);
-          ok = ok && wait_all(&c.p_full[e], par_p);
+        const uint32_t slot = value.slot;
+        if (!mine(i)) {
+          ok = pass(value);
+        } else {
+          const bool more = ahead < nt && ahead <= i + step;      // then ahead is the next own tile
+          ok = wait_all(&c.full[value.slot], value.phase);
+          if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
+          if (ok && more) ok = wait_all(&c.full[key.slot], key.phase);
+          ok = ok && wait_all(&c.p_half[e], par_p) && wait_all(&c.turn[e], turns & 1);
           if (!ok) break;
-          par_p ^= 1;
           tc_fence_after();
           const uint64_t b = sdesc_sw128_mn(ring + value.slot * kTileBytes, kKeys * 128);
           if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < kKeys / 16; ++ks)
+            for (int ks = 0; ks < kKeys / 32; ++ks)
               tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
+          }
+          __syncwarp();
+          ok = wait_all(&c.p_full[e], par_p);
+          if (!ok) break;
+          par_p ^= 1;
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
+              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
             tc_commit(&c.o_full[e]);
             tc_commit(&c.empty[value.slot]);
+            if (more) scores();
+            mbar_arrive(&c.turn[e ^ 1]);
           }
+          __syncwarp();
+          ++turns;
           accumulate = 1;
-        } else if (elect_one()) {
-          mbar_arrive(&c.empty[value.slot]);
+          further(value);
+          if (more) { further(key); ++ahead; }
         }
+        if (i >= from) looked ^= 1u << slot;
+      }
+      // both issuers take as many turns in a unit
+      const int all = both ? (nt + 1) / 2 : nt, own = both ? (nt + 1 - e) / 2 : e ? nt : min(n_first, nt);
+      for (int i = own; i < all && ok; ++i, ++turns) {
+        ok = wait_all(&c.turn[e], turns & 1);
+        if (ok && elect_one()) mbar_arrive(&c.turn[e ^ 1]);
         __syncwarp();
-        if (i >= from) looked ^= 1u << value.slot;
-        further(value);
-        if (mine(i) || i >= n_first)                              // (a first warpgroup past its last tile goes on past the keys)
-          while (ok && ahead < nt && ahead <= i + step) ok = scores(ahead++);
       }
     }
     if (!ok) {                                                    // the products in flight end before TMEM is freed
@@ -672,83 +727,82 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         if (live) {
           const int lim = sees - t * kKeys;
           const bool cut = __any_sync(0xffffffffu, lim < kKeys);
-          auto load = [&](int cb, float (&s)[32]) {
-            tmem_ld32(ts + cb, s);
+          auto hide = [&](int cb, float (&s)[32]) {
             if (cut) {
 #pragma unroll
               for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
             }
           };
-          auto most = [&](const float (&s)[32], float mx) {
-            float a = fmaxf(mx, s[0]), b = s[1];
+          float buf[2][32], mx = -INFINITY;
+          // the maximum; a chunk of 32 columns is on its way while the one before it is looked at
+          tmem_ld32_begin(ts, buf[0]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float (&s)[32] = buf[i & 1];
+            tmem_ld32_end(s);
+            tmem_ld32_begin(ts + (i < 3 ? 32 * (i + 1) : 0), buf[(i + 1) & 1]);
+            hide(32 * i, s);
+            float a = s[0], b = s[1];
 #pragma unroll
             for (int k = 2; k < 32; k += 4) {
               a = fmaxf(fmaxf(a, s[k]), s[k + 1]);
               if (k + 2 < 32) b = fmaxf(fmaxf(b, s[k + 2]), s[k + 3]);
             }
-            return fmaxf(a, b);
-          };
-          float pk[64], mx = -INFINITY;
-          float2 sum[2];
-          // Weights from the reference as it is, and the maximum on the way; if that shows that the reference has to
-          // move (or there is none yet), the maximum first, then the weights again.
-          bool known = begun;
-          for (;;) {
-            if (!known) {
-              if (!begun) {
-#pragma unroll 1
-                for (int cb = 0; cb < kKeys; cb += 32) {
-                  float s[32];
-                  load(cb, s);
-                  mx = most(s, mx);
-                }
-              }
-              float f = 1.f;
-              if (mine && mx > m && (mx - m) * scale_log2 > kSlack) {   // (m = -inf: any score)
-                f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
-                m = mx;
-                mc = mx * scale_log2;
-                l *= f;
-              }
-              if (begun) {                                        // the accumulator's last product has ended
-                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int cb = 0; cb < kHeadDim; cb += 32) {
-                  float v[32];
-                  tmem_ld32(to + cb, v);
-#pragma unroll
-                  for (int k = 0; k < 32; ++k) v[k] *= f;
-                  tmem_st32(to + cb, v);
-                }
-              }
-            }
-            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
-            sum[0] = sum[1] = make_float2(0.f, 0.f);
-            mx = -INFINITY;
-#pragma unroll
-            for (int cb = 0; cb < kKeys; cb += 32) {
-              float s[32];
-              load(cb, s);
-              mx = most(s, mx);
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
-                const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
-                sum[k & 1] = add2(sum[k & 1], w);
-                pk[cb / 2 + k] = __uint_as_float(pack_bf16(w.x, w.y));
-              }
-            }
-            if (!known || !__any_sync(0xffffffffu, mine && mx > m && (mx - m) * scale_log2 > kSlack)) break;
-            known = false;
+            mx = fmaxf(mx, fmaxf(a, b));
           }
-          if (!ok) break;
-          tmem_st32(ts, *reinterpret_cast<float(*)[32]>(pk));
-          tmem_st32(ts + 32, *reinterpret_cast<float(*)[32]>(pk + 32));
+          const bool raise = mine && mx > m && (mx - m) * scale_log2 > kSlack;   // (m = -inf: any score)
+          if (__any_sync(0xffffffffu, raise)) {
+            float f = 1.f;
+            if (raise) {
+              f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
+              m = mx;
+              mc = mx * scale_log2;
+              l *= f;
+            }
+            if (begun) {                                          // the accumulator's last product has ended
+              ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int cb = 0; cb < kHeadDim; cb += 16) {
+                float v[16];
+                tmem_ld16(to + cb, v);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] *= f;
+                tmem_st16(to + cb, reinterpret_cast<const uint32_t(&)[16]>(v));
+              }
+            }
+          }
+          // the weights, over the scores that they were made from; their first half is handed on by itself
+          const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float (&s)[32] = buf[i & 1];
+            tmem_ld32_end(s);
+            if (i < 3) tmem_ld32_begin(ts + 32 * (i + 1), buf[(i + 1) & 1]);
+            hide(32 * i, s);
+            uint32_t pk[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
+              const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
+              sum[k & 1] = add2(sum[k & 1], w);
+              pk[k] = pack_bf16(w.x, w.y);
+            }
+            tmem_st16(ts + 16 * i, pk);
+            if (i == 1) {
+              tmem_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&c.p_half[e]);
+            }
+          }
           const float2 total = add2(sum[0], sum[1]);
           l += total.x + total.y;
           tmem_wait_st();
+        } else if (lane == 0) {
+          mbar_arrive(&c.p_half[e]);
         }
         begun = true;
         ++n_o;
