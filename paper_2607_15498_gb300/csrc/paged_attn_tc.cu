@@ -257,14 +257,6 @@ __device__ __forceinline__ void tmem_ld32_end(float (&v)[32]) {
         "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
       :: "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-      " tcgen05.wait::ld.sync.aligned;\n"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
-        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-      : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
@@ -456,36 +448,36 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         further(x);
         return true;
       };
-      // The keys of the first own tile; then per own tile, once its weights and the keys of the next one are there (the
-      // products are queued behind one another, a wait between them would hold them up): its values, those keys.
-      const int step = both ? 2 : 1;
-      int ahead = 0;                                              // tiles whose keys are done
-      for (; ok && ahead < nt && ahead < step && !mine(ahead); ++ahead) ok = pass(key);
-      if (ok && ahead < nt && mine(ahead)) {
-        ok = wait_all(&c.full[key.slot], key.phase);
-        if (!ok) break;
+      auto next_scores = [&]() {                                  // by themselves, once the keys are there
+        if (!wait_all(&c.full[key.slot], key.phase)) return false;
         tc_fence_after();
         if (elect_one()) scores();
         __syncwarp();
         further(key);
-        ++ahead;
-      }
+        return true;
+      };
+      // The keys of the first own tile; then per own tile its values, and the keys of the next one. Where both warpgroups
+      // use a tile the products are queued behind one another, as a wait between them would hold them up; a decode step
+      // waits for memory, and gives values back before it waits for keys.
+      const int step = both ? 2 : 1;
+      int ahead = 0;                                              // tiles whose keys are done
+      for (; ok && ahead < nt && ahead < step && !mine(ahead); ++ahead) ok = pass(key);
+      if (ok && ahead < nt && ahead < step) { ok = next_scores(); ++ahead; }
       uint32_t accumulate = 0;                                    // the accumulator holds products of this unit
       for (int i = 0; i < nt && ok; ++i) {
-        for (; ok && ahead < nt && ahead <= i + step && !mine(ahead); ++ahead) ok = pass(key);
-        if (!ok) break;
         const uint32_t slot = value.slot;
         if (!mine(i)) {
-          ok = pass(value);
+          if (!both && ahead == i) { ok = pass(key); ++ahead; }
+          ok = ok && pass(value);
         } else {
-          const bool more = ahead < nt && ahead <= i + step;      // then ahead is the next own tile
-          ok = wait_all(&c.full[value.slot], value.phase);
+          const bool queued = !both && ahead < nt && mine(ahead);
+          ok = wait_all(&c.full[slot], value.phase);
           if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
-          if (ok && more) ok = wait_all(&c.full[key.slot], key.phase);
-          ok = ok && wait_all(&c.p_half[e], par_p) && wait_all(&c.turn[e], turns & 1);
+          if (ok && queued) ok = wait_all(&c.full[key.slot], key.phase);
+          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_half[e], par_p);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t b = sdesc_sw128_mn(ring + value.slot * kTileBytes, kKeys * 128);
+          const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
           if (elect_one()) {
 #pragma unroll
             for (int ks = 0; ks < kKeys / 32; ++ks)
@@ -501,15 +493,19 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
             for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
               tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
             tc_commit(&c.o_full[e]);
-            tc_commit(&c.empty[value.slot]);
-            if (more) scores();
+            tc_commit(&c.empty[slot]);
+            if (queued) scores();
             mbar_arrive(&c.turn[e ^ 1]);
           }
           __syncwarp();
-          ++turns;
           accumulate = 1;
+          ++turns;
           further(value);
-          if (more) { further(key); ++ahead; }
+          if (queued) { further(key); ++ahead; }
+          if (both) {
+            for (; ok && ahead < nt && ahead < i + step; ++ahead) ok = pass(key);
+            if (ok && ahead < nt) { ok = next_scores(); ++ahead; }
+          }
         }
         if (i >= from) looked ^= 1u << slot;
       }
@@ -733,15 +729,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
             }
           };
-          float buf[2][32], mx = -INFINITY;
-          // the maximum; a chunk of 32 columns is on its way while the one before it is looked at
-          tmem_ld32_begin(ts, buf[0]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float (&s)[32] = buf[i & 1];
-            tmem_ld32_end(s);
-            tmem_ld32_begin(ts + (i < 3 ? 32 * (i + 1) : 0), buf[(i + 1) & 1]);
-            hide(32 * i, s);
+          // chunks of 32 columns, the next one on its way while one is worked on
+          float x0[32], x1[32], mx = -INFINITY;
+          uint32_t pk[32];
+          float2 sum[2];
+          auto most = [&](const float (&s)[32]) {
             float a = s[0], b = s[1];
 #pragma unroll
             for (int k = 2; k < 32; k += 4) {
@@ -749,55 +741,84 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               if (k + 2 < 32) b = fmaxf(fmaxf(b, s[k + 2]), s[k + 3]);
             }
             mx = fmaxf(mx, fmaxf(a, b));
-          }
-          const bool raise = mine && mx > m && (mx - m) * scale_log2 > kSlack;   // (m = -inf: any score)
-          if (__any_sync(0xffffffffu, raise)) {
-            float f = 1.f;
-            if (raise) {
-              f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
-              m = mx;
-              mc = mx * scale_log2;
-              l *= f;
-            }
-            if (begun) {                                          // the accumulator's last product has ended
-              ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
-              if (!ok) break;
-              tc_fence_after();
-#pragma unroll 1
-              for (int cb = 0; cb < kHeadDim; cb += 16) {
-                float v[16];
-                tmem_ld16(to + cb, v);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) v[k] *= f;
-                tmem_st16(to + cb, reinterpret_cast<const uint32_t(&)[16]>(v));
-              }
-            }
-          }
-          // the weights, over the scores that they were made from; their first half is handed on by itself
-          const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float (&s)[32] = buf[i & 1];
-            tmem_ld32_end(s);
-            if (i < 3) tmem_ld32_begin(ts + 32 * (i + 1), buf[(i + 1) & 1]);
-            hide(32 * i, s);
-            uint32_t pk[16];
+          };
+          auto weights = [&](const float (&s)[32], uint32_t* to16) {
+            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
               const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
               const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
               sum[k & 1] = add2(sum[k & 1], w);
-              pk[k] = pack_bf16(w.x, w.y);
+              to16[k] = pack_bf16(w.x, w.y);
             }
-            tmem_st16(ts + 16 * i, pk);
-            if (i == 1) {
-              tmem_wait_st();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&c.p_half[e]);
+          };
+          auto raises = [&]() { return mine && mx > m && (mx - m) * scale_log2 > kSlack; };   // (m = -inf: any score)
+          // The weights of the first half from the reference as it is, and the maximum of the tile on the way; if that
+          // shows that the reference has to move (or there is none yet), that first, then the weights again.
+          bool known = begun;
+          for (;;) {
+            if (!known) {
+              if (!begun) {
+#pragma unroll 1
+                for (int cb = 0; cb < kKeys; cb += 32) {
+                  tmem_ld32(ts + cb, x0);
+                  hide(cb, x0);
+                  most(x0);
+                }
+              }
+              float f = 1.f;
+              if (raises()) {
+                f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
+                m = mx;
+                mc = mx * scale_log2;
+                l *= f;
+              }
+              if (begun) {                                        // the accumulator's last product has ended
+                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int cb = 0; cb < kHeadDim; cb += 32) {
+                  tmem_ld32(to + cb, x0);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) x0[k] *= f;
+                  tmem_st32(to + cb, x0);
+                }
+              }
             }
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            mx = -INFINITY;
+            tmem_ld32_begin(ts, x0);
+            tmem_ld32_end(x0);
+            tmem_ld32_begin(ts + 32, x1);
+            hide(0, x0);
+            most(x0);
+            weights(x0, pk);
+            tmem_ld32_end(x1);
+            tmem_ld32_begin(ts + 64, x0);
+            hide(32, x1);
+            most(x1);
+            weights(x1, pk + 16);
+            tmem_ld32_end(x0);
+            tmem_ld32_begin(ts + 96, x1);
+            hide(64, x0);
+            most(x0);
+            tmem_ld32_end(x1);
+            hide(96, x1);
+            most(x1);
+            if (!known || !__any_sync(0xffffffffu, raises())) break;
+            known = false;
           }
+          if (!ok) break;
+          // the weights take the place of the scores; their first half is handed on by itself
+          tmem_st32(ts, reinterpret_cast<const float(&)[32]>(pk));
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c.p_half[e]);
+          weights(x0, pk);
+          weights(x1, pk + 16);
+          tmem_st32(ts + 32, reinterpret_cast<const float(&)[32]>(pk));
           const float2 total = add2(sum[0], sum[1]);
           l += total.x + total.y;
           tmem_wait_st();
