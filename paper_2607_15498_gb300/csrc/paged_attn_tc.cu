@@ -9,8 +9,8 @@
 // Two softmax warpgroups (thread = row) work in turn, so that the products of one run under the softmax of the other:
 //   a block of more than tq new tokens gives each warpgroup a query tile of its own, and both use every key tile;
 //   a smaller one (a decode step) gives both the same query tile and every second key tile, merged at the end.
-// The reference maximum of a row moves only when a score exceeds it by kSlack (log2 units); then its accumulator is
-// rescaled in TMEM.
+// The reference of a row (log2 units) is its first tile's maximum and moves only when a tile's weights sum to more than kMove;
+// then its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
 //
 // Work is cut into units (sequence, run of key tiles, block, KV head), taken in that order by one CTA per SM: the first by
 // its number, the others from a counter in the workspace. The length K of a run is the same for the whole batch:
@@ -47,9 +47,9 @@ constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // iss
 constexpr int kRows = 128, kKeys = 128;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
-// Weights stay below 2^kSlack times those from the true maximum: nothing is lost in floating point until sums leave
-// the range, at values of 2^127 / (2^24 keys); a moved reference costs a second pass over the tile.
-constexpr float kSlack = 24.f;
+// Weights of a tile may sum to kMove above the reference before it moves (nothing is lost in floating point, sums have room
+// for values of 2^127 / kMove / keys); a sum past kHuge, or no number, is not used.
+constexpr float kMove = 0x1p24f, kHuge = 0x1p96f;
 constexpr int kCand = 32;
 constexpr int kOverhead = 2;                                // of a unit, in key tiles (start, output)
 constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
@@ -73,7 +73,7 @@ struct Unit {
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], p_half[2], turn[2], o1_full, o1_empty;
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], o1_full, o1_empty;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
@@ -238,25 +238,6 @@ __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem,
       " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// 32 fp32 columns of this warp's 32 TMEM lanes: begun here, there after tmem_ld32_end (which waits for every load begun).
-__device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, float (&v)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
-        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
-        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
-        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld32_end(float (&v)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;\n"
-      : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-        "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
-        "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
-        "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
-      :: "memory");
-}
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
@@ -303,7 +284,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
-      mbar_init(&c.drain[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
     mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4);
     c.err = 0;
@@ -474,24 +455,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
           ok = wait_all(&c.full[slot], value.phase);
           if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
           if (ok && queued) ok = wait_all(&c.full[key.slot], key.phase);
-          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_half[e], par_p);
+          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_full[e], par_p);
           if (!ok) break;
+          par_p ^= 1;
           tc_fence_after();
           const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
           if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < kKeys / 32; ++ks)
+            for (int ks = 0; ks < kKeys / 16; ++ks)
               tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
-          }
-          __syncwarp();
-          ok = wait_all(&c.p_full[e], par_p);
-          if (!ok) break;
-          par_p ^= 1;
-          tc_fence_after();
-          if (elect_one()) {
-#pragma unroll
-            for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
-              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
             tc_commit(&c.o_full[e]);
             tc_commit(&c.empty[slot]);
             if (queued) scores();
@@ -594,7 +566,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
     uint32_t n_s = 0, n_o = 0, n_both = 0;                        // score tiles, value products, merged units so far
     bool ok = true;
-    float m = -INFINITY, l = 0.f;                                 // reference maximum, sum
+    float ref = -INFINITY, l = 0.f;                               // reference, sum
+    int up = 0;                                                   // how far the reference has to move before the next tile
     bool begun = false;                                           // the accumulator holds something of this unit
     // Pass nu: the queries of unit nu, the output of unit nu - 1 (the first scores of nu run under it), the tiles of nu.
     for (uint32_t nu = 0;; ++nu) {
@@ -633,11 +606,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         if (ok && begun) ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
         if (!ok) break;
         tc_fence_after();
+        if (l == 0.f) ref = -INFINITY;                              // nothing with a weight: no say in a merge
         float w0 = 1.f, w1 = 0.f;                                   // weights of the two warpgroups' values
         bool second = false;
         if (x.both) {
           if (e) {
-            c.o1.m[r] = m;
+            c.o1.m[r] = ref;
             c.o1.l[r] = l;
             if (r == 0) c.o1.begun = begun;
             tc_fence_before();
@@ -651,12 +625,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
             tc_fence_after();
             second = c.o1.begun;
             if (second) {
-              const float m1 = c.o1.m[r], l1 = c.o1.l[r];
-              const float mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.f : mm;
-              w0 = fast_exp2((m - ref) * scale_log2);
-              w1 = fast_exp2((m1 - ref) * scale_log2);
+              const float m1 = c.o1.m[r], l1 = c.o1.l[r], mm = fmaxf(ref, m1), at = mm == -INFINITY ? 0.f : mm;
+              w0 = fast_exp2(ref - at);
+              w1 = fast_exp2(m1 - at);
               l = l * w0 + l1 * w1;
-              m = mm;
+              ref = mm;
             }
           }
           ++n_both;
@@ -694,7 +667,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
           }
           if (mine && x.slot >= 0 && begun) {
             float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
-            *reinterpret_cast<float2*>(ml + row * 2) = make_float2(m, l);
+            *reinterpret_cast<float2*>(ml + row * 2) = make_float2(ref, l);
           }
           tc_fence_before();
         }
@@ -711,9 +684,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const bool live = (warp & 3) * 32 < rows, mine = r < rows;
       const int sees = x.pos0 + tok0 + min(r, rows - 1) / grp + 1;   // keys that this row sees
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
-      float mc = 0.f;                                             // reference maximum times the scale
-      m = -INFINITY;
+      ref = -INFINITY;
       l = 0.f;
+      up = 0;
       begun = false;
       for (int t = x.t0 + (both ? e : 0); t < last; t += step) {
         ok = wait_all(&c.s_full[e], n_s & 1);
@@ -729,101 +702,71 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
             }
           };
-          // chunks of 32 columns, the next one on its way while one is worked on
-          float x0[32], x1[32], mx = -INFINITY;
-          uint32_t pk[32];
+          // The weights from the reference as it is. Their sum says whether the reference has to move: past kMove it
+          // does so before the next tile (these weights still stand); a sum that is not finite, or no reference yet:
+          // first the maximum of the tile, then the weights again.
+          float x[32];
+          uint32_t pk[64];
           float2 sum[2];
-          auto most = [&](const float (&s)[32]) {
-            float a = s[0], b = s[1];
-#pragma unroll
-            for (int k = 2; k < 32; k += 4) {
-              a = fmaxf(fmaxf(a, s[k]), s[k + 1]);
-              if (k + 2 < 32) b = fmaxf(fmaxf(b, s[k + 2]), s[k + 3]);
-            }
-            mx = fmaxf(mx, fmaxf(a, b));
-          };
-          auto weights = [&](const float (&s)[32], uint32_t* to16) {
-            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-mc, -mc);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
-              const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
-              sum[k & 1] = add2(sum[k & 1], w);
-              to16[k] = pack_bf16(w.x, w.y);
-            }
-          };
-          auto raises = [&]() { return mine && mx > m && (mx - m) * scale_log2 > kSlack; };   // (m = -inf: any score)
-          // The weights of the first half from the reference as it is, and the maximum of the tile on the way; if that
-          // shows that the reference has to move (or there is none yet), that first, then the weights again.
-          bool known = begun;
+          float total;
+          bool known = begun && !__any_sync(0xffffffffu, mine && ref == -INFINITY);
           for (;;) {
+            float f = 1.f;
+            if (up) { f = __uint_as_float((uint32_t)(127 - up) << 23); ref += (float)up; up = 0; }
             if (!known) {
-              if (!begun) {
+              float mx = -INFINITY;
 #pragma unroll 1
-                for (int cb = 0; cb < kKeys; cb += 32) {
-                  tmem_ld32(ts + cb, x0);
-                  hide(cb, x0);
-                  most(x0);
-                }
+              for (int cb = 0; cb < kKeys; cb += 32) {
+                tmem_ld32(ts + cb, x);
+                hide(cb, x);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) mx = fmaxf(mx, x[k]);
               }
-              float f = 1.f;
-              if (raises()) {
-                f = m == -INFINITY ? 0.f : fast_exp2((m - mx) * scale_log2);
-                m = mx;
-                mc = mx * scale_log2;
-                l *= f;
-              }
+              mx *= scale_log2;
+              if (mine && mx > ref) { f *= ref == -INFINITY ? 0.f : fast_exp2(ref - mx); ref = mx; }
+            }
+            if (__any_sync(0xffffffffu, f != 1.f)) {
+              l *= f;
               if (begun) {                                        // the accumulator's last product has ended
                 ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll 1
                 for (int cb = 0; cb < kHeadDim; cb += 32) {
-                  tmem_ld32(to + cb, x0);
+                  tmem_ld32(to + cb, x);
 #pragma unroll
-                  for (int k = 0; k < 32; ++k) x0[k] *= f;
-                  tmem_st32(to + cb, x0);
+                  for (int k = 0; k < 32; ++k) x[k] *= f;
+                  tmem_st32(to + cb, x);
                 }
               }
             }
+            const float off1 = ref == -INFINITY ? 0.f : -ref;
+            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(off1, off1);
             sum[0] = sum[1] = make_float2(0.f, 0.f);
-            mx = -INFINITY;
-            tmem_ld32_begin(ts, x0);
-            tmem_ld32_end(x0);
-            tmem_ld32_begin(ts + 32, x1);
-            hide(0, x0);
-            most(x0);
-            weights(x0, pk);
-            tmem_ld32_end(x1);
-            tmem_ld32_begin(ts + 64, x0);
-            hide(32, x1);
-            most(x1);
-            weights(x1, pk + 16);
-            tmem_ld32_end(x0);
-            tmem_ld32_begin(ts + 96, x1);
-            hide(64, x0);
-            most(x0);
-            tmem_ld32_end(x1);
-            hide(96, x1);
-            most(x1);
-            if (!known || !__any_sync(0xffffffffu, raises())) break;
+#pragma unroll
+            for (int cb = 0; cb < kKeys; cb += 32) {
+              tmem_ld32(ts + cb, x);
+              hide(cb, x);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const float2 a = fma2(make_float2(x[2 * k], x[2 * k + 1]), sc, off);
+                const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
+                sum[k & 1] = add2(sum[k & 1], w);
+                pk[cb / 2 + k] = pack_bf16(w.x, w.y);
+              }
+            }
+            sum[0] = add2(sum[0], sum[1]);
+            total = sum[0].x + sum[0].y;
+            if (!known || !__any_sync(0xffffffffu, mine && !(total < kHuge))) break;
             known = false;
           }
           if (!ok) break;
-          // the weights take the place of the scores; their first half is handed on by itself
-          tmem_st32(ts, reinterpret_cast<const float(&)[32]>(pk));
+          // the weights take the place of the scores
+          tmem_st32(ts, *reinterpret_cast<const float(*)[32]>(pk));
+          tmem_st32(ts + 32, *reinterpret_cast<const float(*)[32]>(pk + 32));
+          l += total;
+          if (mine && total > kMove && total < kHuge) up = (int)(__float_as_uint(total) >> 23) - 127;
           tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&c.p_half[e]);
-          weights(x0, pk);
-          weights(x1, pk + 16);
-          tmem_st32(ts + 32, reinterpret_cast<const float(&)[32]>(pk));
-          const float2 total = add2(sum[0], sum[1]);
-          l += total.x + total.y;
-          tmem_wait_st();
-        } else if (lane == 0) {
-          mbar_arrive(&c.p_half[e]);
         }
         begun = true;
         ++n_o;
@@ -848,7 +791,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
 __global__ void __launch_bounds__(256)
 paged_attn_combine_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, Header* header,
                           const int* __restrict__ first_part, const float* __restrict__ part, int part_rows, int max_parts,
-                          int grp, float scale_log2) {
+                          int grp) {
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp, tq = kRows / grp, bq = 2 * tq;
@@ -883,7 +826,7 @@ paged_attn_combine_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev
         const int64_t pr = part_row(j);
         const float2 x = __ldcg(reinterpret_cast<const float2*>(ml) + pr);
         const float4 y = __ldcg(reinterpret_cast<const float4*>(part + pr * kHeadDim) + lane);
-        const float w = fast_exp2((x.x - ref) * scale_log2);
+        const float w = fast_exp2(x.x - ref);
         l = fmaf(x.y, w, l);
         v.x = fmaf(y.x, w, v.x); v.y = fmaf(y.y, w, v.y); v.z = fmaf(y.z, w, v.z); v.w = fmaf(y.w, w, v.w);
       }
@@ -936,7 +879,7 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
   const int64_t warps = (int64_t)p.T * p.G * group;
   const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
   if (!launch_pdl(paged_attn_combine_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, header,
-                  (const int*)first_part, (const float*)part, rows, max_parts, group, scale_log2))
+                  (const int*)first_part, (const float*)part, rows, max_parts, group))
     return -1;
   return 2;
 }
