@@ -255,18 +255,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
-// 32 fp32 columns of a row's values: to bf16 in the output, or as they are to a partial.
-__device__ __forceinline__ void put_out(__nv_bfloat16* dst, const float (&v)[32], float f) {
-#pragma unroll
-  for (int k = 0; k < 32; k += 8)
-    *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16(v[k] * f, v[k + 1] * f), pack_bf16(v[k + 2] * f, v[k + 3] * f),
-                                                    pack_bf16(v[k + 4] * f, v[k + 5] * f), pack_bf16(v[k + 6] * f, v[k + 7] * f));
-}
-__device__ __forceinline__ void put_part(float* dst, const float (&v)[32]) {
-#pragma unroll
-  for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __nv_bfloat16* __restrict__ q,
                      __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
@@ -497,7 +485,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     __syncwarp();
   } else if (warp == kValues) {
     // ------------------------------------------------------------------ values that no row, or not every row, sees
-    const int panel = lane >> 4, col = 4 * (lane & 15);           // this lane's columns: 64 panel + col .. + 3
+    // a lane looks at eight columns (chunk) of every second key
+    const int panel = (lane >> 3) & 1, chunk = lane & 7, odd_key = lane >> 4;
     uint32_t n0 = 0, par = 0;
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
@@ -506,9 +495,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const Unit x = c.unit[un & 1];
       __syncwarp();
       if (!x.valid) break;
-      int16_t first[4][3];
-#pragma unroll
-      for (int i = 0; i < 12; ++i) first[i / 3][i % 3] = kNone;
+      int16_t first[8][3];
       bool any = false;
       const int end = x.pos0 + x.ntok;
       for (int t = x.values_from; t < x.t1; ++t) {
@@ -518,37 +505,52 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         par ^= 1u << slot;
         const int lo = min(kKeys, max(0, x.pos0 + 1 - t * kKeys)), hi = min(kKeys, end - t * kKeys);
         unsigned char* v = smem + (2 + slot) * kTileBytes + panel * (kKeys * 128);
-        auto word = [&](int key) { return reinterpret_cast<uint2*>(v + key * 128 + (((col >> 3) ^ (key & 7)) << 4) + (col & 4) * 2); };
-        auto odd = [](uint32_t a) { return (a & 0x7f80u) == 0x7f80u || (a & 0x7f800000u) == 0x7f800000u; };   // infinity or NaN
+        auto at = [&](int key) { return reinterpret_cast<uint4*>(v + key * 128 + ((chunk ^ (key & 7)) << 4)); };
+        // an exponent of all ones: infinity or NaN
+        auto odd = [](uint32_t a) { return __vcmpeq2(a & 0x7f807f80u, 0x7f807f80u); };
+        uint32_t found = 0;
 #pragma unroll 4
-        for (int key = lo; key < hi; ++key) {
-          const uint2 a = *word(key);
-          if (odd(a.x) || odd(a.y)) {
-            any = true;
-            uint32_t b[2] = {a.x, a.y};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t h = ((i < 2 ? a.x : a.y) >> (16 * (i & 1))) & 0xffffu;
-              if ((h & 0x7f80u) != 0x7f80u) continue;
-              b[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
-              const int16_t at = (int16_t)(t * kKeys + key - x.values_from * kKeys);
-              if (h & 0x7f) first[i][2] = min(first[i][2], at);
-              else if (h >> 15) first[i][1] = min(first[i][1], at);
-              else first[i][0] = min(first[i][0], at);
-            }
-            *word(key) = make_uint2(b[0], b[1]);
-          }
+        for (int key = lo + odd_key; key < hi; key += 2) {
+          const uint4 w = *at(key);
+          found |= odd(w.x) | odd(w.y) | odd(w.z) | odd(w.w);
         }
-        for (int key = hi; key < kKeys; ++key) *word(key) = make_uint2(0, 0);
+        if (__any_sync(0xffffffffu, found != 0)) {                // rare: element by element
+          if (!any) {
+#pragma unroll
+            for (int i = 0; i < 24; ++i) first[i / 3][i % 3] = kNone;
+          }
+          any = true;
+#pragma unroll 1
+          for (int key = lo + odd_key; key < hi; key += 2) {
+            const uint4 w = *at(key);
+            uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t h = (a[j >> 1] >> (16 * (j & 1))) & 0xffffu;
+              if ((h & 0x7f80u) != 0x7f80u) continue;
+              a[j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+              const int16_t pos = (int16_t)(t * kKeys + key - x.values_from * kKeys);
+              if (h & 0x7f) first[j][2] = min(first[j][2], pos);
+              else if (h >> 15) first[j][1] = min(first[j][1], pos);
+              else first[j][0] = min(first[j][0], pos);
+            }
+            *at(key) = make_uint4(a[0], a[1], a[2], a[3]);
+          }
+          __syncwarp();
+        }
+#pragma unroll 4
+        for (int key = hi + odd_key; key < kKeys; key += 2) *at(key) = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&c.looked[slot]);
       }
       if (!ok) break;
-      any = __any_sync(0xffffffffu, any);
-      if (any) {
+      if (any) {                                                  // (the same in all lanes)
 #pragma unroll
-        for (int i = 0; i < 12; ++i) c.special[un & 1][i % 3][64 * panel + col + i / 3] = first[i / 3][i % 3];
+        for (int i = 0; i < 24; ++i) {
+          const int other = __shfl_xor_sync(0xffffffffu, (int)first[i / 3][i % 3], 16);
+          if (!odd_key) c.special[un & 1][i % 3][64 * panel + 8 * chunk + i / 3] = min(first[i / 3][i % 3], (int16_t)other);
+        }
       }
       if (lane == 0) c.any_special[un & 1] = any;
       __syncwarp();
@@ -561,7 +563,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     if (!ok) c.err = 1;
   } else {
     // ------------------------------------------------------------------ softmax: one row per thread
-    const int e = warp >> 2, r = tid & 127;
+    const int e = warp >> 2, r = tid & 127, wrow = (warp & 3) * 32;
+    const int tok_of = r / grp;                                   // of the query tile, and the row's place from its first one
+    const int row_off = (tok_of * H + r % grp) * kHeadDim;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
     uint32_t n_s = 0, n_o = 0, n_both = 0;                        // score tiles, value products, merged units so far
@@ -569,39 +573,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     float ref = -INFINITY, l = 0.f;                               // reference, sum
     int up = 0;                                                   // how far the reference has to move before the next tile
     bool begun = false;                                           // the accumulator holds something of this unit
-    // Pass nu: the queries of unit nu, the output of unit nu - 1 (the first scores of nu run under it), the tiles of nu.
+    // Pass nu: the output of unit nu - 1, the queries of unit nu, its tiles. (The code between the tiles is kept short: it
+    // is fetched anew each time.)
     for (uint32_t nu = 0;; ++nu) {
       ok = wait_all(&c.u_full[nu & 1], (nu >> 1) & 1);
       if (!ok) break;
       const bool valid = c.unit[nu & 1].valid;
-      if (valid) {
-        const Unit& x = c.unit[nu & 1];
-        const int tok0 = x.both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;   // at least one token
-        const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (r & 15) * 8;
-#pragma unroll 1
-        for (int b = 0; b < 2; ++b) {
-          uint4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int row = (8 * b + i) * 8 + (r >> 4);
-            if (row < rows) v[i] = __ldg(reinterpret_cast<const uint4*>(src + ((int64_t)(row / grp) * H + row % grp) * kHeadDim));
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int row = (8 * b + i) * 8 + (r >> 4);
-            if (row < rows) *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(row, r & 15, kRows)) = v[i];
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.q_full[e]);
-      }
       if (nu > 0) {
         const uint32_t un = nu - 1;
         const Unit& x = c.unit[un & 1];
         const int tok0 = x.both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
-        const bool live = (warp & 3) * 32 < rows, mine = r < rows;
-        const int tok = tok0 + min(r, rows - 1) / grp, sees = x.pos0 + tok + 1;
+        const bool live = wrow < rows, mine = r < rows;
         ok = wait_all(&c.u_looked[un & 1], (un >> 1) & 1);
         if (ok && begun) ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
         if (!ok) break;
@@ -637,7 +619,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         if (live && !(x.both && e)) {
           const int special = c.any_special[un & 1];
           const float f = l == 0.f ? 0.f : 1.f / l;
-          const int64_t row = x.slot < 0 ? ((int64_t)(x.row0 + tok) * H + x.g * grp + r % grp) : (int64_t)x.slot * part_rows + tok0 * grp + r;
+          const bool whole = x.slot < 0;                          // else a partial
+          // 32 columns of the warp's rows at a time through its own 4 KB of the query tile's first half (whose products have
+          // ended), so that a row's 16-byte pieces leave next to each other
+          uint4* stage = reinterpret_cast<uint4*>(smem + e * kTileBytes + wrow * 128);
+          float* dst_part = part + ((int64_t)x.slot * part_rows + tok0 * grp + wrow) * kHeadDim;
+          __nv_bfloat16* dst = out + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim;
 #pragma unroll 1
           for (int cb = 0; cb < kHeadDim; cb += 32) {
             float v[32];
@@ -650,24 +637,46 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               for (int k = 0; k < 32; ++k) v[k] = fmaf(v[k], w0, v1[k] * w1);
             }
             if (special) {
-              const int at = sees - x.values_from * kKeys;          // positions below it are seen
+              const int at = x.pos0 + tok0 + tok_of + 1 - x.values_from * kKeys;   // positions below it are seen
               for (int k = 0; k < 32; ++k) {
                 const int col = cb + k;
-                  float y = 0.f;
+                float y = 0.f;
                 if (c.special[un & 1][0][col] < at) y += INFINITY;
                 if (c.special[un & 1][1][col] < at) y -= INFINITY;
                 if (c.special[un & 1][2][col] < at) y = NAN;
                 add_at(v, k, y);
               }
             }
-            if (mine) {
-              if (x.slot < 0) put_out(out + row * kHeadDim + cb, v, f);
-              else if (begun) put_part(part + row * kHeadDim + cb, v);
+            if (whole) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                stage[lane * 4 + (k ^ ((lane >> 1) & 3))] =
+                    make_uint4(pack_bf16(v[8 * k] * f, v[8 * k + 1] * f), pack_bf16(v[8 * k + 2] * f, v[8 * k + 3] * f),
+                               pack_bf16(v[8 * k + 4] * f, v[8 * k + 5] * f), pack_bf16(v[8 * k + 6] * f, v[8 * k + 7] * f));
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int in = 8 * i + (lane >> 2), k = lane & 3, off = __shfl_sync(0xffffffffu, row_off, in);
+                if (wrow + in < rows)
+                  *reinterpret_cast<uint4*>(dst + off + cb + 8 * k) = stage[in * 4 + (k ^ ((in >> 1) & 3))];
+              }
+            } else if (begun) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                stage[lane * 8 + (k ^ (lane & 7))] = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]),
+                                                               __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
+              __syncwarp();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int in = 4 * i + (lane >> 3), k = lane & 7;
+                if (wrow + in < rows)
+                  *reinterpret_cast<uint4*>(dst_part + (int64_t)in * kHeadDim + cb + 4 * k) = stage[in * 8 + (k ^ (in & 7))];
+              }
             }
           }
-          if (mine && x.slot >= 0 && begun) {
+          if (mine && !whole && begun) {
             float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
-            *reinterpret_cast<float2*>(ml + row * 2) = make_float2(ref, l);
+            *reinterpret_cast<float2*>(ml + ((int64_t)x.slot * part_rows + tok0 * grp + r) * 2) = make_float2(ref, l);
           }
           tc_fence_before();
         }
@@ -681,8 +690,26 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       if (!valid) break;
       const Unit& x = c.unit[nu & 1];
       const int both = x.both, tok0 = both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
-      const bool live = (warp & 3) * 32 < rows, mine = r < rows;
-      const int sees = x.pos0 + tok0 + min(r, rows - 1) / grp + 1;   // keys that this row sees
+      const bool live = wrow < rows, mine = r < rows;
+      const int sees = x.pos0 + tok0 + (mine ? tok_of : 0) + 1;   // keys that this row sees
+      // the warp's own rows of the query tile, a row by 16 lanes
+      const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (lane & 15) * 8;
+      __syncwarp();
+      if (live) {                                                 // (rows past the last one repeat it)
+#pragma unroll 1
+        for (int i0 = lane >> 4; i0 < 32; i0 += 16) {
+          uint4 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            v[i] = __ldg(reinterpret_cast<const uint4*>(src + __shfl_sync(0xffffffffu, row_off, min(i0 + 2 * i, rows - wrow - 1))));
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(wrow + i0 + 2 * i, lane & 15, kRows)) = v[i];
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&c.q_full[e]);
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
       ref = -INFINITY;
       l = 0.f;
