@@ -307,22 +307,21 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
                          dev_status, stream=None) -> int:
     """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
     ERR_ARG where a tensor is not of the cache's type, shape or device."""
-    G, d, T = pages.c.n_kv_heads, pages.c.head_dim, seqs.c.n_rows
+    G, T = pages.heads, seqs.n_rows
     H = G if q is None else q.shape[1]
-    if H % G or not (pages.takes(k, (T, G, d), True) and pages.takes(v, (T, G, d), True)):
+    if H % G or not (pages.takes_rows(k, T, G) and pages.takes_rows(v, T, G)):
         return ERR_ARG
-    if q is not None and not (pages.takes(q, (T, H, d), True) and pages.takes(q_out, (T, H, d))):
+    if q is not None and not (pages.takes_rows(q, T, H) and pages.takes(q_out, (T, H, 128))):
         return ERR_ARG
-    for w in (q_norm, k_norm):
-        if w is not None and not pages.takes(w, (d,)):
-            return ERR_ARG
-    if rot_dim and not (freq.dtype == torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
-                        and freq.device == pages.pool.device):
+    if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
+        return ERR_ARG
+    if rot_dim and not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
+                        and freq.get_device() == pages.device):
         return ERR_ARG
     return lib().varrate_paged_append(pages.ref, seqs.ref, layer, H // G, _ptr(q), 0 if q is None else q.stride(0),
                                       k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _ptr(q_norm),
                                       _ptr(k_norm), eps, _ptr(freq), rot_dim, _ptr(q_out), _ptr(dev_status),
-                                      _stream(stream))
+                                      pages.stream(stream))
 
 
 def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
@@ -331,25 +330,24 @@ def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
 
 def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream=None) -> int:
     """q and out [T][H][d], dense. ERR_ARG where a tensor is not of the cache's type, shape or device."""
-    shape = (seqs.c.n_rows, pages.c.n_kv_heads * group, pages.c.head_dim)
+    shape = (seqs.n_rows, pages.heads * group, 128)
     if not (pages.takes(q, shape) and pages.takes(out, shape)):
         return ERR_ARG
     return lib().varrate_paged_attn(pages.ref, seqs.ref, layer, group, q.data_ptr(), out.data_ptr(), _ptr(dev_status),
-                                    _ptr(ws), _nbytes(ws), _stream(stream))
+                                    _ptr(ws), _nbytes(ws), pages.stream(stream))
 
 
 def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, dev_status, stream=None) -> int:
     """k_out, v_out [S][n_layers][G][n][d], dense, or None. ERR_ARG where a tensor is not of the cache's
     type, shape or device."""
-    shape = (seqs.c.n_seqs, n_layers, pages.c.n_kv_heads, n, pages.c.head_dim)
-    for t in (k_out, v_out):
-        if t is not None and not pages.takes(t, shape):
-            return ERR_ARG
-    if first is not None and not (first.dtype == torch.int32 and first.is_contiguous()
-                                  and first.shape == (seqs.c.n_seqs,) and first.device == pages.pool.device):
+    shape = (seqs.n_seqs, n_layers, pages.heads, n, 128)
+    if (k_out is not None and not pages.takes(k_out, shape)) or (v_out is not None and not pages.takes(v_out, shape)):
+        return ERR_ARG
+    if first is not None and not (first.dtype is torch.int32 and first.is_contiguous()
+                                  and first.shape == (seqs.n_seqs,) and first.get_device() == pages.device):
         return ERR_ARG
     return lib().varrate_paged_gather(pages.ref, seqs.ref, layer, n_layers, _ptr(first), n, _ptr(k_out), _ptr(v_out),
-                                      _ptr(dev_status), _stream(stream))
+                                      _ptr(dev_status), pages.stream(stream))
 
 
 # ------------------------------------------------------------- device-memory plumbing
@@ -444,12 +442,22 @@ class PagedCache:
 
     def __post_init__(self):
         self.ref = ctypes.byref(self.c)
+        self.heads, self.dtype, self.device = self.c.n_kv_heads, self.pool.dtype, self.pool.get_device()
 
-    def takes(self, t: torch.Tensor, shape, rows_apart=False) -> bool:
-        """Whether t has this shape and the cache's type and device and is dense (or its rows are)."""
-        if t.shape != shape or t.dtype != self.pool.dtype or t.device != self.pool.device:
-            return False
-        return t.is_contiguous() or (rows_apart and t.stride()[1:] == (shape[2], 1))
+    def takes(self, t: torch.Tensor, shape) -> bool:
+        """Whether t has this shape and the cache's type and device and is dense."""
+        return t.shape == shape and t.dtype is self.dtype and t.is_contiguous() and t.get_device() == self.device
+
+    def takes_rows(self, t: torch.Tensor, rows: int, heads: int) -> bool:
+        """The same for [rows][heads][d] whose rows may be apart."""
+        return (t.shape == (rows, heads, 128) and t.dtype is self.dtype and t.get_device() == self.device
+                and (t.is_contiguous() or t.stride()[1:] == (128, 1)))
+
+    def stream(self, stream) -> int | None:
+        """`stream` as _stream takes it; None is torch's current stream on the cache's device."""
+        if stream is None and self.device >= 0:
+            return torch._C._cuda_getCurrentRawStream(self.device)
+        return _stream(stream)
 
 
 @dataclass
@@ -473,6 +481,7 @@ class SeqBatch:
 
     def __post_init__(self):
         self.ref = ctypes.byref(self.c)
+        self.n_seqs, self.n_rows = self.c.n_seqs, self.c.n_rows
 
 
 def paged_attn_workspace(pages: PagedCache, seqs: SeqBatch, group: int) -> torch.Tensor:
