@@ -15,8 +15,8 @@
 // Work is cut into units (sequence, run of key tiles, block, KV head), taken in that order by one CTA per SM: the first by
 // its number, the others from a counter in the workspace. The length K of a run is the same for the whole batch:
 // every CTA weighs the same 32 values of it (make_plan). Blocks of one sequence are taken longest first, and blocks that read
-// the same keys stand next to each other, so that they meet in L2. Units of a block that is cut write maximum, sum and
-// unnormalised values; paged_attn_combine_kernel merges them.
+// the same keys stand next to each other, so that they meet in L2. Units of a block that is cut write reference, sum and
+// unnormalised values of their rows; paged_attn_merge_kernel merges them.
 //
 // Values at positions that a row does not see have weight 0 in P, and 0 times an infinity is no number: in the tiles
 // where that can happen two warps zero every value past the block's last token, and values that are not finite and
@@ -55,12 +55,11 @@ constexpr int kOverhead = 2;                                // of a unit, in key
 constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
 constexpr int kNone = 0x7fff;                               // kSpecial: no such value
 
-// Workspace: header, first partial of every sequence [S + 1], then the partials: values [rows][d], (max, sum) [rows].
+// Workspace: header, then the partials: values [rows][d], then (reference, sum) [rows].
 struct Header {
   unsigned int taken;       // units taken from the counter; zero between calls
-  unsigned int gave_up;     // a CTA that timed out: not all units were taken
-  int run;                  // key tiles of a run
-  int units;
+  unsigned int gave_up;     // a CTA timed out: not all units were taken; zero between calls
+  int run, units, parts;    // key tiles of a run, units, and how many of them are partials
 };
 constexpr size_t kHeaderBytes = 256;
 
@@ -73,11 +72,11 @@ struct Unit {
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], o1_full, o1_empty;
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], o1_full, o1_empty, planned;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
-    struct { unsigned long long weight; int items, most, units[kCand], split[kCand], chunk[kCand]; } plan;
+    struct { int units[kCand], split[kCand], chunk[kCand]; } plan;
   };
   int16_t special[2][3][kHeadDim];                          // first position (from the first looked-at tile) of +inf, -inf, NaN
   int any_special[2];
@@ -113,33 +112,32 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
 // The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
 // j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
-// not hold are left out. Same for every CTA. All threads.
-__device__ void make_plan(const Paged& p, Ctl& c, int bq, int C, int max_parts, int& run, int& units) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) { c.plan.weight = 0; c.plan.items = 0; c.plan.most = 0; }
-  if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
-  __syncthreads();
-  unsigned long long w = 0;
+// not hold are left out. Same for every CTA. Lane = candidate; the warps share the sequences and add up in plan_add, one
+// warp decides in plan_choose.
+__device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
+  float w = 0.f;
   int most = 0;
-  for (int s = tid; s < p.S; s += kThreads) {
+  for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
     if (!seq_range(p, s, r) || r.n == 0) continue;
-    const int nb = (r.n + bq - 1) / bq;
     const int last = tiles_of(r.len), first = tiles_of(r.len - r.n + min(bq, r.n));
-    w += (unsigned long long)p.G * nb * (unsigned long long)(first + last);
+    w += (float)((r.n + bq - 1) / bq) * (0.5f * (float)(first + last));
     most = max(most, last);
   }
-  if (w) { atomicAdd(&c.plan.weight, w); atomicMax(&c.plan.most, most); }
-  __syncthreads();
-  const unsigned long long W = (c.plan.weight + 1) / 2;
-  const int longest = c.plan.most;
-  // this lane's candidate
-  int cand = longest + 1;
-  if (lane < kCand - 1) {
-    const unsigned long long j = 1 + (lane >> 2), i = lane & 3, div = 16ull * j * (unsigned long long)C;
-    const unsigned long long k = (W * (16 + i) + div - 1) / div;
-    cand = k < 1 ? 1 : k < (unsigned long long)cand ? (int)k : cand;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    w += __shfl_xor_sync(0xffffffffu, w, o);
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
   }
+  longest = most;
+  return w * (float)p.G;
+}
+__device__ __forceinline__ int plan_candidate(float W, int longest, int C, int lane) {
+  if (lane == kCand - 1) return longest + 1;
+  const float k = ceilf(W * (float)(16 + (lane & 3)) / (16.f * (float)(1 + (lane >> 2)) * (float)C));
+  return min(max(1, (int)fminf(k, 1e9f)), longest + 1);
+}
+__device__ __forceinline__ void plan_add(const Paged& p, Ctl& c, int bq, int cand, int warp, int lane) {
   int u = 0, split = 0, chunk = 0;
   for (int s = warp; s < p.S; s += kThreads / 32) {
     SeqRange r;
@@ -151,11 +149,12 @@ __device__ void make_plan(const Paged& p, Ctl& c, int bq, int C, int max_parts, 
     chunk = max(chunk, q.chunk);
   }
   if (u) { atomicAdd(&c.plan.units[lane], u); atomicAdd(&c.plan.split[lane], split); atomicMax(&c.plan.chunk[lane], chunk); }
-  __syncthreads();
-  u = c.plan.units[lane];
+}
+__device__ __forceinline__ void plan_choose(const Ctl& c, float W, int cand, int C, int max_parts, int lane, int& run, int& units, int& parts) {
+  const int u = c.plan.units[lane];
   float est = INFINITY;
   if (c.plan.split[lane] <= max_parts) {
-    const float total = (float)W + (float)kOverhead * u, mean = total / fmaxf((float)u, 1.f);
+    const float total = W + (float)kOverhead * u, mean = total / fmaxf((float)u, 1.f);
     est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, c.plan.chunk[lane] + kOverhead - mean));
   }
   int best = lane;
@@ -167,7 +166,7 @@ __device__ void make_plan(const Paged& p, Ctl& c, int bq, int C, int max_parts, 
   }
   run = __shfl_sync(0xffffffffu, cand, best);
   units = __shfl_sync(0xffffffffu, u, best);
-  __syncthreads();
+  parts = c.plan.split[best];
 }
 
 // Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
@@ -209,8 +208,8 @@ struct Walk {
     f.cuts = __shfl_sync(0xffffffffu, q.cuts, l); f.chunk = __shfl_sync(0xffffffffu, q.chunk, l);
     const int units = p.G * f.nb * f.cuts;
     const int at = u - before - (__shfl_sync(0xffffffffu, incl, l) - units);
-    x.g = at % p.G;
-    const int b = f.nb - 1 - at / p.G % f.nb, j = at / p.G / f.nb;
+    const int gb = at / p.G, j = gb / f.nb, b = f.nb - 1 - (gb - j * f.nb);
+    x.g = at - gb * p.G;
     x.ntok = min(bq, f.n - b * bq);
     x.row0 = f.row0 + b * bq;
     x.pos0 = f.len - f.n + b * bq;
@@ -258,7 +257,7 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __nv_bfloat16* __restrict__ q,
                      __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
-                     int* __restrict__ first_part, float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
+                     float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Ctl& c = *reinterpret_cast<Ctl*>(smem + (2 + kRing) * kTileBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -274,47 +273,36 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
       mbar_init(&c.drain[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
-    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4);
+    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads / 32);
     c.err = 0;
     fence_mbar_init();
   }
-  pdl_wait();
-  int run, units;
-  make_plan(p, c, bq, C, max_parts, run, units);
-  if (blockIdx.x == 0) {
-    for (int s = tid; s < p.S; s += kThreads) {
-      SeqRange r;
-      if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
-    }
-    if (tid == 0) { header->run = run; header->units = units; }
-    if (warp == kValues) {
-      Walk w;
-      w.load(p, bq, run, lane);
-      for (;;) {
-        const int mine = w.q.cuts > 1 ? p.G * w.q.nb * w.q.cuts : 0;
-        if (w.s0 + lane < p.S) first_part[w.s0 + lane] = w.parts_before + w.parts_incl - mine;
-        if (w.s0 + 32 >= p.S) break;
-        w.next(p, bq, run, lane);
-      }
-      if (lane == 0) first_part[p.S] = w.parts_before + w.parts;
-    }
-  }
-  if ((int)blockIdx.x >= units) return;
+  if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
   if (warp == kIssuer) tmem_alloc(&c.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
+  pdl_wait();
+  int longest;
+  const float weight = plan_weight(p, bq, lane, longest);
+  const int cand = plan_candidate(weight, longest, C, lane);
+  plan_add(p, c, bq, cand, warp, lane);
+  __syncwarp();
+  if (lane == 0) mbar_arrive(&c.planned);
 
   if (warp == kProducer) {
     // ------------------------------------------------------------------ units, and their keys and values
+    bool ok = wait_all(&c.planned, 0);
+    int run = 1, units = 0, parts = 0;
+    if (ok) plan_choose(c, weight, cand, C, max_parts, lane, run, units, parts);
+    if (blockIdx.x == 0 && lane == 0) { header->run = run; header->units = units; header->parts = parts; }
     Walk w;
     w.load(p, bq, run, lane);
     const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box
     const int per_tile = kKeys / page_keys;
     int u = blockIdx.x;
     uint32_t n = 0;                                               // ring tiles so far
-    bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
       Unit x;
       int s = 0;
@@ -485,6 +473,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     __syncwarp();
   } else if (warp == kValues) {
     // ------------------------------------------------------------------ values that no row, or not every row, sees
+    if (blockIdx.x == 0) {
+      for (int s = lane; s < p.S; s += 32) {
+        SeqRange r;
+        if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      }
+    }
     // a lane looks at eight columns (chunk) of every second key
     const int panel = (lane >> 3) & 1, chunk = lane & 7, odd_key = lane >> 4;
     uint32_t n0 = 0, par = 0;
@@ -746,8 +740,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               for (int cb = 0; cb < kKeys; cb += 32) {
                 tmem_ld32(ts + cb, x);
                 hide(cb, x);
+                float top[4] = {mx, x[0], x[1], x[2]};
 #pragma unroll
-                for (int k = 0; k < 32; ++k) mx = fmaxf(mx, x[k]);
+                for (int k = 3; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], x[k]);
+                mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
               }
               mx *= scale_log2;
               if (mine && mx > ref) { f *= ref == -INFINITY ? 0.f : fast_exp2(ref - mx); ref = mx; }
@@ -814,46 +810,50 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
 }
 
 // Merges the partials of blocks that were cut, a warp per (row, query head), and leaves the header as the next call wants
-// it. A run j of a block counts for a row only where the row's query tile reaches it.
+// it. A run of a block counts for a row only where the row's query tile reaches it.
 __global__ void __launch_bounds__(256)
-paged_attn_combine_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, Header* header,
-                          const int* __restrict__ first_part, const float* __restrict__ part, int part_rows, int max_parts,
-                          int grp) {
+paged_attn_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, Header* header,
+                        const float* __restrict__ part, int part_rows, int max_parts, int grp) {
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp, tq = kRows / grp, bq = 2 * tq;
   const int run = header->run;
-  if (__ldcg(first_part + p.S) > 0) {
-    const float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
+  if (header->parts > 0) {
+    const float2* ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
     for (int64_t i = (int64_t)blockIdx.x * 8 + warp; i < (int64_t)p.T * H; i += (int64_t)gridDim.x * 8) {
-      const int t = (int)(i / H), h = (int)(i % H), g = h / grp;
+      const int t = (int)(i / H), h = (int)(i - (int64_t)t * H), g = h / grp;
       const int s = count_le(p.row_start, p.S + 1, t, lane) - 1;
       SeqRange r;
       if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
       const SeqPlan f = seq_plan(r, bq, run);
       if (f.cuts < 2) continue;
+      int before = 0;                                             // partials of the sequences before this one
+      for (int s1 = lane; s1 < s; s1 += 32) {
+        SeqRange r1;
+        if (!seq_range(p, s1, r1)) continue;
+        const SeqPlan f1 = seq_plan(r1, bq, run);
+        before += f1.cuts > 1 ? p.G * f1.nb * f1.cuts : 0;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
       const int tok = t - f.row0, b = tok / bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
       // the row's query tile: its last token's position decides which runs it reaches
       const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
-      const int tiles = tiles_of(f.len - f.n + b * bq + last);
-      const int runs = (tiles + f.chunk - 1) / f.chunk;
-      const int64_t row = (int64_t)(in * grp + h % grp);
-      auto part_row = [&](int j) {
-        return (int64_t)(__ldcg(first_part + s) + (j * f.nb + f.nb - 1 - b) * p.G + g) * part_rows + row;
-      };
-      float m = -INFINITY;
-      for (int j = lane; j < runs; j += 32) m = fmaxf(m, __ldcg(ml + part_row(j) * 2));
+      const int runs = (tiles_of(f.len - f.n + b * bq + last) + f.chunk - 1) / f.chunk;
+      const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (h - g * grp);
+      const int64_t step = (int64_t)f.nb * p.G * part_rows;       // from run to run
+      float top = -INFINITY;
+      for (int j = lane; j < runs; j += 32) top = fmaxf(top, __ldcg(ml + row0 + j * step).x);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float ref = m == -INFINITY ? 0.f : m;
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (top == -INFINITY) top = 0.f;
       float l = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
       for (int j = 0; j < runs; ++j) {
-        const int64_t pr = part_row(j);
-        const float2 x = __ldcg(reinterpret_cast<const float2*>(ml) + pr);
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(part + pr * kHeadDim) + lane);
-        const float w = fast_exp2(x.x - ref);
+        const float2 x = __ldcg(ml + row0 + j * step);
+        const float4 y = __ldcg(reinterpret_cast<const float4*>(part + (row0 + j * step) * kHeadDim) + lane);
+        const float w = fast_exp2(x.x - top);
         l = fmaf(x.y, w, l);
         v.x = fmaf(y.x, w, v.x); v.y = fmaf(y.y, w, v.y); v.z = fmaf(y.z, w, v.z); v.w = fmaf(y.w, w, v.w);
       }
@@ -872,13 +872,11 @@ int rows_of_part(const Paged& p, int group) {
   const int64_t rows = (int64_t)p.T * group, most = 2 * (kRows / group) * group;
   return (int)(rows < most ? rows : most);
 }
-size_t first_part_bytes(const Paged& p) { return (((size_t)p.S + 1) * sizeof(int) + 255) & ~size_t(255); }
-
 }  // namespace
 
 size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms) {
   const size_t rows = (size_t)kPartsPerSm * num_sms * rows_of_part(p, group);
-  return kHeaderBytes + first_part_bytes(p) + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
+  return kHeaderBytes + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
 }
 
 int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
@@ -896,19 +894,17 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
     return -1;
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
-  int* first_part = reinterpret_cast<int*>(w + kHeaderBytes);
-  float* part = reinterpret_cast<float*>(w + kHeaderBytes + first_part_bytes(p));
+  float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int max_parts = kPartsPerSm * num_sms, rows = rows_of_part(p, group);
   const float scale_log2 = kLog2e / sqrtf((float)kHeadDim);
   if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, p, (const __nv_bfloat16*)q,
-                  (__nv_bfloat16*)out, dev_status, header, first_part, part, rows, max_parts, group, scale_log2))
+                  (__nv_bfloat16*)out, dev_status, header, part, rows, max_parts, group, scale_log2))
     return -1;
   const int64_t warps = (int64_t)p.T * p.G * group;
   const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
-  if (!launch_pdl(paged_attn_combine_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, header,
-                  (const int*)first_part, (const float*)part, rows, max_parts, group))
-    return -1;
-  return 2;
+  return launch_pdl(paged_attn_merge_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, header,
+                    (const float*)part, rows, max_parts, group)
+             ? 2 : -1;
 }
 
 }  // namespace vr
