@@ -12,11 +12,8 @@
 // The reference of a row (log2 units) is its first tile's maximum and moves only when a tile's weights sum to more than kMove;
 // then its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
 //
-// Work is cut into units (sequence, run of key tiles, block, KV head), taken in that order by one CTA per SM: the first by
-// its number, the others from a counter in the workspace. The length K of a run is the same for the whole batch:
-// every CTA weighs the same 32 values of it (make_plan). Blocks of one sequence are taken longest first, and blocks that read
-// the same keys stand next to each other, so that they meet in L2. Units of a block that is cut write reference, sum and
-// unnormalised values of their rows; paged_attn_merge_kernel merges them.
+// Units of work (paged_plan.cuh) are taken by one CTA per SM: the first by its number, the others from a counter in the
+// workspace; paged_attn_merge_kernel merges the partials.
 //
 // Values at positions that a row does not see have weight 0 in P, and 0 times an infinity is no number: in the tiles
 // where that can happen two warps zero every value past the block's last token, and values that are not finite and
@@ -35,6 +32,7 @@
 #include "common.cuh"
 #include "decode_common.cuh"
 #include "paged.h"
+#include "paged_plan.cuh"
 
 namespace vr {
 
@@ -44,39 +42,19 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
-constexpr int kRows = 128, kKeys = 128;
+constexpr int kRows = 128;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // Weights of a tile may sum to kMove above the reference before it moves (nothing is lost in floating point, sums have room
 // for values of 2^127 / kMove / keys); a sum past kHuge, or no number, is not used.
 constexpr float kMove = 0x1p24f, kHuge = 0x1p96f;
-constexpr int kCand = 32;
-constexpr int kOverhead = 2;                                // of a unit, in key tiles (start, output)
-constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
-constexpr int kNone = 0x7fff;                               // kSpecial: no such value
-
-// Workspace: header, then the partials: values [rows][d], then (reference, sum) [rows].
-struct Header {
-  unsigned int taken;       // units taken from the counter; zero between calls
-  unsigned int gave_up;     // a CTA timed out: not all units were taken; zero between calls
-  int run, units, parts;    // key tiles of a run, units, and how many of them are partials
-};
-constexpr size_t kHeaderBytes = 256;
-
-struct Unit {
-  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from;
-  // g: KV head; row0: row of the block's first token; pos0: its position; key tiles t0 .. t1 - 1, of which the first
-  // warpgroup's query tile sees those before e0; both: one query tile for both; slot: partial, or -1; values_from: first
-  // tile whose values have to be looked at
-};
-
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
   uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], o1_full, o1_empty, planned;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
-    struct { int units[kCand], split[kCand], chunk[kCand]; } plan;
+    PlanSums plan;
   };
   int16_t special[2][3][kHeadDim];                          // first position (from the first looked-at tile) of +inf, -inf, NaN
   int any_special[2];
@@ -86,144 +64,11 @@ struct Ctl {
 constexpr size_t kSmemBytes = 2 * kTileBytes + kRing * kTileBytes + sizeof(Ctl);
 static_assert(kSmemBytes <= 232448, "shared memory of a block");
 
-// Key tiles that hold the first `keys` keys (keys < 2^32).
-__device__ __forceinline__ int tiles_of(uint32_t keys) { return (int)((keys + (kKeys - 1)) / kKeys); }
-
-// Blocks, key tiles and cuts of one sequence.
-struct SeqPlan {
-  int row0, n, len, nb, tiles, cuts, chunk;
-};
-__device__ __forceinline__ SeqPlan seq_plan(const SeqRange& r, int bq, int run) {
-  SeqPlan q;
-  q.row0 = r.row0; q.n = r.n; q.len = r.len;
-  q.nb = (r.n + bq - 1) / bq;
-  q.tiles = tiles_of(r.len);
-  q.cuts = q.nb ? (q.tiles + run - 1) / run : 0;
-  q.chunk = q.nb ? (q.tiles + q.cuts - 1) / q.cuts : 0;
-  return q;
-}
-
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
   for (uint32_t i = 0; i < kWaitTries; ++i)
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return false;
 }
-
-// The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
-// j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
-// mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
-// not hold are left out. Same for every CTA. Lane = candidate; the warps share the sequences and add up in plan_add, one
-// warp decides in plan_choose.
-__device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
-  float w = 0.f;
-  int most = 0;
-  for (int s = lane; s < p.S; s += 32) {
-    SeqRange r;
-    if (!seq_range(p, s, r) || r.n == 0) continue;
-    const int last = tiles_of(r.len), first = tiles_of(r.len - r.n + min(bq, r.n));
-    w += (float)((r.n + bq - 1) / bq) * (0.5f * (float)(first + last));
-    most = max(most, last);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    w += __shfl_xor_sync(0xffffffffu, w, o);
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-  }
-  longest = most;
-  return w * (float)p.G;
-}
-__device__ __forceinline__ int plan_candidate(float W, int longest, int C, int lane) {
-  if (lane == kCand - 1) return longest + 1;
-  const float k = ceilf(W * (float)(16 + (lane & 3)) / (16.f * (float)(1 + (lane >> 2)) * (float)C));
-  return min(max(1, (int)fminf(k, 1e9f)), longest + 1);
-}
-__device__ __forceinline__ void plan_add(const Paged& p, Ctl& c, int bq, int cand, int warp, int lane) {
-  int u = 0, split = 0, chunk = 0;
-  for (int s = warp; s < p.S; s += kThreads / 32) {
-    SeqRange r;
-    if (!seq_range(p, s, r)) continue;
-    const SeqPlan q = seq_plan(r, bq, cand);
-    const int n = p.G * q.nb * q.cuts;
-    u += n;
-    split += q.cuts > 1 ? n : 0;
-    chunk = max(chunk, q.chunk);
-  }
-  if (u) { atomicAdd(&c.plan.units[lane], u); atomicAdd(&c.plan.split[lane], split); atomicMax(&c.plan.chunk[lane], chunk); }
-}
-__device__ __forceinline__ void plan_choose(const Ctl& c, float W, int cand, int C, int max_parts, int lane, int& run, int& units, int& parts) {
-  const int u = c.plan.units[lane];
-  float est = INFINITY;
-  if (c.plan.split[lane] <= max_parts) {
-    const float total = W + (float)kOverhead * u, mean = total / fmaxf((float)u, 1.f);
-    est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, c.plan.chunk[lane] + kOverhead - mean));
-  }
-  int best = lane;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float e = __shfl_xor_sync(0xffffffffu, est, o);
-    const int b = __shfl_xor_sync(0xffffffffu, best, o);
-    if (e < est || (e == est && b < best)) { est = e; best = b; }
-  }
-  run = __shfl_sync(0xffffffffu, cand, best);
-  units = __shfl_sync(0xffffffffu, u, best);
-  parts = c.plan.split[best];
-}
-
-// Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
-struct Walk {
-  int s0 = 0, before = 0, parts_before = 0;     // first sequence held; units and partials before it
-  int incl, parts_incl, total, parts;           // scans over the sequences held, and their sums
-  SeqPlan q;
-
-  __device__ __forceinline__ void load(const Paged& p, int bq, int run, int lane) {
-    SeqRange r;
-    r.n = 0; r.len = 0; r.row0 = 0;
-    if (s0 + lane < p.S && !seq_range(p, s0 + lane, r)) r.n = 0;
-    if (r.n == 0) r.len = 0;
-    q = seq_plan(r, bq, run);
-    incl = p.G * q.nb * q.cuts;
-    parts_incl = q.cuts > 1 ? incl : 0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, incl, o), z = __shfl_up_sync(0xffffffffu, parts_incl, o);
-      if (lane >= o) { incl += y; parts_incl += z; }
-    }
-    total = __shfl_sync(0xffffffffu, incl, 31);
-    parts = __shfl_sync(0xffffffffu, parts_incl, 31);
-  }
-  __device__ __forceinline__ void next(const Paged& p, int bq, int run, int lane) {
-    before += total;
-    parts_before += parts;
-    s0 += 32;
-    load(p, bq, run, lane);
-  }
-  // unit u (at or after the last one asked for, below the number of units): its sequence and what it is
-  __device__ __forceinline__ int find(const Paged& p, int bq, int tq, int run, int u, int lane, Unit& x) {
-    while (u >= before + total && s0 < p.S) next(p, bq, run, lane);
-    const int l = __ffs(__ballot_sync(0xffffffffu, u < before + incl)) - 1;
-    if (l < 0) { x.valid = 0; x.t0 = 0; x.t1 = 0; return 0; }
-    SeqPlan f;
-    f.row0 = __shfl_sync(0xffffffffu, q.row0, l); f.n = __shfl_sync(0xffffffffu, q.n, l);
-    f.len = __shfl_sync(0xffffffffu, q.len, l); f.nb = __shfl_sync(0xffffffffu, q.nb, l);
-    f.cuts = __shfl_sync(0xffffffffu, q.cuts, l); f.chunk = __shfl_sync(0xffffffffu, q.chunk, l);
-    const int units = p.G * f.nb * f.cuts;
-    const int at = u - before - (__shfl_sync(0xffffffffu, incl, l) - units);
-    const int gb = at / p.G, j = gb / f.nb, b = f.nb - 1 - (gb - j * f.nb);
-    x.g = at - gb * p.G;
-    x.ntok = min(bq, f.n - b * bq);
-    x.row0 = f.row0 + b * bq;
-    x.pos0 = f.len - f.n + b * bq;
-    const int end = x.pos0 + x.ntok, tiles = tiles_of(end);
-    x.t0 = j * f.chunk;
-    x.t1 = min(x.t0 + f.chunk, tiles);
-    x.both = x.ntok <= tq;
-    x.e0 = max(x.t0, min(x.t1, tiles_of((uint32_t)x.pos0 + tq)));
-    x.slot = f.cuts > 1 ? parts_before + __shfl_sync(0xffffffffu, parts_incl, l) - units + at : -1;
-    x.values_from = max(x.t0, x.ntok > 1 ? (x.pos0 + 1) / kKeys : end / kKeys);
-    x.valid = 1;
-    return s0 + l;
-  }
-};
 
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -287,7 +132,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
   int longest;
   const float weight = plan_weight(p, bq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add(p, c, bq, cand, warp, lane);
+  plan_add(p, c.plan, bq, cand, warp, kThreads / 32, lane);
   __syncwarp();
   if (lane == 0) mbar_arrive(&c.planned);
 
@@ -295,7 +140,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     // ------------------------------------------------------------------ units, and their keys and values
     bool ok = wait_all(&c.planned, 0);
     int run = 1, units = 0, parts = 0;
-    if (ok) plan_choose(c, weight, cand, C, max_parts, lane, run, units, parts);
+    if (ok) plan_choose(c.plan, weight, cand, C, max_parts, lane, run, units, parts);
     if (blockIdx.x == 0 && lane == 0) { header->run = run; header->units = units; header->parts = parts; }
     Walk w;
     w.load(p, bq, run, lane);
@@ -809,74 +654,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
   }
 }
 
-// Merges the partials of blocks that were cut, a warp per (row, query head), and leaves the header as the next call wants
-// it. A run of a block counts for a row only where the row's query tile reaches it.
-__global__ void __launch_bounds__(256)
-paged_attn_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, Header* header,
-                        const float* __restrict__ part, int part_rows, int max_parts, int grp) {
-  pdl_trigger();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp, tq = kRows / grp, bq = 2 * tq;
-  const int run = header->run;
-  if (header->parts > 0) {
-    const float2* ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
-    for (int64_t i = (int64_t)blockIdx.x * 8 + warp; i < (int64_t)p.T * H; i += (int64_t)gridDim.x * 8) {
-      const int t = (int)(i / H), h = (int)(i - (int64_t)t * H), g = h / grp;
-      const int s = count_le(p.row_start, p.S + 1, t, lane) - 1;
-      SeqRange r;
-      if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
-      const SeqPlan f = seq_plan(r, bq, run);
-      if (f.cuts < 2) continue;
-      int before = 0;                                             // partials of the sequences before this one
-      for (int s1 = lane; s1 < s; s1 += 32) {
-        SeqRange r1;
-        if (!seq_range(p, s1, r1)) continue;
-        const SeqPlan f1 = seq_plan(r1, bq, run);
-        before += f1.cuts > 1 ? p.G * f1.nb * f1.cuts : 0;
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-      const int tok = t - f.row0, b = tok / bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
-      // the row's query tile: its last token's position decides which runs it reaches
-      const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
-      const int runs = (tiles_of(f.len - f.n + b * bq + last) + f.chunk - 1) / f.chunk;
-      const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (h - g * grp);
-      const int64_t step = (int64_t)f.nb * p.G * part_rows;       // from run to run
-      float top = -INFINITY;
-      for (int j = lane; j < runs; j += 32) top = fmaxf(top, __ldcg(ml + row0 + j * step).x);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (top == -INFINITY) top = 0.f;
-      float l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int j = 0; j < runs; ++j) {
-        const float2 x = __ldcg(ml + row0 + j * step);
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(part + (row0 + j * step) * kHeadDim) + lane);
-        const float w = fast_exp2(x.x - top);
-        l = fmaf(x.y, w, l);
-        v.x = fmaf(y.x, w, v.x); v.y = fmaf(y.y, w, v.y); v.z = fmaf(y.z, w, v.z); v.w = fmaf(y.w, w, v.w);
-      }
-      const float f1 = l == 0.f ? 0.f : 1.f / l;
-      *reinterpret_cast<uint2*>(out + i * kHeadDim + lane * 4) = make_uint2(pack_bf16(v.x * f1, v.y * f1), pack_bf16(v.z * f1, v.w * f1));
-    }
-  }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (header->taken != (unsigned)header->units && !header->gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
-    header->taken = 0;
-    header->gave_up = 0;
-  }
-}
-
-int rows_of_part(const Paged& p, int group) {
-  const int64_t rows = (int64_t)p.T * group, most = 2 * (kRows / group) * group;
-  return (int)(rows < most ? rows : most);
-}
 }  // namespace
 
 size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms) {
-  const size_t rows = (size_t)kPartsPerSm * num_sms * rows_of_part(p, group);
-  return kHeaderBytes + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
+  return paged_part_bytes(p, group, 2 * (kRows / group), num_sms);
 }
 
 int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
@@ -895,16 +676,12 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
-  const int max_parts = kPartsPerSm * num_sms, rows = rows_of_part(p, group);
-  const float scale_log2 = kLog2e / sqrtf((float)kHeadDim);
+  const int tq = kRows / group;
   if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, p, (const __nv_bfloat16*)q,
-                  (__nv_bfloat16*)out, dev_status, header, part, rows, max_parts, group, scale_log2))
+                  (__nv_bfloat16*)out, dev_status, header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
+                  kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  const int64_t warps = (int64_t)p.T * p.G * group;
-  const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
-  return launch_pdl(paged_attn_merge_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, header,
-                    (const float*)part, rows, max_parts, group)
-             ? 2 : -1;
+  return launch_paged_merge(p, group, out, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr
