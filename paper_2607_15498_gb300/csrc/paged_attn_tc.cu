@@ -166,6 +166,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         mbar_arrive(&c.u_full[un & 1]);
       }
       if (!x.valid) break;
+      for (int i = lane; i < x.ntok; i += 32)                     // the queries: read once the block before is done
+        bulk_prefetch_l2(q + ((int64_t)(x.row0 + i) * H + x.g * grp) * kHeadDim, (uint32_t)grp * kHeadDim * 2);
       int next = 0;
       if (lane == 0) next = C + (int)atomicAdd(&header->taken, 1u);
       const int32_t* table = p.table + (int64_t)s * p.max_pages;
@@ -531,20 +533,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const int both = x.both, tok0 = both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
       const bool live = wrow < rows, mine = r < rows;
       const int sees = x.pos0 + tok0 + (mine ? tok_of : 0) + 1;   // keys that this row sees
-      // the warp's own rows of the query tile, a row by 16 lanes
+      // the warp's own rows of the query tile, a row by 16 lanes (rows past the last one repeat it)
       const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (lane & 15) * 8;
       __syncwarp();
-      if (live) {                                                 // (rows past the last one repeat it)
-#pragma unroll 1
-        for (int i0 = lane >> 4; i0 < 32; i0 += 16) {
-          uint4 v[8];
+      if (live) {
+        uint4 v[16];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            v[i] = __ldg(reinterpret_cast<const uint4*>(src + __shfl_sync(0xffffffffu, row_off, min(i0 + 2 * i, rows - wrow - 1))));
+        for (int i = 0; i < 16; ++i)
+          v[i] = __ldg(reinterpret_cast<const uint4*>(src + __shfl_sync(0xffffffffu, row_off, min(2 * i + (lane >> 4), rows - wrow - 1))));
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(wrow + i0 + 2 * i, lane & 15, kRows)) = v[i];
-        }
+        for (int i = 0; i < 16; ++i)
+          *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(wrow + 2 * i + (lane >> 4), lane & 15, kRows)) = v[i];
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -575,14 +574,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
           uint32_t pk[64];
           float2 sum[2];
           float total;
-          bool known = begun && !__any_sync(0xffffffffu, mine && ref == -INFINITY);
+          bool known = begun && !__any_sync(0xffffffffu, mine && ref == -INFINITY), tried = false;
           for (;;) {
             float f = 1.f;
             if (up) { f = __uint_as_float((uint32_t)(127 - up) << 23); ref += (float)up; up = 0; }
             if (!known) {
+              // no sum to go by: the maximum of the whole tile; no reference yet: of the first 32 keys, if they show a score
               float mx = -INFINITY;
 #pragma unroll 1
-              for (int cb = 0; cb < kKeys; cb += 32) {
+              for (int cb = 0; cb < kKeys && (cb == 0 || tried || __any_sync(0xffffffffu, mine && mx == -INFINITY)); cb += 32) {
                 tmem_ld32(ts + cb, x);
                 hide(cb, x);
                 float top[4] = {mx, x[0], x[1], x[2]};
@@ -625,8 +625,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
             }
             sum[0] = add2(sum[0], sum[1]);
             total = sum[0].x + sum[0].y;
-            if (!known || !__any_sync(0xffffffffu, mine && !(total < kHuge))) break;
+            if (tried || !__any_sync(0xffffffffu, mine && !(total < kHuge))) break;
             known = false;
+            tried = true;
           }
           if (!ok) break;
           // the weights take the place of the scores
