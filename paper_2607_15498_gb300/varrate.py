@@ -308,20 +308,27 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
     """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
     ERR_ARG where a tensor is not of the cache's type, shape or device."""
     G, T = pages.heads, seqs.n_rows
-    H = G if q is None else q.shape[1]
-    if H % G or not (pages.takes_rows(k, T, G) and pages.takes_rows(v, T, G)):
-        return ERR_ARG
-    if q is not None and not (pages.takes_rows(q, T, H) and pages.takes(q_out, (T, H, 128))):
+    k_row, v_row = pages.row_stride(k, T, G), pages.row_stride(v, T, G)
+    if q is None:
+        H, q_row, q_ptr, out_ptr = G, 0, None, None
+    else:
+        H, q_ptr, out_ptr = q.shape[1], q.data_ptr(), q_out.data_ptr()
+        q_row = pages.row_stride(q, T, H)
+        if q_row < 0 or H % G or not pages.takes(q_out, (T, H, 128)):
+            return ERR_ARG
+    if k_row < 0 or v_row < 0:
         return ERR_ARG
     if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
         return ERR_ARG
-    if rot_dim and not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
-                        and freq.get_device() == pages.device):
-        return ERR_ARG
-    return lib().varrate_paged_append(pages.ref, seqs.ref, layer, H // G, _ptr(q), 0 if q is None else q.stride(0),
-                                      k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _ptr(q_norm),
-                                      _ptr(k_norm), eps, _ptr(freq), rot_dim, _ptr(q_out), _ptr(dev_status),
-                                      pages.stream(stream))
+    freq_ptr = None
+    if rot_dim:
+        freq_ptr = freq.data_ptr()
+        if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
+                and freq.get_device() == pages.device):
+            return ERR_ARG
+    return (_lib or lib()).varrate_paged_append(
+        pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, _ptr(q_norm),
+        _ptr(k_norm), eps, freq_ptr, rot_dim, out_ptr, _ptr(dev_status), pages.stream(stream))
 
 
 def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
@@ -333,8 +340,8 @@ def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream
     shape = (seqs.n_rows, pages.heads * group, 128)
     if not (pages.takes(q, shape) and pages.takes(out, shape)):
         return ERR_ARG
-    return lib().varrate_paged_attn(pages.ref, seqs.ref, layer, group, q.data_ptr(), out.data_ptr(), _ptr(dev_status),
-                                    _ptr(ws), _nbytes(ws), pages.stream(stream))
+    return (_lib or lib()).varrate_paged_attn(pages.ref, seqs.ref, layer, group, q.data_ptr(), out.data_ptr(),
+                                              _ptr(dev_status), _ptr(ws), _nbytes(ws), pages.stream(stream))
 
 
 def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, dev_status, stream=None) -> int:
@@ -346,8 +353,8 @@ def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, d
     if first is not None and not (first.dtype is torch.int32 and first.is_contiguous()
                                   and first.shape == (seqs.n_seqs,) and first.get_device() == pages.device):
         return ERR_ARG
-    return lib().varrate_paged_gather(pages.ref, seqs.ref, layer, n_layers, _ptr(first), n, _ptr(k_out), _ptr(v_out),
-                                      _ptr(dev_status), pages.stream(stream))
+    return (_lib or lib()).varrate_paged_gather(pages.ref, seqs.ref, layer, n_layers, _ptr(first), n, _ptr(k_out),
+                                                _ptr(v_out), _ptr(dev_status), pages.stream(stream))
 
 
 # ------------------------------------------------------------- device-memory plumbing
@@ -448,10 +455,13 @@ class PagedCache:
         """Whether t has this shape and the cache's type and device and is dense."""
         return t.shape == shape and t.dtype is self.dtype and t.is_contiguous() and t.get_device() == self.device
 
-    def takes_rows(self, t: torch.Tensor, rows: int, heads: int) -> bool:
-        """The same for [rows][heads][d] whose rows may be apart."""
-        return (t.shape == (rows, heads, 128) and t.dtype is self.dtype and t.get_device() == self.device
-                and (t.is_contiguous() or t.stride()[1:] == (128, 1)))
+    def row_stride(self, t: torch.Tensor, rows: int, heads: int) -> int:
+        """Elements from row to row of t [rows][heads][d], whose rows may be apart, or -1 where it has not this shape, the
+        cache's type and device and dense rows."""
+        if t.shape != (rows, heads, 128) or t.dtype is not self.dtype or t.get_device() != self.device:
+            return -1
+        row, head, elem = t.stride()
+        return row if (head == 128 and elem == 1) or t.is_contiguous() else -1
 
     def stream(self, stream) -> int | None:
         """`stream` as _stream takes it; None is torch's current stream on the cache's device."""
