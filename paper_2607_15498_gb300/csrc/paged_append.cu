@@ -4,8 +4,8 @@
 // position * freq[i]. Eight lanes hold a head, sixteen elements each: for i < rot/2 eight first members of pairs and
 // their eight partners, so that a rotation needs no other lane; the mean square is three shuffles. The angle is kept in
 // turns: freq / 2 pi modulo 1 as a 64-bit integer F (one table per CTA, from doubles), so position * F mod 2^64 is the
-// angle modulo a turn, exact up to the rounding of F however far the position; its sine and cosine are taken once per
-// token and warp.
+// angle modulo a turn, exact up to the rounding of F however far the position; a warp takes sines and cosines once per
+// token, two a lane.
 // Bound by memory: every element is read and written once.
 #include "common.cuh"
 #include "paged.h"
@@ -33,29 +33,31 @@ __device__ __forceinline__ void store_raw(T* p, const Raw<T>& r) {
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.u[i];
 }
-__device__ __forceinline__ void unpack(const Raw<float>& r, float (&x)[8]) {
+// as four pairs of floats, for the packed arithmetic
+__device__ __forceinline__ void unpack(const Raw<float>& r, float2 (&x)[4]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    x[4 * i] = __uint_as_float(r.u[i].x); x[4 * i + 1] = __uint_as_float(r.u[i].y);
-    x[4 * i + 2] = __uint_as_float(r.u[i].z); x[4 * i + 3] = __uint_as_float(r.u[i].w);
+    x[2 * i] = make_float2(__uint_as_float(r.u[i].x), __uint_as_float(r.u[i].y));
+    x[2 * i + 1] = make_float2(__uint_as_float(r.u[i].z), __uint_as_float(r.u[i].w));
   }
 }
-__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16>& r, float (&x)[8]) {
+__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16>& r, float2 (&x)[4]) {
   const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ void pack(const float (&x)[8], Raw<float>& r) {
+__device__ __forceinline__ void pack(const float2 (&x)[4], Raw<float>& r) {
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    r.u[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]),
-                        __float_as_uint(x[4 * i + 3]));
+    r.u[i] = make_uint4(__float_as_uint(x[2 * i].x), __float_as_uint(x[2 * i].y), __float_as_uint(x[2 * i + 1].x),
+                        __float_as_uint(x[2 * i + 1].y));
 }
-__device__ __forceinline__ void pack(const float (&x)[8], Raw<__nv_bfloat16>& r) {
-  r.u[0] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+__device__ __forceinline__ void pack(const float2 (&x)[4], Raw<__nv_bfloat16>& r) {
+  r.u[0] = make_uint4(pack_bf16(x[0].x, x[0].y), pack_bf16(x[1].x, x[1].y), pack_bf16(x[2].x, x[2].y), pack_bf16(x[3].x, x[3].y));
+}
+__device__ __forceinline__ void load_pairs(const float* s, float2 (&x)[4]) {   // eight floats from shared memory
+  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
+  x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
 }
 
 struct AppendArgs {
@@ -70,10 +72,11 @@ struct AppendArgs {
 
 // A unit is `per` heads (a multiple of kHeads) of one token, of its H query, G key and G value heads; a warp takes it.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 3) paged_append_kernel(Paged p, AppendArgs a) {
-  constexpr int kUnroll = sizeof(T) == 2 ? 2 : 1;     // steps in flight
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 3) paged_append_kernel(Paged p, AppendArgs a) {
+  constexpr int kUnroll = sizeof(T) == 2 ? 4 : 1;     // steps in flight
   __shared__ unsigned long long turn[kHeadDim / 2];   // freq / 2 pi modulo 1, times 2^64
   __shared__ __align__(16) float weight[2][kHeadDim];
+  __shared__ __align__(16) float angle[kWarps][2][kHeadDim / 2];   // a warp's token: cosines, sines
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7;
   pdl_trigger();
   pdl_wait();
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 3) paged_append
     const T* q = static_cast<const T*>(a.q) + t * a.q_stride;
     const T* k = static_cast<const T*>(a.k) + t * a.k_stride - (int64_t)a.H * kHeadDim;
     const T* v = static_cast<const T*>(a.v) + t * a.v_stride - (int64_t)(a.H + p.G) * kHeadDim;
-    float c[8], sn[8];
+    float2 c[4], sn[4];                               // cosine and sine for this lane's pairs
     int s = 0, pos = 0, page = -1;
     bool placed = false;                              // the row's sequence and position are known
     for (int r0 = lo; r0 < hi; r0 += kHeads * kUnroll) {
@@ -123,10 +126,17 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 3) paged_append
           page = -1;
           raise_status(a.dev_status, VARRATE_ERR_CORRUPT);
         }
-        if (turns) {
+        if (a.rot) {
+          __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            sincospif(__ll2float_rn((long long)(turn[e0 + i] * (unsigned long long)pos)) * 0x1p-63f, &sn[i], &c[i]);
+          for (int i = lane; i < kHeadDim / 2; i += 32)
+            if (i < a.rot / 2)
+              sincospif(__ll2float_rn((long long)(turn[i] * (unsigned long long)pos)) * 0x1p-63f, &angle[warp][1][i], &angle[warp][0][i]);
+          __syncwarp();
+          if (turns) {
+            load_pairs(angle[warp][0] + e0, c);
+            load_pairs(angle[warp][1] + e0, sn);
+          }
         }
         placed = true;
       }
@@ -135,28 +145,32 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 3 : 3) paged_append
         const int row = r0 + kHeads * i + (lane >> 3);
         const bool is_q = row < a.H, is_v = row >= a.H + p.G;
         const bool normed = is_q ? nq != nullptr : nk != nullptr && !is_v;
-        if (nq || nk || a.rot) {            // else every head is a copy
-          float y0[8], y1[8];
+        if ((nq || nk || a.rot) && r0 + kHeads * i < a.H + p.G) {   // else the warp's heads are copies
+          float2 y0[4], y1[4];
           unpack(x0[i], y0);
           unpack(x1[i], y1);
           if (nq || nk) {
-            float ss = 0.f;
+            float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ss = fmaf(y0[j], y0[j], fmaf(y1[j], y1[j], ss));
+            for (int j = 0; j < 4; ++j) sq = fma2(y0[j], y0[j], fma2(y1[j], y1[j], sq));
+            float ss = sq.x + sq.y;
 #pragma unroll
             for (int o = 4; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
             if (normed) {
-              const float f = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
-              const float* w = weight[is_q ? 0 : 1];
+              const float f1 = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
+              const float2 f = make_float2(f1, f1);
+              float2 w0[4], w1[4];
+              load_pairs(weight[is_q ? 0 : 1] + e0, w0);
+              load_pairs(weight[is_q ? 0 : 1] + e1, w1);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) { y0[j] = y0[j] * f * w[e0 + j]; y1[j] = y1[j] * f * w[e1 + j]; }
+              for (int j = 0; j < 4; ++j) { y0[j] = mul2(mul2(y0[j], f), w0[j]); y1[j] = mul2(mul2(y1[j], f), w1[j]); }
             }
           }
           if (turns) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float z = fmaf(-y1[j], sn[j], y0[j] * c[j]);
-              y1[j] = fmaf(y0[j], sn[j], y1[j] * c[j]);
+            for (int j = 0; j < 4; ++j) {
+              const float2 z = fma2(make_float2(-y1[j].x, -y1[j].y), sn[j], mul2(y0[j], c[j]));
+              y1[j] = fma2(y0[j], sn[j], mul2(y1[j], c[j]));
               y0[j] = z;
             }
           }

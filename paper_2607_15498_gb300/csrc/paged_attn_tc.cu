@@ -86,19 +86,6 @@ __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(reinterpret_cast<uint64_t&>(d))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(reinterpret_cast<uint64_t&>(d))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-  return d;
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __nv_bfloat16* __restrict__ q,
                      __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
