@@ -9,8 +9,8 @@
 // Two softmax warpgroups (thread = row) work in turn, so that the products of one run under the softmax of the other:
 //   a block of more than tq new tokens gives each warpgroup a query tile of its own, and both use every key tile;
 //   a smaller one (a decode step) gives both the same query tile and every second key tile, merged at the end.
-// The reference of a row (log2 units) is its first tile's maximum and moves only when a tile's weights sum to more than kMove;
-// then its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
+// The reference of a row (log2 units) is the maximum of its first 32 scores and moves only when weights would sum to more than
+// kMost: then to the maximum, and its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
 //
 // Units of work (paged_plan.cuh) are taken by one CTA per SM: the first by its number, the others from a counter in the
 // workspace; paged_attn_merge_kernel merges the partials.
@@ -45,12 +45,12 @@ constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // iss
 constexpr int kRows = 128;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
-// Weights of a tile may sum to kMove above the reference before it moves (nothing is lost in floating point, sums have room
-// for values of 2^127 / kMove / keys); a sum past kHuge, or no number, is not used.
-constexpr float kMove = 0x1p24f, kHuge = 0x1p96f;
+// Weights of half a tile may sum to kMost above the reference before it moves: nothing is lost in floating point, and the
+// accumulators have room for values of 2^127 / kMost / keys.
+constexpr float kMost = 0x1p40f;
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], o1_full, o1_empty, planned;
+  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], p_half[2], o_half[2], o1_full, o1_empty, planned;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
@@ -103,7 +103,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
-      mbar_init(&c.drain[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
     mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads / 32);
     c.err = 0;
@@ -265,15 +265,25 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
           ok = wait_all(&c.full[slot], value.phase);
           if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
           if (ok && queued) ok = wait_all(&c.full[key.slot], key.phase);
-          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_full[e], par_p);
+          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_half[e], par_p);
           if (!ok) break;
-          par_p ^= 1;
           tc_fence_after();
           const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
           if (elect_one()) {
 #pragma unroll
-            for (int ks = 0; ks < kKeys / 16; ++ks)
+            for (int ks = 0; ks < kKeys / 32; ++ks)
               tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
+            tc_commit(&c.o_half[e]);
+          }
+          __syncwarp();
+          ok = wait_all(&c.p_full[e], par_p);
+          if (!ok) break;
+          par_p ^= 1;
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
+              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
             tc_commit(&c.o_full[e]);
             tc_commit(&c.empty[slot]);
             if (queued) scores();
@@ -399,7 +409,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     uint32_t n_s = 0, n_o = 0, n_both = 0;                        // score tiles, value products, merged units so far
     bool ok = true;
     float ref = -INFINITY, l = 0.f;                               // reference, sum
-    int up = 0;                                                   // how far the reference has to move before the next tile
+    bool unset = true;                                            // some row of the warp has no reference yet
     bool begun = false;                                           // the accumulator holds something of this unit
     // Pass nu: the output of unit nu - 1, the queries of unit nu, its tiles. (The code between the tiles is kept short: it
     // is fetched anew each time.)
@@ -519,7 +529,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const Unit& x = c.unit[nu & 1];
       const int both = x.both, tok0 = both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
       const bool live = wrow < rows, mine = r < rows;
-      const int sees = x.pos0 + tok0 + (mine ? tok_of : 0) + 1;   // keys that this row sees
+      const int sees = x.pos0 + tok0 + tok_of + 1;                // keys that this row sees
       // the warp's own rows of the query tile, a row by 16 lanes (rows past the last one repeat it)
       const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (lane & 15) * 8;
       __syncwarp();
@@ -535,10 +545,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&c.q_full[e]);
+      const int first_sees = __shfl_sync(0xffffffffu, sees, 0);   // the least of the warp
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
       ref = -INFINITY;
       l = 0.f;
-      up = 0;
+      unset = true;
       begun = false;
       for (int t = x.t0 + (both ? e : 0); t < last; t += step) {
         ok = wait_all(&c.s_full[e], n_s & 1);
@@ -547,88 +558,109 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         tc_fence_after();
         if (live) {
           const int lim = sees - t * kKeys;
-          const bool cut = __any_sync(0xffffffffu, lim < kKeys);
+          const bool cut = first_sees - t * kKeys < kKeys;        // some row of the warp does not see the whole tile
           auto hide = [&](int cb, float (&s)[32]) {
             if (cut) {
 #pragma unroll
               for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
             }
           };
-          // The weights from the reference as it is. Their sum says whether the reference has to move: past kMove it
-          // does so before the next tile (these weights still stand); a sum that is not finite, or no reference yet:
-          // first the maximum of the tile, then the weights again.
+          // The weights from the reference as it is, in halves of 64 keys, each handed on by itself. If their sum is no
+          // number below kMost: the maximum of the scores first, then the weights again.
           float x[32];
-          uint32_t pk[64];
-          float2 sum[2];
-          float total;
-          bool known = begun && !__any_sync(0xffffffffu, mine && ref == -INFINITY), tried = false;
-          for (;;) {
-            float f = 1.f;
-            if (up) { f = __uint_as_float((uint32_t)(127 - up) << 23); ref += (float)up; up = 0; }
-            if (!known) {
-              // no sum to go by: the maximum of the whole tile; no reference yet: of the first 32 keys, if they show a score
-              float mx = -INFINITY;
-#pragma unroll 1
-              for (int cb = 0; cb < kKeys && (cb == 0 || tried || __any_sync(0xffffffffu, mine && mx == -INFINITY)); cb += 32) {
-                tmem_ld32(ts + cb, x);
-                hide(cb, x);
-                float top[4] = {mx, x[0], x[1], x[2]};
-#pragma unroll
-                for (int k = 3; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], x[k]);
-                mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-              }
-              mx *= scale_log2;
-              if (mine && mx > ref) { f *= ref == -INFINITY ? 0.f : fast_exp2(ref - mx); ref = mx; }
-            }
-            if (__any_sync(0xffffffffu, f != 1.f)) {
-              l *= f;
-              if (begun) {                                        // the accumulator's last product has ended
-                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int cb = 0; cb < kHeadDim; cb += 32) {
-                  tmem_ld32(to + cb, x);
-#pragma unroll
-                  for (int k = 0; k < 32; ++k) x[k] *= f;
-                  tmem_st32(to + cb, x);
-                }
-              }
-            }
+          uint32_t pk[32];
+          auto weights = [&](int cb0) {
             const float off1 = ref == -INFINITY ? 0.f : -ref;
             const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(off1, off1);
-            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int cb = 0; cb < kKeys; cb += 32) {
-              tmem_ld32(ts + cb, x);
-              hide(cb, x);
+            for (int i = 0; i < 2; ++i) {
+              tmem_ld32(ts + cb0 + 32 * i, x);
+              hide(cb0 + 32 * i, x);
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
                 const float2 a = fma2(make_float2(x[2 * k], x[2 * k + 1]), sc, off);
                 const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
                 sum[k & 1] = add2(sum[k & 1], w);
-                pk[cb / 2 + k] = pack_bf16(w.x, w.y);
+                pk[16 * i + k] = pack_bf16(w.x, w.y);
               }
             }
             sum[0] = add2(sum[0], sum[1]);
-            total = sum[0].x + sum[0].y;
-            if (tried || !__any_sync(0xffffffffu, mine && !(total < kHuge))) break;
-            known = false;
+            return sum[0].x + sum[0].y;
+          };
+          // the reference up to the maximum of the scores from column cb on; `some`: up to the first 32 that show one
+          auto raise = [&](int cb, bool some) {
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (bool first = true; cb < kKeys && (first || !some || __any_sync(0xffffffffu, mine && mx == -INFINITY)); cb += 32, first = false) {
+              tmem_ld32(ts + cb, x);
+              hide(cb, x);
+              float top[4] = {mx, x[0], x[1], x[2]};
+#pragma unroll
+              for (int k = 3; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], x[k]);
+              mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            }
+            mx *= scale_log2;
+            float f = 1.f;
+            if (mine && mx > ref) { f = ref == -INFINITY ? 0.f : fast_exp2(ref - mx); ref = mx; }
+            return f;
+          };
+          auto rescale = [&](float f) {                           // the accumulator, whose products have ended
+            tc_fence_after();
+#pragma unroll 1
+            for (int cb = 0; cb < kHeadDim; cb += 32) {
+              tmem_ld32(to + cb, x);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) x[k] *= f;
+              tmem_st32(to + cb, x);
+            }
+          };
+          auto unusable = [&](float sum) { return __any_sync(0xffffffffu, mine && !(sum < kMost)); };
+          float total;
+          bool tried = false;
+          for (;;) {
+            if (tried || unset) {                                 // (the same for the warp)
+              const float f = raise(0, !tried);
+              l *= f;
+              if (begun) {
+                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
+                if (!ok) break;
+                rescale(f);
+              }
+            }
+            total = weights(0);
+            if (tried || !unusable(total)) break;
             tried = true;
           }
           if (!ok) break;
           // the weights take the place of the scores
-          tmem_st32(ts, *reinterpret_cast<const float(*)[32]>(pk));
-          tmem_st32(ts + 32, *reinterpret_cast<const float(*)[32]>(pk + 32));
-          l += total;
-          if (mine && total > kMove && total < kHuge) up = (int)(__float_as_uint(total) >> 23) - 127;
+          tmem_st32(ts, reinterpret_cast<const float(&)[32]>(pk));
           tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c.p_half[e]);
+          float rest = weights(64);
+          if (!tried && unusable(rest)) {
+            const float f = raise(64, false);
+            l *= f;
+            total *= f;
+            ok = wait_all(&c.o_half[e], n_o & 1);                 // the first half is in the accumulator
+            if (!ok) break;
+            rescale(f);
+            rest = weights(64);
+          }
+          tmem_st32(ts + 32, reinterpret_cast<const float(&)[32]>(pk));
+          l += total + rest;
+          tmem_wait_st();
+        } else if (lane == 0) {
+          mbar_arrive(&c.p_half[e]);
         }
         begun = true;
         ++n_o;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&c.p_full[e]);
+        unset = __any_sync(0xffffffffu, mine && ref == -INFINITY);
       }
       if (!ok) break;
     }

@@ -321,3 +321,18 @@ def test_pool_of_more_than_2_to_the_32_elements():
         assert torch.equal(x, y)
     want, tol = attn_ref(b, q_outs[0])
     close(outs[1][0], want, tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("jump", [30.0, 90.0, 400.0, 3000.0])
+@pytest.mark.parametrize("at", [5, 40, 70, 100, 130, 200, 300])
+def test_attn_a_score_far_above_those_before_it(dtype, jump, at):
+    """One key whose score stands `jump` above all others, in each quarter of a key tile, in the first tile and later ones:
+    the running reference moves by a little, by much, or past what a weight can hold."""
+    for lens in ([(1, 400)], [(130, 271)]):
+        b = Batch(lens, dtype, 1, 4)
+        q = b.rows(b.H)
+        q[..., 0] = 16.0
+        b.pool[:, :, 0, :, :, 0] = 0.0
+        b.pool[0, b.table_host[0, at // b.ps], 0, 0, at % b.ps, 0] = jump * D ** 0.5 / 16.0
+        run_attn(b, q=q)
