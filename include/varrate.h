@@ -383,8 +383,8 @@ typedef struct {
  * row_start[s] >= 0 new tokens in rows row_start[s] .. row_start[s + 1] - 1; kv_len[s] counts its tokens, the
  * new ones included, so the one in row row_start[s] + i has position kv_len[s] - n_s + i. Rows
  * before row_start[0] and from row_start[n_seqs] on belong to no sequence (a batch padded to a captured
- * size): nothing is read from them or written to them. Entries of page_table past a sequence's last
- * page are not looked at.
+ * size): they have no part in any result and nothing is written to them. Entries of page_table past a
+ * sequence's last page are not looked at.
  * A sequence with row_start out of order or outside [0, n_rows], with kv_len[s] outside
  * [n_s, max_pages * page_size], or with a page number outside [0, n_pages) among those that the call
  * reads or writes raises VARRATE_ERR_CORRUPT in *dev_status; its results are not to be trusted (rows may

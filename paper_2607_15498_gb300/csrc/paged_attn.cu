@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = 64, kStep = 32;      // keys of a step
+constexpr float kOverhead = 0.25f;         // of a unit, in key tiles, as the plan counts it
 constexpr int kPitch = kHeadDim + 4;       // floats of a query or key row: 16-byte reads of 8 rows fall on 32 banks
 constexpr int kPPitch = kStep + 4;
 
@@ -53,7 +54,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
   plan_add(p, sm.plan, tq, cand, warp, kThreads / 32, lane);
   __syncthreads();
   int run, units, parts;
-  plan_choose(sm.plan, weight, cand, C, max_parts, lane, run, units, parts);
+  plan_choose(sm.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
   if (blockIdx.x == 0) {
     if (tid == 0) { header->run = run; header->units = units; header->parts = parts; }
     for (int s = tid; s < p.S; s += kThreads) {
@@ -117,10 +118,11 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
     }
     int buf = 0;
-    for (int k0 = k_first; k0 < end; k0 += kStep, buf ^= 1) {
+    for (int k0 = k_first; k0 < end; k0 += kStep, buf ^= 1) {   // (a warp has 8 of the rows)
       cp_async_wait<0>();
       __syncthreads();                        // these keys are there, the other buffer is free
       if (k0 + kStep < end) fetch(k0 + kStep, buf ^ 1);
+      if (8 * warp >= rows) continue;         // no row of this warp's
       float s[4][2] = {};
 #pragma unroll 8
       for (int d = 0; d < kHeadDim; d += 4) {

@@ -43,6 +43,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kRows = 128;
+constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // Weights of half a tile may sum to kMost above the reference before it moves: nothing is lost in floating point, and the
@@ -127,7 +128,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     // ------------------------------------------------------------------ units, and their keys and values
     bool ok = wait_all(&c.planned, 0);
     int run = 1, units = 0, parts = 0;
-    if (ok) plan_choose(c.plan, weight, cand, C, max_parts, lane, run, units, parts);
+    if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
     if (blockIdx.x == 0 && lane == 0) { header->run = run; header->units = units; header->parts = parts; }
     Walk w;
     w.load(p, bq, run, lane);

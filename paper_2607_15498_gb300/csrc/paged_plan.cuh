@@ -15,7 +15,6 @@ namespace vr {
 
 constexpr int kKeys = 128;                                  // of a key tile
 constexpr int kCand = 32;
-constexpr int kOverhead = 2;                                // of a unit, in key tiles (start, output)
 constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
 constexpr int kNone = 0x7fff;                               // kSpecial: no such value
 
@@ -59,7 +58,7 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
 // j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
-// not hold are left out. Same for every CTA. Lane = candidate; the warps share the sequences and add up in plan_add, one
+// not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the warps share the sequences and add up in plan_add, one
 // warp decides in plan_choose.
 __device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
   float w = 0.f;
@@ -97,12 +96,13 @@ __device__ __forceinline__ void plan_add(const Paged& p, PlanSums& c, int bq, in
   }
   if (u) { atomicAdd(&c.units[lane], u); atomicAdd(&c.split[lane], split); atomicMax(&c.chunk[lane], chunk); }
 }
-__device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand, int C, int max_parts, int lane, int& run, int& units, int& parts) {
+__device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand, int C, int max_parts, float overhead, int lane,
+                                            int& run, int& units, int& parts) {
   const int u = c.units[lane];
   float est = INFINITY;
   if (c.split[lane] <= max_parts) {
-    const float total = W + (float)kOverhead * u, mean = total / fmaxf((float)u, 1.f);
-    est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, c.chunk[lane] + kOverhead - mean));
+    const float total = W + overhead * (float)u, mean = total / fmaxf((float)u, 1.f);
+    est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, (float)c.chunk[lane] + overhead - mean));
   }
   int best = lane;
 #pragma unroll
