@@ -364,8 +364,10 @@ varrate_status varrate_anchor_residual(const varrate_config* cfg, const void* k,
  * a prompt is prefilled and attends over them (varrate_paged_append, varrate_paged_attn), takes
  * the finished prompt out for varrate_encode, and the newer tokens for the exact tail of the
  * decode calls (varrate_paged_gather). The library keeps no state about it: pages are handed out by
- * the caller. Limits: head_dim == 128, 1 <= group <= 8, page_size a power of two in [16, 256],
- * n_pages * 2 * n_kv_heads * page_size < 2^31 (VARRATE_ERR_UNSUPPORTED otherwise). */
+ * the caller. Limits: head_dim == 128, 1 <= group <= 8, page_size a power of two in [16, 256], n_kv_heads <= 4096,
+ * n_pages * 2 * n_kv_heads * page_size < 2^31 (VARRATE_ERR_UNSUPPORTED otherwise). The kernels are launched
+ * with programmatic stream serialization; the rule of varrate_decode_attn applies to a following
+ * kernel launched with that attribute. */
 
 /* The pages. Token u of a sequence is row u mod page_size of the page with the number
  * page_table[u / page_size]; one page number stands for that page of every layer. */
@@ -386,7 +388,7 @@ typedef struct {
  * size): they have no part in any result and nothing is written to them. Entries of page_table past a
  * sequence's last page are not looked at.
  * A sequence with row_start out of order or outside [0, n_rows], with kv_len[s] outside
- * [n_s, max_pages * page_size], or with a page number outside [0, n_pages) among those that the call
+ * [n_s, min(max_pages * page_size, 2^31 - 256)], or with a page number outside [0, n_pages) among those that the call
  * reads or writes raises VARRATE_ERR_CORRUPT in *dev_status; its results are not to be trusted (rows may
  * stay unwritten), the other sequences' are, as long as their rows are not claimed twice. */
 typedef struct {

@@ -376,7 +376,7 @@ static varrate_status paged_check(const varrate_pages* pages, const varrate_seqs
     return VARRATE_ERR_ARG;
   if (pages->head_dim != vr::kHeadDim) return VARRATE_ERR_UNSUPPORTED;
   const int32_t ps = pages->page_size;
-  if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0) return VARRATE_ERR_UNSUPPORTED;
+  if (ps < 16 || ps > 256 || (ps & (ps - 1)) != 0 || pages->n_kv_heads > 4096) return VARRATE_ERR_UNSUPPORTED;
   if ((double)pages->n_pages * 2.0 * pages->n_kv_heads * ps > (double)INT32_MAX) return VARRATE_ERR_UNSUPPORTED;
   return VARRATE_OK;
 }

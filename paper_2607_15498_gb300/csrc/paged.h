@@ -25,6 +25,8 @@ __host__ __device__ __forceinline__ int64_t page_row(const Paged& p, int page, i
   return ((((int64_t)page * 2 + kv) * p.G + g) << p.page_log2) + in_page;
 }
 
+constexpr int kMaxLen = 0x7fffff00;   // tokens of a sequence: positions a key tile further stay below 2^31
+
 // What one sequence brings: its first row, its new tokens and all of its tokens; false where the tables
 // are out of range (see varrate_seqs).
 struct SeqRange {
@@ -33,7 +35,7 @@ struct SeqRange {
 __device__ __forceinline__ bool seq_range(const Paged& p, int s, SeqRange& r) {
   const int a = __ldg(p.row_start + s), b = __ldg(p.row_start + s + 1), len = __ldg(p.kv_len + s);
   r.row0 = a; r.n = b - a; r.len = len;
-  return a >= 0 && b >= a && b <= p.T && len >= r.n && len <= ((int64_t)p.max_pages << p.page_log2);
+  return a >= 0 && b >= a && b <= p.T && len >= r.n && len <= kMaxLen && len <= ((int64_t)p.max_pages << p.page_log2);
 }
 
 // Entries of a[0 .. n) that are <= t, a sorted; one warp. (Unsorted: some number in [0, n].)

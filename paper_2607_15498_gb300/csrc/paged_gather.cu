@@ -34,7 +34,7 @@ paged_gather_kernel(Paged p, int layer0, int n_layers, const int32_t* __restrict
     uint4* out = c ? v_out : k_out;
     if (out == nullptr) continue;
     const int f = first ? __ldg(first + s) : 0, len = __ldg(p.kv_len + s);
-    if (f < 0 || (int64_t)f + n > len || len > ((int64_t)p.max_pages << p.page_log2)) {
+    if (f < 0 || (int64_t)f + n > len || len > kMaxLen || len > ((int64_t)p.max_pages << p.page_log2)) {
       if (tid == 0) raise_status(dev_status, VARRATE_ERR_CORRUPT);
       continue;
     }

@@ -336,3 +336,88 @@ def test_attn_a_score_far_above_those_before_it(dtype, jump, at):
         b.pool[:, :, 0, :, :, 0] = 0.0
         b.pool[0, b.table_host[0, at // b.ps], 0, 0, at % b.ps, 0] = jump * D ** 0.5 / 16.0
         run_attn(b, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_of_many_sequences(dtype):
+    """More sequences than a warp looks at at once, empty ones and single tokens among them, each with few keys."""
+    run_attn(Batch([(s % 4, (7 * s) % 41 + 1) for s in range(500)], dtype, 2, 4, pad=3))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[(1, 9999)], [(1, 6000), (0, 50), (1, 31)], [(40, 5000)]], ids=str)
+def test_attn_one_head_long_context(dtype, lens):
+    """One KV head and few rows: the keys are cut into many runs, merged at the end."""
+    run_attn(Batch(lens, dtype, 1, 8, 64))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_shared_pages(dtype):
+    """Sequences that share the pages of a common prefix (read, not written)."""
+    b = Batch([(1, 95), (40, 96), (1, 200)], dtype, 2, 4)
+    b.table[1, :3] = b.table[0, :3]
+    b.table_host[1, :3] = b.table_host[0, :3]
+    b.table[2, :6] = b.table[0, :6].clone()
+    b.table_host[2, :6] = b.table_host[0, :6]
+    run_attn(b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_workspace_found_used(dtype):
+    """A counter that is not zero is reported once; the next call on the workspace is right again."""
+    b = Batch([(150, 600), (1, 900)], dtype, 2, 4)
+    ws = b.workspace()
+    ws[0] = 3
+    q = b.rows(b.H)
+    out = torch.zeros_like(q)
+    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, ws) == V.OK
+    assert status(b) == V.ERR_CORRUPT
+    b.status.zero_()
+    run_attn(b, ws=ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_two_streams_and_two_graphs(dtype):
+    """Two batches at once on two streams, each with its workspace; then two captured graphs in turn on one workspace."""
+    bs = [Batch([(120, 700), (1, 2000)], dtype, 2, 4, seed=1), Batch([(1, 1500), (9, 100)], dtype, 2, 4, seed=2)]
+    qs = [b.rows(b.H) for b in bs]
+    refs = [attn_ref(b, q) for b, q in zip(bs, qs)]
+    outs, wss = [torch.zeros_like(q) for q in qs], [b.workspace() for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, q, out, ws, s in zip(bs, qs, outs, wss, streams):
+            assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, ws, stream=s) == V.OK
+    torch.cuda.synchronize()
+    for b, out, (want, tol) in zip(bs, outs, refs):
+        close(out, want, tol)
+        assert status(b) == V.OK
+    ws = max(wss, key=lambda w: w.numel())
+    graphs = []
+    for b, q, out in zip(bs, qs, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, ws) == V.OK
+        graphs.append(g)
+    for _ in range(3):
+        for out in outs:
+            out.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for b, out, (want, tol) in zip(bs, outs, refs):
+            close(out, want, tol)
+            assert status(b) == V.OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_is_the_same_from_call_to_call(dtype):
+    b = Batch([(150, 900), (1, 3000), (30, 30)], dtype, 2, 4)
+    q, ws = b.rows(b.H), b.workspace()
+    first = torch.zeros_like(q)
+    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, first, b.status, ws) == V.OK
+    for _ in range(5):
+        out = torch.zeros_like(q)
+        assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, ws) == V.OK
+        assert torch.equal(out, first)
+    assert status(b) == V.OK

@@ -33,7 +33,7 @@ def gather(V, p, s, layer=0, layers=1, first=None, n=7, k=A, v=A, status=None):
     ("head_dim", 64, -5), ("page_size", 8, -5), ("page_size", 48, -5), ("page_size", 512, -5), ("page_size", 0, -1),
     ("n_pages", 0, -1), ("n_layers", 0, -1), ("n_kv_heads", 0, -1), ("dtype", 2, -1), ("n_seqs", -1, -1),
     ("n_rows", -1, -1), ("max_pages", 0, -1), ("pool", 0, -1), ("pool", A + 8, -1), ("kv_len", 0, -1),
-    ("page_table", 0, -1), ("kv_len", A + 4, -1), ("n_pages", 2 ** 30, -5)])
+    ("page_table", 0, -1), ("kv_len", A + 4, -1), ("n_pages", 2 ** 30, -5), ("n_kv_heads", 4097, -5)])
 def test_bad_descriptions(vlib, field, value, want):
     for call in (append, attn, gather):
         assert call(vlib, *structs(vlib, **{field: value})) == want
