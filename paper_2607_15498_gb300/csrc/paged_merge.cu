@@ -12,61 +12,79 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
 }
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 
-// A warp per (row, query head), and leaves the header as the next call wants
-// it. A run of a block counts for a row only where the row's query tile reaches it.
+// A warp per (row, query head); a lane has four columns. A run of a block counts for a row only where the row's query tile
+// reaches it. Eight runs are read at once, merged with the running reference and sum.
+// Bound by latency: what a row needs is read in two steps, first header and tables, then its partials.
 template <typename T>
 __global__ void __launch_bounds__(256)
-paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Header* header,
-                        const float* __restrict__ part, int part_rows, int max_parts, int grp, int tq, int bq) {
+paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Header* header, const float* __restrict__ part,
+                        int part_rows, int max_parts, int grp, int tq, int bq) {
+  constexpr int kBatch = 8;
+  const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
-  const int run = header->run;
-  if (header->parts > 0) {
-    const float2* ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
-    for (int64_t i = (int64_t)blockIdx.x * 8 + warp; i < (int64_t)p.T * H; i += (int64_t)gridDim.x * 8) {
-      const int t = (int)(i / H), h = (int)(i - (int64_t)t * H), g = h / grp;
-      const int s = count_le(p.row_start, p.S + 1, t, lane) - 1;
-      SeqRange r;
-      if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
-      const SeqPlan f = seq_plan(r, bq, run);
-      if (f.cuts < 2) continue;
-      int before = 0;                                             // partials of the sequences before this one
-      for (int s1 = lane; s1 < s; s1 += 32) {
-        SeqRange r1;
-        if (!seq_range(p, s1, r1)) continue;
-        const SeqPlan f1 = seq_plan(r1, bq, run);
+  const Header h = *header;
+  const float2* ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
+  const unsigned total = (unsigned)p.T * H;                       // rows of 128 elements: below 2^31
+  for (unsigned i = blockIdx.x * 8 + warp; i < total; i += gridDim.x * 8) {
+    const int t = (int)(i / H), hq = (int)(i - (unsigned)t * H);
+    const int s = count_le(p.row_start, p.S + 1, t, (int)lane) - 1;
+    SeqRange r;
+    if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
+    if (h.parts == 0) break;
+    const SeqPlan f = seq_plan(r, bq, h.run);
+    if (f.cuts < 2) continue;
+    int before = 0;                                               // partials of the sequences before this one
+    for (int s0 = 0; s0 < s; s0 += 32) {
+      SeqRange r1;
+      if (s0 + (int)lane < s && seq_range(p, s0 + lane, r1)) {
+        const SeqPlan f1 = seq_plan(r1, bq, h.run);
         before += f1.cuts > 1 ? p.G * f1.nb * f1.cuts : 0;
       }
+    }
+    if (s > 0) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-      const int tok = t - f.row0, b = tok / bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
-      // the row's query tile: its last token's position decides which runs it reaches
-      const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
-      const int runs = (tiles_of(f.len - f.n + b * bq + last) + f.chunk - 1) / f.chunk;
-      const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (h - g * grp);
-      const int64_t step = (int64_t)f.nb * p.G * part_rows;       // from run to run
-      float top = -INFINITY;
-      for (int j = lane; j < runs; j += 32) top = fmaxf(top, __ldcg(ml + row0 + j * step).x);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (top == -INFINITY) top = 0.f;
-      float l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int j = 0; j < runs; ++j) {
-        const float2 x = __ldcg(ml + row0 + j * step);
-        const float4 y = __ldcg(reinterpret_cast<const float4*>(part + (row0 + j * step) * kHeadDim) + lane);
-        const float w = fast_exp2(x.x - top);
-        l = fmaf(x.y, w, l);
-        v.x = fmaf(y.x, w, v.x); v.y = fmaf(y.y, w, v.y); v.z = fmaf(y.z, w, v.z); v.w = fmaf(y.w, w, v.w);
-      }
-      const float f1 = l == 0.f ? 0.f : 1.f / l;
-      store4(out + i * kHeadDim + lane * 4, make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1));
     }
+    const int g = hq / (unsigned)grp, tok = t - f.row0, b = (unsigned)tok / (unsigned)bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
+    // the row's query tile: its last token's position decides which runs it reaches
+    const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
+    const int runs = (unsigned)(tiles_of(f.len - f.n + b * bq + last) + f.chunk - 1) / (unsigned)f.chunk;
+    const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (hq - g * grp);
+    const int64_t step = (int64_t)f.nb * p.G * part_rows;         // from run to run
+    float m = -INFINITY, l = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j0 = 0; j0 < runs; j0 += kBatch) {
+      float2 x[kBatch];
+      float4 y[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        x[j] = make_float2(-INFINITY, 0.f);
+        y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j0 + j < runs) {
+          x[j] = __ldcg(ml + row0 + (j0 + j) * step);
+          y[j] = __ldcg(reinterpret_cast<const float4*>(part + (row0 + (j0 + j) * step) * kHeadDim) + lane);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) top = fmaxf(top, x[j].x);
+      const float ref = top == -INFINITY ? 0.f : top, f0 = fast_exp2(m - ref);
+      m = top;
+      l *= f0;
+      v.x *= f0; v.y *= f0; v.z *= f0; v.w *= f0;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const float w = fast_exp2(x[j].x - ref);
+        l = fmaf(x[j].y, w, l);
+        v.x = fmaf(y[j].x, w, v.x); v.y = fmaf(y[j].y, w, v.y); v.z = fmaf(y[j].z, w, v.z); v.w = fmaf(y[j].w, w, v.w);
+      }
+    }
+    const float f1 = l == 0.f ? 0.f : 1.f / l;
+    store4(out + (int64_t)i * kHeadDim + lane * 4, make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1));
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (header->taken != (unsigned)header->units && !header->gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+    if (h.taken != (unsigned)h.units && !h.gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     header->taken = 0;
     header->gave_up = 0;
   }

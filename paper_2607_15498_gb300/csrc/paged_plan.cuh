@@ -44,10 +44,10 @@ struct SeqPlan {
 __device__ __forceinline__ SeqPlan seq_plan(const SeqRange& r, int bq, int run) {
   SeqPlan q;
   q.row0 = r.row0; q.n = r.n; q.len = r.len;
-  q.nb = (r.n + bq - 1) / bq;
+  q.nb = (unsigned)(r.n + bq - 1) / (unsigned)bq;
   q.tiles = tiles_of(r.len);
-  q.cuts = q.nb ? (q.tiles + run - 1) / run : 0;
-  q.chunk = q.nb ? (q.tiles + q.cuts - 1) / q.cuts : 0;
+  q.cuts = q.nb ? (unsigned)(q.tiles + run - 1) / (unsigned)run : 0;
+  q.chunk = q.nb ? (unsigned)(q.tiles + q.cuts - 1) / (unsigned)q.cuts : 0;
   return q;
 }
 
@@ -67,7 +67,7 @@ __device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, i
     SeqRange r;
     if (!seq_range(p, s, r) || r.n == 0) continue;
     const int last = tiles_of(r.len), first = tiles_of(r.len - r.n + min(bq, r.n));
-    w += (float)((r.n + bq - 1) / bq) * (0.5f * (float)(first + last));
+    w += (float)((unsigned)(r.n + bq - 1) / (unsigned)bq) * (0.5f * (float)(first + last));
     most = max(most, last);
   }
 #pragma unroll
@@ -155,7 +155,7 @@ struct Walk {
     f.cuts = __shfl_sync(0xffffffffu, q.cuts, l); f.chunk = __shfl_sync(0xffffffffu, q.chunk, l);
     const int units = p.G * f.nb * f.cuts;
     const int at = u - before - (__shfl_sync(0xffffffffu, incl, l) - units);
-    const int gb = at / p.G, j = gb / f.nb, b = f.nb - 1 - (gb - j * f.nb);
+    const int gb = (unsigned)at / (unsigned)p.G, j = (unsigned)gb / (unsigned)f.nb, b = f.nb - 1 - (gb - j * f.nb);
     x.g = at - gb * p.G;
     x.ntok = min(bq, f.n - b * bq);
     x.row0 = f.row0 + b * bq;
