@@ -83,6 +83,25 @@ __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem,
       " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// 64 fp32 columns of this warp's 32 TMEM lanes.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+      "}, [%64];\n tcgen05.wait::ld.sync.aligned;\n"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+      : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
@@ -154,8 +173,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
         mbar_arrive(&c.u_full[un & 1]);
       }
       if (!x.valid) break;
-      for (int i = lane; i < x.ntok; i += 32)                     // the queries: read once the block before is done
-        bulk_prefetch_l2(q + ((int64_t)(x.row0 + i) * H + x.g * grp) * kHeadDim, (uint32_t)grp * kHeadDim * 2);
       int next = 0;
       if (lane == 0) next = C + (int)atomicAdd(&header->taken, 1u);
       const int32_t* table = p.table + (int64_t)s * p.max_pages;
@@ -574,17 +591,23 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
             const float off1 = ref == -INFINITY ? 0.f : -ref;
             const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(off1, off1);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            float s[64];
+            tmem_ld64(ts + cb0, s);
+            if (cut) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              tmem_ld32(ts + cb0 + 32 * i, x);
-              hide(cb0 + 32 * i, x);
+              for (int k = 0; k < 64; ++k) s[k] = cb0 + k < lim ? s[k] : -INFINITY;
+            }
 #pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const float2 a = fma2(make_float2(x[2 * k], x[2 * k + 1]), sc, off);
-                const float2 w = make_float2(fast_exp2(a.x), fast_exp2(a.y));
-                sum[k & 1] = add2(sum[k & 1], w);
-                pk[16 * i + k] = pack_bf16(w.x, w.y);
-              }
+            for (int k = 0; k < 32; ++k) {
+              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
+              s[2 * k] = fast_exp2(a.x);
+              s[2 * k + 1] = fast_exp2(a.y);
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float2 w = make_float2(s[2 * k], s[2 * k + 1]);
+              sum[k & 1] = add2(sum[k & 1], w);
+              pk[k] = pack_bf16(w.x, w.y);
             }
             sum[0] = add2(sum[0], sum[1]);
             return sum[0].x + sum[0].y;
@@ -617,50 +640,40 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
             }
           };
           auto unusable = [&](float sum) { return __any_sync(0xffffffffu, mine && !(sum < kMost)); };
-          float total;
-          bool tried = false;
-          for (;;) {
-            if (tried || unset) {                                 // (the same for the warp)
-              const float f = raise(0, !tried);
-              l *= f;
-              if (begun) {
-                ok = wait_all(&c.o_full[e], (n_o - 1) & 1);
-                if (!ok) break;
-                rescale(f);
+          // one body for both halves: the loop has to be short, instructions are fetched anew when it is not
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            float total;
+            bool tried = false;
+            for (;;) {
+              if (tried || (unset && half == 0)) {                // (the same for the warp)
+                const float f = raise(64 * half, !tried);
+                l *= f;
+                if (begun || half) {                              // the accumulator's last products have ended
+                  ok = wait_all(half ? &c.o_half[e] : &c.o_full[e], half ? n_o & 1 : (n_o - 1) & 1);
+                  if (!ok) break;
+                  rescale(f);
+                }
               }
+              total = weights(64 * half);
+              if (tried || !unusable(total)) break;
+              tried = true;
             }
-            total = weights(0);
-            if (tried || !unusable(total)) break;
-            tried = true;
+            if (!ok) break;
+            tmem_st32(ts + 32 * half, reinterpret_cast<const float(&)[32]>(pk));   // in place of the scores
+            l += total;
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(half ? &c.p_full[e] : &c.p_half[e]);
           }
           if (!ok) break;
-          // the weights take the place of the scores
-          tmem_st32(ts, reinterpret_cast<const float(&)[32]>(pk));
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&c.p_half[e]);
-          float rest = weights(64);
-          if (!tried && unusable(rest)) {
-            const float f = raise(64, false);
-            l *= f;
-            total *= f;
-            ok = wait_all(&c.o_half[e], n_o & 1);                 // the first half is in the accumulator
-            if (!ok) break;
-            rescale(f);
-            rest = weights(64);
-          }
-          tmem_st32(ts + 32, reinterpret_cast<const float(&)[32]>(pk));
-          l += total + rest;
-          tmem_wait_st();
         } else if (lane == 0) {
           mbar_arrive(&c.p_half[e]);
+          mbar_arrive(&c.p_full[e]);
         }
         begun = true;
         ++n_o;
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.p_full[e]);
         unset = __any_sync(0xffffffffu, mine && ref == -INFINITY);
       }
       if (!ok) break;
