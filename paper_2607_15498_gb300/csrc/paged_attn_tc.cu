@@ -37,6 +37,7 @@
 namespace vr {
 
 bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
+bool make_tmap_heads_bf16(CUtensorMap* map, const void* base, uint32_t heads, uint64_t rows, uint32_t box_heads, uint32_t box_rows);
 
 namespace {
 
@@ -102,12 +103,35 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
         "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
       : "r"(taddr) : "memory");
 }
+// Piece j of lane i to piece i of lane j, in groups of four lanes.
+__device__ __forceinline__ void transpose4(uint4 (&y)[4], int lane) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const bool up = lane & (1 << b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i & (1 << b)) continue;
+      uint4 &a = y[i], &c = y[i | (1 << b)];
+      uint4 t = up ? a : c;
+      t.x = __shfl_xor_sync(0xffffffffu, t.x, 1 << b);
+      t.y = __shfl_xor_sync(0xffffffffu, t.y, 1 << b);
+      t.z = __shfl_xor_sync(0xffffffffu, t.z, 1 << b);
+      t.w = __shfl_xor_sync(0xffffffffu, t.w, 1 << b);
+      if (up) a = t; else c = t;
+    }
+  }
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n"
+      ::"r"(dst), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
 #pragma unroll
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
 }
 __global__ void __launch_bounds__(kThreads, 1)
-paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __nv_bfloat16* __restrict__ q,
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, Paged p, const __nv_bfloat16* __restrict__ q,
                      __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
                      float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -122,7 +146,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       mbar_init(&c.full[i], 1); mbar_init(&c.empty[i], 2); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 4);
+      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 1);
       mbar_init(&c.drain[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
     mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads / 32);
@@ -424,17 +448,27 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
     const int row_off = (tok_of * H + r % grp) * kHeadDim;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
-    uint32_t n_s = 0, n_o = 0, n_both = 0;                        // score tiles, value products, merged units so far
+    uint32_t n_s = 0, n_o = 0, n_both = 0, n_q = 0;               // score tiles, value products, merged units, query tiles so far
     bool ok = true;
     float ref = -INFINITY, l = 0.f;                               // reference, sum
     bool unset = true;                                            // some row of the warp has no reference yet
     bool begun = false;                                           // the accumulator holds something of this unit
-    // Pass nu: the output of unit nu - 1, the queries of unit nu, its tiles. (The code between the tiles is kept short: it
+    // Pass nu: the queries of unit nu on their way, the output of unit nu - 1, the tiles of nu. (The code between the tiles is kept short: it
     // is fetched anew each time.)
     for (uint32_t nu = 0;; ++nu) {
       ok = wait_all(&c.u_full[nu & 1], (nu >> 1) & 1);
       if (!ok) break;
       const bool valid = c.unit[nu & 1].valid;
+      // this warpgroup's query tile: the products that read the last one have ended, as its scores were all there
+      n_q += valid;
+      if (valid && wrow == 0 && lane == 0) {
+        const Unit& x = c.unit[nu & 1];
+        mbar_arrive_expect_tx(&c.q_full[e], (uint32_t)(tq * grp) * 256);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          tma_load_3d(q_addr + e * kTileBytes + half * (kRows * 128), &tmap_q, half * 64, x.g * grp, x.row0 + (x.both ? 0 : e * tq), &c.q_full[e]);
+      }
+      __syncwarp();
       if (nu > 0) {
         const uint32_t un = nu - 1;
         const Unit& x = c.unit[un & 1];
@@ -476,9 +510,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
           const int special = c.any_special[un & 1];
           const float f = l == 0.f ? 0.f : 1.f / l;
           const bool whole = x.slot < 0;                          // else a partial
-          // 32 columns of the warp's rows at a time through its own 4 KB of the query tile's first half (whose products have
-          // ended), so that a row's 16-byte pieces leave next to each other
-          uint4* stage = reinterpret_cast<uint4*>(smem + e * kTileBytes + wrow * 128);
+          // 32 columns of the warp's rows at a time, 16-byte pieces exchanged between four lanes, so that a row's pieces leave
+          // next to each other
           float* dst_part = part + ((int64_t)x.slot * part_rows + tok0 * grp + wrow) * kHeadDim;
           __nv_bfloat16* dst = out + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim;
 #pragma unroll 1
@@ -504,29 +537,32 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
               }
             }
             if (whole) {
+              uint4 y[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                stage[lane * 4 + (k ^ ((lane >> 1) & 3))] =
-                    make_uint4(pack_bf16(v[8 * k] * f, v[8 * k + 1] * f), pack_bf16(v[8 * k + 2] * f, v[8 * k + 3] * f),
-                               pack_bf16(v[8 * k + 4] * f, v[8 * k + 5] * f), pack_bf16(v[8 * k + 6] * f, v[8 * k + 7] * f));
-              __syncwarp();
+                y[k] = make_uint4(pack_bf16(v[8 * k] * f, v[8 * k + 1] * f), pack_bf16(v[8 * k + 2] * f, v[8 * k + 3] * f),
+                                  pack_bf16(v[8 * k + 4] * f, v[8 * k + 5] * f), pack_bf16(v[8 * k + 6] * f, v[8 * k + 7] * f));
+              transpose4(y, lane);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int in = 8 * i + (lane >> 2), k = lane & 3, off = __shfl_sync(0xffffffffu, row_off, in);
-                if (wrow + in < rows)
-                  *reinterpret_cast<uint4*>(dst + off + cb + 8 * k) = stage[in * 4 + (k ^ ((in >> 1) & 3))];
+                const int in = (lane & ~3) + i, off = __shfl_sync(0xffffffffu, row_off, in);
+                if (wrow + in < rows) *reinterpret_cast<uint4*>(dst + off + cb + 8 * (lane & 3)) = y[i];
               }
             } else if (begun) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k)
-                stage[lane * 8 + (k ^ (lane & 7))] = make_uint4(__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]),
-                                                               __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3]));
-              __syncwarp();
+              for (int h = 0; h < 2; ++h) {
+                uint4 y[4];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int in = 4 * i + (lane >> 3), k = lane & 7;
-                if (wrow + in < rows)
-                  *reinterpret_cast<uint4*>(dst_part + (int64_t)in * kHeadDim + cb + 4 * k) = stage[in * 8 + (k ^ (in & 7))];
+                for (int k = 0; k < 4; ++k)
+                  y[k] = make_uint4(__float_as_uint(v[16 * h + 4 * k]), __float_as_uint(v[16 * h + 4 * k + 1]),
+                                    __float_as_uint(v[16 * h + 4 * k + 2]), __float_as_uint(v[16 * h + 4 * k + 3]));
+                transpose4(y, lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int in = (lane & ~3) + i;
+                  if (wrow + in < rows)
+                    *reinterpret_cast<uint4*>(dst_part + (int64_t)in * kHeadDim + cb + 16 * h + 4 * (lane & 3)) = y[i];
+                }
               }
             }
           }
@@ -548,21 +584,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       const int both = x.both, tok0 = both ? 0 : e * tq, rows = min(tq, x.ntok - tok0) * grp;
       const bool live = wrow < rows, mine = r < rows;
       const int sees = x.pos0 + tok0 + tok_of + 1;                // keys that this row sees
-      // the warp's own rows of the query tile, a row by 16 lanes (rows past the last one repeat it)
-      const __nv_bfloat16* src = q + ((int64_t)(x.row0 + tok0) * H + x.g * grp) * kHeadDim + (lane & 15) * 8;
-      __syncwarp();
-      if (live) {
-        uint4 v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          v[i] = __ldg(reinterpret_cast<const uint4*>(src + __shfl_sync(0xffffffffu, row_off, min(2 * i + (lane >> 4), rows - wrow - 1))));
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          *reinterpret_cast<uint4*>(smem + e * kTileBytes + sw128_offset(wrow + 2 * i + (lane >> 4), lane & 15, kRows)) = v[i];
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&c.q_full[e]);
       const int first_sees = __shfl_sync(0xffffffffu, sees, 0);   // the least of the warp
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
       ref = -INFINITY;
@@ -678,7 +699,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const __
       }
       if (!ok) break;
     }
-    if (!ok) c.err = 1;
+    if (!ok) {
+      c.err = 1;
+      if (n_q > 0) wait_all(&c.q_full[e], (n_q - 1) & 1);         // no copy is in flight when the block ends
+    }
   }
   __syncthreads();
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
@@ -703,15 +727,16 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
       return -1;
     if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
   }
-  CUtensorMap tmap;
+  CUtensorMap tmap, tmap_q;
   const int ps = 1 << p.page_log2;
   if (!make_tmap_rows_bf16(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim * 2, (uint64_t)p.layer_rows, ps < kKeys ? ps : kKeys))
     return -1;
+  if (!make_tmap_heads_bf16(&tmap_q, q, (uint32_t)(p.G * group), (uint64_t)p.T, (uint32_t)group, (uint32_t)(kRows / group))) return -1;
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group;
-  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, p, (const __nv_bfloat16*)q,
+  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (const __nv_bfloat16*)q,
                   (__nv_bfloat16*)out, dev_status, header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
                   kLog2e / sqrtf((float)kHeadDim)))
     return -1;

@@ -9,8 +9,10 @@
 
 namespace vr {
 
-bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows) {
-  // driver entry point, looked up once per process (every thread that looks it up finds the same)
+namespace {
+
+// driver entry point, looked up once per process (every thread that looks it up finds the same); null if there is none
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
   static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> cached{nullptr};
   PFN_cuTensorMapEncodeTiled_v12000 encode = cached.load(std::memory_order_acquire);
   if (encode == nullptr) {
@@ -19,10 +21,18 @@ bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
             cudaSuccess ||
         q != cudaDriverEntryPointSuccess || fn == nullptr)
-      return false;
+      return nullptr;
     encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
     cached.store(encode, std::memory_order_release);
   }
+  return encode;
+}
+
+}  // namespace
+
+bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows) {
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = encoder();
+  if (encode == nullptr) return false;
   // [rows][128] bf16, row-major; boxes of 64 columns (128 B, one swizzle span) x box_rows rows
   const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)kHeadDim * 2};
@@ -31,6 +41,20 @@ bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
                 estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// [rows][heads][128] bf16, dense; boxes of 64 columns x box_heads heads x box_rows rows, so that a box is
+// box_rows * box_heads rows of 128 bytes in shared memory. Rows past the last one read as zeros.
+bool make_tmap_heads_bf16(CUtensorMap* map, const void* base, uint32_t heads, uint64_t rows, uint32_t box_heads, uint32_t box_rows) {
+  const PFN_cuTensorMapEncodeTiled_v12000 encode = encoder();
+  if (encode == nullptr) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)heads, (cuuint64_t)rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, (cuuint64_t)heads * kHeadDim * 2};
+  const cuuint32_t box[3] = {64, box_heads, box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace vr
