@@ -5,7 +5,9 @@
 // whole group. Scores of 32 keys at a time, four rows and two keys a thread; a warp's weights go through its own
 // part of shared memory to the values, four rows and eight columns a thread. Keys and values are copied asynchronously,
 // one buffer ahead; two CTAs an SM.
-// Bound by the fp32 pipe and the reads of shared memory beside it.
+// Bound by the fp32 pipe and the reads of shared memory beside it: 1469 new tokens of two sequences, 4 heads over 1, 84 to 99 us
+// (16 to 19 TFLOP/s of what is seen). Without cuts over the keys and with copies a
+// step waits for: 187 us.
 #include <math.h>
 
 #include <atomic>
@@ -20,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = 64, kStep = 32;      // keys of a step
-constexpr float kOverhead = 0.25f;         // of a unit, in key tiles, as the plan counts it
+constexpr float kOverhead = 0.25f;         // of a unit, in key tiles, as the plan counts it: that chunk 84 to 99 us; at 2 104 to 120, at 4 227
 constexpr int kPitch = kHeadDim + 4;       // floats of a query or key row: 16-byte reads of 8 rows fall on 32 banks
 constexpr int kPPitch = kStep + 4;
 

@@ -11,17 +11,30 @@
 //   a smaller one (a decode step) gives both the same query tile and every second key tile, merged at the end.
 // The reference of a row (log2 units) is the maximum of its first 32 scores and moves only when weights would sum to more than
 // kMost: then to the maximum, and its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
+// Weights are handed on in halves of 64 keys: the products of the first run while the second is made.
 //
 // Units of work (paged_plan.cuh) are taken by one CTA per SM: the first by its number, the others from a counter in the
 // workspace; paged_attn_merge_kernel merges the partials.
 //
 // Values at positions that a row does not see have weight 0 in P, and 0 times an infinity is no number: in the tiles
-// where that can happen two warps zero every value past the block's last token, and values that are not finite and
-// that only a part of the block's tokens sees are zeroed too, remembered (kSpecial) and added to the rows that see them.
+// where that can happen one warp zeroes every value past the block's last token, and values that are not finite and
+// that only a part of the block's tokens sees are zeroed too, remembered (Ctl::special) and added to the rows that see them.
 //
-// Warps: 0-3, 4-7 softmax; 8 TMA producer; 9, 10 issue the products of one softmax warpgroup each (the tensor core takes
-// few products ahead, so that a single issuing warp's waits would stand in its way); 11 values. Every wait is bounded; one that gives up
-// raises VARRATE_ERR_TIMEOUT, its CTA takes no further unit and ends after its copies and products in flight have.
+// Warps: 0-3, 4-7 softmax; 8 TMA producer of keys and values; 9, 10 issue the products of one softmax warpgroup each (the
+// tensor core takes few products ahead, so that a single issuing warp's waits would stand in its way), in turns of a tile,
+// which keeps the warpgroups half a period apart; 11 values. Every wait is bounded; one that gives up raises
+// VARRATE_ERR_TIMEOUT, its CTA takes no further unit and ends after its copies and products in flight have.
+//
+// Bound by the tensor cores for prompts: 8192 tokens, 32 heads over 8: 333 us, 1650 TFLOP/s (88 % of the rate of a large bf16
+// product); 512 tokens on 131072: 645 us, 1700 (91 %). By memory for decode steps: eight sequences of 32768 tokens
+// 170 us, 6.3 TB/s (93 % of a copy). By latency for short ones: 900 tokens of one sequence 13.8 us, two launches and
+// one pass through code that is not in the instruction caches; a unit costs 2 to 4 us beside its tiles (output, queries, first scores).
+// What was measured on the way, on that prompt: one issuing warp 609 us, its values in uniform registers 569, two issuing
+// warps 541, in turns and with the weights in halves 474, no maximum in the steady state 427, output and
+// queries in short coalesced loops 405, one threshold for the reference and no votes ahead of the weights 369, one body for
+// both halves with 64 scores a load 342, queries by TMA 333. With a maximum of every tile 473 instead of 427, without the
+// turns 448; with the output in a function that is not inlined 406 instead of 366. Partials merged by the last CTA of a block
+// instead of a kernel: 89 to 117 us instead of 76 on a mixed step, as its loads stand in the way of the next unit.
 #include <math.h>
 #include <stddef.h>
 
@@ -44,15 +57,18 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kRows = 128;
-constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it
+constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it. 512 tokens on 131072, when it took
+                                                            // 680 us: at 1 677, at 4 and 6 690
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // Weights of half a tile may sum to kMost above the reference before it moves: nothing is lost in floating point, and the
 // accumulators have room for values of 2^127 / kMost / keys.
 constexpr float kMost = 0x1p40f;
+
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_full[2], o_full[2], q_full[2], u_full[2], u_empty[2], u_looked[2], drain[2], turn[2], p_half[2], o_half[2], o1_full, o1_empty, planned;
+  uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_full[2], q_full[2], turn[2], drain[2];   // by warpgroup
+  uint64_t u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, planned;
   Unit unit[2];
   union {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
