@@ -16,8 +16,7 @@ namespace vr {
 constexpr int kKeys = 128;                                  // of a key tile
 constexpr int kCand = 32;
 constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
-constexpr int kNone = 0x7fff;                               // kSpecial: no such value
-
+constexpr int kNone = 0x7fff;                               // Ctl::special of the bf16 kernel: no such value
 
 // Workspace: header, then the partials: values [rows][d], then (reference, sum) [rows].
 struct Header {
@@ -58,8 +57,8 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
 // j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
-// not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the warps share the sequences and add up in plan_add, one
-// warp decides in plan_choose.
+// not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the
+// warps share the sequences and add up in plan_add, one warp decides in plan_choose.
 __device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
   float w = 0.f;
   int most = 0;
