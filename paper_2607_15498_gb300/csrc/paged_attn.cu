@@ -21,8 +21,8 @@ namespace vr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 64, kStep = 32;      // keys of a step
-constexpr float kOverhead = 0.25f;         // of a unit, in key tiles, as the plan counts it: that chunk 84 to 99 us; at 2 104 to 120, at 4 227
+constexpr int kRows = 64, kStep = kKeysF32;      // keys of a step
+constexpr float kOverhead = 2.f;         // of a unit, in key tiles, as the plan counts it: that chunk 84 to 99 us; at 2 104 to 120, at 4 227
 constexpr int kPitch = kHeadDim + 4;       // floats of a query or key row: 16-byte reads of 8 rows fall on 32 banks
 constexpr int kPPitch = kStep + 4;
 
@@ -33,7 +33,7 @@ struct Smem {
   float p[kRows][kPPitch];
   PlanSums plan;
   Unit unit;
-  int seq, run, units;
+  int seq, next;
 };
 
 __device__ __forceinline__ float4 get4(const float* s) { return *reinterpret_cast<const float4*>(s); }
@@ -51,9 +51,9 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
   __syncthreads();
   pdl_wait();
   int longest;
-  const float weight = plan_weight(p, tq, lane, longest);
+  const float weight = plan_weight<kStep>(p, tq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add(p, sm.plan, tq, cand, warp, kThreads / 32, lane);
+  plan_add<kStep>(p, sm.plan, tq, cand, warp, kThreads / 32, lane);
   __syncthreads();
   int run, units, parts;
   plan_choose(sm.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
@@ -64,26 +64,30 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     }
   }
-  Walk w;
+  Walk<kStep> w;
   if (warp == 0) w.load(p, tq, run, lane);
   int u = blockIdx.x;
   while (u < units) {
-    // the unit: found by one warp, which also takes the next one's number
+    // the unit: found by one warp
     if (warp == 0) {
       Unit x;
       const int s = w.find(p, tq, tq, run, u, lane, x);
       if (lane == 0) {
         sm.unit = x;
         sm.seq = s;
-        sm.units = C + (int)atomicAdd(&header->taken, 1u);
       }
     }
     __syncthreads();
     const Unit x = sm.unit;
-    u = sm.units;
     const int32_t* table = p.table + (int64_t)sm.seq * p.max_pages;
-    const int rows = x.ntok * grp, end = min(x.pos0 + x.ntok, x.t1 * kKeys), k_first = x.t0 * kKeys;
+    const int rows = x.ntok * grp, end = min(x.pos0 + x.ntok, x.t1 * kStep), k_first = x.t0 * kStep;
     const float* qb = q + ((int64_t)x.row0 * H + (int64_t)x.g * grp) * kHeadDim;
+    if (k_first >= end) {                     // the block ends before this run of keys
+      if (tid == 0) sm.next = C + (int)atomicAdd(&header->taken, 1u);
+      __syncthreads();
+      u = sm.next;
+      continue;
+    }
     // asynchronous copy of 32 keys and values from `k0` on: 4 rows of each a warp; past the end: zeros
     auto fetch = [&](int k0, int buf) {
 #pragma unroll
@@ -101,7 +105,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       }
       cp_async_commit();
     };
-    if (k_first < end) fetch(k_first, 0);
+    fetch(k_first, 0);
     for (int i = tid; i < kRows * 32; i += kThreads) {
       const int row = i >> 5, c = (i & 31) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -119,11 +123,12 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
     }
-    int buf = 0;
+    int buf = 0, next = 0;
     for (int k0 = k_first; k0 < end; k0 += kStep, buf ^= 1) {   // (a warp has 8 of the rows)
       cp_async_wait<0>();
       __syncthreads();                        // these keys are there, the other buffer is free
       if (k0 + kStep < end) fetch(k0 + kStep, buf ^ 1);
+      else if (tid == 0) next = C + (int)atomicAdd(&header->taken, 1u);   // not earlier: others may be free before this CTA
       if (8 * warp >= rows) continue;         // no row of this warp's
       float s[4][2] = {};
 #pragma unroll 8
@@ -194,7 +199,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       float sum = l[i];
 #pragma unroll
       for (int w2 = 8; w2 > 0; w2 >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w2);
-      if (row >= rows || k_first >= end) continue;
+      if (row >= rows) continue;
       const bool whole = x.slot < 0;
       const float f = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
       const int64_t pr = (int64_t)x.slot * part_rows + row;
@@ -204,7 +209,9 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       if (!whole && tx == 0)                  // references of partials are in log2 units; a row without a weight has no say
         reinterpret_cast<float2*>(part + (int64_t)max_parts * part_rows * kHeadDim)[pr] = make_float2(sum == 0.f ? -INFINITY : m[i] * kLog2e, sum);
     }
+    if (tid == 0) sm.next = next;
     __syncthreads();                          // queries, buffers and the unit are free
+    u = sm.next;
   }
 }
 

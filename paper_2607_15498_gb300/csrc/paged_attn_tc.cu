@@ -56,7 +56,7 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
-constexpr int kRows = 128;
+constexpr int kRows = 128, kKeys = kKeysBf16;
 constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it. 512 tokens on 131072, when it took
                                                             // 680 us: at 1 677, at 4 and 6 690
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
@@ -177,9 +177,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   const uint32_t tmem = c.tmem;
   pdl_wait();
   int longest;
-  const float weight = plan_weight(p, bq, lane, longest);
+  const float weight = plan_weight<kKeys>(p, bq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add(p, c.plan, bq, cand, warp, kThreads / 32, lane);
+  plan_add<kKeys>(p, c.plan, bq, cand, warp, kThreads / 32, lane);
   __syncwarp();
   if (lane == 0) mbar_arrive(&c.planned);
 
@@ -189,7 +189,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     int run = 1, units = 0, parts = 0;
     if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
     if (blockIdx.x == 0 && lane == 0) { header->run = run; header->units = units; header->parts = parts; }
-    Walk w;
+    Walk<kKeys> w;
     w.load(p, bq, run, lane);
     const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box
     const int per_tile = kKeys / page_keys;

@@ -19,7 +19,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Header* header, const float* __restrict__ part,
                         int part_rows, int max_parts, int grp, int tq, int bq) {
-  constexpr int kBatch = 8;
+  constexpr int kBatch = 8, kKeys = sizeof(T) == 4 ? kKeysF32 : kKeysBf16;
   const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
   pdl_trigger();
   pdl_wait();
@@ -32,13 +32,13 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     SeqRange r;
     if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
     if (h.parts == 0) break;
-    const SeqPlan f = seq_plan(r, bq, h.run);
+    const SeqPlan f = seq_plan<kKeys>(r, bq, h.run);
     if (f.cuts < 2) continue;
     int before = 0;                                               // partials of the sequences before this one
     for (int s0 = 0; s0 < s; s0 += 32) {
       SeqRange r1;
       if (s0 + (int)lane < s && seq_range(p, s0 + lane, r1)) {
-        const SeqPlan f1 = seq_plan(r1, bq, h.run);
+        const SeqPlan f1 = seq_plan<kKeys>(r1, bq, h.run);
         before += f1.cuts > 1 ? p.G * f1.nb * f1.cuts : 0;
       }
     }
@@ -49,7 +49,7 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     const int g = hq / (unsigned)grp, tok = t - f.row0, b = (unsigned)tok / (unsigned)bq, in = tok - b * bq, ntok = min(bq, f.n - b * bq);
     // the row's query tile: its last token's position decides which runs it reaches
     const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
-    const int runs = (unsigned)(tiles_of(f.len - f.n + b * bq + last) + f.chunk - 1) / (unsigned)f.chunk;
+    const int runs = (unsigned)(tiles_of<kKeys>(f.len - f.n + b * bq + last) + f.chunk - 1) / (unsigned)f.chunk;
     const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (hq - g * grp);
     const int64_t step = (int64_t)f.nb * p.G * part_rows;         // from run to run
     float m = -INFINITY, l = 0.f;

@@ -13,7 +13,7 @@
 
 namespace vr {
 
-constexpr int kKeys = 128;                                  // of a key tile
+constexpr int kKeysBf16 = 128, kKeysF32 = 32;               // of a key tile: what a kernel takes at a time
 constexpr int kCand = 32;
 constexpr int kPartsPerSm = 4;                              // partial units that the workspace holds, per SM
 constexpr int kNone = 0x7fff;                               // Ctl::special of the bf16 kernel: no such value
@@ -34,17 +34,19 @@ struct Unit {
 };
 
 // Key tiles that hold the first `keys` keys (keys < 2^32).
+template <int kKeys>
 __device__ __forceinline__ int tiles_of(uint32_t keys) { return (int)((keys + (kKeys - 1)) / kKeys); }
 
 // Blocks, key tiles and cuts of one sequence.
 struct SeqPlan {
   int row0, n, len, nb, tiles, cuts, chunk;
 };
+template <int kKeys>
 __device__ __forceinline__ SeqPlan seq_plan(const SeqRange& r, int bq, int run) {
   SeqPlan q;
   q.row0 = r.row0; q.n = r.n; q.len = r.len;
   q.nb = (unsigned)(r.n + bq - 1) / (unsigned)bq;
-  q.tiles = tiles_of(r.len);
+  q.tiles = tiles_of<kKeys>(r.len);
   q.cuts = q.nb ? (unsigned)(q.tiles + run - 1) / (unsigned)run : 0;
   q.chunk = q.nb ? (unsigned)(q.tiles + q.cuts - 1) / (unsigned)q.cuts : 0;
   return q;
@@ -59,13 +61,14 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
 // not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the
 // warps share the sequences and add up in plan_add, one warp decides in plan_choose.
+template <int kKeys>
 __device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
   float w = 0.f;
   int most = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
     if (!seq_range(p, s, r) || r.n == 0) continue;
-    const int last = tiles_of(r.len), first = tiles_of(r.len - r.n + min(bq, r.n));
+    const int last = tiles_of<kKeys>(r.len), first = tiles_of<kKeys>(r.len - r.n + min(bq, r.n));
     w += (float)((unsigned)(r.n + bq - 1) / (unsigned)bq) * (0.5f * (float)(first + last));
     most = max(most, last);
   }
@@ -82,12 +85,13 @@ __device__ __forceinline__ int plan_candidate(float W, int longest, int C, int l
   const float k = ceilf(W * (float)(16 + (lane & 3)) / (16.f * (float)(1 + (lane >> 2)) * (float)C));
   return min(max(1, (int)fminf(k, 1e9f)), longest + 1);
 }
+template <int kKeys>
 __device__ __forceinline__ void plan_add(const Paged& p, PlanSums& c, int bq, int cand, int warp, int warps, int lane) {
   int u = 0, split = 0, chunk = 0;
   for (int s = warp; s < p.S; s += warps) {
     SeqRange r;
     if (!seq_range(p, s, r)) continue;
-    const SeqPlan q = seq_plan(r, bq, cand);
+    const SeqPlan q = seq_plan<kKeys>(r, bq, cand);
     const int n = p.G * q.nb * q.cuts;
     u += n;
     split += q.cuts > 1 ? n : 0;
@@ -116,6 +120,7 @@ __device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand
 }
 
 // Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
+template <int kKeys>
 struct Walk {
   int s0 = 0, before = 0, parts_before = 0;     // first sequence held; units and partials before it
   int incl, parts_incl, total, parts;           // scans over the sequences held, and their sums
@@ -126,7 +131,7 @@ struct Walk {
     r.n = 0; r.len = 0; r.row0 = 0;
     if (s0 + lane < p.S && !seq_range(p, s0 + lane, r)) r.n = 0;
     if (r.n == 0) r.len = 0;
-    q = seq_plan(r, bq, run);
+    q = seq_plan<kKeys>(r, bq, run);
     incl = p.G * q.nb * q.cuts;
     parts_incl = q.cuts > 1 ? incl : 0;
 #pragma unroll
@@ -159,11 +164,11 @@ struct Walk {
     x.ntok = min(bq, f.n - b * bq);
     x.row0 = f.row0 + b * bq;
     x.pos0 = f.len - f.n + b * bq;
-    const int end = x.pos0 + x.ntok, tiles = tiles_of(end);
+    const int end = x.pos0 + x.ntok, tiles = tiles_of<kKeys>(end);
     x.t0 = j * f.chunk;
     x.t1 = min(x.t0 + f.chunk, tiles);
     x.both = x.ntok <= tq;
-    x.e0 = max(x.t0, min(x.t1, tiles_of((uint32_t)x.pos0 + tq)));
+    x.e0 = max(x.t0, min(x.t1, tiles_of<kKeys>((uint32_t)x.pos0 + tq)));
     x.slot = f.cuts > 1 ? parts_before + __shfl_sync(0xffffffffu, parts_incl, l) - units + at : -1;
     x.values_from = max(x.t0, x.ntok > 1 ? (x.pos0 + 1) / kKeys : end / kKeys);
     x.valid = 1;
