@@ -5,9 +5,12 @@
 // whole group. Scores of 32 keys at a time, four rows and two keys a thread; a warp's weights go through its own
 // part of shared memory to the values, four rows and eight columns a thread. Keys and values are copied asynchronously,
 // one buffer ahead; two CTAs an SM.
-// Bound by the fp32 pipe and the reads of shared memory beside it: 1469 new tokens of two sequences, 4 heads over 1, 84 to 99 us
-// (16 to 19 TFLOP/s of what is seen). Without cuts over the keys and with copies a
-// step waits for: 187 us.
+// Bound by the fp32 pipe and the latencies around it (16 warps an SM): 1469 new tokens of two sequences, 4 heads over 1, 64 us,
+// 25 TFLOP/s. One token each of 59 sequences of up to 490, 48 heads over 8, 48 us, 1.2 TB/s.
+// What was measured on the way, on the first: no cuts over the keys 187 us; cuts in tiles of 128 keys 84 to 99, in steps of 32
+// with the next unit taken at the start of one 115, in its last step 64. 64 rows by 128 threads with 8 x 4 scores each:
+// 90 us at tiles of 128. Packed products change 1 %, a prefetch to L2 nothing, and units of at most 8 rows with the keys
+// shared among the warps take 43 us on the second, but 5 to 12 % more on small steps.
 #include <math.h>
 
 #include <atomic>
@@ -22,7 +25,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = 64, kStep = kKeysF32;      // keys of a step
-constexpr float kOverhead = 2.f;         // of a unit, in key tiles, as the plan counts it: that chunk 84 to 99 us; at 2 104 to 120, at 4 227
+constexpr float kOverhead = 2.f;           // of a unit, in steps, as the plan counts it: 1 to 8 give the chunk the same 64 us, the
+                                           // steps of 59 sequences 50, 47, 48, 51 at 1, 2, 4, 8
 constexpr int kPitch = kHeadDim + 4;       // floats of a query or key row: 16-byte reads of 8 rows fall on 32 banks
 constexpr int kPPitch = kStep + 4;
 
