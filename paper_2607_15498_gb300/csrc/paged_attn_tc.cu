@@ -475,8 +475,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       ok = wait_all(&c.u_full[nu & 1], (nu >> 1) & 1);
       if (!ok) break;
       const bool valid = c.unit[nu & 1].valid;
-      // this warpgroup's query tile: the products that read the last one have ended, as its scores were all there
+      // this warpgroup's query tile: the products that read the last one have ended, as its scores were all there, and where
+      // the unit had no tile for this warpgroup its copy may still be on the way
       n_q += valid;
+      if (valid && wrow == 0 && nu > 0) {
+        ok = wait_all(&c.q_full[e], (nu - 1) & 1);
+        if (!ok) break;
+      }
       if (valid && wrow == 0 && lane == 0) {
         const Unit& x = c.unit[nu & 1];
         mbar_arrive_expect_tx(&c.q_full[e], (uint32_t)(tq * grp) * 256);

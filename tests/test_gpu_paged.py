@@ -345,6 +345,22 @@ def test_attn_of_many_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, ctx", [(1, 120), (20, 100)])
+def test_attn_of_one_tile_a_sequence(dtype, n, ctx):
+    """Several units in a row for every CTA, each of one key tile: one of the two query tiles has nothing to do. Again and
+    again with one workspace: the same bits."""
+    b = Batch([(n, (5 * s) % ctx) for s in range(300)], dtype, 8, 1, pad=1)
+    ws, q = b.workspace(), 2 * b.rows(b.H)
+    out = run_attn(b, ws=ws, q=q)
+    again = torch.empty_like(out)
+    for _ in range(30):
+        again.fill_(NAN)
+        assert V.varrate_paged_attn(b.pages, b.seqs, 0, 1, q, again, b.status, ws) == V.OK
+        assert torch.equal(again.view(torch.uint8), out.view(torch.uint8))
+    assert status(b) == V.OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[(1, 9999)], [(1, 6000), (0, 50), (1, 31)], [(40, 5000)]], ids=str)
 def test_attn_one_head_long_context(dtype, lens):
     """One KV head and few rows: the keys are cut into many runs, merged at the end."""
