@@ -26,7 +26,7 @@ paged_gather_kernel(Paged p, int layer0, int n_layers, const int32_t* __restrict
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     // (sequence, layer, K or V, head, chunk), the chunk fastest
     int64_t x = u / chunks;
-    const int t0 = (int)(u % chunks) * kTokens;
+    const int chunk = (int)(u % chunks);
     const int g = (int)(x % p.G);
     x /= p.G;
     const int c = (int)(x & 1);
@@ -36,9 +36,10 @@ paged_gather_kernel(Paged p, int layer0, int n_layers, const int32_t* __restrict
     if (out == nullptr) continue;
     const int f = first ? __ldg(first + s) : 0, len = __ldg(p.kv_len + s);
     if (f < 0 || (int64_t)f + n > len || len > kMaxLen || len > ((int64_t)p.max_pages << p.page_log2)) {
-      if (tid == 0) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      if (tid == 0 && chunk == 0) raise_status(dev_status, VARRATE_ERR_CORRUPT);
       continue;
     }
+    const int t0 = chunk * kTokens;                       // n is below a length now
     out += ((((int64_t)s * n_layers + l) * p.G + g) * n) * kPer + piece;
     const uint4* src = pool + (int64_t)(layer0 + l) * p.layer_rows * kPer + piece;
     int64_t from[kUnroll];
@@ -67,7 +68,7 @@ paged_gather_kernel(Paged p, int layer0, int n_layers, const int32_t* __restrict
 int launch_paged_gather(const Paged& p, int layer, int n_layers, const int32_t* first, int n, void* k_out, void* v_out,
                         int32_t* dev_status, int num_sms, cudaStream_t st) {
   const int tokens = kThreads / (p.dtype == VARRATE_F32 ? 32 : 16) * kUnroll;
-  const int chunks = (n + tokens - 1) / tokens;
+  const int chunks = n > kMaxLen ? 1 : (n + tokens - 1) / tokens;   // no sequence has more than kMaxLen
   const int64_t units = (int64_t)p.S * n_layers * 2 * p.G * chunks;
   const int grid = (int)(units < (int64_t)num_sms * 8 ? units : (int64_t)num_sms * 8);
   return launch_pdl(p.dtype == VARRATE_F32 ? paged_gather_kernel<512> : paged_gather_kernel<256>, dim3(grid), kThreads, 0, st,

@@ -291,6 +291,17 @@ def test_gather_range_out_of_sequence():
                 assert (outs[1][s] == 5).all()
 
 
+def test_gather_of_more_tokens_than_a_sequence_may_have():
+    """As many as the argument holds, which no sequence has: nothing is written."""
+    b = Batch([(1, 99), (1, 30)], "bf16", 2, 4)
+    out = torch.full((2, 1, 2, 50, D), 5.0, dtype=b.dt, device="cuda")
+    for n in (2 ** 31 - 1, 2 ** 31 - 63, 2 ** 31 - 255):
+        b.status.zero_()
+        assert V.lib().varrate_paged_gather(b.pages.ref, b.seqs.ref, 0, 1, None, n, out.data_ptr(), None, b.status.data_ptr(),
+                                            b.pages.stream(None)) == V.OK
+        assert status(b) == V.ERR_CORRUPT and (out == 5).all()
+
+
 # ------------------------------------------------------------------------------------ offsets past 32 bits
 
 def test_pool_of_more_than_2_to_the_32_elements():
