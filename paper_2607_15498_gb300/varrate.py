@@ -19,6 +19,14 @@ Typical use (one encode of a prompt's cache, then one decode call per layer and 
                               ws), "varrate_decode_attn")
     # after a synchronise: status.item() is OK (0), FLOOR_BINDS (1) or a negative error
 
+While a prompt is prefilled its keys and values stand in the pages of a PagedCache::
+
+    pages, seqs = PagedCache.allocate(n_layers, n_pages, n_kv_heads, 64), SeqBatch.of(row_start, kv_len, table, n_rows)
+    ws = paged_attn_workspace(pages, seqs, group)         # zero-filled; reusable by every call on the stream
+    check(varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out, status))
+    check(varrate_paged_attn(pages, seqs, layer, group, q_out, out, status, ws))
+    check(varrate_paged_gather(pages, seqs, 0, n_layers, None, n, k, v, status))   # for varrate_encode
+
 Shapes: q_win [B][L][w][H][d], k and v [B][L][G][N][d], bases [L][G][d][d] (row j = basis vector
 j), q and out [B][H][d]; every tensor contiguous on the GPU and 16-byte aligned.
 """
@@ -312,16 +320,17 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
     if q is None:
         H, q_row, q_ptr, out_ptr = G, 0, None, None
     else:
-        H, q_ptr, out_ptr = q.shape[1], q.data_ptr(), q_out.data_ptr()
+        H = q.shape[1] if q.dim() == 3 else 0
         q_row = pages.row_stride(q, T, H)
         if q_row < 0 or H % G or not pages.takes(q_out, (T, H, 128)):
             return ERR_ARG
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     if k_row < 0 or v_row < 0:
         return ERR_ARG
     if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
         return ERR_ARG
     freq_ptr = None
-    if rot_dim:
+    if rot_dim and freq is not None:
         freq_ptr = freq.data_ptr()
         if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
                 and freq.get_device() == pages.device):
@@ -453,15 +462,18 @@ class PagedCache:
 
     def takes(self, t: torch.Tensor, shape) -> bool:
         """Whether t has this shape and the cache's type and device and is dense."""
-        return t.shape == shape and t.dtype is self.dtype and t.is_contiguous() and t.get_device() == self.device
+        return (t is not None and t.shape == shape and t.dtype is self.dtype and t.is_contiguous()
+                and t.get_device() == self.device)
 
     def row_stride(self, t: torch.Tensor, rows: int, heads: int) -> int:
         """Elements from row to row of t [rows][heads][d], whose rows may be apart, or -1 where it has not this shape, the
         cache's type and device and dense rows."""
-        if t.shape != (rows, heads, 128) or t.dtype is not self.dtype or t.get_device() != self.device:
+        if t is None or t.shape != (rows, heads, 128) or t.dtype is not self.dtype or t.get_device() != self.device:
             return -1
         row, head, elem = t.stride()
-        return row if (head == 128 and elem == 1) or t.is_contiguous() else -1
+        if elem != 1 or (head != 128 and heads > 1):
+            return -1 if rows else 0
+        return row if rows > 1 else heads * 128      # of one row: any number
 
     def stream(self, stream) -> int | None:
         """`stream` as _stream takes it; None is torch's current stream on the cache's device."""

@@ -122,3 +122,29 @@ def test_binding_looks_at_tensors(vlib):
         V.SeqBatch.of(i32(0, 3), i32(1, 5), torch.zeros((2, 2), dtype=torch.int32), 3)
     with pytest.raises(V.VarrateError):
         V.PagedCache.of(pool.transpose(3, 4))
+
+
+def test_binding_refuses_what_is_missing(vlib):
+    V = vlib
+    pages = V.PagedCache.of(torch.zeros((1, 4, 2, 2, 16, 128), dtype=torch.bfloat16))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)   # noqa: E731
+    seqs = V.SeqBatch.of(i32(0, 1, 3), i32(1, 5), torch.zeros((2, 2), dtype=torch.int32), 3)
+    q, k = torch.zeros((3, 4, 128), dtype=torch.bfloat16), torch.zeros((3, 2, 128), dtype=torch.bfloat16)
+    freq, st = torch.zeros(64, dtype=torch.float64), torch.zeros(1, dtype=torch.int32)
+    for a in ((q, None, k, freq, q), (q, k, None, freq, q), (q, k, k, None, q), (q, k, k, freq, None), (q[0], k, k, freq, q)):
+        assert V.varrate_paged_append(pages, seqs, 0, *a[:3], None, None, 1e-6, a[3], 128, a[4], st, stream=0) == V.ERR_ARG
+    assert V.varrate_paged_attn(pages, seqs, 0, 2, None, q, st, q, stream=0) == V.ERR_ARG
+    assert V.varrate_paged_attn(pages, seqs, 0, 2, q, None, st, q, stream=0) == V.ERR_ARG
+    assert V.varrate_paged_attn(pages, seqs, 0, 2, q, q.clone(), st, None, stream=0) == V.ERR_WORKSPACE
+
+
+def test_rows_apart_in_every_form(vlib):
+    """Distance of the rows of a tensor: parts of wider rows, one head, and one row, of which it can be any number."""
+    pages = vlib.PagedCache.of(torch.zeros((1, 1, 2, 1, 16, 128), dtype=torch.bfloat16))
+    x = torch.zeros((5, 8, 128), dtype=torch.bfloat16)
+    assert pages.row_stride(x, 5, 8) == 1024 and pages.row_stride(x[:, 2:4], 5, 2) == 1024
+    assert pages.row_stride(x[:, 3:4], 5, 1) == 1024 and pages.row_stride(x[:, 3:4].transpose(0, 1), 1, 5) == -1
+    assert pages.row_stride(x.view(5, 1, 1024)[:, :, 128:256], 5, 1) == 1024
+    assert pages.row_stride(x[::2], 3, 8) == 2048 and pages.row_stride(x[:, ::2], 5, 4) == -1
+    one = torch.zeros((8, 1, 128), dtype=torch.bfloat16).transpose(0, 1)      # [1][8][d] with 128 from row to row
+    assert one.stride(0) == 128 and pages.row_stride(one, 1, 8) == 1024
