@@ -57,8 +57,8 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kRows = 128, kKeys = kKeysBf16;
-constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it. 512 tokens on 131072, when it took
-                                                            // 680 us: at 1 677, at 4 and 6 690
+constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it. 512 tokens on
+                                                            // 131072, when it took 680 us: at 1 677, at 4 and 6 690
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // Weights of half a tile may sum to kMost above the reference before it moves: nothing is lost in floating point, and the
@@ -67,7 +67,7 @@ constexpr float kMost = 0x1p40f;
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
-  uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_full[2], q_full[2], turn[2], drain[2];   // by warpgroup
+  uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_full[2], q_full[2], q_seen[2], turn[2], drain[2];   // by warpgroup
   uint64_t u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, planned;
   Unit unit[2];
   union {
@@ -147,7 +147,7 @@ __device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[
   for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
 }
 __global__ void __launch_bounds__(kThreads, 1)
-paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, Paged p, const __nv_bfloat16* __restrict__ q,
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, Paged p,
                      __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
                      float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -163,7 +163,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 1);
-      mbar_init(&c.drain[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
+      mbar_init(&c.q_seen[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
     mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads / 32);
     c.err = 0;
@@ -279,6 +280,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
       ok = wait_all(&c.q_full[e], un & 1);
       if (!ok) break;
+      if (lane == 0) mbar_arrive(&c.q_seen[e]);
       auto mine = [&](int i) { return both ? (i & 1) == e : e || i < n_first; };
       auto scores = [&]() {                                       // issued by the elected lane
         const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
@@ -469,17 +471,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     float ref = -INFINITY, l = 0.f;                               // reference, sum
     bool unset = true;                                            // some row of the warp has no reference yet
     bool begun = false;                                           // the accumulator holds something of this unit
-    // Pass nu: the queries of unit nu on their way, the output of unit nu - 1, the tiles of nu. (The code between the tiles is kept short: it
-    // is fetched anew each time.)
+    // Pass nu: the queries of unit nu on their way, the output of unit nu - 1, the tiles of nu. (The code between the tiles
+    // is kept short: it is fetched anew each time.)
     for (uint32_t nu = 0;; ++nu) {
       ok = wait_all(&c.u_full[nu & 1], (nu >> 1) & 1);
       if (!ok) break;
       const bool valid = c.unit[nu & 1].valid;
-      // this warpgroup's query tile: the products that read the last one have ended, as its scores were all there, and where
-      // the unit had no tile for this warpgroup its copy may still be on the way
+      // this warpgroup's query tile: the products that read the last one have ended, as its scores were all there; but where
+      // the unit had no tile for this warpgroup, its copy may be on the way and the issuer may not have seen it
       n_q += valid;
       if (valid && wrow == 0 && nu > 0) {
-        ok = wait_all(&c.q_full[e], (nu - 1) & 1);
+        ok = wait_all(&c.q_seen[e], (nu - 1) & 1);
         if (!ok) break;
       }
       if (valid && wrow == 0 && lane == 0) {
@@ -487,7 +489,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
         mbar_arrive_expect_tx(&c.q_full[e], (uint32_t)(tq * grp) * 256);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
-          tma_load_3d(q_addr + e * kTileBytes + half * (kRows * 128), &tmap_q, half * 64, x.g * grp, x.row0 + (x.both ? 0 : e * tq), &c.q_full[e]);
+          tma_load_3d(q_addr + e * kTileBytes + half * (kRows * 128), &tmap_q, half * 64, x.g * grp,
+                      x.row0 + (x.both ? 0 : e * tq), &c.q_full[e]);
       }
       __syncwarp();
       if (nu > 0) {
@@ -757,8 +760,7 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group;
-  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (const __nv_bfloat16*)q,
-                  (__nv_bfloat16*)out, dev_status, header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
+  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (__nv_bfloat16*)out, dev_status, header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
                   kLog2e / sqrtf((float)kHeadDim)))
     return -1;
   return launch_paged_merge(p, group, out, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
