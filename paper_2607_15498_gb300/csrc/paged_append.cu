@@ -6,10 +6,12 @@
 // turns: freq / 2 pi modulo 1 as a 64-bit integer F (one table per CTA, from doubles), so position * F mod 2^64 is the
 // angle modulo a turn, exact up to the rounding of F however far the position; a warp takes sines and cosines once per
 // token, two a lane.
-// Bound by memory: every element is read and written once. 8192 tokens of 32 + 8 + 8 heads, bf16: 38 us, 5.3 TB/s (78 % of a
-// copy); 32770 tokens of 28 + 4 + 4 heads with norms: 121 us, 5.0 TB/s. Sixteen warps an SM with four heads in flight each;
-// 24 warps with two in flight take 50 us on the first, an L2 prefetch of the next token changes nothing. A head on
-// 16 lanes that exchange the pairs by shuffles: 94 us.
+// Bound by memory: every element is read and written once. 8192 tokens of 32 + 8 + 8 heads, bf16: 37 us, 5.5 TB/s (80 % of a
+// copy); 32770 tokens of 28 + 4 + 4 heads with norms: 115 us, 5.2 TB/s. Sixteen warps an SM with sixteen heads in flight
+// each, all of them resident (with eight CTAs an SM 38 and 122). More in flight is not faster: 24 warps take 50 us on the
+// first, copies to shared memory two steps ahead 38, an L2 prefetch of the next token changes nothing. Stores that are
+// evicted first would take 36, but the attention that follows reads what they write. A head on 16 lanes that exchange the
+// pairs by shuffles: 94 us.
 #include "common.cuh"
 #include "paged.h"
 
@@ -20,6 +22,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kHeads = 4;                  // heads of a warp's step
+template <typename T> constexpr int kCtas = sizeof(T) == 2 ? 2 : 3;   // per SM
 
 // Eight elements as they are stored.
 template <typename T> struct Raw { uint4 u[sizeof(T) / 2]; };
@@ -28,7 +31,7 @@ template <typename T>
 __device__ __forceinline__ Raw<T> load_raw(const T* p) {   // (q may be q_out: no read-only loads)
   Raw<T> r;
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = reinterpret_cast<const uint4*>(p)[i];
   return r;
 }
 template <typename T>
@@ -75,7 +78,7 @@ struct AppendArgs {
 
 // A unit is `per` heads (a multiple of kHeads) of one token, of its H query, G key and G value heads; a warp takes it.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 3) paged_append_kernel(Paged p, AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtas<T>) paged_append_kernel(Paged p, AppendArgs a) {
   constexpr int kUnroll = sizeof(T) == 2 ? 4 : 1;     // steps in flight
   __shared__ unsigned long long turn[kHeadDim / 2];   // freq / 2 pi modulo 1, times 2^64
   __shared__ __align__(16) float weight[2][kHeadDim];
@@ -202,7 +205,7 @@ int launch(const Paged& p, AppendArgs& a, int layer, int num_sms, cudaStream_t s
   while (a.per > kHeads && (int64_t)p.T * ((rows + a.per - 1) / a.per) < (int64_t)num_sms * kWarps * 4)
     a.per = (a.per / 2 + kHeads - 1) / kHeads * kHeads;
   a.pool = reinterpret_cast<T*>(p.pool) + (int64_t)layer * p.layer_rows * kHeadDim;
-  const int64_t ctas = ((int64_t)p.T * ((rows + a.per - 1) / a.per) + kWarps - 1) / kWarps, most = (int64_t)num_sms * 8;
+  const int64_t ctas = ((int64_t)p.T * ((rows + a.per - 1) / a.per) + kWarps - 1) / kWarps, most = (int64_t)num_sms * kCtas<T>;
   return launch_pdl(paged_append_kernel<T>, dim3((unsigned)(ctas < most ? ctas : most)), kThreads, 0, st, p, a) ? 1 : -1;
 }
 
