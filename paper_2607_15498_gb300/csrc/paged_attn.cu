@@ -87,7 +87,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
     const int rows = x.ntok * grp, end = min(x.pos0 + x.ntok, x.t1 * kStep), k_first = x.t0 * kStep;
     const float* qb = q + ((int64_t)x.row0 * H + (int64_t)x.g * grp) * kHeadDim;
     if (k_first >= end) {                     // the block ends before this run of keys
-      if (tid == 0) sm.next = C + (int)atomicAdd(&header->taken, 1u);
+      if (tid == 0) sm.next = take_unit(header, C, units);
       __syncthreads();
       u = sm.next;
       continue;
@@ -132,7 +132,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
       cp_async_wait<0>();
       __syncthreads();                        // these keys are there, the other buffer is free
       if (k0 + kStep < end) fetch(k0 + kStep, buf ^ 1);
-      else if (tid == 0) next = C + (int)atomicAdd(&header->taken, 1u);   // not earlier: others may be free before this CTA
+      else if (tid == 0) next = take_unit(header, C, units);   // not earlier: others may be free before this CTA
       if (8 * warp >= rows) continue;         // no row of this warp's
       float s[4][2] = {};
 #pragma unroll 8

@@ -204,7 +204,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
         s = w.find(p, bq, tq, run, u, lane, x);
         if (x.t0 < x.t1) break;                                   // else: the block ends before this run
         x.valid = 0;
-        if (lane == 0) u = C + (int)atomicAdd(&header->taken, 1u);
+        if (lane == 0) u = take_unit(header, C, units);
         u = __shfl_sync(0xffffffffu, u, 0);
       }
       ok = wait_all(&c.u_empty[un & 1], ((un >> 1) & 1) ^ 1);
@@ -215,7 +215,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       }
       if (!x.valid) break;
       int next = 0;
-      if (lane == 0) next = C + (int)atomicAdd(&header->taken, 1u);
+      if (lane == 0) next = take_unit(header, C, units);
       const int32_t* table = p.table + (int64_t)s * p.max_pages;
       const int end = x.pos0 + x.ntok;
       const int piece = lane >> 1, half = lane & 1;               // this lane's box of a tile

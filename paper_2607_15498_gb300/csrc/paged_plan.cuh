@@ -26,6 +26,13 @@ struct Header {
 };
 constexpr size_t kHeaderBytes = 256;
 
+// A CTA's next unit, after its first one, which has its own number. At or past `units`: none, also where the counter was not
+// zero before the call and is out of range.
+__device__ __forceinline__ int take_unit(Header* h, int ctas, int units) {
+  const unsigned int t = atomicAdd(&h->taken, 1u);
+  return t < (unsigned int)units ? ctas + (int)t : units;
+}
+
 struct Unit {
   int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from;
   // g: KV head; row0: row of the block's first token; pos0: its position; key tiles t0 .. t1 - 1, of which the first

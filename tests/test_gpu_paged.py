@@ -404,6 +404,28 @@ def test_attn_workspace_found_used(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("count", [10 ** 6, 2 ** 30, 2 ** 31 - 1, -2 ** 31, -2 ** 31 + 7, -1, -151, -400])
+def test_attn_workspace_with_any_count(dtype, count):
+    """Whatever the counter holds, no unit out of range is taken; the call after is right again."""
+    b = Batch([(150, 600), (1, 900), (300, 40)], dtype, 4, 2)
+    ws, q = b.workspace(), b.rows(b.H)
+    ws[:4].view(torch.int32)[0] = count
+    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, torch.zeros_like(q), b.status, ws) == V.OK
+    assert status(b) == V.ERR_CORRUPT
+    b.status.zero_()
+    run_attn(b, ws=ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[(0, 0)], [(0, 40), (0, 0), (0, 7)]], ids=str)
+def test_batch_without_new_tokens(dtype, lens):
+    """A captured step of which no sequence is alive: rows and pages stay as they are."""
+    b = Batch(lens, dtype, 2, 4, pad=5)
+    run_append(b)
+    run_attn(b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attn_two_streams_and_two_graphs(dtype):
     """Two batches at once on two streams, each with its workspace; then two captured graphs in turn on one workspace."""
     bs = [Batch([(120, 700), (1, 2000)], dtype, 2, 4, seed=1), Batch([(1, 1500), (9, 100)], dtype, 2, 4, seed=2)]
