@@ -50,8 +50,13 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     // the row's query tile: its last token's position decides which runs it reaches
     const int last = ntok <= tq ? ntok : in < tq ? tq : ntok;
     const int runs = (unsigned)(tiles_of<kKeys>(f.len - f.n + b * bq + last) + f.chunk - 1) / (unsigned)f.chunk;
-    const int64_t row0 = (int64_t)(before + (f.nb - 1 - b) * p.G + g) * part_rows + in * grp + (hq - g * grp);
-    const int64_t step = (int64_t)f.nb * p.G * part_rows;         // from run to run
+    const int64_t slot = before + (int64_t)(f.nb - 1 - b) * p.G + g, slots = (int64_t)f.nb * p.G;   // first one, from run to run
+    if (slot < 0 || slot + (runs - 1) * slots >= max_parts) {     // the header is another call's
+      if (lane == 0) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      continue;
+    }
+    const int64_t row0 = slot * part_rows + in * grp + (hq - g * grp);
+    const int64_t step = slots * part_rows;
     float m = -INFINITY, l = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int j0 = 0; j0 < runs; j0 += kBatch) {

@@ -417,6 +417,30 @@ def test_attn_workspace_with_any_count(dtype, count):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_calls_that_overlap_on_one_workspace(dtype):
+    """Not allowed, and their results are not to be trusted: but nothing outside the outputs and the workspace is touched, and
+    the workspace serves again once it is zeroed."""
+    bs = [Batch([(1, 3000), (1, 5000)], dtype, 1, 8, seed=1), Batch([(400, 900), (300, 2000)], dtype, 2, 4, seed=2)]
+    qs = [b.rows(b.H) for b in bs]
+    big = [torch.full((b.T + 2, b.H, D), 7.0, dtype=b.dt, device="cuda") for b in bs]
+    n = max(b.workspace().numel() for b in bs)
+    ws = torch.full((n + 4096,), 90, dtype=torch.uint8, device="cuda")
+    ws[:n] = 0
+    streams = [torch.cuda.Stream() for _ in bs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for b, q, out, s in zip(bs, qs, big, streams):
+            assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out[1:-1], b.status, ws[:n], stream=s) == V.OK
+    torch.cuda.synchronize()
+    assert (ws[n:] == 90).all()
+    for b, out in zip(bs, big):
+        assert (out[0] == 7).all() and (out[-1] == 7).all()
+        ws[:n] = 0
+        b.status.zero_()
+        run_attn(b, ws=ws[:n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[(0, 0)], [(0, 40), (0, 0), (0, 7)]], ids=str)
 def test_batch_without_new_tokens(dtype, lens):
     """A captured step of which no sequence is alive: rows and pages stay as they are."""
