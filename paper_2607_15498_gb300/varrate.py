@@ -311,6 +311,14 @@ def varrate_decode_attn_q(cfg, qpacked, basis_k, basis_v, q, layer, tail_k, tail
                                        _stream(stream))
 
 
+def _on_device(pages, call, *args) -> int:
+    """The call with the cache's device as the current one."""
+    if pages.device < 0 or pages.device == torch._C._cuda_getDevice():
+        return call(*args)
+    with torch.cuda.device(pages.device):
+        return call(*args)
+
+
 def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
                          dev_status, stream=None) -> int:
     """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
@@ -335,13 +343,14 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
         if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
                 and freq.get_device() == pages.device):
             return ERR_ARG
-    return (_lib or lib()).varrate_paged_append(
-        pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, _ptr(q_norm),
-        _ptr(k_norm), eps, freq_ptr, rot_dim, out_ptr, _ptr(dev_status), pages.stream(stream))
+    return _on_device(
+        pages, (_lib or lib()).varrate_paged_append, pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row,
+        v.data_ptr(), v_row, _ptr(q_norm), _ptr(k_norm), eps, freq_ptr, rot_dim, out_ptr, _ptr(dev_status),
+        pages.stream(stream))
 
 
 def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
-    return lib().varrate_paged_attn_ws_bytes(pages.ref, seqs.ref, group)
+    return _on_device(pages, lib().varrate_paged_attn_ws_bytes, pages.ref, seqs.ref, group)
 
 
 def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream=None) -> int:
@@ -349,8 +358,8 @@ def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream
     shape = (seqs.n_rows, pages.heads * group, 128)
     if not (pages.takes(q, shape) and pages.takes(out, shape)):
         return ERR_ARG
-    return (_lib or lib()).varrate_paged_attn(pages.ref, seqs.ref, layer, group, q.data_ptr(), out.data_ptr(),
-                                              _ptr(dev_status), _ptr(ws), _nbytes(ws), pages.stream(stream))
+    return _on_device(pages, (_lib or lib()).varrate_paged_attn, pages.ref, seqs.ref, layer, group, q.data_ptr(),
+                      out.data_ptr(), _ptr(dev_status), _ptr(ws), _nbytes(ws), pages.stream(stream))
 
 
 def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, dev_status, stream=None) -> int:
@@ -362,8 +371,8 @@ def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, d
     if first is not None and not (first.dtype is torch.int32 and first.is_contiguous()
                                   and first.shape == (seqs.n_seqs,) and first.get_device() == pages.device):
         return ERR_ARG
-    return (_lib or lib()).varrate_paged_gather(pages.ref, seqs.ref, layer, n_layers, _ptr(first), n, _ptr(k_out),
-                                                _ptr(v_out), _ptr(dev_status), pages.stream(stream))
+    return _on_device(pages, (_lib or lib()).varrate_paged_gather, pages.ref, seqs.ref, layer, n_layers, _ptr(first), n,
+                      _ptr(k_out), _ptr(v_out), _ptr(dev_status), pages.stream(stream))
 
 
 # ------------------------------------------------------------- device-memory plumbing

@@ -148,3 +148,30 @@ def test_rows_apart_in_every_form(vlib):
     assert pages.row_stride(x[::2], 3, 8) == 2048 and pages.row_stride(x[:, ::2], 5, 4) == -1
     one = torch.zeros((8, 1, 128), dtype=torch.bfloat16).transpose(0, 1)      # [1][8][d] with 128 from row to row
     assert one.stride(0) == 128 and pages.row_stride(one, 1, 8) == 1024
+
+
+def test_calls_run_with_the_cache_s_device_as_the_current_one(vlib, monkeypatch):
+    V = vlib
+    entered, current = [], [0]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            entered.append(self.index)
+
+        def __exit__(self, *a):
+            entered.append(None)
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    pages = V.PagedCache.of(torch.zeros((1, 4, 2, 2, 16, 128), dtype=torch.bfloat16))
+    call = lambda *a: entered.append(a) or 5   # noqa: E731
+    assert V._on_device(pages, call, 1, 2) == 5 and entered == [(1, 2)]          # on the CPU: as it is
+    pages.device = 1
+    entered.clear()
+    assert V._on_device(pages, call, 7) == 5 and entered == [1, (7,), None]
+    current[0] = 1
+    entered.clear()
+    assert V._on_device(pages, call, 7) == 5 and entered == [(7,)]
