@@ -760,7 +760,8 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group;
-  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (__nv_bfloat16*)out, dev_status, header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
+  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (__nv_bfloat16*)out, dev_status,
+                  header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
                   kLog2e / sqrtf((float)kHeadDim)))
     return -1;
   return launch_paged_merge(p, group, out, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
