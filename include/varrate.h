@@ -432,10 +432,11 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
  *   q     [T][H][d];  out [T][H][d], not overlapping q
  *   ws    at least varrate_paged_attn_ws_bytes(pages, seqs, group) bytes (which looks at no device
  *         memory: n_seqs, n_rows and max_pages only), zero-filled before the first call that uses it.
- *         It starts with a counter that a call leaves at zero again, the rest is written before it is read:
- *         one workspace serves any number of calls that are ordered on one stream, of any shape that it is large
- *         enough for. Calls that overlap on one workspace race; a call that finds the counter used raises
- *         VARRATE_ERR_CORRUPT.
+ *         It starts with a counter and marks that a call leaves at zero again, the rest is written before it is
+ *         read: one workspace serves any number of calls that are ordered on one stream, of any shape that it is
+ *         large enough for. Calls that overlap on one workspace race; a call that finds the counter or a mark used
+ *         (by an overlapping call, or one whose second kernel could not be launched) raises VARRATE_ERR_CORRUPT;
+ *         its results are not to be trusted, the next call's are.
  * bf16: products on the tensor cores, weights rounded to bf16 before they meet the values, everything else in fp32.
  * fp32: fp32 throughout. */
 size_t varrate_paged_attn_ws_bytes(const varrate_pages* pages, const varrate_seqs* seqs, int32_t group);

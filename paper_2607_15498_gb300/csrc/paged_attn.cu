@@ -54,6 +54,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
   if (tid < kCand) { sm.plan.units[tid] = 0; sm.plan.split[tid] = 0; sm.plan.chunk[tid] = 0; }
   __syncthreads();
   pdl_wait();
+  const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;   // by a call whose merge did not run, or runs still
   int longest;
   const float weight = plan_weight<kStep>(p, tq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
@@ -62,7 +63,10 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
   int run, units, parts;
   plan_choose(sm.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
   if (blockIdx.x == 0) {
-    if (tid == 0) { header->run = run; header->units = units; header->parts = parts; }
+    if (tid == 0) {
+      if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      header->run = run; header->units = units; header->parts = parts; header->open = 1;
+    }
     for (int s = tid; s < p.S; s += kThreads) {
       SeqRange r;
       if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);

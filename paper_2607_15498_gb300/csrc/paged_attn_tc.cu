@@ -177,6 +177,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = c.tmem;
   pdl_wait();
+  const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;   // by a call whose merge did not run, or runs still
   int longest;
   const float weight = plan_weight<kKeys>(p, bq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
@@ -189,7 +190,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     bool ok = wait_all(&c.planned, 0);
     int run = 1, units = 0, parts = 0;
     if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
-    if (blockIdx.x == 0 && lane == 0) { header->run = run; header->units = units; header->parts = parts; }
+    if (blockIdx.x == 0 && lane == 0) {
+      if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      header->run = run; header->units = units; header->parts = parts; header->open = 1;
+    }
     Walk<kKeys> w;
     w.load(p, bq, run, lane);
     const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box

@@ -89,9 +89,11 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     store4(out + (int64_t)i * kHeadDim + lane * 4, make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1));
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (h.taken != (unsigned)h.units && !h.gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+    if ((h.taken != (unsigned)h.units || h.first != h.units) && !h.gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     header->taken = 0;
     header->gave_up = 0;
+    header->first = 0;
+    header->open = 0;
   }
 }
 

@@ -23,13 +23,17 @@ struct Header {
   unsigned int taken;       // units taken from the counter; zero between calls
   unsigned int gave_up;     // a CTA timed out: not all units were taken; zero between calls
   int run, units, parts;    // key tiles of a run, units, and how many of them are partials
+  int first;                // the number of units, from the take that found the counter at zero; zero between calls
+  int open;                 // a call is between its start and the end of its merge; zero between calls
 };
 constexpr size_t kHeaderBytes = 256;
 
 // A CTA's next unit, after its first one, which has its own number. At or past `units`: none, also where the counter was not
-// zero before the call and is out of range.
+// zero before the call and is out of range. A counter found at c with 0 < c <= units - ctas ends at `units` like one found at
+// zero (c units are skipped, and as many takes), so the merge looks for the take that got zero as well.
 __device__ __forceinline__ int take_unit(Header* h, int ctas, int units) {
   const unsigned int t = atomicAdd(&h->taken, 1u);
+  if (t == 0) h->first = units;
   return t < (unsigned int)units ? ctas + (int)t : units;
 }
 
