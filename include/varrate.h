@@ -438,7 +438,8 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
  *         (by an overlapping call, or one whose second kernel could not be launched) raises VARRATE_ERR_CORRUPT;
  *         its results are not to be trusted, the next call's are.
  * bf16: products on the tensor cores, weights rounded to bf16 before they meet the values, everything else in fp32.
- * fp32: fp32 throughout. */
+ * fp32: fp32 throughout. Sums of weights stay below 1 on the way, so finite values of any size give finite results; what is
+ * lost instead are parts of a result below about 2^-90 (bf16) or 2^-110 (fp32). */
 size_t varrate_paged_attn_ws_bytes(const varrate_pages* pages, const varrate_seqs* seqs, int32_t group);
 varrate_status varrate_paged_attn(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
                                   int32_t group, const void* q, void* out, int32_t* dev_status, void* ws,

@@ -4,7 +4,8 @@
 // rows of a unit (paged_plan.cuh) are up to kRows (token, query head) pairs of one KV head, so a key read once serves the
 // whole group. Scores of 32 keys at a time, four rows and two keys a thread; a warp's weights go through its own
 // part of shared memory to the values, four rows and eight columns a thread. Keys and values are copied asynchronously,
-// one buffer ahead; two CTAs an SM.
+// one buffer ahead; two CTAs an SM. Weights carry a factor `room`, a power of two that cancels and keeps the sum of as many as a
+// sequence can have at 1 or below, so that no accumulator grows past the largest value.
 // Bound by the fp32 pipe and the latencies around it (16 warps an SM): 1469 new tokens of two sequences, 4 heads over 1, 64 us,
 // 25 TFLOP/s. One token each of 59 sequences of up to 490, 48 heads over 8, 48 us, 1.2 TB/s.
 // What was measured on the way, on the first: no cuts over the keys 187 us; cuts in tiles of 128 keys 84 to 99, in steps of 32
@@ -44,7 +45,8 @@ __device__ __forceinline__ float4 get4(const float* s) { return *reinterpret_cas
 
 __global__ void __launch_bounds__(kThreads, 2)
 paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __restrict__ q, float* __restrict__ out,
-                      int32_t* dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts, int grp, float scale) {
+                      int32_t* dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts, int grp, float scale,
+                      float room) {
   extern __shared__ __align__(16) unsigned char raw[];
   Smem& sm = *reinterpret_cast<Smem*>(raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = p.G * grp, C = gridDim.x;
@@ -166,7 +168,7 @@ paged_attn_f32_kernel(Paged p, const float* __restrict__ pool, const float* __re
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float e = exp2f((s[i][j] - ref) * kLog2e);
+          const float e = exp2f((s[i][j] - ref) * kLog2e) * room;
           sm.p[4 * ty + i][tx + 16 * j] = e;
           sum += e;
         }
@@ -243,8 +245,11 @@ int launch_paged_attn(const Paged& p, int layer, int group, const void* q, void*
   Header* header = static_cast<Header*>(ws);
   float* part = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + kHeaderBytes);
   const float* pool = reinterpret_cast<const float*>(p.pool) + (int64_t)layer * p.layer_rows * kHeadDim;
+  int bits = 0;
+  while (bits < 31 && ((int64_t)1 << bits) < ((int64_t)p.max_pages << p.page_log2)) ++bits;   // keys of a sequence: 2^bits at most
   if (!launch_pdl(paged_attn_f32_kernel, dim3(ctas), kThreads, sizeof(Smem), st, p, pool, (const float*)q, (float*)out, dev_status,
-                  header, part, paged_part_rows(p, group, tq), paged_max_parts(ctas), group, 1.f / sqrtf((float)kHeadDim)))
+                  header, part, paged_part_rows(p, group, tq), paged_max_parts(ctas), group, 1.f / sqrtf((float)kHeadDim),
+                  ldexpf(1.f, -bits)))
     return -1;
   return launch_paged_merge(p, group, out, dev_status, header, part, tq, tq, ctas, st) < 0 ? -1 : 2;
 }

@@ -9,8 +9,9 @@
 // Two softmax warpgroups (thread = row) work in turn, so that the products of one run under the softmax of the other:
 //   a block of more than tq new tokens gives each warpgroup a query tile of its own, and both use every key tile;
 //   a smaller one (a decode step) gives both the same query tile and every second key tile, merged at the end.
-// The reference of a row (log2 units) is the maximum of its first 32 scores and moves only when weights would sum to more than
-// kMost: then to the maximum, and its accumulator is rescaled in TMEM. So a tile is read once, without a maximum.
+// The reference of a row (log2 units) stands kRoom above the maximum of its first 32 scores and moves only when its weights would
+// sum to kMost: then to kRoom above the maximum, and its accumulator is rescaled in TMEM. So a tile is read once, without a
+// maximum, and as the weights sum to less than 1, accumulators stay below the largest value.
 // Weights are handed on in halves of 64 keys: the products of the first run while the second is made.
 //
 // Units of work (paged_plan.cuh) are taken by one CTA per SM: the first by its number, the others from a counter in the
@@ -61,9 +62,12 @@ constexpr float kOverhead = 2.f;                            // of a unit, in key
                                                             // 131072, when it took 680 us: at 1 677, at 4 and 6 690
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
-// Weights of half a tile may sum to kMost above the reference before it moves: nothing is lost in floating point, and the
-// accumulators have room for values of 2^127 / kMost / keys.
-constexpr float kMost = 0x1p40f;
+// The weights of a row sum to less than kMost, so that neither an accumulator nor the sum of the two warpgroups' overflows,
+// whatever the values. kRoom (log2) is what scores may rise, and their number grow, before the reference moves: 8192 tokens with
+// some scores 10 deviations above the rest take 411 us at 24, 392 at 28, 377 at 32, 366 at 36, 359 at 40 (355 with no bound on the
+// sum of a row, 2^40 for half a tile's). What it costs is the low end: products with values below 2^-90 or so leave the range
+// of fp32.
+constexpr float kMost = 0.25f, kRoom = 40.f;
 
 struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
@@ -632,8 +636,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
               for (int k = 0; k < 32; ++k) s[k] = cb + k < lim ? s[k] : -INFINITY;
             }
           };
-          // The weights from the reference as it is, in halves of 64 keys, each handed on by itself. If their sum is no
-          // number below kMost: the maximum of the scores first, then the weights again.
+          // The weights from the reference as it is, in halves of 64 keys, each handed on by itself. If the row's sum is no
+          // number below kMost with them: the maximum of the scores first, then the weights again.
           float x[32];
           uint32_t pk[32];
           auto weights = [&](int cb0) {
@@ -661,7 +665,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             sum[0] = add2(sum[0], sum[1]);
             return sum[0].x + sum[0].y;
           };
-          // the reference up to the maximum of the scores from column cb on; `some`: up to the first 32 that show one
+          // the reference up to kRoom above the maximum of the scores from column cb on; `some`: up to the first 32 that show one
           auto raise = [&](int cb, bool some) {
             float mx = -INFINITY;
 #pragma unroll 1
@@ -674,8 +678,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
               mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             }
             mx *= scale_log2;
+            const float up = (l < 0.5f * kMost ? mx : fmaxf(mx, ref)) + kRoom;   // a sum that has grown makes room too
             float f = 1.f;
-            if (mine && mx > ref) { f = ref == -INFINITY ? 0.f : fast_exp2(ref - mx); ref = mx; }
+            if (mine && up > ref) { f = ref == -INFINITY ? 0.f : fast_exp2(ref - up); ref = up; }
             return f;
           };
           auto rescale = [&](float f) {                           // the accumulator, whose products have ended
@@ -688,7 +693,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
               tmem_st32(to + cb, x);
             }
           };
-          auto unusable = [&](float sum) { return __any_sync(0xffffffffu, mine && !(sum < kMost)); };
+          // (fminf: where l is no number already the weights are as good as any)
+          auto unusable = [&](float sum) { return __any_sync(0xffffffffu, mine && !(sum < fminf(kMost - l, kMost))); };
           // one body for both halves: the loop has to be short, instructions are fetched anew when it is not
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {

@@ -57,6 +57,8 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     }
     const int64_t row0 = slot * part_rows + in * grp + (hq - g * grp);
     const int64_t step = slots * part_rows;
+    // a part's weights sum to 1 at most: with this factor, a power of two that cancels, those of all parts do
+    const float room = __int_as_float((127 - (32 - __clz(runs - 1))) << 23);
     float m = -INFINITY, l = 0.f;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int j0 = 0; j0 < runs; j0 += kBatch) {
@@ -80,7 +82,7 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
       v.x *= f0; v.y *= f0; v.z *= f0; v.w *= f0;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const float w = fast_exp2(x[j].x - ref);
+        const float w = fast_exp2(x[j].x - ref) * room;
         l = fmaf(x[j].y, w, l);
         v.x = fmaf(y[j].x, w, v.x); v.y = fmaf(y[j].y, w, v.y); v.z = fmaf(y[j].z, w, v.z); v.w = fmaf(y[j].w, w, v.w);
       }

@@ -1,9 +1,9 @@
-"""Edges of the paged calls on the GPU: headers of the workspace that a call may find. Tolerances are derived in
-paged_helpers."""
+"""Edges of the paged calls on the GPU: headers of the workspace that a call may find, values as large and as small as their
+type holds. Tolerances are derived in paged_helpers."""
 import pytest
 import torch
 
-from paged_helpers import V, Batch
+from paged_helpers import D, V, Batch
 from test_gpu_paged import run_attn, status
 
 pytestmark = pytest.mark.gpu
@@ -58,3 +58,52 @@ def test_attn_header_never_zeroed(dtype, count):
     """Every word of the header holds something, as a call whose merge was never launched leaves it."""
     b = Batch([(1, s % 30) for s in range(500)], dtype, 2, 4)
     found(b, b.workspace(), [count, 0, 1, 1000, 0, 1000, 1, 1])
+
+
+# ------------------------------------------------------------------------------------ values at the ends of their type
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [124, -90])
+@pytest.mark.parametrize("lens", [[(1, 2000), (1, 7)], [(150, 600), (1, 900)], [(1, 9999)], [(40, 5000)]], ids=str)
+def test_attn_values_near_the_ends_of_the_range(dtype, power, lens):
+    """A mean of values is no larger than the largest one, however many keys there are and however far scores rise: values
+    of 2^126 give finite results, values of 2^-90 keep their precision."""
+    b = Batch(lens, dtype, 1, 8, 64)
+    b.pool[:, :, 1] *= 2.0 ** power
+    run_attn(b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("jump", [10.0, 16.0, 17.0, 25.0, 60.0, 100.0])
+@pytest.mark.parametrize("lens", [[(1, 400)], [(130, 271)]], ids=str)
+def test_attn_large_values_and_a_score_that_rises(dtype, jump, lens):
+    """The keys from some position on stand `jump` above the ones before."""
+    for at in (20, 40, 100, 130, 300):
+        b = Batch(lens, dtype, 1, 4)
+        b.pool[:, :, 1] *= 2.0 ** 124
+        q = b.rows(b.H)
+        q[..., 0] = 16.0
+        for u in range(b.len[0]):
+            b.pool[0, b.table_host[0, u // b.ps], 0, 0, u % b.ps, 0] = jump * D ** 0.5 / 16.0 if u >= at else 0.0
+        run_attn(b, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_large_values_of_one_sign_and_equal_scores(dtype):
+    """The sum of the weights reaches the number of keys: as many times the values must not appear on the way."""
+    b = Batch([(1, 20000), (200, 3000)], dtype, 1, 2, 128)
+    b.pool[:, :, 1] = b.pool[:, :, 1].abs() * 2.0 ** 124
+    run_attn(b, q=torch.zeros((b.T, b.H, D), dtype=b.dt, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attn_scores_that_rise_slowly(dtype):
+    """Every key stands a little above the one before it: the sum of the weights comes near its bound again and again."""
+    b = Batch([(1, 6000), (140, 1500)], dtype, 1, 4, 64)
+    q = b.rows(b.H)
+    q[..., 0] = 16.0
+    for s in range(2):
+        for u in range(b.len[s]):
+            b.pool[0, b.table_host[s, u // b.ps], 0, 0, u % b.ps, 0] = u * (0.25 if s else 0.0625) * D ** 0.5 / 16.0
+    b.pool[:, :, 1] *= 2.0 ** 124
+    run_attn(b, q=q)
