@@ -410,7 +410,7 @@ typedef struct {
  *             (parts of one joint projection, say): each stride at least the row's length and a multiple
  *             of 16 bytes. q may be NULL (keys and values only; q_out is not looked at).
  *   q_norm    [d] dtype, or NULL: no norm of the queries;  k_norm the same for the keys
- *   eps       >= 0, finite
+ *   eps       >= 0, finite in fp32; one that fp32 would round to 0 counts as the smallest number above it
  *   freq      [rot_dim / 2] double; rot_dim a multiple of 16 in [0, d] (0: no rotation, freq may be NULL)
  *   q_out     [T][H][d]: rotated queries. It may be q itself where q_stride == H * d; any other overlap
  *             of an output with an input is not allowed.

@@ -3,6 +3,8 @@
 #include <algorithm>
 #include <atomic>
 #include <initializer_list>
+
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -406,18 +408,19 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
                                     void* q_out, int32_t* dev_status, void* stream) {
   varrate_status st = paged_check(pages, seqs);
   if (st != VARRATE_OK) return st;
-  if (layer < 0 || layer >= pages->n_layers || group < 1 || !(eps >= 0.0) || !isfinite(eps)) return VARRATE_ERR_ARG;
+  if (layer < 0 || layer >= pages->n_layers || group < 1 || !(eps >= 0.0) || !isfinite((float)eps)) return VARRATE_ERR_ARG;
   if (group > 8) return VARRATE_ERR_UNSUPPORTED;
   if (rot_dim < 0 || rot_dim > vr::kHeadDim || (rot_dim % 16) != 0) return VARRATE_ERR_ARG;
   if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
   if ((st = paged_pointers(pages, seqs, true)) != VARRATE_OK) return st;
   if (!k || !v || (q && !q_out) || (rot_dim > 0 && !freq)) return VARRATE_ERR_ARG;
   if (!aligned16({q, k, v, q_norm, k_norm, freq, q_out, dev_status})) return VARRATE_ERR_ARG;
+  const float eps32 = eps > 0.0 ? fmaxf((float)eps, FLT_TRUE_MIN) : 0.f;   // never rounded to 0: a head of zeros is no 0 / 0 then
   const int64_t vec = pages->dtype == VARRATE_F32 ? 4 : 8, kd = (int64_t)pages->n_kv_heads * vr::kHeadDim;
   if (k_stride < kd || k_stride % vec != 0 || v_stride < kd || v_stride % vec != 0) return VARRATE_ERR_ARG;
   if (q && (q_stride < kd * group || q_stride % vec != 0 || (q == q_out && q_stride != kd * group))) return VARRATE_ERR_ARG;
   if (vr::launch_paged_append(make_paged(pages, seqs), layer, group, q, q_stride, k, k_stride, v, v_stride, q_norm,
-                              k_norm, (float)eps, freq, rot_dim, q_out, dev_status, num_sms(), (cudaStream_t)stream) < 0)
+                              k_norm, eps32, freq, rot_dim, q_out, dev_status, num_sms(), (cudaStream_t)stream) < 0)
     return VARRATE_ERR_CUDA;
   return launched();
 }

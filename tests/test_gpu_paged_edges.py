@@ -1,10 +1,10 @@
 """Edges of the paged calls on the GPU: headers of the workspace that a call may find, values as large and as small as their
-type holds. Tolerances are derived in paged_helpers."""
+type holds, norms of zeros. Tolerances are derived in paged_helpers."""
 import pytest
 import torch
 
 from paged_helpers import D, V, Batch
-from test_gpu_paged import run_attn, status
+from test_gpu_paged import NAN, run_attn, status
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,20 @@ def test_attn_scores_that_rise_slowly(dtype):
             b.pool[0, b.table_host[s, u // b.ps], 0, 0, u % b.ps, 0] = u * (0.25 if s else 0.0625) * D ** 0.5 / 16.0
     b.pool[:, :, 1] *= 2.0 ** 124
     run_attn(b, q=q)
+
+
+# ------------------------------------------------------------------------------------ norms
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("eps", [1e-45, 1e-46, 1e-300, 1e-6])
+def test_append_norm_of_zeros(dtype, eps):
+    """A head of zeros is zeros after its norm wherever eps is above zero, one that fp32 cannot hold included."""
+    b = Batch([(5, 3)], dtype, 2, 2)
+    q, k, v = b.rows(b.H), b.rows(b.G), b.rows(b.G)
+    q[1], k[2], q[3, 1] = 0.0, 0.0, 0.0
+    w = torch.ones(D, dtype=b.dt, device="cuda")
+    q_out = torch.full_like(q, NAN)
+    assert V.varrate_paged_append(b.pages, b.seqs, 0, q, k, v, w, w, eps, None, 0, q_out, b.status) == V.OK
+    assert (q_out[1] == 0).all() and (q_out[3, 1] == 0).all() and (b.tokens(0, 0)[:, 3 + 2] == 0).all()
+    assert torch.isfinite(q_out).all() and torch.isfinite(b.tokens(0, 0)).all()
+    assert status(b) == V.OK
