@@ -323,6 +323,8 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
                          dev_status, stream=None) -> int:
     """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
     ERR_ARG where a tensor is not of the cache's type, shape or device."""
+    if not pages.works_with(seqs, dev_status):
+        return ERR_ARG
     G, T = pages.heads, seqs.n_rows
     k_row, v_row = pages.row_stride(k, T, G), pages.row_stride(v, T, G)
     if q is None:
@@ -358,6 +360,8 @@ def varrate_paged_attn(pages, seqs, layer, group, q, out, dev_status, ws, stream
     shape = (seqs.n_rows, pages.heads * group, 128)
     if not (pages.takes(q, shape) and pages.takes(out, shape)):
         return ERR_ARG
+    if ws is not None and not (pages.works_with(seqs, dev_status) and ws.get_device() == pages.device and ws.is_contiguous()):
+        return ERR_ARG                                # (without one the C call launches nothing)
     return _on_device(pages, (_lib or lib()).varrate_paged_attn, pages.ref, seqs.ref, layer, group, q.data_ptr(),
                       out.data_ptr(), _ptr(dev_status), _ptr(ws), _nbytes(ws), pages.stream(stream))
 
@@ -367,6 +371,8 @@ def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, d
     type, shape or device."""
     shape = (seqs.n_seqs, n_layers, pages.heads, n, 128)
     if (k_out is not None and not pages.takes(k_out, shape)) or (v_out is not None and not pages.takes(v_out, shape)):
+        return ERR_ARG
+    if not pages.works_with(seqs, dev_status):
         return ERR_ARG
     if first is not None and not (first.dtype is torch.int32 and first.is_contiguous()
                                   and first.shape == (seqs.n_seqs,) and first.get_device() == pages.device):
@@ -484,6 +490,11 @@ class PagedCache:
             return -1 if rows else 0
         return row if rows > 1 else heads * 128      # of one row: any number
 
+    def works_with(self, seqs, dev_status) -> bool:
+        """Whether the cache, a batch's tables and a status word (int32; None or a raw pointer pass) are on one GPU."""
+        return seqs.device == self.device >= 0 and (not isinstance(dev_status, torch.Tensor) or (
+            dev_status.dtype is torch.int32 and dev_status.get_device() == self.device and dev_status.numel() > 0))
+
     def stream(self, stream) -> int | None:
         """`stream` as _stream takes it; None is torch's current stream on the cache's device."""
         if stream is None and self.device >= 0:
@@ -494,7 +505,7 @@ class PagedCache:
 @dataclass
 class SeqBatch:
     """A batch of sequences with new tokens: row_start [S + 1], kv_len [S] and page_table [S][max_pages],
-    int32 on the GPU, n_rows rows of queries, keys and values; plus the C struct. The tensors may be
+    int32 on the cache's GPU, n_rows rows of queries, keys and values; plus the C struct. The tensors may be
     refilled in place from step to step (the calls read them on the stream)."""
     row_start: torch.Tensor
     kv_len: torch.Tensor
@@ -505,14 +516,15 @@ class SeqBatch:
     def of(row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int) -> "SeqBatch":
         S = kv_len.numel()
         for t, shape in ((row_start, (S + 1,)), (kv_len, (S,)), (page_table, (S, page_table.shape[-1]))):
-            if t is not None and (t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous()):
+            if t is not None and (t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous()
+                                  or t.get_device() != kv_len.get_device()):
                 raise VarrateError(ERR_ARG, "SeqBatch.of")
         c = varrate_seqs(_ptr(row_start), _ptr(kv_len), _ptr(page_table), S, page_table.shape[-1], n_rows)
         return SeqBatch(row_start, kv_len, page_table, c)
 
     def __post_init__(self):
         self.ref = ctypes.byref(self.c)
-        self.n_seqs, self.n_rows = self.c.n_seqs, self.c.n_rows
+        self.n_seqs, self.n_rows, self.device = self.c.n_seqs, self.c.n_rows, self.kv_len.get_device()
 
 
 def paged_attn_workspace(pages: PagedCache, seqs: SeqBatch, group: int) -> torch.Tensor:
