@@ -514,6 +514,8 @@ class SeqBatch:
 
     @staticmethod
     def of(row_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, n_rows: int) -> "SeqBatch":
+        if kv_len is None or page_table is None or page_table.dim() != 2:   # row_start may be missing, to gather
+            raise VarrateError(ERR_ARG, "SeqBatch.of")
         S = kv_len.numel()
         for t, shape in ((row_start, (S + 1,)), (kv_len, (S,)), (page_table, (S, page_table.shape[-1]))):
             if t is not None and (t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous()

@@ -82,3 +82,13 @@ def test_tables_on_one_device(vlib):
         moved[i].index = 0
         with pytest.raises(vlib.VarrateError):
             vlib.SeqBatch.of(*moved, 3)
+
+
+def test_a_batch_without_tables(vlib):
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32)   # noqa: E731
+    table = torch.zeros((2, 2), dtype=torch.int32)
+    for bad in ((i32(0, 1, 3), None, table), (i32(0, 1, 3), i32(1, 5), None), (i32(0, 1, 3), i32(1, 5), table.view(4)),
+                (i32(0, 1, 3), i32(1, 5), torch.zeros((), dtype=torch.int32))):
+        with pytest.raises(vlib.VarrateError):
+            vlib.SeqBatch.of(*bad, 3)
+    assert vlib.SeqBatch.of(None, i32(1, 5), table, 3).n_seqs == 2      # to gather
