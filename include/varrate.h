@@ -390,7 +390,8 @@ typedef struct {
  * A sequence with row_start out of order or outside [0, n_rows], with kv_len[s] outside
  * [n_s, min(max_pages * page_size, 2^31 - 256)], or with a page number outside [0, n_pages) among those that the call
  * reads or writes raises VARRATE_ERR_CORRUPT in *dev_status; its results are not to be trusted (rows may
- * stay unwritten), the other sequences' are, as long as their rows are not claimed twice. */
+ * stay unwritten), the other sequences' are. But where row_start is out of order, no row of the batch is to be
+ * trusted: a row finds its sequence by bisection. */
 typedef struct {
   const int32_t* row_start;    /* [n_seqs + 1] */
   const int32_t* kv_len;       /* [n_seqs] */

@@ -1,5 +1,5 @@
 """Edges of the paged calls on the GPU: headers of the workspace that a call may find, values as large and as small as their
-type holds, norms of zeros. Tolerances are derived in paged_helpers."""
+type holds, norms of zeros, row ranges out of order. Tolerances are derived in paged_helpers."""
 import pytest
 import torch
 
@@ -124,3 +124,29 @@ def test_append_norm_of_zeros(dtype, eps):
     assert (q_out[1] == 0).all() and (q_out[3, 1] == 0).all() and (b.tokens(0, 0)[:, 3 + 2] == 0).all()
     assert torch.isfinite(q_out).all() and torch.isfinite(b.tokens(0, 0)).all()
     assert status(b) == V.OK
+
+
+# ------------------------------------------------------------------------------------ row ranges out of order
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("start", [[4, 8, 0, 4], [9, 5, 3, 0], [0, 9, 2, 9], [8, 2, 9, 9]], ids=str)
+def test_row_ranges_out_of_order(dtype, start):
+    """Reported, and nothing outside the rows and the sequences' own places in the pages is written."""
+    b = Batch([(3, 30), (3, 40), (3, 50)], dtype, 2, 2)
+    b.row_start.copy_(torch.tensor(start, dtype=torch.int32))
+    q, k, v = b.rows(b.H), b.rows(b.G), b.rows(b.G)
+    own = torch.zeros(b.pool.shape, dtype=torch.bool, device="cuda")
+    for s in range(3):
+        for u in range(b.len[s]):
+            own[0, b.table_host[s, u // b.ps], :, :, u % b.ps] = True
+    rest = b.pool.clone()
+    big = torch.full((b.T + 2, b.H, D), 7.0, dtype=b.dt, device="cuda")
+    assert V.varrate_paged_append(b.pages, b.seqs, 0, q, k, v, None, None, 0.0, None, 0, big[1:-1], b.status) == V.OK
+    assert status(b) == V.ERR_CORRUPT
+    assert (big[0] == 7).all() and (big[-1] == 7).all()
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(b.pool.view(bits)[~own], rest.view(bits)[~own])
+    b.status.zero_()
+    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, big[1:-1], b.status, b.workspace()) == V.OK
+    assert status(b) == V.ERR_CORRUPT
+    assert (big[0] == 7).all() and (big[-1] == 7).all()
