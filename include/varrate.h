@@ -431,8 +431,9 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
  * What stands in the pages at positions after p (unused slots, later tokens: NaN and infinities as
  * well) has no part in the result. A row whose scores are all -infinity gives zeros.
  *   q     [T][H][d];  out [T][H][d], not overlapping q
- *   ws    at least varrate_paged_attn_ws_bytes(pages, seqs, group) bytes (which looks at no device
- *         memory: n_seqs, n_rows and max_pages only), zero-filled before the first call that uses it.
+ *   ws    at least varrate_paged_attn_ws_bytes(pages, seqs, group) bytes, zero-filled before the first call that
+ *         uses it. The size depends on n_rows, group, dtype and the current device, grows with n_rows up to a
+ *         bound, and is found without a look at device memory.
  *         It starts with a counter and marks that a call leaves at zero again, the rest is written before it is
  *         read: one workspace serves any number of calls that are ordered on one stream, of any shape that it is
  *         large enough for. Calls that overlap on one workspace race; a call that finds the counter or a mark used

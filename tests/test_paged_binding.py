@@ -1,4 +1,6 @@
 """What the paged-cache calls refuse on the host, beside test_paged_abi.py (no GPU needed)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -92,3 +94,17 @@ def test_a_batch_without_tables(vlib):
         with pytest.raises(vlib.VarrateError):
             vlib.SeqBatch.of(*bad, 3)
     assert vlib.SeqBatch.of(None, i32(1, 5), table, 3).n_seqs == 2      # to gather
+
+
+def test_workspace_size_goes_by_rows_group_and_type(vlib):
+    """Not by sequences or pages; never less for more rows."""
+    def size(dtype=vlib.BF16, group=4, **kw):
+        p, s = structs(vlib, dtype, **kw)
+        return vlib.lib().varrate_paged_attn_ws_bytes(ctypes.byref(p), ctypes.byref(s), group)
+
+    for dtype in (vlib.BF16, vlib.F32):
+        for group in (1, 3, 8):
+            assert size(dtype, group) == size(dtype, group, n_seqs=900, max_pages=70) == size(dtype, group, n_pages=77)
+            sizes = [size(dtype, group, n_rows=n) for n in (0, 1, 7, 40, 128, 129, 500, 10 ** 6)]
+            assert sizes == sorted(sizes) and sizes[-1] == sizes[-2]
+    assert size(vlib.BF16) != size(vlib.F32) and size(group=1) != size(group=8)
