@@ -492,8 +492,8 @@ class PagedCache:
 
     def works_with(self, seqs, dev_status) -> bool:
         """Whether the cache, a batch's tables and a status word (int32; None or a raw pointer pass) are on one GPU."""
-        return seqs.device == self.device >= 0 and (not isinstance(dev_status, torch.Tensor) or (
-            dev_status.dtype is torch.int32 and dev_status.get_device() == self.device and dev_status.numel() > 0))
+        return seqs.device == self.device >= 0 and (dev_status is None or type(dev_status) is int or (
+            dev_status.dtype is torch.int32 and dev_status.get_device() == self.device))
 
     def stream(self, stream) -> int | None:
         """`stream` as _stream takes it; None is torch's current stream on the cache's device."""
