@@ -1,9 +1,10 @@
 """Edges of the paged calls on the GPU: headers of the workspace that a call may find, values as large and as small as their
-type holds, norms of zeros, row ranges out of order. Tolerances are derived in paged_helpers."""
+type holds, norms of zeros, row ranges out of order, rows without a finite score, every number of heads in a group. Tolerances
+are derived in paged_helpers."""
 import pytest
 import torch
 
-from paged_helpers import D, V, Batch
+from paged_helpers import D, V, Batch, attn_ref, close
 from test_gpu_paged import NAN, run_attn, status
 
 pytestmark = pytest.mark.gpu
@@ -21,15 +22,18 @@ def ctas(dtype):
     return torch.cuda.get_device_properties(0).multi_processor_count * (1 if dtype == "bf16" else 2)
 
 
-def found(b, ws, words):
-    """A call that finds `words` at the start of the workspace raises CORRUPT; the call after it is right."""
-    head = ws[:4 * len(words)].view(torch.int32)
-    head.copy_(torch.tensor(words, dtype=torch.int32))
+def found(b, ws, headers):
+    """A call that finds such words at the start of the workspace raises CORRUPT; the call after it is right."""
     q = b.rows(b.H)
-    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, torch.zeros_like(q), b.status, ws) == V.OK
-    assert status(b) == V.ERR_CORRUPT
-    b.status.zero_()
-    run_attn(b, ws=ws, q=q)
+    want, tol = attn_ref(b, q)
+    for words in headers:
+        ws[:4 * len(words)].view(torch.int32).copy_(torch.tensor(words, dtype=torch.int32))
+        for expected in (V.ERR_CORRUPT, V.OK):
+            b.status.zero_()
+            out = torch.full_like(q, NAN)
+            assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, ws) == V.OK
+            assert status(b) == expected
+        close(out, want, tol)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -39,25 +43,20 @@ def test_attn_counter_found_used_with_units_left_to_take(dtype):
     units, C = 1000, ctas(dtype)
     assert C < units
     b = Batch([(1, s % 30) for s in range(units // 2)], dtype, 2, 4)
-    ws = b.workspace()
-    for count in (1, 3, units - C - 1, units - C, units - C + 1, units - 1, units):
-        found(b, ws, [count])
+    found(b, b.workspace(), [[c] for c in (1, 3, units - C - 1, units - C, units - C + 1, units - 1, units)])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attn_counter_found_used_by_a_long_prompt(dtype):
     b = Batch([(3000, 100), (1, 2000)], dtype, 4, 2)
-    ws = b.workspace()
-    for count in (1, 3, 100):
-        found(b, ws, [count])
+    found(b, b.workspace(), [[1], [3], [100]])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("count", [0, 1, 3, 100, 1000])
-def test_attn_header_never_zeroed(dtype, count):
+def test_attn_header_never_zeroed(dtype):
     """Every word of the header holds something, as a call whose merge was never launched leaves it."""
     b = Batch([(1, s % 30) for s in range(500)], dtype, 2, 4)
-    found(b, b.workspace(), [count, 0, 1, 1000, 0, 1000, 1, 1])
+    found(b, b.workspace(), [[c, 0, 1, 1000, 0, 1000, 1, 1] for c in (0, 1, 3, 100, 1000)])
 
 
 # ------------------------------------------------------------------------------------ values at the ends of their type
@@ -150,3 +149,47 @@ def test_row_ranges_out_of_order(dtype, start):
     assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, big[1:-1], b.status, b.workspace()) == V.OK
     assert status(b) == V.ERR_CORRUPT
     assert (big[0] == 7).all() and (big[-1] == 7).all()
+
+
+# ------------------------------------------------------------------------------------ rows without a finite score
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grp", [1, 4, 7])
+@pytest.mark.parametrize("lens", [[(1, 0)], [(1, 700), (1, 3)], [(150, 300)], [(300, 0), (1, 1000)], [(1, 9999)]], ids=str)
+def test_attn_scores_of_minus_infinity(dtype, grp, lens):
+    """Keys whose score is -infinity for some queries: rows that see nothing else give zeros, the others leave them out."""
+    b = Batch(lens, dtype, 2, grp, 64)
+    q = b.rows(b.H)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    finite = [0, 200]                        # KV head 0: no key; KV head 1: the keys from position 200 on, then every third
+    for s in range(len(lens)):
+        for u in range(b.len[s]):
+            at = (b.table_host[s, u // b.ps], u % b.ps)
+            b.pool[0, at[0], 0, 0, at[1], 0] = -float("inf")
+            if u < finite[1] or u % 3:
+                b.pool[0, at[0], 0, 1, at[1], 0] = -float("inf")
+    want, tol = attn_ref(b, q)
+    for s, (n, c) in enumerate(lens):
+        rows = torch.arange(b.start[s], b.start[s + 1], device="cuda")
+        seen = torch.arange(c, c + n, device="cuda")
+        want[rows, :grp] = 0.0
+        tol[rows, :grp] = 0.0
+        none = rows[seen < 201]              # 201 is the first multiple of three from 200 on
+        want[none, grp:] = 0.0
+        tol[none, grp:] = 0.0
+    assert not torch.isnan(want).any()
+    out = torch.full((b.T, b.H, D), NAN, dtype=b.dt, device="cuda")
+    assert V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, q, out, b.status, b.workspace()) == V.OK
+    close(out, want, tol)
+    assert status(b) == V.OK
+
+
+# ------------------------------------------------------------------------------------ heads of a group
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grp", [2, 3, 5, 6])
+@pytest.mark.parametrize("lens", [[(1, 0)], [(1, 700), (1, 3), (1, 129)], [(64, 64), (0, 5), (3, 200)], [(129, 0)],
+                                  [(300, 0), (1, 1000), (33, 95)], [(40, 1500)]], ids=str)
+def test_attn_heads_of_a_group(dtype, grp, lens):
+    """Groups whose query tiles leave rows of the matrix product unused (126 or 125 of 128) among them."""
+    run_attn(Batch(lens, dtype, 2, grp, pad=2, lead=1))
