@@ -412,7 +412,7 @@ typedef struct {
  *             of 16 bytes. q may be NULL (keys and values only; q_out is not looked at).
  *   q_norm    [d] dtype, or NULL: no norm of the queries;  k_norm the same for the keys
  *   eps       >= 0, finite in fp32; one that fp32 would round to 0 counts as the smallest number above it
- *   freq      [rot_dim / 2] double; rot_dim a multiple of 16 in [0, d] (0: no rotation, freq may be NULL)
+ *   freq      [rot_dim / 2] double, finite; rot_dim a multiple of 16 in [0, d] (0: no rotation, freq may be NULL)
  *   q_out     [T][H][d]: rotated queries. It may be q itself where q_stride == H * d; any other overlap
  *             of an output with an input is not allowed.
  * V goes to its page unchanged. Two tokens may not have the same place in the pages (pages that two
@@ -441,7 +441,7 @@ varrate_status varrate_paged_append(const varrate_pages* pages, const varrate_se
  *         its results are not to be trusted, the next call's are.
  * bf16: products on the tensor cores, weights rounded to bf16 before they meet the values, everything else in fp32.
  * fp32: fp32 throughout. Sums of weights stay below 1 on the way, so finite values of any size give finite results; what is
- * lost instead are parts of a result below about 2^-90 (bf16) or 2^-110 (fp32). */
+ * lost instead are parts of a result below about 2^-90. */
 size_t varrate_paged_attn_ws_bytes(const varrate_pages* pages, const varrate_seqs* seqs, int32_t group);
 varrate_status varrate_paged_attn(const varrate_pages* pages, const varrate_seqs* seqs, int32_t layer,
                                   int32_t group, const void* q, void* out, int32_t* dev_status, void* ws,

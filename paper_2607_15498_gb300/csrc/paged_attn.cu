@@ -6,12 +6,14 @@
 // part of shared memory to the values, four rows and eight columns a thread. Keys and values are copied asynchronously,
 // one buffer ahead; two CTAs an SM. Weights carry a factor `room`, a power of two that cancels and keeps the sum of as many as a
 // sequence can have at 1 or below, so that no accumulator grows past the largest value.
-// Bound by the fp32 pipe and the latencies around it (16 warps an SM): 1469 new tokens of two sequences, 4 heads over 1, 64 us,
-// 25 TFLOP/s. One token each of 59 sequences of up to 490, 48 heads over 8, 48 us, 1.2 TB/s.
+// Bound by shared memory and the fp32 pipe alike (four columns of a score step: six 16-byte reads a thread for 32
+// multiply-adds) and by the latencies of a step (shuffles, two barriers) at 16 warps an SM: 1469 new tokens of two sequences, 4 heads over
+// 1, 64 us, 25 TFLOP/s. One token each of 59 sequences of up to 490, 48 heads over 8, 48 us, 1.2 TB/s: six rows of 64 are in use, so
+// one warp of eight works.
 // What was measured on the way, on the first: no cuts over the keys 187 us; cuts in tiles of 128 keys 84 to 99, in steps of 32
 // with the next unit taken at the start of one 115, in its last step 64. 64 rows by 128 threads with 8 x 4 scores each:
-// 90 us at tiles of 128. Packed products change 1 %, a prefetch to L2 nothing, and units of at most 8 rows with the keys
-// shared among the warps take 43 us on the second, but 5 to 12 % more on small steps.
+// 90 us at tiles of 128, not measured in steps of 32. Packed products change 1 %, a prefetch to L2 nothing, and units of at most 8
+// rows with the keys shared among the warps take 43 us on the second, but 5 to 12 % more on small steps.
 #include <math.h>
 
 #include <atomic>

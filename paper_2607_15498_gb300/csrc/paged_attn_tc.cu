@@ -26,16 +26,18 @@
 // which keeps the warpgroups half a period apart; 11 values. Every wait is bounded; one that gives up raises
 // VARRATE_ERR_TIMEOUT, its CTA takes no further unit and ends after its copies and products in flight have.
 //
-// Bound by the tensor cores for prompts: 8192 tokens, 32 heads over 8: 333 us, 1650 TFLOP/s (88 % of the rate of a large bf16
-// product); 512 tokens on 131072: 645 us, 1700 (91 %). By memory for decode steps: eight sequences of 32768 tokens
-// 170 us, 6.3 TB/s (93 % of a copy). By latency for short ones: 900 tokens of one sequence 13.8 us, two launches and
+// Bound by the tensor cores for prompts: 8192 tokens, 32 heads over 8: 335 us, 1640 TFLOP/s (88 % of the rate of a large bf16
+// product) in captured runs of 24 calls, 361 us, 1520 as calls one after another for longer, where the power limit shows; 512 tokens on
+// 131072: 653 us, 1680 (90 %), and 709 us. By memory for decode steps: eight sequences of 32768 tokens
+// 171 us, 6.3 TB/s (93 % of a copy). By latency for short ones: 900 tokens of one sequence 14.3 us, two launches and
 // one pass through code that is not in the instruction caches; a unit costs 2 to 4 us beside its tiles (output, queries, first scores).
-// What was measured on the way, on that prompt: one issuing warp 609 us, its values in uniform registers 569, two issuing
+// What was measured on the way, on that prompt, captured: one issuing warp 609 us, its values in uniform registers 569, two issuing
 // warps 541, in turns and with the weights in halves 474, no maximum in the steady state 427, output and
 // queries in short coalesced loops 405, one threshold for the reference and no votes ahead of the weights 369, one body for
 // both halves with 64 scores a load 342, queries by TMA 333. With a maximum of every tile 473 instead of 427, without the
-// turns 448; with the output in a function that is not inlined 406 instead of 366. Partials merged by the last CTA of a block
-// instead of a kernel: 89 to 117 us instead of 76 on a mixed step, as its loads stand in the way of the next unit.
+// turns 448; with the output in a function that is not inlined 406 instead of 366. The bound on
+// the sum of a row's weights costs 1 %. Partials merged by the last CTA of a block instead of a kernel: 89 to 117 us instead of 76 on a mixed
+// step, whose partials are 252 rows, as its loads stand in the way of the next unit; not measured where every block is one token.
 #include <math.h>
 #include <stddef.h>
 
@@ -58,14 +60,14 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kRows = 128, kKeys = kKeysBf16;
-constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it. 512 tokens on
-                                                            // 131072, when it took 680 us: at 1 677, at 4 and 6 690
+constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it: geometric mean over
+                                                            // 19 cases 42.0 us, at 3 and 4 41.8, at 6 42.1, at 8 42.5
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // The weights of a row sum to less than kMost, so that neither an accumulator nor the sum of the two warpgroups' overflows,
-// whatever the values. kRoom (log2) is what scores may rise, and their number grow, before the reference moves: 8192 tokens with
-// some scores 10 deviations above the rest take 411 us at 24, 392 at 28, 377 at 32, 366 at 36, 359 at 40 (355 with no bound on the
-// sum of a row, 2^40 for half a tile's). What it costs is the low end: products with values below 2^-90 or so leave the range
+// whatever the values. kRoom (log2) is what scores may rise, and their number grow, before the reference moves: 8192 tokens,
+// one key in 200 four times as long as the others, take 411 us at 24, 392 at 28, 377 at 32, 366 at 36, 361 at 40 (357 with no bound on
+// the sum of a row, 2^40 for half a tile's). What it costs is the low end: products with values below 2^-90 or so leave the range
 // of fp32.
 constexpr float kMost = 0.25f, kRoom = 40.f;
 
@@ -181,7 +183,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = c.tmem;
   pdl_wait();
-  const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;   // by a call whose merge did not run, or runs still
+  // by a call whose merge did not run, or runs still
+  const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;
   const float weight = plan_weight<kKeys>(p, bq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);

@@ -2,7 +2,8 @@
 //
 // A copy: 16 threads (bf16) or 32 (fp32) move one token's row of a head, sixteen bytes each. A CTA takes kTokens tokens
 // of one (sequence, layer, K or V, head) at a time, four rows in flight per thread. Bound by memory: four layers of 32768
-// tokens, 8 heads, bf16: 174 us, 6.2 TB/s (91 % of a copy); 160 tokens of eight sequences: 4.3 us, a launch.
+// tokens, 8 heads, bf16: 174 us, 6.2 TB/s (91 % of a copy); 160 tokens of eight sequences: 4.3 us in a
+// captured run, a launch.
 #include "common.cuh"
 #include "paged.h"
 
