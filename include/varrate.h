@@ -458,6 +458,81 @@ varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_se
                                     int32_t n_layers, const int32_t* first, int32_t n, void* k_out,
                                     void* v_out, int32_t* dev_status, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Paged cache in 8 bits: sequences that run on uncoded tokens at half the bytes, and within a bound on their length. Same
+ * pages, batches, limits and rules as above, for bf16 rows. An element is an e4m3 code times a power of two that the 16 tokens of a
+ * block (places 16 i .. 16 i + 15 of a sequence) of one head share, keys and values apart; beside them each token has, per KV head,
+ * the attention weight that it has had since it was appended. varrate_paged8_append stores new tokens, varrate_paged8_attn
+ * attends over the pages, varrate_paged8_mass adds the weights up, and varrate_paged8_evict keeps the tokens with
+ * most of it. Limit: n_pages * 2 * n_kv_heads * page_size < 2^31, as above. */
+typedef struct {
+  void* codes;           /* [n_layers][n_pages][2][n_kv_heads][page_size][d] e4m3; 0 is K, 1 is V */
+  void* scale;           /* [n_layers][n_pages][2][n_kv_heads][page_size / 16] bytes: b stands for 2^(b - 127), b <= 246;
+                            0 only where every code of the block's tokens is a zero */
+  float* mass;           /* [n_layers][n_pages][n_kv_heads][page_size], or NULL: no weights are kept */
+  int32_t n_layers;
+  int32_t n_pages;
+  int32_t n_kv_heads;    /* G */
+  int32_t page_size;
+  int32_t head_dim;      /* d (must be 128) */
+} varrate_pages8;
+
+/* Append: as varrate_paged_append for bf16 rows, with the keys z and values stored as codes. For the new tokens of a
+ * block, one head, K or V:
+ *   b = least byte in [1, 246] with max |z| <= 448 * 2^(b - 127) over the finite z, 0 where they are all zero,
+ *       and at least the block's byte so far where it holds older tokens of the sequence;
+ *   code = z / 2^(b - 127) in fp32, rounded once to e4m3 (nearest, ties to even);
+ * and the older tokens' codes are divided by what the scale grew by, a power of two, and rounded again: exact but for numbers below
+ * 2^-6 of the new scale. |z| above 448 * 2^119 is stored as that; infinities and NaN are stored as NaN. What stands in a
+ * block past the sequence's last token is left alone.
+ *   gone      [S] int32 >= 0, or NULL: tokens that eviction has taken out of each sequence; the new ones rotate to
+ *             position place + gone[s]. A negative one raises VARRATE_ERR_CORRUPT; its sequence is not appended to.
+ * The mass of the new tokens is set to 0. One kernel, no workspace. */
+varrate_status varrate_paged8_append(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
+                                     int32_t group, const void* q, int64_t q_stride, const void* k,
+                                     int64_t k_stride, const void* v, int64_t v_stride,
+                                     const void* q_norm, const void* k_norm, double eps,
+                                     const double* freq, int32_t rot_dim, const int32_t* gone, void* q_out,
+                                     int32_t* dev_status, void* stream);
+
+/* Attention of the new tokens over the pages of one layer, as varrate_paged_attn with
+ *   k_u, v_u = code * 2^(b - 127).
+ * What stands at positions after a token's (NaN as well), in codes or scales of blocks past the last one, has no part in its
+ * result.
+ *   q     [T][H][d];  out [T][H][d], not overlapping q
+ *   lse   [T][H] fp32, or NULL: log sum_{u <= p} exp(<q, k_u> / sqrt(d)) of every row; -infinity where the scores all are
+ *   ws    as for varrate_paged_attn, of varrate_paged8_attn_ws_bytes(pages, seqs, group) bytes. */
+size_t varrate_paged8_attn_ws_bytes(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t group);
+varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
+                                   int32_t group, const void* q, void* out, float* lse, int32_t* dev_status,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/* Attention weights: for every sequence with new tokens, every KV head g and place u,
+ *   mass[u] += sum over the new tokens (rows t) that see u, and the query heads h of g, of exp(<q_th, k_u> / sqrt(d) - lse[t][h]),
+ * in fp32, in an order that does not change from call to call. lse as varrate_paged8_attn gives it for these queries; a row
+ * whose lse is not finite adds nothing. pages->mass must not be NULL. One kernel, no workspace. */
+varrate_status varrate_paged8_mass(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
+                                   int32_t group, const void* q, const float* lse, int32_t* dev_status,
+                                   void* stream);
+
+/* Eviction: sequences longer than `budget` tokens are cut to it, for the layers layer .. layer + n_layers - 1, each
+ * layer and KV head by itself: the first n_first tokens stay, the last n_last, and of the others the budget - n_first - n_last
+ * with most mass (of equal ones those with the lowest place; a NaN counts as most). The kept tokens move together in their order,
+ * codes, scales and mass: token j of a head is what token kept[j] was. A block's scale becomes the largest of the scales that its tokens
+ * came with, and codes that came with a smaller one are divided and rounded as by varrate_paged8_append. Keys keep the rotation that they have.
+ *   budget    >= 1;  n_first, n_last >= 0, n_first + n_last <= budget (looked at where a sequence is cut)
+ *   kept      [S][n_layers][G][budget] int32: old places of the kept tokens, ascending; -1 behind them
+ *   new_len   [S] int32: min(kv_len[s], budget); not overlapping kv_len. The caller makes it the sequences' kv_len once every layer
+ *             has been cut; the pages past it are free.
+ *   gone      [S] int32, or NULL: kv_len[s] - new_len[s] is added (give it to one call where several cut the layers)
+ * Uses kv_len and page_table of `seqs`, not row_start (which may be NULL). A sequence with kv_len or a page out of range raises
+ * VARRATE_ERR_CORRUPT: its pages stay as they were, its new_len is 0, its kept are -1 and its gone is left alone. Pages that two
+ * sequences share must not belong to one that is cut. pages->mass must not be NULL. One kernel, no workspace. */
+varrate_status varrate_paged8_evict(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
+                                    int32_t n_layers, int32_t budget, int32_t n_first, int32_t n_last,
+                                    int32_t* kept, int32_t* new_len, int32_t* gone, int32_t* dev_status,
+                                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "paged.h"
+#include "paged8.h"
 
 using vr::Shape;
 
@@ -458,6 +459,114 @@ varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_se
   if (!aligned16({first, k_out, v_out, dev_status})) return VARRATE_ERR_ARG;
   if (vr::launch_paged_gather(make_paged(pages, seqs), layer, n_layers, first, n, k_out, v_out, dev_status, num_sms(),
                               (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+// The 8-bit pages' sizes as those of bf16 pages, for the checks and the kernels that both share.
+static varrate_pages as_pages(const varrate_pages8* pages) {
+  varrate_pages p = {};
+  p.pool = pages->codes; p.n_layers = pages->n_layers; p.n_pages = pages->n_pages; p.n_kv_heads = pages->n_kv_heads;
+  p.page_size = pages->page_size; p.head_dim = pages->head_dim; p.dtype = VARRATE_BF16;
+  return p;
+}
+
+static varrate_status paged8_check(const varrate_pages8* pages, const varrate_seqs* seqs) {
+  if (pages == nullptr) return VARRATE_ERR_ARG;
+  const varrate_pages p = as_pages(pages);
+  return paged_check(&p, seqs);
+}
+
+static varrate_status paged8_pointers(const varrate_pages8* pages, const varrate_seqs* seqs, bool rows) {
+  const varrate_pages p = as_pages(pages);
+  if (!pages->scale || !aligned16({pages->scale, pages->mass})) return VARRATE_ERR_ARG;
+  return paged_pointers(&p, seqs, rows);
+}
+
+static vr::Paged8 make_paged8(const varrate_pages8* pages, const varrate_seqs* seqs) {
+  const varrate_pages p = as_pages(pages);
+  vr::Paged8 c;
+  c.p = make_paged(&p, seqs);
+  c.scale = static_cast<unsigned char*>(pages->scale);
+  c.mass = pages->mass;
+  return c;
+}
+
+varrate_status varrate_paged8_append(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer, int32_t group,
+                                     const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                     int64_t v_stride, const void* q_norm, const void* k_norm, double eps,
+                                     const double* freq, int32_t rot_dim, const int32_t* gone, void* q_out,
+                                     int32_t* dev_status, void* stream) {
+  varrate_status st = paged8_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers || group < 1 || !(eps >= 0.0) || !isfinite((float)eps)) return VARRATE_ERR_ARG;
+  if (group > 8) return VARRATE_ERR_UNSUPPORTED;
+  if (rot_dim < 0 || rot_dim > vr::kHeadDim || (rot_dim % 16) != 0) return VARRATE_ERR_ARG;
+  if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
+  if ((st = paged8_pointers(pages, seqs, true)) != VARRATE_OK) return st;
+  if (!k || !v || (q && !q_out) || (rot_dim > 0 && !freq)) return VARRATE_ERR_ARG;
+  if (!aligned16({q, k, v, q_norm, k_norm, freq, gone, q_out, dev_status})) return VARRATE_ERR_ARG;
+  const float eps32 = eps > 0.0 ? fmaxf((float)eps, FLT_TRUE_MIN) : 0.f;   // never rounded to 0: a head of zeros is no 0 / 0 then
+  const int64_t kd = (int64_t)pages->n_kv_heads * vr::kHeadDim;
+  if (k_stride < kd || k_stride % 8 != 0 || v_stride < kd || v_stride % 8 != 0) return VARRATE_ERR_ARG;
+  if (q && (q_stride < kd * group || q_stride % 8 != 0 || (q == q_out && q_stride != kd * group))) return VARRATE_ERR_ARG;
+  if (vr::launch_paged8_append(make_paged8(pages, seqs), layer, group, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm,
+                               eps32, freq, rot_dim, gone, q_out, dev_status, num_sms(), (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+size_t varrate_paged8_attn_ws_bytes(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t group) {
+  if (paged8_check(pages, seqs) != VARRATE_OK || group < 1 || group > 8) return 0;
+  return vr::paged8_attn_ws_bytes(make_paged8(pages, seqs), group, num_sms());
+}
+
+varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer, int32_t group,
+                                   const void* q, void* out, float* lse, int32_t* dev_status, void* ws, size_t ws_bytes_,
+                                   void* stream) {
+  varrate_status st = paged8_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers || group < 1) return VARRATE_ERR_ARG;
+  if (group > 8) return VARRATE_ERR_UNSUPPORTED;
+  if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
+  if ((st = paged8_pointers(pages, seqs, true)) != VARRATE_OK) return st;
+  if (!q || !out || q == out || !aligned16({q, out, lse, dev_status, ws})) return VARRATE_ERR_ARG;
+  const vr::Paged8 c = make_paged8(pages, seqs);
+  const int sms = num_sms();
+  if (ws_bytes_ < vr::paged8_attn_ws_bytes(c, group, sms) || ws == nullptr) return VARRATE_ERR_WORKSPACE;
+  if (vr::launch_paged8_attn(c, layer, group, q, out, lse, dev_status, ws, sms, (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+varrate_status varrate_paged8_mass(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer, int32_t group,
+                                   const void* q, const float* lse, int32_t* dev_status, void* stream) {
+  varrate_status st = paged8_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || layer >= pages->n_layers || group < 1) return VARRATE_ERR_ARG;
+  if (group > 8) return VARRATE_ERR_UNSUPPORTED;
+  if (seqs->n_seqs == 0 || seqs->n_rows == 0) return VARRATE_OK;
+  if ((st = paged8_pointers(pages, seqs, true)) != VARRATE_OK) return st;
+  if (!pages->mass || !q || !lse || !aligned16({q, lse, dev_status})) return VARRATE_ERR_ARG;
+  if (vr::launch_paged8_mass(make_paged8(pages, seqs), layer, group, q, lse, dev_status, num_sms(), (cudaStream_t)stream) < 0)
+    return VARRATE_ERR_CUDA;
+  return launched();
+}
+
+varrate_status varrate_paged8_evict(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer, int32_t n_layers,
+                                    int32_t budget, int32_t n_first, int32_t n_last, int32_t* kept, int32_t* new_len,
+                                    int32_t* gone, int32_t* dev_status, void* stream) {
+  varrate_status st = paged8_check(pages, seqs);
+  if (st != VARRATE_OK) return st;
+  if (layer < 0 || n_layers < 1 || n_layers > pages->n_layers - layer) return VARRATE_ERR_ARG;
+  if (budget < 1 || n_first < 0 || n_last < 0 || n_first > budget - n_last) return VARRATE_ERR_ARG;
+  if (seqs->n_seqs == 0) return VARRATE_OK;
+  if ((st = paged8_pointers(pages, seqs, false)) != VARRATE_OK) return st;
+  if (!pages->mass || !kept || !new_len || new_len == seqs->kv_len || gone == new_len || !aligned16({kept, new_len, gone, dev_status}))
+    return VARRATE_ERR_ARG;
+  if ((double)seqs->n_seqs * n_layers * pages->n_kv_heads > (double)(1 << 26)) return VARRATE_ERR_UNSUPPORTED;   // clusters of the grid
+  if (vr::launch_paged8_evict(make_paged8(pages, seqs), layer, n_layers, budget, n_first, n_last, kept, new_len, gone,
+                              dev_status, num_sms(), (cudaStream_t)stream) < 0)
     return VARRATE_ERR_CUDA;
   return launched();
 }

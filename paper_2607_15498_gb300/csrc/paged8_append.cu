@@ -1,0 +1,281 @@
+// Paged cache in 8 bits, append: head norm, rotation to the token's position, queries out, keys and values as codes into
+// their pages, with a scale for each block of 16 tokens of a head.
+//
+// y = x / sqrt(mean(x^2) + eps) * w, the pairs (i, i + rot/2) turned by position * freq[i] (the angle in turns as a 64-bit
+// integer, as in the append of the uncompressed cache), then for keys and values
+//   byte = max(byte of the block's older tokens, least with max |z| <= 448 * 2^(byte - 127)),  code = e4m3(z / 2^(byte - 127)),
+// and the older codes of the block times 2^(their byte - byte).
+// A unit is a block of 16 places of one sequence that gets new tokens; a warp takes the 16 tokens of one of its H + 2 G heads:
+// eight lanes a token, sixteen elements each (eight first members of pairs and their partners), four tokens at a time, so
+// that a block's largest element is in one warp's registers. Sines and cosines of the 16 tokens are made once for the CTA's heads.
+#include "common.cuh"
+#include "paged.h"
+#include "paged8.h"
+
+namespace vr {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 2;
+constexpr int kSteps = kBlock / 4;            // a warp's rows of a task, four at a time
+
+struct Append8Args {
+  const __nv_bfloat16 *q, *k, *v, *q_norm, *k_norm;
+  int64_t q_stride, k_stride, v_stride;
+  const double* freq;
+  const int32_t* gone;
+  unsigned char *codes, *scale;               // of the layer
+  float* mass;
+  __nv_bfloat16* q_out;
+  int32_t* dev_status;
+  float eps;
+  int rot, H, per;                            // H: 0 without queries; per: heads of an item
+};
+
+__device__ __forceinline__ void unpack(const uint4& u, float2 (&x)[4]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void load_pairs(const float* s, float2 (&x)[4]) {   // eight floats from shared memory
+  const float4 a = reinterpret_cast<const float4*>(s)[0], b = reinterpret_cast<const float4*>(s)[1];
+  x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
+}
+__device__ __forceinline__ float most(const float2 (&x)[4], float m) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = fmaxf(m, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
+  return m;
+}
+// the largest of the finite ones (an infinity is stored as NaN)
+__device__ __forceinline__ float most_finite(float2 (&x)[4], float m) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (fabsf(x[i].x) == INFINITY) x[i].x = NAN;
+    if (fabsf(x[i].y) == INFINITY) x[i].y = NAN;
+  }
+  return most(x, m);
+}
+__device__ __forceinline__ uint2 codes8(const float2 (&x)[4], float f) {
+  uint32_t c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = codes2(x[i].x * f, x[i].y * f);
+  return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+}
+
+// Units of the sequences before s: more than there are, found without a sum over the sequences (n new tokens lie in at most
+// (n + 14) / 16 + 1 <= n / 16 + 2 blocks).
+__device__ __forceinline__ int first_unit(const int32_t* row_start, int s) { return (__ldg(row_start + s) >> kBlockLog2) + 2 * s; }
+
+// The sequence whose units u is among: entries of first_unit[0 .. S] that are <= u, less one; one warp.
+__device__ __forceinline__ int seq_of_unit(const Paged& p, int u, int lane) {
+  int lo = 0, n = p.S + 1;
+  while (n > 32) {
+    const int step = (n + 31) >> 5, i = (lane + 1) * step - 1;
+    const int k = __popc(__ballot_sync(0xffffffffu, i < n && first_unit(p.row_start, lo + i) <= u));
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo + __popc(__ballot_sync(0xffffffffu, lane < n && first_unit(p.row_start, lo + lane) <= u)) - 1;
+}
+
+__global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p, Append8Args a) {
+  __shared__ unsigned long long turn[kHeadDim / 2];   // freq / 2 pi modulo 1, times 2^64
+  __shared__ __align__(16) float weight[2][kHeadDim];
+  __shared__ __align__(16) float angle[2][kBlock][2][kHeadDim / 2];   // [item & 1][token][cosine, sine]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7;
+  pdl_trigger();
+  pdl_wait();
+  if (tid < a.rot / 2) {
+    const double t = a.freq[tid] * 0.15915494309189535;   // 1 / 2 pi
+    turn[tid] = __double2ull_rn((t - floor(t)) * 18446744073709551616.0);
+  }
+  if (const __nv_bfloat16* w = tid < kHeadDim ? a.q_norm : a.k_norm) weight[tid / kHeadDim][tid % kHeadDim] = __bfloat162float(w[tid % kHeadDim]);
+  __syncthreads();
+  const int tasks = a.H + 2 * p.G, chunks = (tasks + a.per - 1) / a.per, h8 = a.rot / 16;
+  const int64_t items = (int64_t)((p.T >> kBlockLog2) + 2 * p.S + 1) * chunks;
+  // this lane's two groups of eight elements: a group of first members and its partners, or two groups that stay
+  const bool turns = sub < h8;
+  const int e0 = 8 * (turns ? sub : 2 * sub), e1 = 8 * (turns ? sub + h8 : 2 * sub + 1);
+
+  int buf = 0;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int u = (int)(it / chunks), lo = (int)(it % chunks) * a.per, hi = min(lo + a.per, tasks);
+    const int s = seq_of_unit(p, u, lane);
+    if (s < 0 || s >= p.S) continue;                  // (the same for the CTA)
+    SeqRange r;
+    if (!seq_range(p, s, r) || r.n == 0) continue;    // the status is raised below
+    const int start = r.len - r.n;                    // place of the first new token
+    const int64_t base64 = (((int64_t)start >> kBlockLog2) + (u - first_unit(p.row_start, s))) << kBlockLog2;
+    if (base64 >= r.len) continue;
+    const int base = (int)base64, old = max(start - base, 0), end = min(r.len - base, kBlock);   // new tokens: rows old .. end - 1
+    const int row0 = r.row0 + (base - start);         // row of the block's first place
+    int page = __ldg(p.table + (int64_t)s * p.max_pages + (base >> p.page_log2));
+    const int gone = a.gone ? __ldg(a.gone + s) : 0;
+    if (page < 0 || page >= p.n_pages || gone < 0) {
+      if (tid == 0 && lo == 0) raise_status(a.dev_status, VARRATE_ERR_CORRUPT);
+      if (gone < 0) continue;
+      page = -1;
+    }
+    bool made = a.rot == 0;                           // the item's sines and cosines are there
+    buf ^= 1;
+    for (int t0 = lo; t0 < hi; t0 += kWarps) {
+      const int task = t0 + warp;
+      const bool is_q = task < a.H, is_v = task >= a.H + p.G, live = task < hi;
+      uint4 x0[kSteps], x1[kSteps];
+      int64_t code_row = 0;
+      int before = 0;
+      if (live) {
+        const __nv_bfloat16* src = is_q ? a.q + task * kHeadDim : (is_v ? a.v + (task - a.H - p.G) * kHeadDim : a.k + (task - a.H) * kHeadDim);
+        const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const int row = 4 * i + (lane >> 3);
+          if (row < old || row >= end) continue;
+          const __nv_bfloat16* x = src + (row0 + row) * stride;   // (q may be q_out: no read-only loads)
+          x0[i] = *reinterpret_cast<const uint4*>(x + e0);
+          x1[i] = *reinterpret_cast<const uint4*>(x + e1);
+        }
+        if (!is_q && page >= 0) {
+          code_row = page_row(p, page, is_v, task - a.H - (is_v ? p.G : 0), base & ((1 << p.page_log2) - 1));
+          if (old) before = a.scale[scale_at(code_row)];
+        }
+      }
+      if (!made) {                                    // behind the first loads
+        for (int i = tid; i < kBlock * (a.rot / 2); i += kThreads) {
+          const int row = i / (a.rot / 2), j = i % (a.rot / 2);
+          if (row < old || row >= end) continue;
+          const unsigned long long pos = (unsigned long long)base + row + gone;
+          sincospif(__ll2float_rn((long long)(turn[j] * pos)) * 0x1p-63f, &angle[buf][row][1][j], &angle[buf][row][0][j]);
+        }
+        __syncthreads();
+        made = true;
+      }
+      if (!live) continue;
+      const bool normed = is_q ? a.q_norm != nullptr : a.k_norm != nullptr && !is_v, turned = turns && !is_v;
+      if (is_q && !normed && a.rot == 0) {            // a copy
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const int row = 4 * i + (lane >> 3);
+          if (row < old || row >= end) continue;
+          __nv_bfloat16* y = a.q_out + ((int64_t)(row0 + row) * a.H + task) * kHeadDim;
+          *reinterpret_cast<uint4*>(y + e0) = x0[i];
+          *reinterpret_cast<uint4*>(y + e1) = x1[i];
+        }
+        continue;
+      }
+      float2 y0[kSteps][4], y1[kSteps][4];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int row = 4 * i + (lane >> 3);
+        if (row >= old && row < end) {
+          unpack(x0[i], y0[i]);
+          unpack(x1[i], y1[i]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y0[i][j] = y1[i][j] = make_float2(0.f, 0.f);
+        }
+        if (normed) {                                 // (the same for the warp)
+          float2 sq = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sq = fma2(y0[i][j], y0[i][j], fma2(y1[i][j], y1[i][j], sq));
+          float ss = sq.x + sq.y;
+#pragma unroll
+          for (int o = 4; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          const float f1 = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
+          const float2 f = make_float2(f1, f1);
+          float2 w0[4], w1[4];
+          load_pairs(weight[is_q ? 0 : 1] + e0, w0);
+          load_pairs(weight[is_q ? 0 : 1] + e1, w1);
+          if (row >= old && row < end) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { y0[i][j] = mul2(mul2(y0[i][j], f), w0[j]); y1[i][j] = mul2(mul2(y1[i][j], f), w1[j]); }
+          }
+        }
+        if (turned && row >= old && row < end) {
+          float2 c[4], sn[4];
+          load_pairs(angle[buf][row][0] + e0, c);
+          load_pairs(angle[buf][row][1] + e0, sn);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 z = fma2(make_float2(-y1[i][j].x, -y1[i][j].y), sn[j], mul2(y0[i][j], c[j]));
+            y1[i][j] = fma2(y0[i][j], sn[j], mul2(y1[i][j], c[j]));
+            y0[i][j] = z;
+          }
+        }
+        if (is_q) {
+          if (row >= old && row < end) {
+            __nv_bfloat16* y = a.q_out + ((int64_t)(row0 + row) * a.H + task) * kHeadDim;
+            const float2(&b0)[4] = y0[i], (&b1)[4] = y1[i];
+            *reinterpret_cast<uint4*>(y + e0) = make_uint4(pack_bf16(b0[0].x, b0[0].y), pack_bf16(b0[1].x, b0[1].y), pack_bf16(b0[2].x, b0[2].y), pack_bf16(b0[3].x, b0[3].y));
+            *reinterpret_cast<uint4*>(y + e1) = make_uint4(pack_bf16(b1[0].x, b1[0].y), pack_bf16(b1[1].x, b1[1].y), pack_bf16(b1[2].x, b1[2].y), pack_bf16(b1[3].x, b1[3].y));
+          }
+        } else {
+          top = most(y1[i], most(y0[i], top));
+        }
+      }
+      if (is_q || page < 0) continue;
+      if (__any_sync(0xffffffffu, top == INFINITY)) {
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) top = most_finite(y1[i], most_finite(y0[i], top));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int byte = max(before, scale_byte(top));
+      const float f = byte ? scale_inverse(byte) : 1.f;
+      unsigned char* dst = a.codes + code_row * kHeadDim;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int row = 4 * i + (lane >> 3);
+        uint2 *z0 = reinterpret_cast<uint2*>(dst + row * kHeadDim + e0), *z1 = reinterpret_cast<uint2*>(dst + row * kHeadDim + e1);
+        if (row < old) {
+          if (byte != before) {
+            const Rescale by(byte - before);
+            const uint2 o0 = *z0, o1 = *z1;
+            *z0 = make_uint2(by.four(o0.x), by.four(o0.y));
+            *z1 = make_uint2(by.four(o1.x), by.four(o1.y));
+          }
+        } else if (row < end) {
+          *z0 = codes8(y0[i], f);
+          *z1 = codes8(y1[i], f);
+        }
+      }
+      if (lane == 0) a.scale[scale_at(code_row)] = (unsigned char)byte;
+      if (!is_v && a.mass && lane >= old && lane < end)
+        a.mass[mass_at(p, page, task - a.H, (base & ((1 << p.page_log2) - 1)) + lane)] = 0.f;
+    }
+  }
+  // every sequence's tables are checked, rows or not
+  for (int s = blockIdx.x * kThreads + tid; s < p.S; s += gridDim.x * kThreads) {
+    SeqRange r;
+    if (!seq_range(p, s, r)) raise_status(a.dev_status, VARRATE_ERR_CORRUPT);
+  }
+}
+
+}  // namespace
+
+int launch_paged8_append(const Paged8& c, int layer, int group, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm,
+                         float eps, const double* freq, int rot, const int32_t* gone, void* q_out, int32_t* dev_status,
+                         int num_sms, cudaStream_t st) {
+  const Paged& p = c.p;
+  Append8Args a;
+  a.q = (const __nv_bfloat16*)q; a.k = (const __nv_bfloat16*)k; a.v = (const __nv_bfloat16*)v;
+  a.q_norm = q ? (const __nv_bfloat16*)q_norm : nullptr; a.k_norm = (const __nv_bfloat16*)k_norm;
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.freq = freq; a.gone = gone; a.q_out = (__nv_bfloat16*)q_out; a.dev_status = dev_status; a.eps = eps; a.rot = rot;
+  a.H = q ? group * p.G : 0;
+  a.codes = p.pool + (int64_t)layer * p.layer_rows * kHeadDim;
+  a.scale = c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2);
+  a.mass = c.mass ? c.mass + (int64_t)layer * (p.layer_rows / 2) : nullptr;
+  // whole units per CTA where there are enough of them, else their heads over several CTAs
+  const int tasks = a.H + 2 * p.G;
+  const int64_t units = (p.T >> kBlockLog2) + 2 * (int64_t)p.S + 1, most = (int64_t)num_sms * kCtas;
+  a.per = (tasks + kWarps - 1) / kWarps * kWarps;
+  while (a.per > kWarps && units * ((tasks + a.per - 1) / a.per) < 4 * most) a.per = (a.per / 2 + kWarps - 1) / kWarps * kWarps;
+  const int64_t items = units * ((tasks + a.per - 1) / a.per);
+  return launch_pdl(paged8_append_kernel, dim3((unsigned)(items < most ? items : most)), kThreads, 0, st, p, a) ? 1 : -1;
+}
+
+}  // namespace vr

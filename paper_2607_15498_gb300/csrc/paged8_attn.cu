@@ -1,0 +1,324 @@
+// Paged cache in 8 bits, attention of few new tokens: codes go from memory to registers and, as they are, into tensor-core
+// products of fp16 fragments (mma.sync).
+//
+// A row is a (token, query head) pair of one KV head; a CTA works for a block of at most 8 rows, a warp on steps of 16 keys, which
+// share a scale. Per step, transposed so that 8 rows fill the products:
+//   S^T[key][row] = K[key][.] Q[row][.]     8 products of 16 keys x 8 rows x 16 elements,
+//   O^T[element][row] += V^T[element][key] P^T[key][row]     8 products of 16 elements x 8 rows x 16 keys.
+// An e4m3 code is exact in fp16 and two are expanded by one instruction. Which element of a head an operand's index means is
+// free as long as both operands agree, so that a lane takes 16 bytes of a key (or of four keys' values) as they stand in the page.
+//   queries  x 2^n with the largest element of a row in [2^14, 2^15): exact in fp16 down to 2^-38 of it;
+//   scores   x (scale of the block) x (2^-n log2 e / sqrt(d)) in fp32;
+//   weights  p x 2^(4 + b - u) in fp16, b the scale byte of the step's values and u that of the accumulator, which is
+//            in units of 2^(u - 127): u rises where b is more than 3 above it. A step more than 10 below goes in bf16, where the weight
+//            has the range of fp32 (and values below 2^-100 or so of the largest block's are lost at the end of that range).
+// The reference of a row moves only when a score is 8 (log2) above it.
+// Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh).
+#include <float.h>
+#include <math.h>
+
+#include "common.cuh"
+#include "paged.h"
+#include "paged8.h"
+#include "paged8_mma.cuh"
+#include "paged_plan.cuh"
+
+namespace vr {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 2;
+constexpr int kRows = 8, kKeys = kKeysBf16;
+constexpr float kOverhead = 8.f;             // of a unit, in key tiles, as the plan counts it
+constexpr float kSlack = 8.f;                // what scores may rise above the reference before it moves (log2)
+constexpr int kUp = 4;                       // weights are stored times 2^kUp
+
+struct Shared {
+  PlanSums plan;
+  Unit unit;
+  int seq;
+  float m[kWarps][kRows], l[kWarps][kRows];
+  int u[kWarps];
+  __align__(16) float o[kWarps][kRows][kHeadDim + 4];
+};
+
+// Values of a step with rows that do not see all of its keys: those past the batch's tokens are zeroed; NaN codes of keys that
+// only a part of the rows sees are zeroed and returned as bits, 16 codes a key.
+__device__ __forceinline__ bool take_nan(uint4& v, uint32_t& bits) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t n = __vcmpeq4(w[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+    w[i] &= ~n;
+    bits |= ((n & 1) | (n >> 7 & 2) | (n >> 14 & 4) | (n >> 21 & 8)) << (4 * i);
+  }
+  return bits != 0;
+}
+
+__global__ void __launch_bounds__(kThreads, kCtas)
+paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scale,
+                   const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
+                   int32_t* __restrict__ dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts,
+                   int grp, float scale_log2) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  Shared& c = *reinterpret_cast<Shared*>(smem);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
+  const int tq = kRows / grp, H = p.G * grp, C = gridDim.x;
+  pdl_trigger();
+  if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
+  __syncthreads();
+  pdl_wait();
+  const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
+  int longest, run = 1, units = 0, parts = 0;
+  const float weight = plan_weight<kKeys>(p, tq, lane, longest);
+  const int cand = plan_candidate(weight, longest, C, lane);
+  plan_add<kKeys>(p, c.plan, tq, cand, warp, kWarps, lane);
+  __syncthreads();
+  plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
+  if (blockIdx.x == 0) {
+    if (tid == 0) {
+      if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);   // by a call whose merge did not run, or runs still
+      header->run = run; header->units = units; header->parts = parts; header->open = 1;
+    }
+    for (int s = tid; s < p.S; s += kThreads) {
+      SeqRange r;
+      if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+    }
+  }
+  Walk<kKeys> w;
+  if (warp == 0) w.load(p, tq, run, lane);
+  int next = blockIdx.x;                                            // of warp 0
+  for (;;) {
+    if (warp == 0) {
+      Unit x;
+      int s = 0;
+      x.valid = 0;
+      while (next < units) {
+        s = w.find(p, tq, tq, run, next, lane, x);
+        int n = 0;
+        if (lane == 0) n = take_unit(header, C, units);
+        next = __shfl_sync(0xffffffffu, n, 0);
+        if (x.t0 < x.t1) break;                                     // else: the block ends before this run
+        x.valid = 0;
+      }
+      if (lane == 0) { c.unit = x; c.seq = s; }
+    }
+    __syncthreads();
+    const Unit x = c.unit;
+    const int s = c.seq;
+    if (!x.valid) break;
+    const int rows = x.ntok * grp, end = x.pos0 + x.ntok;
+    const int32_t* table = p.table + (int64_t)s * p.max_pages;
+    const int last = min(8 * x.t1, (end + 15) >> 4), in_page = (1 << p.page_log2) - 1;
+    const int64_t to_v = (int64_t)p.G << p.page_log2;               // rows from a key to its value
+
+    QueryFrags qf;
+    qf.load(q + ((int64_t)(x.row0 + g8 / grp) * H + x.g * grp + g8 % grp) * kHeadDim, g8 < rows, scale_log2, lane);
+    const int sees0 = x.pos0 + 2 * t4 / grp + 1, sees1 = x.pos0 + (2 * t4 + 1) / grp + 1;   // keys that rows 2 t4, 2 t4 + 1 see
+    float o[8][4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    int unit = -1;                                                  // scale byte of the accumulator's unit, none yet
+
+    int st = 8 * x.t0 + warp;
+    auto row_of = [&](int step) {                                   // of the codes: the step's first key
+      int page = __ldg(table + ((step << 4) >> p.page_log2));
+      if (page < 0 || page >= p.n_pages) { raise_status(dev_status, VARRATE_ERR_CORRUPT); page = 0; }
+      return page_row(p, page, 0, x.g, (step << 4) & in_page);
+    };
+    uint4 kq[4], vq[4];
+    int bk = 0, bv = 0;
+    auto load_k = [&](int64_t row) {
+      const unsigned char* src = codes + row * kHeadDim + 16 * t4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kq[i] = ld_nc_early_v4(reinterpret_cast<const uint4*>(src + (g8 + 8 * (i >> 1)) * kHeadDim + 64 * (i & 1)));
+    };
+    auto load_v = [&](int64_t row) {
+      const unsigned char* src = codes + (row + to_v) * kHeadDim + 16 * g8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vq[i] = ld_nc_early_v4(reinterpret_cast<const uint4*>(src + (2 * t4 + (i & 1) + 8 * (i >> 1)) * kHeadDim));
+    };
+    int64_t row = 0;
+    if (st < last) {
+      row = row_of(st);
+      load_k(row);
+      bk = __ldg(scale + scale_at(row));
+      load_v(row);
+      bv = __ldg(scale + scale_at(row + to_v));
+    }
+    for (; st < last; st += kWarps) {
+      const int key0 = st << 4, more = st + kWarps < last;
+      const bool edge = key0 + 16 > x.pos0 + 1;                     // some row does not see all of its keys
+      const int64_t row1 = more ? row_of(st + kWarps) : 0;
+      float sc[4];
+      key_scores(kq, qf, sc);
+      // (of two extremes: no infinity that would make a number of a zero)
+      const float f = __uint_as_float((uint32_t)bk << 23), f0 = fminf(qf.f0 * f, FLT_MAX), f1 = fminf(qf.f1 * f, FLT_MAX);
+      if (more) {
+        load_k(row1);
+        bk = __ldg(scale + scale_at(row1));
+      }
+      float x0 = sc[0] * f0, x1 = sc[1] * f1, x2 = sc[2] * f0, x3 = sc[3] * f1;
+      if (edge) {
+        const int a = key0 + g8, b = a + 8;
+        if (a >= sees0) x0 = -INFINITY;
+        if (a >= sees1) x1 = -INFINITY;
+        if (b >= sees0) x2 = -INFINITY;
+        if (b >= sees1) x3 = -INFINITY;
+      }
+      if (__any_sync(0xffffffffu, fmaxf(x0, x2) > m0 + kSlack || fmaxf(x1, x3) > m1 + kSlack)) {
+        float a = fmaxf(x0, x2), b = fmaxf(x1, x3);
+#pragma unroll
+        for (int i = 4; i < 32; i <<= 1) {
+          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, i));
+          b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, i));
+        }
+        float fa = 1.f, fb = 1.f;
+        if (a > m0 + kSlack) { fa = fast_exp2(m0 - a); m0 = a; }
+        if (b > m1 + kSlack) { fb = fast_exp2(m1 - b); m1 = b; }
+        l0 *= fa;
+        l1 *= fb;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { o[j][0] *= fa; o[j][2] *= fa; o[j][1] *= fb; o[j][3] *= fb; }
+      }
+      const float r0 = m0 == -INFINITY ? 0.f : m0, r1 = m1 == -INFINITY ? 0.f : m1;
+      x0 = fast_exp2(x0 - r0); x2 = fast_exp2(x2 - r0);
+      x1 = fast_exp2(x1 - r1); x3 = fast_exp2(x3 - r1);
+      l0 += x0 + x2;
+      l1 += x1 + x3;
+
+      uint32_t nan[4];
+      bool odd = false;
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 2 * t4 + (i & 1) + 8 * (i >> 1);
+          nan[i] = 0;
+          if (key >= end) vq[i] = make_uint4(0, 0, 0, 0);
+          else if (key > x.pos0) odd |= take_nan(vq[i], nan[i]);
+        }
+        odd = __any_sync(0xffffffffu, odd);
+      }
+      if (unit < 0 || bv > unit + 3) {                              // (the same for the warp)
+        if (unit >= 0) {
+          const float down = exp2f((float)(unit - bv));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) { o[j][0] *= down; o[j][1] *= down; o[j][2] *= down; o[j][3] *= down; }
+        }
+        unit = bv;
+      }
+      const int d = bv ? bv - unit : 0;
+      if (d >= -10) {
+        const float up = __uint_as_float((uint32_t)(127 + kUp + d) << 23);
+        const uint32_t b0 = movmatrix_trans(pack_f16(x0 * up, x1 * up)), b1 = movmatrix_trans(pack_f16(x2 * up, x3 * up));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
+          const uint32_t a[4] = {f16_codes(lo), f16_codes(lo >> 16), f16_codes(hi), f16_codes(hi >> 16)};
+          mma_f16_16816(o[j], a, b0, b1);
+        }
+      } else {
+        const float up = exp2f((float)(kUp + d));
+        const uint32_t b0 = movmatrix_trans(pack_bf16(x0 * up, x1 * up)), b1 = movmatrix_trans(pack_bf16(x2 * up, x3 * up));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
+          const uint32_t a[4] = {bf16_codes(lo), bf16_codes(lo >> 16), bf16_codes(hi), bf16_codes(hi >> 16)};
+          mma_bf16_16816(o[j], a, b0, b1);
+        }
+      }
+      if (odd) {                                                    // rare: NaN of keys that a part of the rows sees
+#pragma unroll 1
+        for (int k = 0; k < 16; ++k) {
+          const int i = (k & 1) + 2 * (k >> 3), key = key0 + k;
+          const uint32_t mine = i == 0 ? nan[0] : i == 1 ? nan[1] : i == 2 ? nan[2] : nan[3];
+          const uint32_t bits = __shfl_sync(0xffffffffu, mine, (lane & ~3) | ((k & 7) >> 1));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool a = bits >> (2 * j) & 1, b = bits >> (2 * j + 1) & 1;
+            if (a && key < sees0) o[j][0] = NAN;
+            if (a && key < sees1) o[j][1] = NAN;
+            if (b && key < sees0) o[j][2] = NAN;
+            if (b && key < sees1) o[j][3] = NAN;
+          }
+        }
+      }
+      if (more) {
+        load_v(row1);
+        bv = __ldg(scale + scale_at(row1 + to_v));
+      }
+    }
+    // the warps' rows
+#pragma unroll
+    for (int i = 4; i < 32; i <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, i);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, i);
+    }
+    if (lane < 4) {
+      c.m[warp][2 * lane] = m0; c.m[warp][2 * lane + 1] = m1;
+      c.l[warp][2 * lane] = l0; c.l[warp][2 * lane + 1] = l1;
+      if (lane == 0) c.u[warp] = max(unit, 0);
+    }
+    {
+      const float down = 1.f / (1 << kUp);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        *reinterpret_cast<float2*>(&c.o[warp][2 * t4][16 * g8 + 2 * j]) = make_float2(o[j][0] * down, o[j][2] * down);
+        *reinterpret_cast<float2*>(&c.o[warp][2 * t4 + 1][16 * g8 + 2 * j]) = make_float2(o[j][1] * down, o[j][3] * down);
+      }
+    }
+    __syncthreads();
+    if (warp < rows) {                                              // a row a warp, four elements a lane
+      float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, c.m[i][warp]);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) ll += c.l[i][warp] * fast_exp2(c.m[i][warp] - ref);
+      const float f = ll == 0.f ? 0.f : 1.f / ll;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float f1 = fast_exp2(c.m[i][warp] - ref) * f, f2 = __uint_as_float((uint32_t)c.u[i] << 23);   // normalised, then its unit
+        const float4 v = *reinterpret_cast<const float4*>(&c.o[i][warp][4 * lane]);
+        y.x += v.x * f1 * f2; y.y += v.y * f1 * f2; y.z += v.z * f1 * f2; y.w += v.w * f1 * f2;
+      }
+      const float at = ll == 0.f ? -INFINITY : ref + log2f(ll);
+      if (x.slot < 0) {
+        const int64_t i = (int64_t)(x.row0 + warp / grp) * H + x.g * grp + warp % grp;
+        *reinterpret_cast<uint2*>(out + i * kHeadDim + 4 * lane) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+        if (lse && lane == 0) lse[i] = at * 0.69314718f;
+      } else {
+        const int64_t i = (int64_t)x.slot * part_rows + warp;
+        *reinterpret_cast<float4*>(part + i * kHeadDim + 4 * lane) = y;
+        if (lane == 0)
+          reinterpret_cast<float2*>(part + (int64_t)max_parts * part_rows * kHeadDim)[i] = make_float2(at, ll == 0.f ? 0.f : 1.f);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms) {
+  return paged_part_bytes(c.p, group, kRows / group, num_sms);
+}
+
+int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
+                       void* ws, int num_sms, cudaStream_t st) {
+  const Paged& p = c.p;
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  Header* header = reinterpret_cast<Header*>(w);
+  float* part = reinterpret_cast<float*>(w + kHeaderBytes);
+  const int tq = kRows / group;
+  if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, p,
+                  p.pool + (int64_t)layer * p.layer_rows * kHeadDim, c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
+                  (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
+                  paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim)))
+    return -1;
+  return launch_paged_merge(p, group, out, lse, dev_status, header, part, tq, tq, num_sms, st) < 0 ? -1 : 2;
+}
+
+}  // namespace vr

@@ -777,7 +777,7 @@ int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, vo
                   header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
                   kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  return launch_paged_merge(p, group, out, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
+  return launch_paged_merge(p, group, out, nullptr, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr

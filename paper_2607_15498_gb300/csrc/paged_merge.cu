@@ -17,7 +17,7 @@ __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<f
 // Bound by latency: what a row needs is read in two steps, first header and tables, then its partials.
 template <typename T>
 __global__ void __launch_bounds__(256)
-paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Header* header, const float* __restrict__ part,
+paged_attn_merge_kernel(Paged p, T* __restrict__ out, float* __restrict__ lse, int32_t* dev_status, Header* header, const float* __restrict__ part,
                         int part_rows, int max_parts, int grp, int tq, int bq) {
   constexpr int kBatch = 8, kKeys = sizeof(T) == 4 ? kKeysF32 : kKeysBf16;
   const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
@@ -89,6 +89,7 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     }
     const float f1 = l == 0.f ? 0.f : 1.f / l;
     store4(out + (int64_t)i * kHeadDim + lane * 4, make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1));
+    if (lse && lane == 0) lse[i] = l == 0.f ? -INFINITY : (m + log2f(l) + (float)(32 - __clz(runs - 1))) * 0.69314718f;   // (room left out again)
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if ((h.taken != (unsigned)h.units || h.first != h.units) && !h.gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
@@ -100,21 +101,21 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
 }
 
 template <typename T>
-int launch(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq, int bq,
+int launch(const Paged& p, int group, void* out, float* lse, int32_t* dev_status, Header* header, const float* part, int tq, int bq,
            int num_sms, cudaStream_t st) {
   const int64_t warps = (int64_t)p.T * p.G * group;
   const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
-  return launch_pdl(paged_attn_merge_kernel<T>, dim3(grid), 256, 0, st, p, (T*)out, dev_status, header, part,
+  return launch_pdl(paged_attn_merge_kernel<T>, dim3(grid), 256, 0, st, p, (T*)out, lse, dev_status, header, part,
                     paged_part_rows(p, group, bq), paged_max_parts(num_sms), group, tq, bq)
              ? 1 : -1;
 }
 
 }  // namespace
 
-int launch_paged_merge(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
-                       int bq, int num_sms, cudaStream_t st) {
-  return p.dtype == VARRATE_F32 ? launch<float>(p, group, out, dev_status, header, part, tq, bq, num_sms, st)
-                                : launch<__nv_bfloat16>(p, group, out, dev_status, header, part, tq, bq, num_sms, st);
+int launch_paged_merge(const Paged& p, int group, void* out, float* lse, int32_t* dev_status, Header* header, const float* part,
+                       int tq, int bq, int num_sms, cudaStream_t st) {
+  return p.dtype == VARRATE_F32 ? launch<float>(p, group, out, lse, dev_status, header, part, tq, bq, num_sms, st)
+                                : launch<__nv_bfloat16>(p, group, out, lse, dev_status, header, part, tq, bq, num_sms, st);
 }
 
 }  // namespace vr

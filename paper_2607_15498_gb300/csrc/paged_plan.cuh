@@ -198,8 +198,8 @@ inline size_t paged_part_bytes(const Paged& p, int group, int bq, int num_sms) {
   return kHeaderBytes + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
 }
 // Merges partials into `out` and leaves the header as the next call wants it. tq: tokens of a query tile, of which a block has
-// one or two.
-int launch_paged_merge(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
-                       int bq, int num_sms, cudaStream_t st);
+// one or two. lse: [T][H], or null: the logarithm of a row's sum as well.
+int launch_paged_merge(const Paged& p, int group, void* out, float* lse, int32_t* dev_status, Header* header, const float* part,
+                       int tq, int bq, int num_sms, cudaStream_t st);
 
 }  // namespace vr

@@ -80,6 +80,12 @@ class varrate_seqs(ctypes.Structure):
                 ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32)]
 
 
+class varrate_pages8(ctypes.Structure):
+    _fields_ = [("codes", _c_void_p), ("scale", _c_void_p), ("mass", _c_void_p), ("n_layers", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
 _lib = None
 
 _SIGS = {
@@ -144,6 +150,23 @@ _SIGS = {
     "varrate_paged_gather": (ctypes.c_int32, [ctypes.POINTER(varrate_pages), ctypes.POINTER(varrate_seqs),
                                               ctypes.c_int32, ctypes.c_int32, _c_void_p, ctypes.c_int32,
                                               _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
+    "varrate_paged8_append": (ctypes.c_int32, [ctypes.POINTER(varrate_pages8), ctypes.POINTER(varrate_seqs),
+                                               ctypes.c_int32, ctypes.c_int32, _c_void_p, ctypes.c_int64,
+                                               _c_void_p, ctypes.c_int64, _c_void_p, ctypes.c_int64,
+                                               _c_void_p, _c_void_p, ctypes.c_double, _c_void_p,
+                                               ctypes.c_int32, _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
+    "varrate_paged8_attn_ws_bytes": (ctypes.c_size_t, [ctypes.POINTER(varrate_pages8),
+                                                       ctypes.POINTER(varrate_seqs), ctypes.c_int32]),
+    "varrate_paged8_attn": (ctypes.c_int32, [ctypes.POINTER(varrate_pages8), ctypes.POINTER(varrate_seqs),
+                                             ctypes.c_int32, ctypes.c_int32, _c_void_p, _c_void_p, _c_void_p,
+                                             _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+    "varrate_paged8_mass": (ctypes.c_int32, [ctypes.POINTER(varrate_pages8), ctypes.POINTER(varrate_seqs),
+                                             ctypes.c_int32, ctypes.c_int32, _c_void_p, _c_void_p, _c_void_p,
+                                             _c_void_p]),
+    "varrate_paged8_evict": (ctypes.c_int32, [ctypes.POINTER(varrate_pages8), ctypes.POINTER(varrate_seqs),
+                                              ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                              ctypes.c_int32, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                              _c_void_p]),
 }
 
 EXPORTED = tuple(_SIGS)
@@ -319,12 +342,9 @@ def _on_device(pages, call, *args) -> int:
         return call(*args)
 
 
-def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
-                         dev_status, stream=None) -> int:
-    """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
-    ERR_ARG where a tensor is not of the cache's type, shape or device."""
-    if not pages.works_with(seqs, dev_status):
-        return ERR_ARG
+def _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out):
+    """(group, q, q_stride, k, k_stride, v, v_stride, freq, q_out) as an append's C call takes them, or None where a tensor is
+    not of the cache's type, shape or device."""
     G, T = pages.heads, seqs.n_rows
     k_row, v_row = pages.row_stride(k, T, G), pages.row_stride(v, T, G)
     if q is None:
@@ -333,22 +353,33 @@ def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq,
         H = q.shape[1] if q.dim() == 3 else 0
         q_row = pages.row_stride(q, T, H)
         if q_row < 0 or H % G or not pages.takes(q_out, (T, H, 128)):
-            return ERR_ARG
+            return None
         q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     if k_row < 0 or v_row < 0:
-        return ERR_ARG
+        return None
     if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
-        return ERR_ARG
+        return None
     freq_ptr = None
     if rot_dim and freq is not None:
         freq_ptr = freq.data_ptr()
         if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
                 and freq.get_device() == pages.device):
-            return ERR_ARG
+            return None
+    return H // G, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, freq_ptr, out_ptr
+
+
+def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
+                         dev_status, stream=None) -> int:
+    """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
+    ERR_ARG where a tensor is not of the cache's type, shape or device."""
+    if not pages.works_with(seqs, dev_status):
+        return ERR_ARG
+    a = _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out)
+    if a is None:
+        return ERR_ARG
     return _on_device(
-        pages, (_lib or lib()).varrate_paged_append, pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row,
-        v.data_ptr(), v_row, _ptr(q_norm), _ptr(k_norm), eps, freq_ptr, rot_dim, out_ptr, _ptr(dev_status),
-        pages.stream(stream))
+        pages, (_lib or lib()).varrate_paged_append, pages.ref, seqs.ref, layer, *a[:7], _ptr(q_norm), _ptr(k_norm), eps, a[7],
+        rot_dim, a[8], _ptr(dev_status), pages.stream(stream))
 
 
 def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
@@ -379,6 +410,61 @@ def varrate_paged_gather(pages, seqs, layer, n_layers, first, n, k_out, v_out, d
         return ERR_ARG
     return _on_device(pages, (_lib or lib()).varrate_paged_gather, pages.ref, seqs.ref, layer, n_layers, _ptr(first), n,
                       _ptr(k_out), _ptr(v_out), _ptr(dev_status), pages.stream(stream))
+
+
+def _i32(pages, t, shape) -> bool:
+    """Whether t is None or dense int32 of this shape on the cache's device."""
+    return t is None or (t.dtype is torch.int32 and t.shape == shape and t.is_contiguous() and t.get_device() == pages.device)
+
+
+def varrate_paged8_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, gone, q_out,
+                          dev_status, stream=None) -> int:
+    """As varrate_paged_append, on a Paged8Cache and bf16 rows; gone [S] int32 or None."""
+    if not pages.works_with(seqs, dev_status) or not _i32(pages, gone, (seqs.n_seqs,)):
+        return ERR_ARG
+    a = _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out)
+    if a is None:
+        return ERR_ARG
+    return _on_device(
+        pages, (_lib or lib()).varrate_paged8_append, pages.ref, seqs.ref, layer, *a[:7], _ptr(q_norm), _ptr(k_norm), eps, a[7],
+        rot_dim, _ptr(gone), a[8], _ptr(dev_status), pages.stream(stream))
+
+
+def varrate_paged8_attn_ws_bytes(pages, seqs, group) -> int:
+    return _on_device(pages, lib().varrate_paged8_attn_ws_bytes, pages.ref, seqs.ref, group)
+
+
+def varrate_paged8_attn(pages, seqs, layer, group, q, out, lse, dev_status, ws, stream=None) -> int:
+    """q and out [T][H][d] bf16, lse [T][H] fp32 or None, dense. ERR_ARG where a tensor is not of that type or shape
+    or not on the cache's device."""
+    shape = (seqs.n_rows, pages.heads * group, 128)
+    if not (pages.takes(q, shape) and pages.takes(out, shape)) or (lse is not None and not pages.takes_f32(lse, shape[:2])):
+        return ERR_ARG
+    if ws is not None and not (pages.works_with(seqs, dev_status) and ws.get_device() == pages.device and ws.is_contiguous()):
+        return ERR_ARG                                # (without one the C call launches nothing)
+    return _on_device(pages, (_lib or lib()).varrate_paged8_attn, pages.ref, seqs.ref, layer, group, q.data_ptr(),
+                      out.data_ptr(), _ptr(lse), _ptr(dev_status), _ptr(ws), _nbytes(ws), pages.stream(stream))
+
+
+def varrate_paged8_mass(pages, seqs, layer, group, q, lse, dev_status, stream=None) -> int:
+    """q [T][H][d] bf16, lse [T][H] fp32, dense. ERR_ARG where a tensor is not of that type or shape or not on the cache's device."""
+    shape = (seqs.n_rows, pages.heads * group, 128)
+    if not (pages.takes(q, shape) and pages.takes_f32(lse, shape[:2]) and pages.works_with(seqs, dev_status)):
+        return ERR_ARG
+    return _on_device(pages, (_lib or lib()).varrate_paged8_mass, pages.ref, seqs.ref, layer, group, q.data_ptr(),
+                      lse.data_ptr(), _ptr(dev_status), pages.stream(stream))
+
+
+def varrate_paged8_evict(pages, seqs, layer, n_layers, budget, n_first, n_last, kept, new_len, gone, dev_status,
+                         stream=None) -> int:
+    """kept [S][n_layers][G][budget], new_len [S], gone [S] or None: int32, dense. ERR_ARG where a tensor is not of that
+    type or shape or not on the cache's device."""
+    S = seqs.n_seqs
+    if kept is None or new_len is None or not pages.works_with(seqs, dev_status) or not (
+            _i32(pages, kept, (S, n_layers, pages.heads, budget)) and _i32(pages, new_len, (S,)) and _i32(pages, gone, (S,))):
+        return ERR_ARG
+    return _on_device(pages, (_lib or lib()).varrate_paged8_evict, pages.ref, seqs.ref, layer, n_layers, budget, n_first,
+                      n_last, kept.data_ptr(), new_len.data_ptr(), _ptr(gone), _ptr(dev_status), pages.stream(stream))
 
 
 # ------------------------------------------------------------- device-memory plumbing
@@ -450,30 +536,8 @@ class QPackedCache:
         return QPackedCache(data, qbase, source, bits, cap, c)
 
 
-@dataclass
-class PagedCache:
-    """The pages of a paged cache: pool [n_layers][n_pages][2][G][page_size][d] (0 is K, 1 is V) plus the
-    C struct pointing at it. Which page belongs to which sequence is the caller's."""
-    pool: torch.Tensor
-    c: varrate_pages
-
-    @staticmethod
-    def of(pool: torch.Tensor) -> "PagedCache":
-        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in (
-                torch.bfloat16, torch.float32):
-            raise VarrateError(ERR_ARG, "PagedCache.of")
-        L, P, _, G, ps, d = pool.shape
-        c = varrate_pages(pool.data_ptr(), L, P, G, ps, d, BF16 if pool.dtype == torch.bfloat16 else F32)
-        return PagedCache(pool, c)
-
-    @staticmethod
-    def allocate(n_layers, n_pages, n_kv_heads, page_size, dtype=BF16, device="cuda") -> "PagedCache":
-        return PagedCache.of(torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size, 128), device=device,
-                                         dtype=torch.bfloat16 if dtype == BF16 else torch.float32))
-
-    def __post_init__(self):
-        self.ref = ctypes.byref(self.c)
-        self.heads, self.dtype, self.device = self.c.n_kv_heads, self.pool.dtype, self.pool.get_device()
+class _Pages:
+    """What the paged calls ask of a cache: `dtype` of the rows, `heads` and `device`."""
 
     def takes(self, t: torch.Tensor, shape) -> bool:
         """Whether t has this shape and the cache's type and device and is dense."""
@@ -500,6 +564,76 @@ class PagedCache:
         if stream is None and self.device >= 0:
             return torch._C._cuda_getCurrentRawStream(self.device)
         return _stream(stream)
+
+    def takes_f32(self, t: torch.Tensor, shape) -> bool:
+        """Whether t is dense fp32 of this shape on the cache's device."""
+        return (t is not None and t.shape == shape and t.dtype is torch.float32 and t.is_contiguous()
+                and t.get_device() == self.device)
+
+
+@dataclass
+class PagedCache(_Pages):
+    """The pages of a paged cache: pool [n_layers][n_pages][2][G][page_size][d] (0 is K, 1 is V) plus the
+    C struct pointing at it. Which page belongs to which sequence is the caller's."""
+    pool: torch.Tensor
+    c: varrate_pages
+
+    @staticmethod
+    def of(pool: torch.Tensor) -> "PagedCache":
+        if pool.dim() != 6 or pool.shape[2] != 2 or not pool.is_contiguous() or pool.dtype not in (
+                torch.bfloat16, torch.float32):
+            raise VarrateError(ERR_ARG, "PagedCache.of")
+        L, P, _, G, ps, d = pool.shape
+        c = varrate_pages(pool.data_ptr(), L, P, G, ps, d, BF16 if pool.dtype == torch.bfloat16 else F32)
+        return PagedCache(pool, c)
+
+    @staticmethod
+    def allocate(n_layers, n_pages, n_kv_heads, page_size, dtype=BF16, device="cuda") -> "PagedCache":
+        return PagedCache.of(torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size, 128), device=device,
+                                         dtype=torch.bfloat16 if dtype == BF16 else torch.float32))
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.c)
+        self.heads, self.dtype, self.device = self.c.n_kv_heads, self.pool.dtype, self.pool.get_device()
+
+
+@dataclass
+class Paged8Cache(_Pages):
+    """The pages of a paged cache in 8 bits: codes [n_layers][n_pages][2][G][page_size][d] (float8_e4m3fn or uint8; 0 is K, 1 is
+    V), scale [n_layers][n_pages][2][G][page_size / 16] (float8_e8m0fnu or uint8), mass [n_layers][n_pages][G][page_size]
+    fp32 or None, plus the C struct pointing at them. Which page belongs to which sequence is the caller's."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    mass: torch.Tensor | None
+    c: varrate_pages8
+
+    @staticmethod
+    def of(codes: torch.Tensor, scale: torch.Tensor, mass: torch.Tensor | None = None) -> "Paged8Cache":
+        bad = codes.dim() != 6 or codes.shape[2] != 2 or codes.shape[4] % 16 != 0
+        if not bad:
+            L, P, _, G, ps, d = codes.shape
+            bad = scale.shape != (L, P, 2, G, ps // 16) or (mass is not None and mass.shape != (L, P, G, ps))
+        bad = bad or codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or scale.dtype not in (
+            torch.uint8, torch.float8_e8m0fnu) or (mass is not None and mass.dtype != torch.float32)
+        for t in (codes, scale, mass):
+            bad = bad or (t is not None and not (t.is_contiguous() and t.get_device() == codes.get_device()))
+        if bad:
+            raise VarrateError(ERR_ARG, "Paged8Cache.of")
+        c = varrate_pages8(codes.data_ptr(), scale.data_ptr(), _ptr(mass), L, P, G, ps, d)
+        return Paged8Cache(codes, scale, mass, c)
+
+    @staticmethod
+    def allocate(n_layers, n_pages, n_kv_heads, page_size, mass=True, device="cuda") -> "Paged8Cache":
+        """`mass`: with room for the tokens' attention weight, as varrate_paged8_mass and varrate_paged8_evict want it."""
+        u8 = dict(dtype=torch.uint8, device=device)
+        codes = torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size, 128), **u8).view(torch.float8_e4m3fn)
+        scale = torch.empty((n_layers, n_pages, 2, n_kv_heads, page_size // 16), **u8).view(torch.float8_e8m0fnu)
+        m = torch.empty((n_layers, n_pages, n_kv_heads, page_size), dtype=torch.float32, device=device) if mass else None
+        return Paged8Cache.of(codes, scale, m)
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.c)
+        self.heads, self.dtype, self.device = self.c.n_kv_heads, torch.bfloat16, self.codes.get_device()
 
 
 @dataclass
@@ -533,6 +667,12 @@ def paged_attn_workspace(pages: PagedCache, seqs: SeqBatch, group: int) -> torch
     """Device scratch of varrate_paged_attn for batches of this size, zero-filled as its first call wants it."""
     n = varrate_paged_attn_ws_bytes(pages, seqs, group)
     return torch.zeros(max(n, 256), dtype=torch.uint8, device=pages.pool.device)
+
+
+def paged8_attn_workspace(pages: Paged8Cache, seqs: SeqBatch, group: int) -> torch.Tensor:
+    """Device scratch of varrate_paged8_attn for batches of this size, zero-filled as its first call wants it."""
+    n = varrate_paged8_attn_ws_bytes(pages, seqs, group)
+    return torch.zeros(max(n, 256), dtype=torch.uint8, device=pages.codes.device)
 
 
 def workspace(cfg: varrate_config, which_call: int, device="cuda") -> torch.Tensor:
