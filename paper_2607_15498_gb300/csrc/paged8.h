@@ -71,8 +71,15 @@ int launch_paged8_append(const Paged8& c, int layer, int group, const void* q, i
 size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms);
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
                        void* ws, int num_sms, cudaStream_t st);
+// The part of the sequences c.p.n_min .. c.p.n_max, on tcgen05; partials are not merged.
+size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms);
+int launch_paged8_attn_tc(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
+                          void* ws, int num_sms, cudaStream_t st);
 int launch_paged8_mass(const Paged8& c, int layer, int group, const void* q, const float* lse, int32_t* dev_status,
                        int num_sms, cudaStream_t st);
+// The sequences of more than few_tokens(group) new tokens, on tcgen05.
+int launch_paged8_mass_tc(const Paged8& c, int layer, int group, const void* q, const float* lse, int32_t* dev_status,
+                          int num_sms, cudaStream_t st);
 int launch_paged8_evict(const Paged8& c, int layer, int n_layers, int budget, int n_first, int n_last, int32_t* kept,
                         int32_t* new_len, int32_t* gone, int32_t* dev_status, int num_sms, cudaStream_t st);
 

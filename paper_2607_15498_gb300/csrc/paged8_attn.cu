@@ -17,6 +17,10 @@
 #include <float.h>
 #include <math.h>
 
+#include <atomic>
+
+#include <cudaTypedefs.h>
+
 #include "common.cuh"
 #include "paged.h"
 #include "paged8.h"
@@ -24,6 +28,8 @@
 #include "paged_plan.cuh"
 
 namespace vr {
+
+bool make_tmap_rows_u8(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
 
 namespace {
 
@@ -33,14 +39,20 @@ constexpr float kOverhead = 8.f;             // of a unit, in key tiles, as the 
 constexpr float kSlack = 8.f;                // what scores may rise above the reference before it moves (log2)
 constexpr int kUp = 4;                       // weights are stored times 2^kUp
 
+constexpr int kStages = 3, kStepBytes = 16 * kHeadDim * 2;           // a warp's steps in flight: keys, then values
 struct Shared {
+  union {
+    unsigned char ring[kWarps][kStages][kStepBytes];
+    float o[kWarps][kRows][kHeadDim + 4];                           // at the end of a unit
+  };
+  uint64_t full[kWarps][kStages];
   PlanSums plan;
   Unit unit;
-  int seq;
+  int err;
   float m[kWarps][kRows], l[kWarps][kRows];
   int u[kWarps];
-  __align__(16) float o[kWarps][kRows][kHeadDim + 4];
 };
+static_assert(kCtas * (sizeof(Shared) + 2048) <= 228 * 1024, "shared memory of an SM");
 
 // Values of a step with rows that do not see all of its keys: those past the batch's tokens are zeroed; NaN codes of keys that
 // only a part of the rows sees are zeroed and returned as bits, 16 codes a key.
@@ -57,23 +69,28 @@ __device__ __forceinline__ bool take_nan(uint4& v, uint32_t& bits) {
 }
 
 __global__ void __launch_bounds__(kThreads, kCtas)
-paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scale,
+paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
                    const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                    int32_t* __restrict__ dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts,
                    int grp, float scale_log2) {
-  extern __shared__ __align__(16) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   const int tq = kRows / grp, H = p.G * grp, C = gridDim.x;
   pdl_trigger();
   if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&c.full[warp][i], 1);
+    fence_mbar_init();
+  }
+  if (tid == 0) c.err = 0;
   __syncthreads();
   pdl_wait();
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
-  const float weight = plan_weight<kKeys>(p, tq, lane, longest);
+  const float weight = plan_weight<kKeys, true>(p, tq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add<kKeys>(p, c.plan, tq, cand, warp, kWarps, lane);
+  plan_add<kKeys, true>(p, c.plan, tq, cand, warp, kWarps, lane);
   __syncthreads();
   plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
   if (blockIdx.x == 0) {
@@ -86,9 +103,11 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
       if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     }
   }
-  Walk<kKeys> w;
+  Walk<kKeys, true> w;
   if (warp == 0) w.load(p, tq, run, lane);
   int next = blockIdx.x;                                            // of warp 0
+  uint32_t stage = 0, phase = 0;                                    // of the warp's next step
+  bool ok = true;
   for (;;) {
     if (warp == 0) {
       Unit x;
@@ -102,17 +121,32 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
         if (x.t0 < x.t1) break;                                     // else: the block ends before this run
         x.valid = 0;
       }
-      if (lane == 0) { c.unit = x; c.seq = s; }
+      if (c.err) x.valid = 0;
+      if (lane == 0) { x.seq = s; c.unit = x; }
     }
     __syncthreads();
     const Unit x = c.unit;
-    const int s = c.seq;
     if (!x.valid) break;
     const int rows = x.ntok * grp, end = x.pos0 + x.ntok;
-    const int32_t* table = p.table + (int64_t)s * p.max_pages;
-    const int last = min(8 * x.t1, (end + 15) >> 4), in_page = (1 << p.page_log2) - 1;
-    const int64_t to_v = (int64_t)p.G << p.page_log2;               // rows from a key to its value
-
+    // this warp's steps
+    const int last = min(8 * x.t1, (end + 15) >> 4), st0 = 8 * x.t0 + warp, n = last > st0 ? (last - st0 + kWarps - 1) / kWarps : 0;
+    Steps steps{p, scale, p.table + (int64_t)x.seq * p.max_pages, dev_status, x.g, st0, kWarps, n};
+    steps.start(lane);
+    const int to_v = p.G << p.page_log2;                            // rows from a key to its value
+    auto request = [&](int i, uint32_t at) {                        // step i into stage `at`
+      const int row = steps.row(steps.page(i), i);
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&c.full[warp][at], kStepBytes);
+        const uint32_t dst = smem_addr(c.ring[warp][at]);
+        tma_load_2d(dst, &tmap, 0, row, &c.full[warp][at]);
+        tma_load_2d(dst + kStepBytes / 2, &tmap, 0, row + to_v, &c.full[warp][at]);
+      }
+    };
+    uint32_t ahead = stage;
+    for (int i = 0; i < min(n, kStages); ++i) {
+      request(i, ahead);
+      ahead = ahead + 1 == kStages ? 0 : ahead + 1;
+    }
     QueryFrags qf;
     qf.load(q + ((int64_t)(x.row0 + g8 / grp) * H + x.g * grp + g8 % grp) * kHeadDim, g8 < rows, scale_log2, lane);
     const int sees0 = x.pos0 + 2 * t4 / grp + 1, sees1 = x.pos0 + (2 * t4 + 1) / grp + 1;   // keys that rows 2 t4, 2 t4 + 1 see
@@ -122,44 +156,22 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
     int unit = -1;                                                  // scale byte of the accumulator's unit, none yet
 
-    int st = 8 * x.t0 + warp;
-    auto row_of = [&](int step) {                                   // of the codes: the step's first key
-      int page = __ldg(table + ((step << 4) >> p.page_log2));
-      if (page < 0 || page >= p.n_pages) { raise_status(dev_status, VARRATE_ERR_CORRUPT); page = 0; }
-      return page_row(p, page, 0, x.g, (step << 4) & in_page);
-    };
-    uint4 kq[4], vq[4];
-    int bk = 0, bv = 0;
-    auto load_k = [&](int64_t row) {
-      const unsigned char* src = codes + row * kHeadDim + 16 * t4;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) kq[i] = ld_nc_early_v4(reinterpret_cast<const uint4*>(src + (g8 + 8 * (i >> 1)) * kHeadDim + 64 * (i & 1)));
-    };
-    auto load_v = [&](int64_t row) {
-      const unsigned char* src = codes + (row + to_v) * kHeadDim + 16 * g8;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vq[i] = ld_nc_early_v4(reinterpret_cast<const uint4*>(src + (2 * t4 + (i & 1) + 8 * (i >> 1)) * kHeadDim));
-    };
-    int64_t row = 0;
-    if (st < last) {
-      row = row_of(st);
-      load_k(row);
-      bk = __ldg(scale + scale_at(row));
-      load_v(row);
-      bv = __ldg(scale + scale_at(row + to_v));
-    }
-    for (; st < last; st += kWarps) {
-      const int key0 = st << 4, more = st + kWarps < last;
+    int i = 0;
+    for (; i < n; ++i) {
+      ok = warp_wait(&c.full[warp][stage], phase);
+      if (!ok) break;
+      const unsigned char* tile = c.ring[warp][stage];
+      const int key0 = (st0 + i * kWarps) << 4;
       const bool edge = key0 + 16 > x.pos0 + 1;                     // some row does not see all of its keys
-      const int64_t row1 = more ? row_of(st + kWarps) : 0;
+      const uint32_t bytes = steps.bytes(i);
+      const int bv = (int)(bytes >> 8);
+      uint4 kq[4], vq[4];
+      read_keys(tile, lane, kq);
       float sc[4];
       key_scores(kq, qf, sc);
+      read_values(tile + kStepBytes / 2, lane, vq);
       // (of two extremes: no infinity that would make a number of a zero)
-      const float f = __uint_as_float((uint32_t)bk << 23), f0 = fminf(qf.f0 * f, FLT_MAX), f1 = fminf(qf.f1 * f, FLT_MAX);
-      if (more) {
-        load_k(row1);
-        bk = __ldg(scale + scale_at(row1));
-      }
+      const float f = __uint_as_float((bytes & 0xff) << 23), f0 = fminf(qf.f0 * f, FLT_MAX), f1 = fminf(qf.f1 * f, FLT_MAX);
       float x0 = sc[0] * f0, x1 = sc[1] * f1, x2 = sc[2] * f0, x3 = sc[3] * f1;
       if (edge) {
         const int a = key0 + g8, b = a + 8;
@@ -245,11 +257,19 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
           }
         }
       }
-      if (more) {
-        load_v(row1);
-        bv = __ldg(scale + scale_at(row1 + to_v));
-      }
+      __syncwarp();                                                 // the tile has been read
+      if (i + kStages < n) request(i + kStages, stage);
+      steps.done(i, lane);
+      if (++stage == kStages) { stage = 0; phase ^= 1; }
     }
+    if (!ok) {                                                      // no copy is in flight when the block ends
+      for (int j = i; j < min(n, i + kStages); ++j) {
+        warp_wait(&c.full[warp][stage], phase);
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+      c.err = 1;
+    }
+    __syncthreads();                                                // the rings are empty
     // the warps' rows
 #pragma unroll
     for (int i = 4; i < 32; i <<= 1) {
@@ -261,7 +281,7 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
       c.l[warp][2 * lane] = l0; c.l[warp][2 * lane + 1] = l1;
       if (lane == 0) c.u[warp] = max(unit, 0);
     }
-    {
+    {                                                               // (a step that timed out leaves no part of its unit)
       const float down = 1.f / (1 << kUp);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -297,28 +317,52 @@ paged8_attn_kernel(Paged p, const unsigned char* __restrict__ codes, const unsig
           reinterpret_cast<float2*>(part + (int64_t)max_parts * part_rows * kHeadDim)[i] = make_float2(at, ll == 0.f ? 0.f : 1.f);
       }
     }
+    fence_proxy_async_smem();                                       // copies come where `o` was
+    __syncthreads();
+  }
+  if (tid == 0 && c.err) {
+    raise_status(dev_status, VARRATE_ERR_TIMEOUT);
+    atomicExch(&header->gave_up, 1u);
   }
 }
 
 }  // namespace
 
 size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms) {
-  return paged_part_bytes(c.p, group, kRows / group, num_sms);
+  const size_t mine = paged_part_bytes(c.p, group, kRows / group, num_sms);
+  return c.p.T <= few_tokens(group) ? mine : mine + paged_attn_tc_ws_bytes(c.p, group, num_sms);
 }
 
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
                        void* ws, int num_sms, cudaStream_t st) {
-  const Paged& p = c.p;
+  Paged p = c.p;
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
-  const int tq = kRows / group;
-  if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, p,
-                  p.pool + (int64_t)layer * p.layer_rows * kHeadDim, c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
+  const int tq = kRows / group, few = few_tokens(group);
+  p.n_max = few;
+  CUtensorMap tmap;
+  if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;
+  static std::atomic<int> smem_set[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || smem_set[dev].load(std::memory_order_acquire) == 0) {
+    if (cudaFuncSetAttribute(paged8_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess) return -1;
+    if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
+  }
+  if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
+                  c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
                   (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
                   paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  return launch_paged_merge(p, group, out, lse, dev_status, header, part, tq, tq, num_sms, st) < 0 ? -1 : 2;
+  MergeTwo two = {};
+  two.lse = lse; two.few = few; two.tq = 128 / group; two.bq = 2 * two.tq;
+  if (p.T > few) {                                                  // else no sequence can have more
+    Paged8 many = c;
+    many.p.n_min = few + 1;
+    two.second = w + paged_part_bytes(c.p, group, tq, num_sms);
+    if (launch_paged8_attn_tc(many, layer, group, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
+  }
+  return launch_paged_merge_two(c.p, group, out, dev_status, header, part, tq, tq, two, num_sms, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "decode_common.cuh"
 #include "paged8.h"
 
 namespace vr {
@@ -34,7 +35,7 @@ __device__ __forceinline__ uint32_t value_bytes(const uint4& a, const uint4& b, 
   return __byte_perm(wa, wb, j & 1 ? 0x7362 : 0x5140);
 }
 
-// Eight rows of queries as the B operand: lane (row g, t) has the elements 16 t .. 16 t + 15 and those 64 further. fp16 times
+// Eight rows of queries as the B operand: lane (row g, t) has the elements 32 t .. 32 t + 31. fp16 times
 // 2^n, the row's largest in [2^14, 2^15).
 struct QueryFrags {
   uint32_t b[8][2];
@@ -45,7 +46,7 @@ struct QueryFrags {
     uint4 u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      u[i] = live ? __ldg(reinterpret_cast<const uint4*>(row + 16 * t + 64 * (i >> 1) + 8 * (i & 1))) : make_uint4(0, 0, 0, 0);
+      u[i] = live ? __ldg(reinterpret_cast<const uint4*>(row + 32 * t + 8 * i)) : make_uint4(0, 0, 0, 0);
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -68,7 +69,73 @@ struct QueryFrags {
   }
 };
 
-// Products of 16 keys with the rows: keys[2 i + h] is the 16 bytes at element 16 t + 64 h of key g + 8 i. Out: (key g, row 2 t),
+// Tiles of 16 tokens in shared memory: rows of 128 bytes, 16-byte pieces exchanged by the 128-byte swizzle, so that these reads meet
+// no bank twice. tile: 1024-byte aligned.
+__device__ __forceinline__ void read_keys(const unsigned char* tile, int lane, uint4 (&k)[4]) {
+  const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    k[i] = *reinterpret_cast<const uint4*>(tile + (g + 8 * (i >> 1)) * 128 + (((2 * t + (i & 1)) ^ g) << 4));
+}
+// Elements 16 g .. 16 g + 15 of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9.
+__device__ __forceinline__ void read_values(const unsigned char* tile, int lane, uint4 (&v)[4]) {
+  const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = 2 * t + (i & 1);
+    v[i] = *reinterpret_cast<const uint4*>(tile + (key + 8 * (i >> 1)) * 128 + ((g ^ key) << 4));
+  }
+}
+
+// A warp's steps of 16 keys: first, first + stride, ..., n of them, of one sequence and KV head. Pages and scale bytes are
+// fetched for 32 steps at a time, a lane each, one batch ahead.
+struct Steps {
+  const Paged& p;
+  const unsigned char* scale;
+  const int32_t* table;
+  int32_t* dev_status;
+  int g, first, stride, n, batch;
+  int page0, page1;
+  uint32_t bytes0, bytes1;   // of the key's block, and times 256 of the value's
+
+  __device__ __forceinline__ int in_page(int i) const { return ((first + i * stride) << 4) & ((1 << p.page_log2) - 1); }
+  __device__ __forceinline__ int row(int page, int i) const { return (int)page_row(p, max(page, 0), 0, g, in_page(i)); }
+  __device__ __forceinline__ void fetch(int b, int lane, int& page, uint32_t& bytes) {
+    const int i = 32 * b + lane;
+    page = 0;
+    bytes = 0;
+    if (i >= n) return;
+    page = __ldg(table + (((first + i * stride) << 4) >> p.page_log2));
+    if (page < 0 || page >= p.n_pages) { raise_status(dev_status, VARRATE_ERR_CORRUPT); page = -1; }
+    const int r = row(page, i);
+    bytes = __ldg(scale + scale_at(r)) | (uint32_t)__ldg(scale + scale_at(r + (p.G << p.page_log2))) << 8;
+  }
+  __device__ __forceinline__ void start(int lane) {
+    batch = 0;
+    fetch(0, lane, page0, bytes0);
+    fetch(1, lane, page1, bytes1);
+  }
+  // of step i, of the current batch or the next one; a page out of range is -1 (its row is one of page 0)
+  __device__ __forceinline__ int page(int i) const { return __shfl_sync(0xffffffffu, (i >> 5) == batch ? page0 : page1, i & 31); }
+  __device__ __forceinline__ uint32_t bytes(int i) const { return __shfl_sync(0xffffffffu, (i >> 5) == batch ? bytes0 : bytes1, i & 31); }
+  __device__ __forceinline__ void done(int i, int lane) {   // with step i
+    if ((i & 31) != 31) return;
+    page0 = page1;
+    bytes0 = bytes1;
+    fetch(++batch + 1, lane, page1, bytes1);
+  }
+};
+
+// Sequences of at most this many new tokens are taken by mma.sync: one or two blocks of eight rows; more by tcgen05.
+__host__ __device__ __forceinline__ int few_tokens(int group) { return 2 * (8 / group); }
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kWaitTries; ++i)
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return false;
+}
+
+// Products of 16 keys with the rows: keys[2 i + h] is the 16 bytes at element 32 t + 16 h of key g + 8 i. Out: (key g, row 2 t),
 // (g, 2 t + 1), (g + 8, 2 t), (g + 8, 2 t + 1).
 __device__ __forceinline__ void key_scores(const uint4 (&keys)[4], const QueryFrags& q, float (&s)[4]) {
   float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};

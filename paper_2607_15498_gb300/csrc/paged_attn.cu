@@ -253,7 +253,7 @@ int launch_paged_attn(const Paged& p, int layer, int group, const void* q, void*
                   header, part, paged_part_rows(p, group, tq), paged_max_parts(ctas), group, 1.f / sqrtf((float)kHeadDim),
                   ldexpf(1.f, -bits)))
     return -1;
-  return launch_paged_merge(p, group, out, nullptr, dev_status, header, part, tq, tq, ctas, st) < 0 ? -1 : 2;
+  return launch_paged_merge(p, group, out, dev_status, header, part, tq, tq, ctas, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr

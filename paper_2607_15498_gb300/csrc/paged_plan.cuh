@@ -38,11 +38,19 @@ __device__ __forceinline__ int take_unit(Header* h, int ctas, int units) {
 }
 
 struct Unit {
-  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from;
+  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from, seq;
   // g: KV head; row0: row of the block's first token; pos0: its position; key tiles t0 .. t1 - 1, of which the first
   // warpgroup's query tile sees those before e0; both: one query tile for both; slot: partial, or -1; values_from: first
-  // tile whose values have to be looked at
+  // tile whose values have to be looked at; seq: its sequence, where a kernel has set it
 };
+
+// A sequence as a kernel's plan has it; kSome: without new tokens where it is another kernel's.
+template <bool kSome>
+__device__ __forceinline__ bool plan_range(const Paged& p, int s, SeqRange& r) {
+  if (!seq_range(p, s, r)) return false;
+  if (kSome && (r.n < p.n_min || r.n > p.n_max)) r.n = 0;
+  return true;
+}
 
 // Key tiles that hold the first `keys` keys (keys < 2^32).
 template <int kKeys>
@@ -72,13 +80,13 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
 // not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the
 // warps share the sequences and add up in plan_add, one warp decides in plan_choose.
-template <int kKeys>
+template <int kKeys, bool kSome = false>
 __device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
   float w = 0.f;
   int most = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
-    if (!seq_range(p, s, r) || r.n == 0) continue;
+    if (!plan_range<kSome>(p, s, r) || r.n == 0) continue;
     const int last = tiles_of<kKeys>(r.len), first = tiles_of<kKeys>(r.len - r.n + min(bq, r.n));
     w += (float)((unsigned)(r.n + bq - 1) / (unsigned)bq) * (0.5f * (float)(first + last));
     most = max(most, last);
@@ -96,12 +104,12 @@ __device__ __forceinline__ int plan_candidate(float W, int longest, int C, int l
   const float k = ceilf(W * (float)(16 + (lane & 3)) / (16.f * (float)(1 + (lane >> 2)) * (float)C));
   return min(max(1, (int)fminf(k, 1e9f)), longest + 1);
 }
-template <int kKeys>
+template <int kKeys, bool kSome = false>
 __device__ __forceinline__ void plan_add(const Paged& p, PlanSums& c, int bq, int cand, int warp, int warps, int lane) {
   int u = 0, split = 0, chunk = 0;
   for (int s = warp; s < p.S; s += warps) {
     SeqRange r;
-    if (!seq_range(p, s, r)) continue;
+    if (!plan_range<kSome>(p, s, r)) continue;
     const SeqPlan q = seq_plan<kKeys>(r, bq, cand);
     const int n = p.G * q.nb * q.cuts;
     u += n;
@@ -131,7 +139,7 @@ __device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand
 }
 
 // Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
-template <int kKeys>
+template <int kKeys, bool kSome = false>
 struct Walk {
   int s0 = 0, before = 0, parts_before = 0;     // first sequence held; units and partials before it
   int incl, parts_incl, total, parts;           // scans over the sequences held, and their sums
@@ -140,7 +148,7 @@ struct Walk {
   __device__ __forceinline__ void load(const Paged& p, int bq, int run, int lane) {
     SeqRange r;
     r.n = 0; r.len = 0; r.row0 = 0;
-    if (s0 + lane < p.S && !seq_range(p, s0 + lane, r)) r.n = 0;
+    if (s0 + lane < p.S && !plan_range<kSome>(p, s0 + lane, r)) r.n = 0;
     if (r.n == 0) r.len = 0;
     q = seq_plan<kKeys>(r, bq, run);
     incl = p.G * q.nb * q.cuts;
@@ -198,8 +206,18 @@ inline size_t paged_part_bytes(const Paged& p, int group, int bq, int num_sms) {
   return kHeaderBytes + ((rows * (kHeadDim + 2) * sizeof(float) + 255) & ~size_t(255));
 }
 // Merges partials into `out` and leaves the header as the next call wants it. tq: tokens of a query tile, of which a block has
-// one or two. lse: [T][H], or null: the logarithm of a row's sum as well.
-int launch_paged_merge(const Paged& p, int group, void* out, float* lse, int32_t* dev_status, Header* header, const float* part,
-                       int tq, int bq, int num_sms, cudaStream_t st);
+// one or two.
+int launch_paged_merge(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
+                       int bq, int num_sms, cudaStream_t st);
+// The same where one kernel took the sequences of at most `few` new tokens and another the rest, each with header and partials of
+// its own: of the second one from `second` on, or null where it was not launched. bf16. lse: [T][H], or null: the logarithm
+// of a row's sum as well.
+struct MergeTwo {
+  unsigned char* second;
+  float* lse;
+  int few, tq, bq;          // tq, bq: of the second
+};
+int launch_paged_merge_two(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
+                           int bq, const MergeTwo& two, int num_sms, cudaStream_t st);
 
 }  // namespace vr

@@ -82,6 +82,8 @@ ATTN = [
     dict(lens=[(31, 1), (5, 2), (260, 3)], G=1, grp=6, ps=16),
     dict(lens=[(257, 0)], G=2, grp=2, ps=32, layers=2),
     dict(lens=[(1, 33), (8, 120)], G=3, grp=1, ps=16),
+    dict(lens=[(40, 3000), (24, 2500), (1, 3300), (90, 1800), (4, 2000)], G=8, grp=4, ps=64),
+    dict(lens=[(17, 900)] * 40, G=2, grp=7, ps=128),
 ]
 
 
