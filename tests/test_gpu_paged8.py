@@ -240,9 +240,9 @@ def test_evict_counts_what_is_gone():
     assert gone.tolist() == [67, 8]
 
 
-def test_evict_more_than_shared_memory_holds():
-    """A head of more tokens than a cluster keeps the weights of: 360 thousand."""
-    n, budget = 360000, 30000
+@pytest.mark.parametrize("n, budget", [(360000, 30000), (360000, 300000), (900000, 100000)])
+def test_evict_more_than_shared_memory_holds(n, budget):
+    """A head of more tokens than a cluster keeps the weights of, or of more tiles than the move knows the first tokens of."""
     pages = n // 256 + 1
     codes = torch.randint(0, 127, (1, pages, 2, 1, 256, D), dtype=torch.uint8, device="cuda")
     scale = torch.full((1, pages, 2, 1, 16), 120, dtype=torch.uint8, device="cuda")
