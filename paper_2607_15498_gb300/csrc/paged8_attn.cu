@@ -39,7 +39,7 @@ constexpr float kOverhead = 8.f;             // of a unit, in key tiles, as the 
 constexpr float kSlack = 8.f;                // what scores may rise above the reference before it moves (log2)
 constexpr int kUp = 4;                       // weights are stored times 2^kUp
 
-constexpr int kStages = 3, kStepBytes = 16 * kHeadDim * 2;           // a warp's steps in flight: keys, then values
+constexpr int kStages = 2, kStepBytes = 16 * kHeadDim * 2;           // a warp's steps in flight: keys, then values
 struct Shared {
   union {
     unsigned char ring[kWarps][kStages][kStepBytes];
@@ -77,7 +77,6 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   const int tq = kRows / grp, H = p.G * grp, C = gridDim.x;
-  pdl_trigger();
   if (tid < kCand) { c.plan.units[tid] = 0; c.plan.split[tid] = 0; c.plan.chunk[tid] = 0; }
   if (lane == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(&c.full[warp][i], 1);
@@ -86,6 +85,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   if (tid == 0) c.err = 0;
   __syncthreads();
   pdl_wait();
+  pdl_trigger();                                                    // (the tcgen05 kernel goes by it: not before)
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
   const float weight = plan_weight<kKeys, true>(p, tq, lane, longest);
@@ -330,7 +330,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
 
 size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms) {
   const size_t mine = paged_part_bytes(c.p, group, kRows / group, num_sms);
-  return c.p.T <= few_tokens(group) ? mine : mine + paged_attn_tc_ws_bytes(c.p, group, num_sms);
+  return c.p.T <= few_tokens(c.p, group) ? mine : mine + paged_attn_tc_ws_bytes(c.p, group, num_sms);
 }
 
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
@@ -339,7 +339,7 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
-  const int tq = kRows / group, few = few_tokens(group);
+  const int tq = kRows / group, few = few_tokens(p, group);
   p.n_max = few;
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;

@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 2;
 constexpr int kRows = 8;
-constexpr int kStages = 6, kStepBytes = 16 * kHeadDim;              // a warp's steps in flight
+constexpr int kStages = 3, kStepBytes = 16 * kHeadDim;              // a warp's steps in flight
 
 struct Shared {
   unsigned char ring[kWarps][kStages][kStepBytes];
@@ -39,17 +39,17 @@ __device__ __forceinline__ int64_t steps_of(const Paged& p, int s, int few, SeqR
 __global__ void __launch_bounds__(kThreads, kCtas)
 paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
                    float* __restrict__ mass, const __nv_bfloat16* __restrict__ q, const float* __restrict__ lse,
-                   int32_t* __restrict__ dev_status, int grp, float scale_log2) {
+                   int32_t* __restrict__ dev_status, int grp, int few, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3, H = p.G * grp, tq = kRows / grp, few = few_tokens(grp);
-  pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3, H = p.G * grp, tq = kRows / grp;
   if (lane == 0) {                                                  // (a warp's own)
     for (int i = 0; i < kStages; ++i) mbar_init(&c.full[warp][i], 1);
     fence_mbar_init();
   }
   __syncwarp();
   pdl_wait();
+  pdl_trigger();                                                    // (the tcgen05 kernel goes by it: not before)
   int64_t total = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
@@ -126,7 +126,7 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     Rows rows[2];
     load_rows(0, rows[0]);
     load_rows(1, rows[1]);
-    const int blocks = n > tq ? 2 : 1;
+    const int blocks = (n + tq - 1) / tq;                           // the first two stay in registers
     int i = 0;
     for (; i < steps.n; ++i) {
       ok = warp_wait(&c.full[warp][stage], phase);
@@ -136,10 +136,7 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
       const int page = steps.page(i), key0 = (st0 + i) << 4;
       const float f = __uint_as_float((steps.bytes(i) & 0xff) << 23);
       float w0 = 0.f, w1 = 0.f;                                     // of keys g8, g8 + 8
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (b == blocks) break;
-        const Rows& x = rows[b];
+      auto add = [&](const Rows& x) {
         float sc[4];
         key_scores(kq, x.q, sc);
         const float f0 = fminf(x.q.f0 * f, FLT_MAX), f1 = fminf(x.q.f1 * f, FLT_MAX);
@@ -148,6 +145,13 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
         if (a < x.sees1 && x.e1 < INFINITY) w0 += fast_exp2(sc[1] * f1 - x.e1);
         if (d < x.sees0 && x.e0 < INFINITY) w1 += fast_exp2(sc[2] * f0 - x.e0);
         if (d < x.sees1 && x.e1 < INFINITY) w1 += fast_exp2(sc[3] * f1 - x.e1);
+      };
+      add(rows[0]);
+      if (blocks > 1) add(rows[1]);
+      for (int b = 2; b < blocks; ++b) {
+        Rows x;
+        load_rows(b, x);
+        add(x);
       }
       __syncwarp();                                                 // the tile has been read
       if (i + kStages < steps.n) request(i + kStages, stage);
@@ -188,9 +192,9 @@ int launch_paged8_mass(const Paged8& c, int layer, int group, const void* q, con
   }
   if (!launch_pdl(paged8_mass_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2), c.mass + (int64_t)layer * (p.layer_rows / 2),
-                  (const __nv_bfloat16*)q, lse, dev_status, group, kLog2e / sqrtf((float)kHeadDim)))
+                  (const __nv_bfloat16*)q, lse, dev_status, group, few_tokens(p, group), kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  if (p.T <= few_tokens(group)) return 1;                           // no sequence can have more
+  if (p.T <= few_tokens(p, group)) return 1;                           // no sequence can have more
   return launch_paged8_mass_tc(c, layer, group, q, lse, dev_status, num_sms, st) < 0 ? -1 : 2;
 }
 

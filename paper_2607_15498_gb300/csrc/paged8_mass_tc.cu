@@ -85,7 +85,7 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
-  pdl_wait();
+  __threadfence();   // the kernel before this one takes other sequences, and lets this one start when what comes before both has ended
 
   if (warp == kProducer) {
     // ------------------------------------------------------------------ units, keys and queries
@@ -293,7 +293,7 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       for (int e = 0; e < 2; ++e) {
         ok = ok && warp_wait(&c.raw[un & 1][e], (un >> 1) & 1);
         if (!ok) break;
-        expand_row(c.keys[un & 1][e], kTile, key_in, x.key0 + e * kTile + key_in < x.len, byte[e]);
+        expand_row<true>(c.keys[un & 1][e], kTile, key_in, x.key0 + e * kTile + key_in < x.len, byte[e]);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&c.k_full[un & 1][e]);
@@ -374,6 +374,7 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
   if (tid == 0 && c.err) raise_status(dev_status, VARRATE_ERR_TIMEOUT);
+  pdl_wait();                                                 // so that what waits for this kernel waits for both
 }
 
 }  // namespace
@@ -393,7 +394,7 @@ int launch_paged8_mass_tc(const Paged8& c, int layer, int group, const void* q, 
   if (!make_tmap_heads_bf16(&tmap_q, q, (uint32_t)(p.G * group), (uint64_t)p.T, (uint32_t)group, (uint32_t)(kTile / group))) return -1;
   return launch_pdl(paged8_mass_tc_kernel, dim3(num_sms), kThreads, sizeof(Shared), st, tmap, tmap_q, p,
                     c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2), c.mass + (int64_t)layer * (p.layer_rows / 2), lse,
-                    dev_status, group, few_tokens(group), kLog2e / sqrtf((float)kHeadDim))
+                    dev_status, group, few_tokens(p, group), kLog2e / sqrtf((float)kHeadDim))
              ? 1 : -1;
 }
 

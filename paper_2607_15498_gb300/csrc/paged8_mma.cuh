@@ -126,8 +126,10 @@ struct Steps {
   }
 };
 
-// Sequences of at most this many new tokens are taken by mma.sync: one or two blocks of eight rows; more by tcgen05.
-__host__ __device__ __forceinline__ int few_tokens(int group) { return 2 * (8 / group); }
+// Sequences of at most this many new tokens are taken by mma.sync: one or two blocks of eight rows; more by tcgen05. A batch with no
+// more rows than sequences is one of single tokens, or nearly so: mma.sync takes all of it, and the other kernel, which would look for
+// work for 8 us, is not launched.
+inline int few_tokens(const Paged& p, int group) { return p.T <= p.S ? p.T : 2 * (8 / group); }
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
   for (uint32_t i = 0; i < kWaitTries; ++i)

@@ -38,6 +38,7 @@
 // turns 448; with the output in a function that is not inlined 406 instead of 366. The bound on
 // the sum of a row's weights costs 1 %. Partials merged by the last CTA of a block instead of a kernel: 89 to 117 us instead of 76 on a mixed
 // step, whose partials are 252 rows, as its loads stand in the way of the next unit; not measured where every block is one token.
+#include <float.h>
 #include <math.h>
 #include <stddef.h>
 
@@ -77,10 +78,15 @@ constexpr int kRing = 5;                                    // key and value til
 // of fp32.
 constexpr float kMost = 0.25f, kRoom = 40.f;
 
+template <bool kCoded> struct CodedCtl {};
+template <> struct CodedCtl<true> {
+  uint64_t raw[kRing], q_raw[2];                            // codes and bf16 queries, as they come
+  __align__(16) float key_scale[4][kKeys / kBlock];         // of the last key tiles' blocks
+};
 template <bool kCoded>
-struct Ctl {
+struct Ctl : CodedCtl<kCoded> {
   static constexpr int kKinds = kCoded ? 1 : 3;             // of values that are not finite: +inf, -inf, NaN; codes have NaN alone
-  uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing], raw[kCoded ? kRing : 1];
+  uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
   uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_full[2], q_full[2], q_seen[2], turn[2], drain[2];   // by warpgroup
   uint64_t u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, planned;
   Unit unit[2];
@@ -146,14 +152,24 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   const int tq = kRows / grp, bq = 2 * tq, H = p.G * grp, C = gridDim.x;
   const uint32_t q_addr = smem_addr(smem), ring = q_addr + 2 * kTileBytes;
 
+  // the barriers of copies
+  auto tile_bar = [&](uint32_t i) {
+    if constexpr (kCoded) return &c.raw[i];
+    else return &c.full[i];
+  };
+  auto query_bar = [&](int i) {
+    if constexpr (kCoded) return &c.q_raw[i];
+    else return &c.q_full[i];
+  };
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
-      if (kCoded) mbar_init(&c.raw[i], 1);
+      if constexpr (kCoded) mbar_init(&c.raw[i], 1);
       mbar_init(&c.full[i], kCoded ? kExpandWarps : 1); mbar_init(&c.empty[i], 2); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 1);
+      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], kCoded ? 4 : 1);
+      if constexpr (kCoded) mbar_init(&c.q_raw[i], 1);
       mbar_init(&c.q_seen[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1);
       mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3 + (kCoded ? kExpandWarps : 0)); mbar_init(&c.u_looked[i], 1);
     }
@@ -167,7 +183,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
-  pdl_wait();
+  // Coded: the kernel before this one takes other sequences, and lets this one start when what comes before both has ended.
+  if constexpr (kCoded) __threadfence();
+  else pdl_wait();
   // by a call whose merge did not run, or runs still
   const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;
@@ -240,10 +258,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             const uint32_t slot = n % kRing;
             ok = ok && wait_all(&c.empty[slot], ((n / kRing) & 1) ^ 1);
             if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(kCoded ? &c.raw[slot] : &c.full[slot], (uint32_t)boxes * page_keys * (kCoded ? 128 : 256));
+            if (lane == 0) mbar_arrive_expect_tx(tile_bar(slot), (uint32_t)boxes * page_keys * (kCoded ? 128 : 256));
             __syncwarp();
             if (kCoded && mine)                                     // codes come to where the tile's second half will be
-              tma_load_2d(ring + slot * kTileBytes + kKeys * 128 + piece * page_keys * 128, &tmap, 0, kv ? row_v : row, &c.raw[slot]);
+              tma_load_2d(ring + slot * kTileBytes + kKeys * 128 + piece * page_keys * 128, &tmap, 0, kv ? row_v : row, tile_bar(slot));
             if (!kCoded && mine)
               tma_load_2d(ring + slot * kTileBytes + half * (kKeys * 128) + piece * page_keys * 128, &tmap, half * 64,
                           kv ? row_v : row, &c.full[slot]);
@@ -255,7 +273,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       if (!ok) {
         c.err = 1;
         const uint32_t oldest = n > kRing ? n - kRing : 0;          // no copy is in flight when the block ends
-        for (uint32_t i = oldest; i < n; ++i) wait_all(kCoded ? &c.raw[i % kRing] : &c.full[i % kRing], (i / kRing) & 1);
+        for (uint32_t i = oldest; i < n; ++i) wait_all(tile_bar(i % kRing), (i / kRing) & 1);
       }
     } else if (warp == kIssuer || warp == kIssuer + 1) {
       // ------------------------------------------------------------------ products of warpgroup e
@@ -263,7 +281,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       // memory), so that descriptors stay in uniform registers; one elected lane issues. Both issuers pass every tile of
       // the ring in order, whether they use it or not.
       const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
-      constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
+      // codes: queries and keys in fp16
+      constexpr uint32_t idesc_s = kCoded ? idesc_f16_f32(kRows, kKeys) : idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + 128 * e, to = tm + 256 + 128 * e;
       struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
       auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
@@ -461,10 +480,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
         n0 += 2 * (uint32_t)(x.t1 - x.t0);
       }
       if (!ok) c.err = 1;
-    } else if (kCoded && warp >= kExpand) {
+    } else if constexpr (kCoded) {
       // ------------------------------------------------------------------ codes to bf16: one key per thread
       const int key_in = tid - 32 * kExpand;
-      uint32_t n = 0;
+      uint32_t n = 0, n_k = 0;
       bool ok = true;
       for (uint32_t un = 0; ok; ++un) {
         ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
@@ -498,7 +517,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             const uint32_t slot = n % kRing;
             ok = ok && wait_all(&c.raw[slot], (n / kRing) & 1);
             if (!ok) break;
-            expand_row(smem + (2 + slot) * kTileBytes, kKeys, key_in, there, kv ? sv : sk);
+              if (kv) {
+              expand_row<true>(smem + (2 + slot) * kTileBytes, kKeys, key_in, there, sv);
+            } else {
+              expand_row<false>(smem + (2 + slot) * kTileBytes, kKeys, key_in, there, 0);
+              if ((key_in & (kBlock - 1)) == 0) c.key_scale[n_k & 3][key_in >> kBlockLog2] = __uint_as_float(sk << 23);
+              ++n_k;
+            }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&c.full[slot]);
@@ -517,6 +542,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     const int row_off = (tok_of * H + r % grp) * kHeadDim;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
+    [[maybe_unused]] uint32_t n_k = 0;                            // key tiles of the units before
     uint32_t n_s = 0, n_o = 0, n_both = 0, n_q = 0;               // score tiles, value products, merged units, query tiles so far
     bool ok = true;
     float ref = -INFINITY, l = 0.f;                               // reference, sum
@@ -537,11 +563,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       }
       if (valid && wrow == 0 && lane == 0) {
         const Unit& x = c.unit[nu & 1];
-        mbar_arrive_expect_tx(&c.q_full[e], (uint32_t)(tq * grp) * 256);
+        mbar_arrive_expect_tx(query_bar(e), (uint32_t)(tq * grp) * 256);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
           tma_load_3d(q_addr + e * kTileBytes + half * (kRows * 128), &tmap_q, half * 64, x.g * grp,
-                      x.row0 + (x.both ? 0 : e * tq), &c.q_full[e]);
+                      x.row0 + (x.both ? 0 : e * tq), query_bar(e));
       }
       __syncwarp();
       if (nu > 0) {
@@ -665,12 +691,20 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       const int sees = x.pos0 + tok0 + tok_of + 1;                // keys that this row sees
       const int first_sees = __shfl_sync(0xffffffffu, sees, 0);   // the least of the warp
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
+      [[maybe_unused]] const int t_first = x.t0, tiles = x.t1 - x.t0;
       ref = -INFINITY;
       l = 0.f;
       unset = true;
       begun = false;
-      // scores so large that they are rounded before the reference is taken off, not with it
-      [[maybe_unused]] bool far = false, any_far = false;
+      [[maybe_unused]] float row_scale = scale_log2;
+      if constexpr (kCoded) {                                     // the queries in fp16, and what that takes off their size
+        ok = wait_all(&c.q_raw[e], (n_q - 1) & 1);
+        if (!ok) break;
+        row_scale *= row_to_f16(smem + e * kTileBytes, kRows, r);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.q_full[e]);
+      }
       for (int t = x.t0 + (both ? e : 0); t < last; t += step) {
         ok = wait_all(&c.s_full[e], n_s & 1);
         if (!ok) break;
@@ -689,10 +723,24 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
           // number below kMost with them: the maximum of the scores first, then the weights again.
           float x[32];
           uint32_t pk[32];
+          // coded: what a score of a block of keys is multiplied by (neither an infinity, for scores of 0, nor 0, for hidden ones)
+          [[maybe_unused]] auto block_scale = [&](int b) {
+            if constexpr (kCoded) return fminf(fmaxf(row_scale * c.key_scale[(n_k + (t - t_first)) & 3][b], FLT_MIN), FLT_MAX);
+            else return scale_log2;
+          };
+          [[maybe_unused]] auto block_scales = [&](int b, float (&y)[4]) {
+            if constexpr (kCoded) {
+              const float4 k = *reinterpret_cast<const float4*>(&c.key_scale[(n_k + (t - t_first)) & 3][b]);
+              const float z[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = fminf(fmaxf(row_scale * z[i], FLT_MIN), FLT_MAX);
+            }
+          };
           auto weights = [&](int cb0) {
             const float off1 = ref == -INFINITY ? 0.f : -ref;
-            const float sc1 = kCoded && far ? 1.f : scale_log2;
-            const float2 sc = make_float2(sc1, sc1), off = make_float2(off1, off1);
+            const float2 off = make_float2(off1, off1);
+            float sc1[4] = {scale_log2, scale_log2, scale_log2, scale_log2};   // by 16 keys
+            if constexpr (kCoded) block_scales(cb0 / kBlock, sc1);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             float s[64];
             tmem_ld64(ts + cb0, s);
@@ -700,13 +748,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
 #pragma unroll
               for (int k = 0; k < 64; ++k) s[k] = cb0 + k < lim ? s[k] : -INFINITY;
             }
-            if (kCoded && any_far) {
-#pragma unroll
-              for (int k = 0; k < 64; ++k) s[k] *= far ? scale_log2 : 1.f;
-            }
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
-              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
+              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), make_float2(sc1[k / 8], sc1[k / 8]), off);
               s[2 * k] = fast_exp2(a.x);
               s[2 * k + 1] = fast_exp2(a.y);
             }
@@ -726,18 +770,31 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             for (bool first = true; cb < kKeys && (first || !some || __any_sync(0xffffffffu, mine && mx == -INFINITY)); cb += 32, first = false) {
               tmem_ld32(ts + cb, x);
               hide(cb, x);
+              if constexpr (kCoded) {
+                const float b0 = block_scale(cb / kBlock), b1 = block_scale(cb / kBlock + 1);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) x[k] *= k < 16 ? b0 : b1;
+              }
               float top[4] = {mx, x[0], x[1], x[2]};
 #pragma unroll
               for (int k = 3; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], x[k]);
               mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             }
-            mx *= scale_log2;
+            if constexpr (!kCoded) mx *= scale_log2;
             const float up = (l < 0.5f * kMost ? mx : fmaxf(mx, ref)) + kRoom;   // a sum that has grown makes room too
             float f = 1.f;
-            if (mine && up > ref) { f = ref == -INFINITY ? 0.f : fast_exp2(ref - up); ref = up; }
-            if constexpr (kCoded) {                               // a rounding of the reference is no longer small beside kRoom
-              far = fabsf(ref) > 0x1p28f && fabsf(ref) < INFINITY;
-              any_far = __any_sync(0xffffffffu, far);
+            if (mine && up > ref) {
+              f = ref == -INFINITY ? 0.f : fast_exp2(ref - up);
+              ref = up;
+              if constexpr (kCoded) {
+                // So large that a rounding of the reference is not small beside kRoom: the row's scores are taken at 2^24 from here on.
+                // They are not known to a unit, the largest decides alone, and does so as well where they are smaller.
+                if (fabsf(ref) > 0x1p24f && fabsf(ref) < INFINITY) {
+                  const float down = __uint_as_float((uint32_t)(127 + 127 + 23 - (int)(__float_as_uint(fabsf(ref)) >> 23)) << 23);
+                  row_scale *= down;
+                  ref = fmaf(ref, down, kRoom);
+                }
+              }
             }
             return f;
           };
@@ -790,10 +847,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
         unset = __any_sync(0xffffffffu, mine && ref == -INFINITY);
       }
       if (!ok) break;
+      n_k += tiles;
     }
     if (!ok) {
       c.err = 1;
-      if (n_q > 0) wait_all(&c.q_full[e], (n_q - 1) & 1);         // no copy is in flight when the block ends
+      if (n_q > 0) wait_all(query_bar(e), (n_q - 1) & 1);   // no copy is in flight when the block ends
     }
   }
   __syncthreads();
@@ -802,6 +860,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     raise_status(dev_status, VARRATE_ERR_TIMEOUT);
     atomicExch(&header->gave_up, 1u);
   }
+  if constexpr (kCoded) pdl_wait();                           // so that what waits for this kernel waits for both
 }
 
 }  // namespace
