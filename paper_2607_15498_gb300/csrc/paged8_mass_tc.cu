@@ -3,11 +3,12 @@
 // A unit is 256 keys of a sequence and KV head, in two tiles of 128, with every row that sees them:
 //   S[key][row] = K[key][.] Q[row][.]     M = 128, N = 128, K = 128,
 //   mass[key] += sum over rows of 2^(S scale - log2 e lse[row]).
-// The keys stay, expanded to bf16 (exact, with the block's scale), and the queries of 128 rows at a time go past them; both key tiles use every
-// query tile. A thread of the two epilogue warpgroups has a key and adds up in registers, so a token's sum has one order and is added to
-// its mass once. Rows of a query tile are (token, head) pairs, tq = 128 / group tokens.
+// The keys stay, expanded to bf16 (exact, with the block's scale) in TMEM, and the queries of 128 rows at a time go past them; both key tiles
+// use every query tile. (With the keys in shared memory its bandwidth was the bound: 64 KB a product of 512 cycles.) Two threads of the four epilogue warpgroups have a key, each half of the rows of a query tile, and add up in registers, so
+// a token's sum has one order and is added to its mass once. Rows of a query tile are (token, head) pairs, tq = 128 / group tokens.
 //
-// Warps: 0-3, 4-7 sums of a key tile each; 8 TMA producer; 9 issues products; 10 fetches log2 e lse; 12-15 expand keys, a thread a key.
+// Warps: 0-3, 4-7 sums of a key tile each over the first 64 rows, 8-11, 12-15 over the others; 16 TMA producer; 17, 18 issue the
+// products of a key tile each; 19 fetches log2 e lse; 20-23 expand keys, a thread a key.
 // Units are dealt out in turns, back and forth, the first of a sequence (which most rows see) first. Every wait is bounded; one
 // that gives up raises VARRATE_ERR_TIMEOUT and its CTA ends after its copies and products in flight have.
 #include <math.h>
@@ -31,28 +32,40 @@ bool make_tmap_heads_bf16(CUtensorMap* map, const void* base, uint32_t heads, ui
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kSumWarps = 8, kProducer = 8, kIssuer = 9, kRowsWarp = 10, kExpand = 12;
+constexpr int kThreads = 768;
+constexpr int kSumWarps = 16, kProducer = 16, kIssuer = 17, kRowsWarp = 19, kExpand = 20;   // issuers: 17 and 18
 constexpr int kTile = 128, kPair = 2 * kTile;               // keys of a tile, of a unit
 constexpr int kTileBytes = kTile * kHeadDim * 2;
-constexpr int kQueries = 3, kLse = 4, kUnits = 4;           // query tiles, rows of lse and units in flight
+constexpr int kCodeBytes = kTile * kHeadDim;
+constexpr int kQueries = 5, kLse = 4, kUnits = 4;           // query tiles, rows of lse and units in flight
+constexpr int kScores = 3;                                  // score tiles in TMEM, 128 columns each; behind them the keys, 64 a tile
 
 struct MassUnit {
   int valid, seq, g, key0, row0, n, len, q0, q1;            // row0: row of the sequence's first new token; query tiles q0 .. q1 - 1
 };
 
 struct Shared {
-  unsigned char keys[2][2][kTileBytes];                     // [unit & 1][tile]
+  unsigned char codes[2][2][kCodeBytes];                    // [unit & 1][tile]
   unsigned char query[kQueries][kTileBytes];
-  float lse[kLse][kTile];                                   // log2 e lse of a query tile's rows; infinity where one adds nothing
-  uint64_t raw[2][2], k_full[2][2], k_empty[2], q_full[kQueries], q_empty[kQueries], e_full[kLse], e_empty[kLse];
-  uint64_t s_full[2][2], s_empty[2][2], u_full[kUnits], u_empty[kUnits], drain;
+  float lse[kLse][kTile];                                   // -log2 e lse of a query tile's rows; -infinity where one adds nothing
+  uint64_t raw[2][2], raw_empty[2][2], k_full[2], k_empty[2], q_full[kQueries], q_empty[kQueries], e_full[kLse], e_empty[kLse];
+  uint64_t s_full[2][4], s_done[2][4], half_full[2],          // of a key tile's score tiles, by their number
+  u_full[kUnits], u_empty[kUnits], drain[2];
   MassUnit unit[kUnits];
   int dead[kLse];                                           // some row of the tile adds nothing
   int err;
   uint32_t tmem;
 };
 static_assert(sizeof(Shared) <= 232448, "shared memory of a block");
+
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+  float v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n tcgen05.wait::ld.sync.aligned;\n" : "=f"(v) : "r"(taddr) : "memory");
+  return v;
+}
 
 __global__ void __launch_bounds__(kThreads, 1)
 paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, Paged p,
@@ -65,15 +78,15 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c.k_empty[i], 1);
-      for (int j = 0; j < 2; ++j) {
-        mbar_init(&c.raw[i][j], 1); mbar_init(&c.k_full[i][j], 4); mbar_init(&c.s_full[i][j], 1); mbar_init(&c.s_empty[i][j], 4);
-      }
+      mbar_init(&c.k_full[i], 4); mbar_init(&c.k_empty[i], 1); mbar_init(&c.half_full[i], 4);
+      for (int j = 0; j < 2; ++j) { mbar_init(&c.raw[i][j], 1); mbar_init(&c.raw_empty[i][j], 4); }
     }
-    for (int i = 0; i < kQueries; ++i) { mbar_init(&c.q_full[i], 1); mbar_init(&c.q_empty[i], 1); }
+    for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < 2; ++j) { mbar_init(&c.s_full[j][i], 1); mbar_init(&c.s_done[j][i], 8); }
+    for (int i = 0; i < kQueries; ++i) { mbar_init(&c.q_full[i], 1); mbar_init(&c.q_empty[i], 2); }
     for (int i = 0; i < kLse; ++i) { mbar_init(&c.e_full[i], 1); mbar_init(&c.e_empty[i], kSumWarps); }
-    for (int i = 0; i < kUnits; ++i) { mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSumWarps + 2 + 4); }
-    mbar_init(&c.drain, 1);
+    for (int i = 0; i < kUnits; ++i) { mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSumWarps + 3 + 4); }
+    for (int i = 0; i < 2; ++i) mbar_init(&c.drain[i], 1);
     c.err = 0;
     fence_mbar_init();
   }
@@ -141,8 +154,9 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       return true;
     };
     auto keys = [&](const MassUnit& x) {
-      const uint32_t slot = nk & 1;
-      if (!warp_wait(&c.k_empty[slot], ((nk >> 1) & 1) ^ 1)) return false;
+      const uint32_t slot = nk & 1, fill = nk >> 1;
+      for (int e = 0; e < 2; ++e)
+        if (!warp_wait(&c.raw_empty[slot][e], (fill & 1) ^ 1)) return false;
       ++nk;
       for (int e = 0; e < 2; ++e) {
         const int base = x.key0 + e * kTile, key = base + lane * page_keys;
@@ -155,7 +169,7 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
             raise_status(dev_status, VARRATE_ERR_CORRUPT);
             page = 0;
           }
-          tma_load_2d(smem_addr(c.keys[slot][e]) + kTile * 128 + lane * page_keys * 128, &tmap, 0,
+          tma_load_2d(smem_addr(c.codes[slot][e]) + lane * page_keys * 128, &tmap, 0,
                       (int)page_row(p, page, 0, x.g, key & ((1 << p.page_log2) - 1)), &c.raw[slot][e]);
         }
       }
@@ -191,11 +205,14 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       for (uint32_t i = nk > 2 ? nk - 2 : 0; i < nk; ++i)
         for (int e = 0; e < 2; ++e) warp_wait(&c.raw[i & 1][e], (i >> 1) & 1);
     }
-  } else if (warp == kIssuer) {
-    // ------------------------------------------------------------------ products
+  } else if (warp == kIssuer || warp == kIssuer + 1) {
+    // ------------------------------------------------------------------ products of key tile e
+    // (values that are the same in every lane, broadcast from lane 0 where they come from memory, stay in uniform registers)
     constexpr uint32_t idesc = idesc_bf16_f32(kTile, kTile);
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = smem_addr(c.keys), queries = smem_addr(c.query);
-    uint32_t n = 0;                                               // query tiles so far
+    const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + kScores * kTile + 64 * e;
+    const uint64_t queries = sdesc_sw128(smem_addr(c.query));
+    uint32_t slot = 0, q_phase = 0, at = e, n = 0;                // of the next query tile; where its scores go; its number
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
       ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
@@ -204,42 +221,46 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       const int valid = __shfl_sync(0xffffffffu, x->valid, 0), tiles = __shfl_sync(0xffffffffu, x->q1 - x->q0, 0);
       if (!valid) break;
       if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
-      for (int t = 0; t < tiles && ok; ++t, ++n) {
-        const uint32_t slot = n % kQueries, b = n & 1;
-        ok = warp_wait(&c.q_full[slot], (n / kQueries) & 1);
+      ok = warp_wait(&c.k_full[e], un & 1);
+      for (int t = 0; t < tiles && ok; ++t) {
+        ok = warp_wait(&c.q_full[slot], q_phase);
+        // the scores' place: of the two key tiles' products, taken in turn, it was that of the third before this one, of the other tile
+        const uint32_t m = n + e - 2;
+        if (ok && n + e >= 2) ok = warp_wait(&c.s_done[e ^ 1][m & 3], (m >> 2) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t q = queries + slot * (kTileBytes / 16);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (ok && t == 0) ok = warp_wait(&c.k_full[un & 1][e], (un >> 1) & 1);
-          ok = ok && warp_wait(&c.s_empty[e][b], ((n >> 1) & 1) ^ 1);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint64_t a = sdesc_sw128(keys + ((un & 1) * 2 + e) * kTileBytes), q = sdesc_sw128(queries + slot * kTileBytes);
-#pragma unroll
-            for (int ks = 0; ks < kHeadDim / 16; ++ks) {
-              const uint64_t o = (uint64_t)((ks >> 2) * (kTile * 128) + (ks & 3) * 32) / 16;
-              tc_mma_bf16(tm + (2 * e + b) * kTile, a + o, q + o, idesc, ks != 0);
-            }
-            tc_commit(&c.s_full[e][b]);
-            if (e == 1) {
-              tc_commit(&c.q_empty[slot]);
-              if (t == tiles - 1) tc_commit(&c.k_empty[un & 1]);
-            }
-          }
-          __syncwarp();
+          for (int ks = 0; ks < kHeadDim / 16; ++ks)
+            tc_mma_bf16_ts(tm + at * kTile, keys + 8 * ks, q + ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) / 16, idesc, ks != 0);
+          tc_commit(&c.s_full[e][n & 3]);
+          tc_commit(&c.q_empty[slot]);
+          if (t == tiles - 1) tc_commit(&c.k_empty[e]);
         }
+        __syncwarp();
+        if (++slot == kQueries) { slot = 0; q_phase ^= 1; }
+        at = at + 2 >= kScores ? at + 2 - kScores : at + 2;
+        ++n;
       }
     }
     if (!ok) {                                                    // the products in flight end before TMEM is freed
       c.err = 1;
-      if (elect_one()) tc_commit(&c.drain);
-      warp_wait(&c.drain, 0);
+      if (elect_one()) tc_commit(&c.drain[e]);
+      warp_wait(&c.drain[e], 0);
     }
     __syncwarp();
   } else if (warp == kRowsWarp) {
     // ------------------------------------------------------------------ log2 e lse of the rows
     uint32_t n = 0;
     bool ok = true;
+    int token[4], off[4];                                         // of this lane's rows of a tile: past every tile's where there is none
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = lane + 32 * i;
+      token[i] = row < tq * grp ? row / grp : INT32_MAX / 2;
+      off[i] = row / grp * H + row % grp;
+    }
     for (uint32_t un = 0; ok; ++un) {
       ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
       if (!ok) break;
@@ -247,26 +268,38 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       __syncwarp();
       if (!x.valid) break;
       if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
-      for (int t = x.q0; t < x.q1; ++t, ++n) {
-        float y[4];
-        bool dead = false;
+      float z[2][4];                                              // lse of the next two tiles' rows
+      auto fetch = [&](int t, float (&z)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = lane + 32 * i, tok = t * tq + row / grp;
-          y[i] = INFINITY;
-          if (row >= tq * grp || tok >= x.n) continue;
-          const float z = __ldg(lse + (int64_t)(x.row0 + tok) * H + x.g * grp + row % grp);
-          if (fabsf(z) < INFINITY) y[i] = z * kLog2e;
-          else dead = true;
+        for (int i = 0; i < 4; ++i)
+          z[i] = t < x.q1 && token[i] < x.n - t * tq ? __ldg(lse + (int64_t)(x.row0 + t * tq) * H + x.g * grp + off[i]) : 0.f;
+      };
+      fetch(x.q0, z[0]);
+      fetch(x.q0 + 1, z[1]);
+      for (int t0 = x.q0; t0 < x.q1 && ok; t0 += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = t0 + h;
+          if (t >= x.q1 || !ok) break;
+          float y[4];
+          bool dead = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool there = token[i] < x.n - t * tq, finite = fabsf(z[h][i]) < INFINITY;
+            y[i] = there && finite ? -z[h][i] * kLog2e : -INFINITY;
+            dead |= there && !finite;
+          }
+          dead = __any_sync(0xffffffffu, dead);
+          fetch(t + 2, z[h]);
+          ok = warp_wait(&c.e_empty[n % kLse], ((n / kLse) & 1) ^ 1);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) c.lse[n % kLse][lane + 32 * i] = y[i];
+          if (lane == 0) c.dead[n % kLse] = dead;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&c.e_full[n % kLse]);
+          ++n;
         }
-        dead = __any_sync(0xffffffffu, dead);
-        ok = warp_wait(&c.e_empty[n % kLse], ((n / kLse) & 1) ^ 1);
-        if (!ok) break;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c.lse[n % kLse][lane + 32 * i] = y[i];
-        if (lane == 0) c.dead[n % kLse] = dead;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.e_full[n % kLse]);
       }
     }
     if (!ok) c.err = 1;
@@ -291,19 +324,37 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        ok = ok && warp_wait(&c.raw[un & 1][e], (un >> 1) & 1);
+        ok = ok && warp_wait(&c.raw[un & 1][e], (un >> 1) & 1) && warp_wait(&c.k_empty[e], (un & 1) ^ 1);
         if (!ok) break;
-        expand_row<true>(c.keys[un & 1][e], kTile, key_in, x.key0 + e * kTile + key_in < x.len, byte[e]);
-        fence_proxy_async_smem();
+        tc_fence_after();
+        const unsigned char* row = c.codes[un & 1][e] + key_in * 128;
+        const uint32_t scale2 = byte[e] * 0x00800080u, to = tmem + kScores * kTile + 64 * e + ((uint32_t)((warp & 3) * 32) << 16);
+        const bool there = x.key0 + e * kTile + key_in < x.len;
+#pragma unroll 1
+        for (int h = 0; h < 4; ++h) {                             // 32 elements, 16 columns
+          uint4 y[4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint4 w = *reinterpret_cast<const uint4*>(row + (((2 * h + i) ^ (key_in & 7)) << 4));
+            if (!there) w = make_uint4(0, 0, 0, 0);
+            expand16(w, scale2, y[2 * i], y[2 * i + 1]);
+          }
+          tmem_st16(to + 16 * h, reinterpret_cast<const uint32_t(&)[16]>(y));
+        }
+        tmem_wait_st();
+        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&c.k_full[un & 1][e]);
+        if (lane == 0) {
+          mbar_arrive(&c.raw_empty[un & 1][e]);
+          mbar_arrive(&c.k_full[e]);
+        }
       }
     }
     if (!ok) c.err = 1;
   } else if (warp < kSumWarps) {
     // ------------------------------------------------------------------ sums: one key per thread
-    const int e = warp >> 2, r = tid & 127;
-    const uint32_t ts = tmem + 2 * e * kTile + ((uint32_t)((warp & 3) * 32) << 16);
+    const int e = warp >> 2 & 1, half = warp >> 3, r = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     uint32_t n = 0;
     bool ok = true;
     for (uint32_t un = 0; ok; ++un) {
@@ -317,57 +368,80 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       const int page = key < x.len ? __ldg(p.table + (int64_t)x.seq * p.max_pages + (key >> p.page_log2)) : -1;
       const int top = __shfl_sync(0xffffffffu, ahead, 31);
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      float total = 0.f;
       for (int t = x.q0; t < x.q1; ++t, ++n) {
-        const uint32_t b = n & 1, slot = n % kLse;
-        ok = warp_wait(&c.e_full[slot], (n / kLse) & 1) && warp_wait(&c.s_full[e][b], (n >> 1) & 1);
+        const uint32_t at = (2 * n + e) % kScores, slot = n % kLse, ts = tmem + at * kTile + lanes;
+        ok = warp_wait(&c.e_full[slot], (n / kLse) & 1) && warp_wait(&c.s_full[e][n & 3], (n >> 2) & 1);
         if (!ok) break;
         tc_fence_after();
         // some key of the warp is behind some row of the tile, or the tile has rows that add nothing
         const bool cut = top > t * tq || (t + 1) * tq > x.n || c.dead[slot];
         const int lo = max(0, ahead - t * tq) * grp, hi = min(tq, x.n - t * tq) * grp;
         float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        const uint32_t mine = ts + 64 * half;
+        const float* less = c.lse[slot] + 64 * half;
+        if (cut) {
 #pragma unroll 1
-        for (int cb = 0; cb < kTile; cb += 64) {
-          float s[64];
-          tmem_ld64(ts + b * kTile + cb, s);
-          const float4* y = reinterpret_cast<const float4*>(c.lse[slot] + cb);
-          if (cut) {
+          for (int cb = 0; cb < 64; cb += 32) {
+            float s[32];
+            tmem_ld32(mine + cb, s);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float4 l4 = y[k];
-              const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int col = cb + 4 * k + j;
-                s[4 * k + j] = col >= lo && col < hi && l[j] < INFINITY ? fmaf(s[4 * k + j], scale_log2, -l[j]) : -INFINITY;
-              }
+            for (int k = 0; k < 32; ++k) {
+              const int col = 64 * half + cb + k;
+              const float l = less[cb + k];
+              s[k] = col >= lo && col < hi && l > -INFINITY ? fmaf(s[k], scale_log2, l) : -INFINITY;
             }
-          } else {
-            const float2 sc = make_float2(scale_log2, scale_log2);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float4 l = y[k];
-              const float2 u = fma2(make_float2(s[4 * k], s[4 * k + 1]), sc, make_float2(-l.x, -l.y));
-              const float2 v = fma2(make_float2(s[4 * k + 2], s[4 * k + 3]), sc, make_float2(-l.z, -l.w));
-              s[4 * k] = u.x; s[4 * k + 1] = u.y; s[4 * k + 2] = v.x; s[4 * k + 3] = v.y;
-            }
+            for (int k = 0; k < 16; ++k) part[k & 1] = add2(part[k & 1], make_float2(fast_exp2(s[2 * k]), fast_exp2(s[2 * k + 1])));
           }
+        } else {
+          const float2 sc = make_float2(scale_log2, scale_log2);
+          float s0[32], s1[32];
+          auto add = [&](float (&s)[32], const float* l) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) part[k & 1] = add2(part[k & 1], make_float2(fast_exp2(s[2 * k]), fast_exp2(s[2 * k + 1])));
+            for (int k = 0; k < 8; ++k) {
+              const float4 y = reinterpret_cast<const float4*>(l)[k];
+              const float2 u = fma2(make_float2(s[4 * k], s[4 * k + 1]), sc, make_float2(y.x, y.y));
+              const float2 v = fma2(make_float2(s[4 * k + 2], s[4 * k + 3]), sc, make_float2(y.z, y.w));
+              part[0] = add2(part[0], make_float2(fast_exp2(u.x), fast_exp2(u.y)));
+              part[1] = add2(part[1], make_float2(fast_exp2(v.x), fast_exp2(v.y)));
+            }
+          };
+          tmem_ld32_async(mine, s0);
+          tmem_wait_ld32(s0);
+          tmem_ld32_async(mine + 32, s1);                         // under the sum of the first
+          add(s0, less);
+          tmem_wait_ld32(s1);
+          add(s1, less + 32);
+        }
+        sum[0] = add2(sum[0], part[0]);
+        sum[1] = add2(sum[1], part[1]);
+        if (t == x.q1 - 1) {                                      // the two halves meet in the scores' place
+          const float2 w = add2(sum[0], sum[1]);
+          total = w.x + w.y;
+          if (half) {
+            tmem_st1(ts + 64, total);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.half_full[e]);
+          } else {
+            ok = warp_wait(&c.half_full[e], un & 1);
+            if (!ok) break;
+            tc_fence_after();
+            total += tmem_ld1(ts + 64);
+          }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&c.s_empty[e][b]);
+          mbar_arrive(&c.s_done[e][n & 3]);
           mbar_arrive(&c.e_empty[slot]);
         }
-        sum[0] = add2(sum[0], part[0]);
-        sum[1] = add2(sum[1], part[1]);
       }
       if (!ok) break;
-      const float2 w = add2(sum[0], sum[1]);
       // one addition to a token in a call: the order is no matter
-      if (page >= 0 && page < p.n_pages) atomicAdd(mass + mass_at(p, page, x.g, key & ((1 << p.page_log2) - 1)), w.x + w.y);
+      if (!half && page >= 0 && page < p.n_pages) atomicAdd(mass + mass_at(p, page, x.g, key & ((1 << p.page_log2) - 1)), total);
     }
     if (!ok) c.err = 1;
   }

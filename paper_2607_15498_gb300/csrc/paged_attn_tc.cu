@@ -108,13 +108,6 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
   return false;
 }
 
-// D[tmem] (+)= A[tmem] * B[smem]^T (A: bf16 pairs, row = lane, 8 columns per K = 16), issued by one thread.
-__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
 // Piece j of lane i to piece i of lane j, in groups of four lanes.
 __device__ __forceinline__ void transpose4(uint4 (&y)[4], int lane) {
 #pragma unroll
