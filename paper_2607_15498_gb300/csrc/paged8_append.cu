@@ -7,7 +7,7 @@
 // and the older codes of the block times 2^(their byte - byte).
 // A unit is a block of 16 places of one sequence that gets new tokens; a warp takes the 16 tokens of one of its H + 2 G heads:
 // eight lanes a token, sixteen elements each (eight first members of pairs and their partners), four tokens at a time, so
-// that a block's largest element is in one warp's registers. Sines and cosines of the 16 tokens are made once for the CTA's heads.
+// that a block's largest element is found by one warp. Sines and cosines of the 16 tokens are made once for the CTA's heads.
 #include "common.cuh"
 #include "paged.h"
 #include "paged8.h"
@@ -16,7 +16,7 @@ namespace vr {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 2;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 4;
 constexpr int kSteps = kBlock / 4;            // a warp's rows of a task, four at a time
 
 struct Append8Args {
@@ -81,7 +81,8 @@ __device__ __forceinline__ int seq_of_unit(const Paged& p, int u, int lane) {
 __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p, Append8Args a) {
   __shared__ unsigned long long turn[kHeadDim / 2];   // freq / 2 pi modulo 1, times 2^64
   __shared__ __align__(16) float weight[2][kHeadDim];
-  __shared__ __align__(16) float angle[2][kBlock][2][kHeadDim / 2];   // [item & 1][token][cosine, sine]
+  __shared__ __align__(16) float angle[kBlock][2][kHeadDim / 2];   // of the item's tokens: cosines, sines
+  __shared__ uint4 raw[kWarps][kSteps][2][32];                     // a warp's rows as they come, a lane's own
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7;
   pdl_trigger();
   pdl_wait();
@@ -95,9 +96,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
   const int64_t items = (int64_t)((p.T >> kBlockLog2) + 2 * p.S + 1) * chunks;
   // this lane's two groups of eight elements: a group of first members and its partners, or two groups that stay
   const bool turns = sub < h8;
-  const int e0 = 8 * (turns ? sub : 2 * sub), e1 = 8 * (turns ? sub + h8 : 2 * sub + 1);
+  const int e0 = 8 * (turns ? sub : sub + h8), e1 = 8 * (turns ? sub + h8 : sub + 8);
 
-  int buf = 0;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int u = (int)(it / chunks), lo = (int)(it % chunks) * a.per, hi = min(lo + a.per, tasks);
     const int s = seq_of_unit(p, u, lane);
@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
     SeqRange r;
     if (!seq_range(p, s, r) || r.n == 0) continue;    // the status is raised below
     const int start = r.len - r.n;                    // place of the first new token
-    const int64_t base64 = (((int64_t)start >> kBlockLog2) + (u - first_unit(p.row_start, s))) << kBlockLog2;
-    if (base64 >= r.len) continue;
+    const int64_t nth = (int64_t)u - first_unit(p.row_start, s), base64 = (((int64_t)start >> kBlockLog2) + nth) << kBlockLog2;
+    if (nth < 0 || base64 >= r.len) continue;         // (below 0: row ranges out of order)
     const int base = (int)base64, old = max(start - base, 0), end = min(r.len - base, kBlock);   // new tokens: rows old .. end - 1
     const int row0 = r.row0 + (base - start);         // row of the block's first place
     int page = __ldg(p.table + (int64_t)s * p.max_pages + (base >> p.page_log2));
@@ -117,118 +117,125 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
       page = -1;
     }
     bool made = a.rot == 0;                           // the item's sines and cosines are there
-    buf ^= 1;
     for (int t0 = lo; t0 < hi; t0 += kWarps) {
       const int task = t0 + warp;
       const bool is_q = task < a.H, is_v = task >= a.H + p.G, live = task < hi;
-      uint4 x0[kSteps], x1[kSteps];
+      const int row_in = lane >> 3;                   // of the first of this lane's four rows; the others are 4, 8 and 12 further
       int64_t code_row = 0;
       int before = 0;
       if (live) {
-        const __nv_bfloat16* src = is_q ? a.q + task * kHeadDim : (is_v ? a.v + (task - a.H - p.G) * kHeadDim : a.k + (task - a.H) * kHeadDim);
         const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+        const __nv_bfloat16* src = is_q ? a.q + task * kHeadDim : is_v ? a.v + (task - a.H - p.G) * kHeadDim : a.k + (task - a.H) * kHeadDim;
+        src += (row0 + row_in) * stride;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const int row = 4 * i + (lane >> 3);
-          if (row < old || row >= end) continue;
-          const __nv_bfloat16* x = src + (row0 + row) * stride;   // (q may be q_out: no read-only loads)
-          x0[i] = *reinterpret_cast<const uint4*>(x + e0);
-          x1[i] = *reinterpret_cast<const uint4*>(x + e1);
+        for (int i = 0; i < kSteps; ++i) {            // rows that are none read as zeros
+          const bool there = 4 * i + row_in >= old && 4 * i + row_in < end;
+          const __nv_bfloat16* x = there ? src + 4 * i * stride : a.k;
+          cp_async16(smem_addr(&raw[warp][i][0][lane]), x + e0, there ? 16 : 0);
+          cp_async16(smem_addr(&raw[warp][i][1][lane]), x + e1, there ? 16 : 0);
         }
         if (!is_q && page >= 0) {
           code_row = page_row(p, page, is_v, task - a.H - (is_v ? p.G : 0), base & ((1 << p.page_log2) - 1));
           if (old) before = a.scale[scale_at(code_row)];
         }
       }
+      cp_async_commit();
       if (!made) {                                    // behind the first loads
+        __syncthreads();                              // (the last item's have been read)
         for (int i = tid; i < kBlock * (a.rot / 2); i += kThreads) {
           const int row = i / (a.rot / 2), j = i % (a.rot / 2);
           if (row < old || row >= end) continue;
           const unsigned long long pos = (unsigned long long)base + row + gone;
-          sincospif(__ll2float_rn((long long)(turn[j] * pos)) * 0x1p-63f, &angle[buf][row][1][j], &angle[buf][row][0][j]);
+          sincospif(__ll2float_rn((long long)(turn[j] * pos)) * 0x1p-63f, &angle[row][1][j], &angle[row][0][j]);
         }
         __syncthreads();
         made = true;
       }
-      if (!live) continue;
+      cp_async_wait<0>();
+      if (!live || (!is_q && page < 0)) continue;
       const bool normed = is_q ? a.q_norm != nullptr : a.k_norm != nullptr && !is_v, turned = turns && !is_v;
-      if (is_q && !normed && a.rot == 0) {            // a copy
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const int row = 4 * i + (lane >> 3);
-          if (row < old || row >= end) continue;
-          __nv_bfloat16* y = a.q_out + ((int64_t)(row0 + row) * a.H + task) * kHeadDim;
-          *reinterpret_cast<uint4*>(y + e0) = x0[i];
-          *reinterpret_cast<uint4*>(y + e1) = x1[i];
-        }
-        continue;
-      }
-      float2 y0[kSteps][4], y1[kSteps][4];
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        const int row = 4 * i + (lane >> 3);
-        if (row >= old && row < end) {
-          unpack(x0[i], y0[i]);
-          unpack(x1[i], y1[i]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y0[i][j] = y1[i][j] = make_float2(0.f, 0.f);
-        }
+      // Row i of this lane's four with its norm and rotation. Rows of keys and values are formed twice, for the scale and for the
+      // codes, and read from shared memory each time: registers are the bound on the warps of an SM.
+      auto form = [&](int i, float2 (&y0)[4], float2 (&y1)[4]) {
+        const int row = 4 * i + row_in;
+        unpack(raw[warp][i][0][lane], y0);
+        unpack(raw[warp][i][1][lane], y1);
         if (normed) {                                 // (the same for the warp)
           float2 sq = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sq = fma2(y0[i][j], y0[i][j], fma2(y1[i][j], y1[i][j], sq));
+          for (int j = 0; j < 4; ++j) sq = fma2(y0[j], y0[j], fma2(y1[j], y1[j], sq));
           float ss = sq.x + sq.y;
 #pragma unroll
           for (int o = 4; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float f1 = rsqrtf(ss * (1.f / kHeadDim) + a.eps);
+          const float f1 = row >= old && row < end ? rsqrtf(ss * (1.f / kHeadDim) + a.eps) : 0.f;
           const float2 f = make_float2(f1, f1);
-          float2 w0[4], w1[4];
-          load_pairs(weight[is_q ? 0 : 1] + e0, w0);
-          load_pairs(weight[is_q ? 0 : 1] + e1, w1);
-          if (row >= old && row < end) {
+          float2 w[4];
+          load_pairs(weight[is_q ? 0 : 1] + e0, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { y0[i][j] = mul2(mul2(y0[i][j], f), w0[j]); y1[i][j] = mul2(mul2(y1[i][j], f), w1[j]); }
-          }
+          for (int j = 0; j < 4; ++j) y0[j] = mul2(mul2(y0[j], f), w[j]);
+          load_pairs(weight[is_q ? 0 : 1] + e1, w);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y1[j] = mul2(mul2(y1[j], f), w[j]);
         }
         if (turned && row >= old && row < end) {
           float2 c[4], sn[4];
-          load_pairs(angle[buf][row][0] + e0, c);
-          load_pairs(angle[buf][row][1] + e0, sn);
+          load_pairs(angle[row][0] + e0, c);
+          load_pairs(angle[row][1] + e0, sn);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 z = fma2(make_float2(-y1[i][j].x, -y1[i][j].y), sn[j], mul2(y0[i][j], c[j]));
-            y1[i][j] = fma2(y0[i][j], sn[j], mul2(y1[i][j], c[j]));
-            y0[i][j] = z;
+            const float2 z = fma2(make_float2(-y1[j].x, -y1[j].y), sn[j], mul2(y0[j], c[j]));
+            y1[j] = fma2(y0[j], sn[j], mul2(y1[j], c[j]));
+            y0[j] = z;
           }
         }
-        if (is_q) {
-          if (row >= old && row < end) {
-            __nv_bfloat16* y = a.q_out + ((int64_t)(row0 + row) * a.H + task) * kHeadDim;
-            const float2(&b0)[4] = y0[i], (&b1)[4] = y1[i];
-            *reinterpret_cast<uint4*>(y + e0) = make_uint4(pack_bf16(b0[0].x, b0[0].y), pack_bf16(b0[1].x, b0[1].y), pack_bf16(b0[2].x, b0[2].y), pack_bf16(b0[3].x, b0[3].y));
-            *reinterpret_cast<uint4*>(y + e1) = make_uint4(pack_bf16(b1[0].x, b1[0].y), pack_bf16(b1[1].x, b1[1].y), pack_bf16(b1[2].x, b1[2].y), pack_bf16(b1[3].x, b1[3].y));
+      };
+      float2 y0[4], y1[4];
+      if (is_q) {
+        const bool copy = !normed && a.rot == 0;
+        __nv_bfloat16* y = a.q_out + ((int64_t)(row0 + row_in) * a.H + task) * kHeadDim;
+#pragma unroll 2
+        for (int i = 0; i < kSteps; ++i) {
+          uint4 z0, z1;
+          if (copy) {
+            z0 = raw[warp][i][0][lane];
+            z1 = raw[warp][i][1][lane];
+          } else {
+            form(i, y0, y1);
+            z0 = make_uint4(pack_bf16(y0[0].x, y0[0].y), pack_bf16(y0[1].x, y0[1].y), pack_bf16(y0[2].x, y0[2].y), pack_bf16(y0[3].x, y0[3].y));
+            z1 = make_uint4(pack_bf16(y1[0].x, y1[0].y), pack_bf16(y1[1].x, y1[1].y), pack_bf16(y1[2].x, y1[2].y), pack_bf16(y1[3].x, y1[3].y));
           }
-        } else {
-          top = most(y1[i], most(y0[i], top));
+          if (4 * i + row_in < old || 4 * i + row_in >= end) continue;
+          *reinterpret_cast<uint4*>(y + (int64_t)4 * i * a.H * kHeadDim + e0) = z0;
+          *reinterpret_cast<uint4*>(y + (int64_t)4 * i * a.H * kHeadDim + e1) = z1;
         }
+        continue;
       }
-      if (is_q || page < 0) continue;
-      if (__any_sync(0xffffffffu, top == INFINITY)) {
+      float top = 0.f;
+#pragma unroll 2
+      for (int i = 0; i < kSteps; ++i) {
+        form(i, y0, y1);
+        top = most(y1, most(y0, top));
+      }
+      const bool odd = __any_sync(0xffffffffu, top == INFINITY);   // rare: infinities, which count as NaN
+      if (odd) {
         top = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) top = most_finite(y1[i], most_finite(y0[i], top));
+#pragma unroll 1
+        for (int i = 0; i < kSteps; ++i) {
+          form(i, y0, y1);
+          top = most_finite(y1, most_finite(y0, top));
+        }
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       const int byte = max(before, scale_byte(top));
       const float f = byte ? scale_inverse(byte) : 1.f;
-      unsigned char* dst = a.codes + code_row * kHeadDim;
-#pragma unroll
+      unsigned char* dst = a.codes + (code_row + row_in) * kHeadDim;
+#pragma unroll 2
       for (int i = 0; i < kSteps; ++i) {
-        const int row = 4 * i + (lane >> 3);
-        uint2 *z0 = reinterpret_cast<uint2*>(dst + row * kHeadDim + e0), *z1 = reinterpret_cast<uint2*>(dst + row * kHeadDim + e1);
+        const int row = 4 * i + row_in;
+        uint2 *z0 = reinterpret_cast<uint2*>(dst + 4 * i * kHeadDim + e0), *z1 = reinterpret_cast<uint2*>(dst + 4 * i * kHeadDim + e1);
+        form(i, y0, y1);
+        if (odd) { most_finite(y0, 0.f); most_finite(y1, 0.f); }
         if (row < old) {
           if (byte != before) {
             const Rescale by(byte - before);
@@ -237,8 +244,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
             *z1 = make_uint2(by.four(o1.x), by.four(o1.y));
           }
         } else if (row < end) {
-          *z0 = codes8(y0[i], f);
-          *z1 = codes8(y1[i], f);
+          *z0 = codes8(y0, f);
+          *z1 = codes8(y1, f);
         }
       }
       if (lane == 0) a.scale[scale_at(code_row)] = (unsigned char)byte;
@@ -273,7 +280,7 @@ int launch_paged8_append(const Paged8& c, int layer, int group, const void* q, i
   const int tasks = a.H + 2 * p.G;
   const int64_t units = (p.T >> kBlockLog2) + 2 * (int64_t)p.S + 1, most = (int64_t)num_sms * kCtas;
   a.per = (tasks + kWarps - 1) / kWarps * kWarps;
-  while (a.per > kWarps && units * ((tasks + a.per - 1) / a.per) < 4 * most) a.per = (a.per / 2 + kWarps - 1) / kWarps * kWarps;
+  while (a.per > kWarps && units * ((tasks + a.per - 1) / a.per) < 2 * most) a.per = (a.per / 2 + kWarps - 1) / kWarps * kWarps;
   const int64_t items = units * ((tasks + a.per - 1) / a.per);
   return launch_pdl(paged8_append_kernel, dim3((unsigned)(items < most ? items : most)), kThreads, 0, st, p, a) ? 1 : -1;
 }

@@ -84,9 +84,12 @@ template <bool kScaled>
 __device__ __forceinline__ void expand_row(unsigned char* tile, int rows, int key, bool there, uint32_t byte) {
   unsigned char *row = tile + key * 128, *codes = row + rows * 128;
   const uint32_t scale2 = byte * 0x00800080u;
+  auto read = [&](int i) { return *reinterpret_cast<const uint4*>(codes + ((i ^ (key & 7)) << 4)); };
+  uint4 next = read(0);
 #pragma unroll 1
   for (int i = 0; i < 8; ++i) {                             // elements 16 i .. 16 i + 15
-    uint4 w = *reinterpret_cast<const uint4*>(codes + ((i ^ (key & 7)) << 4)), lo, hi;
+    uint4 w = next, lo, hi;
+    next = read((i + 1) & 7);                               // (the last one is not used)
     if (!there) w = make_uint4(0, 0, 0, 0);
     if constexpr (kScaled) {
       expand16(w, scale2, lo, hi);

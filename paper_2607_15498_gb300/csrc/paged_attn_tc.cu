@@ -64,8 +64,8 @@ namespace {
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
 constexpr int kExpand = 12, kExpandWarps = 4;               // of the coded form
 template <bool kCoded> constexpr int kThreads = 32 * (kExpand + (kCoded ? kExpandWarps : 0));
-// Registers a thread of the coded form, by warpgroup: softmax 0 and 1, the others: 2 * 168 + 2 * 88 = 4 * 128 of the launch.
-constexpr int kSoftRegs = 168, kOtherRegs = 88;
+// Registers a thread of the coded form, by warpgroup: softmax 0 and 1, the others: 2 * 184 + 2 * 72 = 4 * 128 of the launch.
+constexpr int kSoftRegs = 184, kOtherRegs = 72;
 constexpr int kRows = 128, kKeys = kKeysBf16;
 constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it: geometric mean over
                                                             // 19 cases 42.0 us, at 3 and 4 41.8, at 6 42.1, at 8 42.5

@@ -84,6 +84,10 @@ ATTN = [
     dict(lens=[(1, 33), (8, 120)], G=3, grp=1, ps=16),
     dict(lens=[(40, 3000), (24, 2500), (1, 3300), (90, 1800), (4, 2000)], G=8, grp=4, ps=64),
     dict(lens=[(17, 900)] * 40, G=2, grp=7, ps=128),
+    dict(lens=[(1, 13 * i % 90) for i in range(100)], G=1, grp=2, ps=16, pad=4),
+    dict(lens=[(1, 7 * i % 60) for i in range(40)] + [(30, 50), (0, 9)] + [(2, 5)] * 30 + [(150, 10)], G=2, grp=4, ps=16),
+    dict(lens=[(20, 100)] + [(0, 5)] * 30, G=2, grp=5, ps=32),          # many tokens of one sequence, but no more rows than sequences
+    dict(lens=[(0, 3)] * 20 + [(9, 0)], G=1, grp=8, ps=16),
 ]
 
 
