@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
                    const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                    int32_t* __restrict__ dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts,
-                   int grp, float scale_log2) {
+                   int grp, int follows, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
@@ -84,8 +84,11 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   }
   if (tid == 0) c.err = 0;
   __syncthreads();
-  pdl_wait();
-  pdl_trigger();                                                    // (the tcgen05 kernel goes by it: not before)
+  // The kernel before this one takes other sequences, and lets this one start when what comes before both has ended. So this one fills
+  // the SMs that the other has no unit for, or is done with.
+  if (follows) __threadfence();
+  else pdl_wait();
+  pdl_trigger();
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
   const float weight = plan_weight<kKeys, true>(p, tq, lane, longest);
@@ -324,6 +327,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     raise_status(dev_status, VARRATE_ERR_TIMEOUT);
     atomicExch(&header->gave_up, 1u);
   }
+  if (follows) pdl_wait();                                          // so that what waits for this kernel waits for both
 }
 
 }  // namespace
@@ -340,6 +344,14 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group, few = few_tokens(p, group);
+  MergeTwo two = {};
+  two.lse = lse; two.few = few; two.tq = 128 / group; two.bq = 2 * two.tq;
+  if (p.T > few) {                                                  // else no sequence can have more
+    Paged8 many = c;
+    many.p.n_min = few + 1;
+    two.second = w + paged_part_bytes(c.p, group, tq, num_sms);
+    if (launch_paged8_attn_tc(many, layer, group, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
+  }
   p.n_max = few;
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;
@@ -352,16 +364,8 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
                   (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
-                  paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim)))
+                  paged_max_parts(num_sms), group, (int)(two.second != nullptr), kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  MergeTwo two = {};
-  two.lse = lse; two.few = few; two.tq = 128 / group; two.bq = 2 * two.tq;
-  if (p.T > few) {                                                  // else no sequence can have more
-    Paged8 many = c;
-    many.p.n_min = few + 1;
-    two.second = w + paged_part_bytes(c.p, group, tq, num_sms);
-    if (launch_paged8_attn_tc(many, layer, group, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
-  }
   return launch_paged_merge_two(c.p, group, out, dev_status, header, part, tq, tq, two, num_sms, st) < 0 ? -1 : 2;
 }
 

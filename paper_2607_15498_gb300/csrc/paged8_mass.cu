@@ -39,7 +39,7 @@ __device__ __forceinline__ int64_t steps_of(const Paged& p, int s, int few, SeqR
 __global__ void __launch_bounds__(kThreads, kCtas)
 paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
                    float* __restrict__ mass, const __nv_bfloat16* __restrict__ q, const float* __restrict__ lse,
-                   int32_t* __restrict__ dev_status, int grp, int few, float scale_log2) {
+                   int32_t* __restrict__ dev_status, int grp, int few, int follows, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3, H = p.G * grp, tq = kRows / grp;
@@ -48,8 +48,9 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     fence_mbar_init();
   }
   __syncwarp();
-  pdl_wait();
-  pdl_trigger();                                                    // (the tcgen05 kernel goes by it: not before)
+  if (follows) __threadfence();                                     // (as in the attention of few rows)
+  else pdl_wait();
+  pdl_trigger();
   int64_t total = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
@@ -61,7 +62,10 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   const int64_t warps = (int64_t)gridDim.x * kWarps, id = (int64_t)blockIdx.x * kWarps + warp;
   int64_t at = total * id / warps;
   const int64_t stop = total * (id + 1) / warps;
-  if (at >= stop) return;
+  if (at >= stop) {
+    if (follows) pdl_wait();
+    return;
+  }
   uint32_t stage = 0, phase = 0;
   bool ok = true;
 
@@ -126,7 +130,7 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     Rows rows[2];
     load_rows(0, rows[0]);
     load_rows(1, rows[1]);
-    const int blocks = (n + tq - 1) / tq;                           // the first two stay in registers
+    const int blocks = (n + tq - 1) / tq;                           // two stay in registers
     int i = 0;
     for (; i < steps.n; ++i) {
       ok = warp_wait(&c.full[warp][stage], phase);
@@ -147,11 +151,10 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
         if (d < x.sees1 && x.e1 < INFINITY) w1 += fast_exp2(sc[3] * f1 - x.e1);
       };
       add(rows[0]);
-      if (blocks > 1) add(rows[1]);
-      for (int b = 2; b < blocks; ++b) {
-        Rows x;
-        load_rows(b, x);
-        add(x);
+#pragma unroll 1
+      for (int b = 1; b < blocks; ++b) {
+        if (blocks > 2) load_rows(b, rows[1]);
+        add(rows[1]);
       }
       __syncwarp();                                                 // the tile has been read
       if (i + kStages < steps.n) request(i + kStages, stage);
@@ -175,6 +178,7 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     }
     at += st1 - st0;
   }
+  if (follows) pdl_wait();                                          // so that what waits for this kernel waits for both
 }
 
 }  // namespace
@@ -182,6 +186,8 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
 int launch_paged8_mass(const Paged8& c, int layer, int group, const void* q, const float* lse, int32_t* dev_status,
                        int num_sms, cudaStream_t st) {
   const Paged& p = c.p;
+  const bool many = p.T > few_tokens(p, group);                        // else no sequence can have more
+  if (many && launch_paged8_mass_tc(c, layer, group, q, lse, dev_status, num_sms, st) < 0) return -1;
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;
   static std::atomic<int> smem_set[64];
@@ -192,10 +198,9 @@ int launch_paged8_mass(const Paged8& c, int layer, int group, const void* q, con
   }
   if (!launch_pdl(paged8_mass_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2), c.mass + (int64_t)layer * (p.layer_rows / 2),
-                  (const __nv_bfloat16*)q, lse, dev_status, group, few_tokens(p, group), kLog2e / sqrtf((float)kHeadDim)))
+                  (const __nv_bfloat16*)q, lse, dev_status, group, few_tokens(p, group), (int)many, kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  if (p.T <= few_tokens(p, group)) return 1;                           // no sequence can have more
-  return launch_paged8_mass_tc(c, layer, group, q, lse, dev_status, num_sms, st) < 0 ? -1 : 2;
+  return many ? 2 : 1;
 }
 
 }  // namespace vr

@@ -75,7 +75,6 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tq = kTile / grp, H = p.G * grp, C = gridDim.x;
-  pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&c.k_full[i], 4); mbar_init(&c.k_empty[i], 1); mbar_init(&c.half_full[i], 4);
@@ -98,7 +97,8 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
-  __threadfence();   // the kernel before this one takes other sequences, and lets this one start when what comes before both has ended
+  pdl_wait();
+  pdl_trigger();                                              // the kernel of few rows goes by it: not before
 
   if (warp == kProducer) {
     // ------------------------------------------------------------------ units, keys and queries
@@ -448,7 +448,6 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   if (warp == kIssuer) tmem_dealloc(tmem, 512);
   if (tid == 0 && c.err) raise_status(dev_status, VARRATE_ERR_TIMEOUT);
-  pdl_wait();                                                 // so that what waits for this kernel waits for both
 }
 
 }  // namespace

@@ -154,7 +154,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     if constexpr (kCoded) return &c.q_raw[i];
     else return &c.q_full[i];
   };
-  pdl_trigger();
+  if constexpr (!kCoded) pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
       if constexpr (kCoded) mbar_init(&c.raw[i], 1);
@@ -176,9 +176,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
-  // Coded: the kernel before this one takes other sequences, and lets this one start when what comes before both has ended.
-  if constexpr (kCoded) __threadfence();
-  else pdl_wait();
+  pdl_wait();
+  if constexpr (kCoded) pdl_trigger();                        // the kernel of few rows goes by it: not before
   // by a call whose merge did not run, or runs still
   const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;
@@ -853,7 +852,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
     raise_status(dev_status, VARRATE_ERR_TIMEOUT);
     atomicExch(&header->gave_up, 1u);
   }
-  if constexpr (kCoded) pdl_wait();                           // so that what waits for this kernel waits for both
 }
 
 }  // namespace

@@ -256,7 +256,7 @@ def test_row_ranges_out_of_order_stay_in_range():
         V.check(V.varrate_paged8_attn(b.pages, b.seqs, 0, b.grp, q, out, lse, b.status, b.workspace()))
         V.check(V.varrate_paged8_mass(b.pages, b.seqs, 0, b.grp, q, lse, b.status))
         torch.cuda.synchronize()
-        assert b.status.item() == (V.ERR_CORRUPT if starts != [2 ** 31 - 1] * 4 else V.ERR_CORRUPT)
+        assert b.status.item() == V.ERR_CORRUPT
 
 
 def test_a_layer_far_into_a_large_pool():
@@ -267,7 +267,6 @@ def test_a_layer_far_into_a_large_pool():
     small.codes.view(torch.uint8).random_(0, 127)
     small.scale.view(torch.uint8).fill_(120)
     small.mass.uniform_()
-    there = torch.arange(pages - 40, pages, dtype=torch.int32, device="cuda")
     for name in ("codes", "scale", "mass"):
         x, y = (getattr(c, name) for c in (big, small))
         x, y = (t.view(torch.uint8) if t.dtype != torch.float32 else t for t in (x, y))
@@ -290,6 +289,5 @@ def test_a_layer_far_into_a_large_pool():
         assert st.item() == 0
         got.append([out, lse, kept, cache.codes.view(torch.uint8)[layer, first:first + 40].clone(),
                     cache.scale.view(torch.uint8)[layer, first:first + 40].clone(), cache.mass[layer, first:first + 40].clone()])
-    assert there.numel() == 40
     for x, y in zip(*got):
         assert torch.equal(x, y)
