@@ -501,7 +501,9 @@ varrate_status varrate_paged8_append(const varrate_pages8* pages, const varrate_
  * result.
  *   q     [T][H][d];  out [T][H][d], not overlapping q
  *   lse   [T][H] fp32, or NULL: log sum_{u <= p} exp(<q, k_u> / sqrt(d)) of every row; -infinity where the scores all are
- *   ws    as for varrate_paged_attn, of varrate_paged8_attn_ws_bytes(pages, seqs, group) bytes. */
+ *   ws    as for varrate_paged_attn, of varrate_paged8_attn_ws_bytes(pages, seqs, group) bytes.
+ * Finite values of any size give finite results, as there; parts of a result whose blocks' scales are 2^85 and more below the largest
+ * one's may be lost. Scores of a row past 2^24 in size are compared to 2^-23 of it. */
 size_t varrate_paged8_attn_ws_bytes(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t group);
 varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
                                    int32_t group, const void* q, void* out, float* lse, int32_t* dev_status,
@@ -510,7 +512,8 @@ varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_se
 /* Attention weights: for every sequence with new tokens, every KV head g and place u,
  *   mass[u] += sum over the new tokens (rows t) that see u, and the query heads h of g, of exp(<q_th, k_u> / sqrt(d) - lse[t][h]),
  * in fp32, in an order that does not change from call to call. lse as varrate_paged8_attn gives it for these queries; a row
- * whose lse is not finite adds nothing. pages->mass must not be NULL. One kernel, no workspace. */
+ * whose lse is not finite adds nothing. A page that two sequences share gets the weights of both, in either order.
+ * pages->mass must not be NULL. No workspace. */
 varrate_status varrate_paged8_mass(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
                                    int32_t group, const void* q, const float* lse, int32_t* dev_status,
                                    void* stream);
@@ -525,7 +528,7 @@ varrate_status varrate_paged8_mass(const varrate_pages8* pages, const varrate_se
  *   new_len   [S] int32: min(kv_len[s], budget); not overlapping kv_len. The caller makes it the sequences' kv_len once every layer
  *             has been cut; the pages past it are free.
  *   gone      [S] int32, or NULL: kv_len[s] - new_len[s] is added (give it to one call where several cut the layers)
- * Uses kv_len and page_table of `seqs`, not row_start (which may be NULL). A sequence with kv_len or a page out of range raises
+ * Uses kv_len and page_table of `seqs`, not row_start (which may be NULL). A sequence with kv_len out of range, or that is to be cut and has a page out of range, raises
  * VARRATE_ERR_CORRUPT: its pages stay as they were, its new_len is 0, its kept are -1 and its gone is left alone. Pages that two
  * sequences share must not belong to one that is cut. pages->mass must not be NULL. One kernel, no workspace. */
 varrate_status varrate_paged8_evict(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,

@@ -393,7 +393,6 @@ static vr::Paged make_paged(const varrate_pages* pages, const varrate_seqs* seqs
   while ((1 << p.page_log2) < pages->page_size) ++p.page_log2;
   p.row_start = seqs->row_start; p.kv_len = seqs->kv_len; p.table = seqs->page_table;
   p.S = seqs->n_seqs; p.max_pages = seqs->max_pages; p.T = seqs->n_rows;
-  p.n_min = 0; p.n_max = INT32_MAX;
   return p;
 }
 

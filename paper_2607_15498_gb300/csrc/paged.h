@@ -18,7 +18,6 @@ struct Paged {
   const int32_t* kv_len;
   const int32_t* table;
   int S, max_pages, T;
-  int n_min, n_max;        // attention: a kernel takes the sequences whose number of new tokens is in this range
 };
 
 // Row of the pool (of d elements, in one layer) that holds token `in_page` of page `page`, head g, K (0) or V (1).

@@ -13,7 +13,14 @@
 //            in units of 2^(u - 127): u rises where b is more than 3 above it. A step more than 10 below goes in bf16, where the weight
 //            has the range of fp32 (and values below 2^-100 or so of the largest block's are lost at the end of that range).
 // The reference of a row moves only when a score is 8 (log2) above it.
-// Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh).
+// Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh). Codes come by TMA into
+// a ring of each warp's own, two steps of keys and values in flight a warp and sixteen warps an SM: 128 KB.
+//
+// Bound by memory for batches: eight sequences of 32768 tokens 90 us with the merge, 538 MB at 5.9 TB/s (0.87 of a copy). By latency for
+// short ones: one sequence of 900 tokens 10.5 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
+// On the way, that batch: three stages of one CTA an SM 95 us, the next step's codes in registers 133, sixteen warps in one CTA 100.
+// Where other sequences of the batch have many new tokens, the kernel on tcgen05 is launched first and this one beside it
+// (`follows`): its CTAs come to the SMs as those end.
 #include <float.h>
 #include <math.h>
 
@@ -47,7 +54,7 @@ struct Shared {
   };
   uint64_t full[kWarps][kStages];
   PlanSums plan;
-  Unit unit;
+  SeqUnit unit;
   int err;
   float m[kWarps][kRows], l[kWarps][kRows];
   int u[kWarps];
@@ -69,7 +76,7 @@ __device__ __forceinline__ bool take_nan(uint4& v, uint32_t& bits) {
 }
 
 __global__ void __launch_bounds__(kThreads, kCtas)
-paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
+paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const unsigned char* __restrict__ scale,
                    const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                    int32_t* __restrict__ dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts,
                    int grp, int follows, float scale_log2) {
@@ -91,9 +98,9 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   pdl_trigger();
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
-  const float weight = plan_weight<kKeys, true>(p, tq, lane, longest);
+  const float weight = plan_weight<kKeys>(p, tq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add<kKeys, true>(p, c.plan, tq, cand, warp, kWarps, lane);
+  plan_add<kKeys>(p, c.plan, tq, cand, warp, kWarps, lane);
   __syncthreads();
   plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
   if (blockIdx.x == 0) {
@@ -106,14 +113,14 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
       if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     }
   }
-  Walk<kKeys, true> w;
+  Walk<kKeys, PagedSome> w;
   if (warp == 0) w.load(p, tq, run, lane);
   int next = blockIdx.x;                                            // of warp 0
   uint32_t stage = 0, phase = 0;                                    // of the warp's next step
   bool ok = true;
   for (;;) {
     if (warp == 0) {
-      Unit x;
+      SeqUnit x;
       int s = 0;
       x.valid = 0;
       while (next < units) {
@@ -128,7 +135,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
       if (lane == 0) { x.seq = s; c.unit = x; }
     }
     __syncthreads();
-    const Unit x = c.unit;
+    const SeqUnit x = c.unit;
     if (!x.valid) break;
     const int rows = x.ntok * grp, end = x.pos0 + x.ntok;
     // this warp's steps
@@ -339,20 +346,17 @@ size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms) {
 
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
                        void* ws, int num_sms, cudaStream_t st) {
-  Paged p = c.p;
+  const Paged& p = c.p;
   unsigned char* w = static_cast<unsigned char*>(ws);
   Header* header = reinterpret_cast<Header*>(w);
   float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group, few = few_tokens(p, group);
-  MergeTwo two = {};
-  two.lse = lse; two.few = few; two.tq = 128 / group; two.bq = 2 * two.tq;
+  Merge8 two = {};
+  two.lse = lse; two.few = few; two.tq2 = 128 / group;
   if (p.T > few) {                                                  // else no sequence can have more
-    Paged8 many = c;
-    many.p.n_min = few + 1;
-    two.second = w + paged_part_bytes(c.p, group, tq, num_sms);
-    if (launch_paged8_attn_tc(many, layer, group, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
+    two.second = w + paged_part_bytes(p, group, tq, num_sms);
+    if (launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
   }
-  p.n_max = few;
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;
   static std::atomic<int> smem_set[64];
@@ -361,12 +365,12 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
     if (cudaFuncSetAttribute(paged8_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess) return -1;
     if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
   }
-  if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
+  if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, PagedSome{p, 0, few},
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
                   (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
                   paged_max_parts(num_sms), group, (int)(two.second != nullptr), kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  return launch_paged_merge_two(c.p, group, out, dev_status, header, part, tq, tq, two, num_sms, st) < 0 ? -1 : 2;
+  return launch_paged8_merge(p, group, out, dev_status, ws, tq, two, num_sms, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr

@@ -2,7 +2,10 @@
 //
 // The products are those of the attention of few rows (paged8_mma.cuh): a warp takes 16 keys and eight rows at a time, every
 // row that sees a key, and adds up in registers, so a token's sum has one order. The steps of 16 keys of all sequences and KV heads
-// are one line that the warps share equally. Bound by memory for single tokens (keys and 8 bytes a token and head).
+// are one line that the warps share equally.
+//
+// Bound by memory: single tokens on eight sequences of 32768, 50 us for 285 MB (keys, scales, and 8 bytes a token and head), 5.7 TB/s
+// (0.84 of a copy). Three steps in flight a warp, sixteen warps an SM (96 KB); 70 us in a form whose registers spilled.
 #include <float.h>
 #include <math.h>
 

@@ -38,7 +38,6 @@
 // turns 448; with the output in a function that is not inlined 406 instead of 366. The bound on
 // the sum of a row's weights costs 1 %. Partials merged by the last CTA of a block instead of a kernel: 89 to 117 us instead of 76 on a mixed
 // step, whose partials are 252 rows, as its loads stand in the way of the next unit; not measured where every block is one token.
-#include <float.h>
 #include <math.h>
 #include <stddef.h>
 
@@ -49,23 +48,18 @@
 #include "common.cuh"
 #include "decode_common.cuh"
 #include "paged.h"
-#include "paged8.h"
-#include "paged8_tc.cuh"
 #include "paged_plan.cuh"
+#include "paged_tc.cuh"
 
 namespace vr {
 
 bool make_tmap_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
-bool make_tmap_rows_u8(CUtensorMap* map, const void* base, uint64_t rows, uint32_t box_rows);
 bool make_tmap_heads_bf16(CUtensorMap* map, const void* base, uint32_t heads, uint64_t rows, uint32_t box_heads, uint32_t box_rows);
 
 namespace {
 
+constexpr int kThreads = 384;
 constexpr int kSoftWarps = 8, kProducer = 8, kIssuer = 9, kValues = 11;   // issuers: 9 and 10
-constexpr int kExpand = 12, kExpandWarps = 4;               // of the coded form
-template <bool kCoded> constexpr int kThreads = 32 * (kExpand + (kCoded ? kExpandWarps : 0));
-// Registers a thread of the coded form, by warpgroup: softmax 0 and 1, the others: 2 * 184 + 2 * 72 = 4 * 128 of the launch.
-constexpr int kSoftRegs = 184, kOtherRegs = 72;
 constexpr int kRows = 128, kKeys = kKeysBf16;
 constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it: geometric mean over
                                                             // 19 cases 42.0 us, at 3 and 4 41.8, at 6 42.1, at 8 42.5
@@ -78,14 +72,7 @@ constexpr int kRing = 5;                                    // key and value til
 // of fp32.
 constexpr float kMost = 0.25f, kRoom = 40.f;
 
-template <bool kCoded> struct CodedCtl {};
-template <> struct CodedCtl<true> {
-  uint64_t raw[kRing], q_raw[2];                            // codes and bf16 queries, as they come
-  __align__(16) float key_scale[4][kKeys / kBlock];         // of the last key tiles' blocks
-};
-template <bool kCoded>
-struct Ctl : CodedCtl<kCoded> {
-  static constexpr int kKinds = kCoded ? 1 : 3;             // of values that are not finite: +inf, -inf, NaN; codes have NaN alone
+struct Ctl {
   uint64_t full[kRing], empty[kRing], look[kRing], looked[kRing];
   uint64_t s_full[2], p_half[2], p_full[2], o_half[2], o_full[2], q_full[2], q_seen[2], turn[2], drain[2];   // by warpgroup
   uint64_t u_full[2], u_empty[2], u_looked[2], o1_full, o1_empty, planned;
@@ -94,79 +81,35 @@ struct Ctl : CodedCtl<kCoded> {
     struct { float m[kRows], l[kRows]; int begun; } o1;                // second warpgroup's rows where both have one query tile
     PlanSums plan;
   };
-  int16_t special[2][kKinds][kHeadDim];                     // first position (from the first looked-at tile) of each
+  int16_t special[2][3][kHeadDim];                          // first position (from the first looked-at tile) of +inf, -inf, NaN
   int any_special[2];
   int err;
   uint32_t tmem;
 };
-template <bool kCoded> constexpr size_t kSmemBytes = 2 * kTileBytes + kRing * kTileBytes + sizeof(Ctl<kCoded>);
-static_assert(kSmemBytes<false> <= 232448 && kSmemBytes<true> <= 232448, "shared memory of a block");
+constexpr size_t kSmemBytes = 2 * kTileBytes + kRing * kTileBytes + sizeof(Ctl);
+static_assert(kSmemBytes <= 232448, "shared memory of a block");
 
-__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kWaitTries; ++i)
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return false;
-}
-
-// Piece j of lane i to piece i of lane j, in groups of four lanes.
-__device__ __forceinline__ void transpose4(uint4 (&y)[4], int lane) {
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const bool up = lane & (1 << b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i & (1 << b)) continue;
-      uint4 &a = y[i], &c = y[i | (1 << b)];
-      uint4 t = up ? a : c;
-      t.x = __shfl_xor_sync(0xffffffffu, t.x, 1 << b);
-      t.y = __shfl_xor_sync(0xffffffffu, t.y, 1 << b);
-      t.z = __shfl_xor_sync(0xffffffffu, t.z, 1 << b);
-      t.w = __shfl_xor_sync(0xffffffffu, t.w, 1 << b);
-      if (up) a = t; else c = t;
-    }
-  }
-}
-__device__ __forceinline__ void add_at(float (&v)[32], int k, float y) {   // v[k] += y without an indexed register array
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = i == k ? v[i] + y : v[i];
-}
-template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
-template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
-
-template <bool kCoded>
-__global__ void __launch_bounds__(kThreads<kCoded>, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, Paged p,
-                     const unsigned char* __restrict__ scale, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
-                     int32_t* __restrict__ dev_status, Header* header,
+                     __nv_bfloat16* __restrict__ out, int32_t* __restrict__ dev_status, Header* header,
                      float* __restrict__ part, int part_rows, int max_parts, int grp, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
-  Ctl<kCoded>& c = *reinterpret_cast<Ctl<kCoded>*>(smem + (2 + kRing) * kTileBytes);
+  Ctl& c = *reinterpret_cast<Ctl*>(smem + (2 + kRing) * kTileBytes);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tq = kRows / grp, bq = 2 * tq, H = p.G * grp, C = gridDim.x;
   const uint32_t q_addr = smem_addr(smem), ring = q_addr + 2 * kTileBytes;
 
-  // the barriers of copies
-  auto tile_bar = [&](uint32_t i) {
-    if constexpr (kCoded) return &c.raw[i];
-    else return &c.full[i];
-  };
-  auto query_bar = [&](int i) {
-    if constexpr (kCoded) return &c.q_raw[i];
-    else return &c.q_full[i];
-  };
-  if constexpr (!kCoded) pdl_trigger();
+  pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
-      if constexpr (kCoded) mbar_init(&c.raw[i], 1);
-      mbar_init(&c.full[i], kCoded ? kExpandWarps : 1); mbar_init(&c.empty[i], 2); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 1);
+      mbar_init(&c.full[i], 1); mbar_init(&c.empty[i], 2); mbar_init(&c.look[i], 1); mbar_init(&c.looked[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], kCoded ? 4 : 1);
-      if constexpr (kCoded) mbar_init(&c.q_raw[i], 1);
+      mbar_init(&c.s_full[i], 1); mbar_init(&c.p_full[i], 4); mbar_init(&c.o_full[i], 1); mbar_init(&c.q_full[i], 1);
       mbar_init(&c.q_seen[i], 1); mbar_init(&c.p_half[i], 4); mbar_init(&c.o_half[i], 1); mbar_init(&c.turn[i], 1);
-      mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3 + (kCoded ? kExpandWarps : 0)); mbar_init(&c.u_looked[i], 1);
+      mbar_init(&c.drain[i], 1); mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSoftWarps + 3); mbar_init(&c.u_looked[i], 1);
     }
-    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads<kCoded> / 32);
+    mbar_init(&c.o1_full, 4); mbar_init(&c.o1_empty, 4); mbar_init(&c.planned, kThreads / 32);
     c.err = 0;
     fence_mbar_init();
   }
@@ -177,364 +120,300 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = c.tmem;
   pdl_wait();
-  if constexpr (kCoded) pdl_trigger();                        // the kernel of few rows goes by it: not before
   // by a call whose merge did not run, or runs still
   const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;
-  const float weight = plan_weight<kKeys, kCoded>(p, bq, lane, longest);
+  const float weight = plan_weight<kKeys>(p, bq, lane, longest);
   const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add<kKeys, kCoded>(p, c.plan, bq, cand, warp, kThreads<kCoded> / 32, lane);
+  plan_add<kKeys>(p, c.plan, bq, cand, warp, kThreads / 32, lane);
   __syncwarp();
   if (lane == 0) mbar_arrive(&c.planned);
 
-  if (warp >= kSoftWarps) {
-    if constexpr (kCoded) fewer_registers<kOtherRegs>();
-    if (warp == kProducer) {
-      // ------------------------------------------------------------------ units, and their keys and values
-      bool ok = wait_all(&c.planned, 0);
-      int run = 1, units = 0, parts = 0;
-      if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
-      if (blockIdx.x == 0 && lane == 0) {
-        if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
-        header->run = run; header->units = units; header->parts = parts; header->open = 1;
-      }
-      Walk<kKeys, kCoded> w;
-      w.load(p, bq, run, lane);
-      const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box
-      const int per_tile = kKeys / page_keys;
-      int u = blockIdx.x;
-      uint32_t n = 0;                                               // ring tiles so far
-      for (uint32_t un = 0; ok; ++un) {
-        Unit x;
-        int s = 0;
+  if (warp == kProducer) {
+    // ------------------------------------------------------------------ units, and their keys and values
+    bool ok = wait_all(&c.planned, 0);
+    int run = 1, units = 0, parts = 0;
+    if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
+    if (blockIdx.x == 0 && lane == 0) {
+      if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      header->run = run; header->units = units; header->parts = parts; header->open = 1;
+    }
+    Walk<kKeys> w;
+    w.load(p, bq, run, lane);
+    const int page_keys = min(1 << p.page_log2, kKeys);           // rows of a box
+    const int per_tile = kKeys / page_keys;
+    int u = blockIdx.x;
+    uint32_t n = 0;                                               // ring tiles so far
+    for (uint32_t un = 0; ok; ++un) {
+      Unit x;
+      int s = 0;
+      x.valid = 0;
+      while (u < units) {
+        s = w.find(p, bq, tq, run, u, lane, x);
+        if (x.t0 < x.t1) break;                                   // else: the block ends before this run
         x.valid = 0;
-        while (u < units) {
-          s = w.find(p, bq, tq, run, u, lane, x);
-          if (x.t0 < x.t1) break;                                   // else: the block ends before this run
-          x.valid = 0;
-          if (lane == 0) u = take_unit(header, C, units);
-          u = __shfl_sync(0xffffffffu, u, 0);
-        }
-        ok = wait_all(&c.u_empty[un & 1], ((un >> 1) & 1) ^ 1);
-        if (!ok) break;
-        if (lane == 0) {
-          x.seq = s;
-          c.unit[un & 1] = x;
-          mbar_arrive(&c.u_full[un & 1]);
-        }
-        if (!x.valid) break;
-        int next = 0;
-        if (lane == 0) next = take_unit(header, C, units);
-        const int32_t* table = p.table + (int64_t)s * p.max_pages;
-        const int end = x.pos0 + x.ntok;
-        const int piece = kCoded ? lane : lane >> 1, half = lane & 1;   // this lane's box of a tile
-        auto page_at = [&](int t) {
-          const int key = t * kKeys + piece * page_keys;
-          return piece < per_tile && key < end ? __ldg(table + (key >> p.page_log2)) : 0;
-        };
-        int page = page_at(x.t0);
-        for (int t = x.t0; t < x.t1 && ok; ++t) {
-          const int key = t * kKeys + piece * page_keys;
-          const bool mine = piece < per_tile && key < end;
-          const int boxes = min(per_tile, (end - t * kKeys + page_keys - 1) / page_keys);
-          int pg = page;
-          if (mine && (pg < 0 || pg >= p.n_pages)) {
-            raise_status(dev_status, VARRATE_ERR_CORRUPT);
-            pg = 0;
-          }
-          const int row = (int)page_row(p, pg, 0, x.g, key & ((1 << p.page_log2) - 1));
-          const int row_v = row + (p.G << p.page_log2);
-          if (t + 1 < x.t1) page = page_at(t + 1);
-  #pragma unroll
-          for (int kv = 0; kv < 2; ++kv, ++n) {
-            const uint32_t slot = n % kRing;
-            ok = ok && wait_all(&c.empty[slot], ((n / kRing) & 1) ^ 1);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(tile_bar(slot), (uint32_t)boxes * page_keys * (kCoded ? 128 : 256));
-            __syncwarp();
-            if (kCoded && mine)                                     // codes come to where the tile's second half will be
-              tma_load_2d(ring + slot * kTileBytes + kKeys * 128 + piece * page_keys * 128, &tmap, 0, kv ? row_v : row, tile_bar(slot));
-            if (!kCoded && mine)
-              tma_load_2d(ring + slot * kTileBytes + half * (kKeys * 128) + piece * page_keys * 128, &tmap, half * 64,
-                          kv ? row_v : row, &c.full[slot]);
-            if (kv && t >= x.values_from && lane == 0) mbar_arrive(&c.look[slot]);
-          }
-        }
-        u = __shfl_sync(0xffffffffu, next, 0);
+        if (lane == 0) u = take_unit(header, C, units);
+        u = __shfl_sync(0xffffffffu, u, 0);
       }
-      if (!ok) {
-        c.err = 1;
-        const uint32_t oldest = n > kRing ? n - kRing : 0;          // no copy is in flight when the block ends
-        for (uint32_t i = oldest; i < n; ++i) wait_all(tile_bar(i % kRing), (i / kRing) & 1);
+      ok = wait_all(&c.u_empty[un & 1], ((un >> 1) & 1) ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        c.unit[un & 1] = x;
+        mbar_arrive(&c.u_full[un & 1]);
       }
-    } else if (warp == kIssuer || warp == kIssuer + 1) {
-      // ------------------------------------------------------------------ products of warpgroup e
-      // The warp stays together and its values are the same in every lane (broadcast from lane 0 where they come from
-      // memory), so that descriptors stay in uniform registers; one elected lane issues. Both issuers pass every tile of
-      // the ring in order, whether they use it or not.
-      const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
-      // codes: queries and keys in fp16
-      constexpr uint32_t idesc_s = kCoded ? idesc_f16_f32(kRows, kKeys) : idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
-      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + 128 * e, to = tm + 256 + 128 * e;
-      struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
-      auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
-      Ring key = {0, 0}, value = {1, 0};
-      uint32_t looked = 0, par_p = 0, turns = e ^ 1;                // parities; the first warpgroup begins
-      bool ok = true;
-      for (uint32_t un = 0; ok; ++un) {
-        ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
-        if (!ok) break;
-        const Unit* x = &c.unit[un & 1];
-        const int valid = __shfl_sync(0xffffffffu, x->valid, 0), t0 = __shfl_sync(0xffffffffu, x->t0, 0);
-        const int nt = __shfl_sync(0xffffffffu, x->t1, 0) - t0, n_first = __shfl_sync(0xffffffffu, x->e0, 0) - t0;
-        const int both = __shfl_sync(0xffffffffu, x->both, 0), from = __shfl_sync(0xffffffffu, x->values_from, 0) - t0;
-        if (!valid) break;
-        if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
-        ok = wait_all(&c.q_full[e], un & 1);
-        if (!ok) break;
-        if (lane == 0) mbar_arrive(&c.q_seen[e]);
-        auto mine = [&](int i) { return both ? (i & 1) == e : e || i < n_first; };
-        auto scores = [&]() {                                       // issued by the elected lane
-          const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
-  #pragma unroll
-          for (int ks = 0; ks < kHeadDim / 16; ++ks) {
-            const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
-            tc_mma_bf16(ts, a + o, b + o, idesc_s, ks != 0);
-          }
-          tc_commit(&c.s_full[e]);
-          tc_commit(&c.empty[key.slot]);
-        };
-        auto pass = [&](Ring& x) {                                  // a tile that the other issuer uses alone
-          if (!wait_all(&c.full[x.slot], x.phase)) return false;
-          if (elect_one()) mbar_arrive(&c.empty[x.slot]);
-          __syncwarp();
-          further(x);
-          return true;
-        };
-        auto next_scores = [&]() {                                  // by themselves, once the keys are there
-          if (!wait_all(&c.full[key.slot], key.phase)) return false;
-          tc_fence_after();
-          if (elect_one()) scores();
-          __syncwarp();
-          further(key);
-          return true;
-        };
-        // The keys of the first own tile; then per own tile its values, and the keys of the next one. Where both warpgroups
-        // use a tile the products are queued behind one another, as a wait between them would hold them up; a decode step
-        // waits for memory, and gives values back before it waits for keys.
-        const int step = both ? 2 : 1;
-        int ahead = 0;                                              // tiles whose keys are done
-        for (; ok && ahead < nt && ahead < step && !mine(ahead); ++ahead) ok = pass(key);
-        if (ok && ahead < nt && ahead < step) { ok = next_scores(); ++ahead; }
-        uint32_t accumulate = 0;                                    // the accumulator holds products of this unit
-        for (int i = 0; i < nt && ok; ++i) {
-          const uint32_t slot = value.slot;
-          if (!mine(i)) {
-            if (!both && ahead == i) { ok = pass(key); ++ahead; }
-            ok = ok && pass(value);
-          } else {
-            const bool queued = !both && ahead < nt && mine(ahead);
-            ok = wait_all(&c.full[slot], value.phase);
-            if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
-            if (ok && queued) ok = wait_all(&c.full[key.slot], key.phase);
-            ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_half[e], par_p);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
-            if (elect_one()) {
-  #pragma unroll
-              for (int ks = 0; ks < kKeys / 32; ++ks)
-                tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
-              tc_commit(&c.o_half[e]);
-            }
-            __syncwarp();
-            ok = wait_all(&c.p_full[e], par_p);
-            if (!ok) break;
-            par_p ^= 1;
-            tc_fence_after();
-            if (elect_one()) {
-  #pragma unroll
-              for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
-                tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
-              tc_commit(&c.o_full[e]);
-              tc_commit(&c.empty[slot]);
-              if (queued) scores();
-              mbar_arrive(&c.turn[e ^ 1]);
-            }
-            __syncwarp();
-            accumulate = 1;
-            ++turns;
-            further(value);
-            if (queued) { further(key); ++ahead; }
-            if (both) {
-              for (; ok && ahead < nt && ahead < i + step; ++ahead) ok = pass(key);
-              if (ok && ahead < nt) { ok = next_scores(); ++ahead; }
-            }
-          }
-          if (i >= from) looked ^= 1u << slot;
+      if (!x.valid) break;
+      int next = 0;
+      if (lane == 0) next = take_unit(header, C, units);
+      const int32_t* table = p.table + (int64_t)s * p.max_pages;
+      const int end = x.pos0 + x.ntok;
+      const int piece = lane >> 1, half = lane & 1;               // this lane's box of a tile
+      auto page_at = [&](int t) {
+        const int key = t * kKeys + piece * page_keys;
+        return piece < per_tile && key < end ? __ldg(table + (key >> p.page_log2)) : 0;
+      };
+      int page = page_at(x.t0);
+      for (int t = x.t0; t < x.t1 && ok; ++t) {
+        const int key = t * kKeys + piece * page_keys;
+        const bool mine = piece < per_tile && key < end;
+        const int boxes = min(per_tile, (end - t * kKeys + page_keys - 1) / page_keys);
+        int pg = page;
+        if (mine && (pg < 0 || pg >= p.n_pages)) {
+          raise_status(dev_status, VARRATE_ERR_CORRUPT);
+          pg = 0;
         }
-        // both issuers take as many turns in a unit
-        const int all = both ? (nt + 1) / 2 : nt, own = both ? (nt + 1 - e) / 2 : e ? nt : min(n_first, nt);
-        for (int i = own; i < all && ok; ++i, ++turns) {
-          ok = wait_all(&c.turn[e], turns & 1);
-          if (ok && elect_one()) mbar_arrive(&c.turn[e ^ 1]);
-          __syncwarp();
-        }
-      }
-      if (!ok) {                                                    // the products in flight end before TMEM is freed
-        c.err = 1;
-        if (elect_one()) tc_commit(&c.drain[e]);
-        wait_all(&c.drain[e], 0);
-      }
-      __syncwarp();
-    } else if (warp == kValues) {
-      // ------------------------------------------------------------------ values that no row, or not every row, sees
-      if (blockIdx.x == 0) {
-        for (int s = lane; s < p.S; s += 32) {
-          SeqRange r;
-          if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
-        }
-      }
-      // a lane looks at eight columns (chunk) of every second key
-      const int panel = (lane >> 3) & 1, chunk = lane & 7, odd_key = lane >> 4;
-      uint32_t n0 = 0, par = 0;
-      bool ok = true;
-      for (uint32_t un = 0; ok; ++un) {
-        ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
-        if (!ok) break;
-        const Unit x = c.unit[un & 1];
-        __syncwarp();
-        if (!x.valid) break;
-        constexpr int kKinds = Ctl<kCoded>::kKinds;
-        int16_t first[8][kKinds];
-        bool any = false;
-        const int end = x.pos0 + x.ntok;
-        for (int t = x.values_from; t < x.t1; ++t) {
-          const uint32_t n = n0 + 2 * (t - x.t0) + 1, slot = n % kRing;
-          ok = wait_all(&c.look[slot], (par >> slot) & 1) && wait_all(&c.full[slot], (n / kRing) & 1);
+        const int row = (int)page_row(p, pg, 0, x.g, key & ((1 << p.page_log2) - 1));
+        const int row_v = row + (p.G << p.page_log2);
+        if (t + 1 < x.t1) page = page_at(t + 1);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          const uint32_t slot = n % kRing;
+          ok = ok && wait_all(&c.empty[slot], ((n / kRing) & 1) ^ 1);
           if (!ok) break;
-          par ^= 1u << slot;
-          const int lo = min(kKeys, max(0, x.pos0 + 1 - t * kKeys)), hi = min(kKeys, end - t * kKeys);
-          unsigned char* v = smem + (2 + slot) * kTileBytes + panel * (kKeys * 128);
-          auto at = [&](int key) { return reinterpret_cast<uint4*>(v + key * 128 + ((chunk ^ (key & 7)) << 4)); };
-          // an exponent of all ones: infinity or NaN
-          auto odd = [](uint32_t a) { return __vcmpeq2(a & 0x7f807f80u, 0x7f807f80u); };
-          uint32_t found = 0;
-  #pragma unroll 4
+          if (lane == 0) mbar_arrive_expect_tx(&c.full[slot], (uint32_t)boxes * page_keys * 256);
+          __syncwarp();
+          if (mine)
+            tma_load_2d(ring + slot * kTileBytes + half * (kKeys * 128) + piece * page_keys * 128, &tmap, half * 64,
+                        kv ? row_v : row, &c.full[slot]);
+          if (kv && t >= x.values_from && lane == 0) mbar_arrive(&c.look[slot]);
+        }
+      }
+      u = __shfl_sync(0xffffffffu, next, 0);
+    }
+    if (!ok) {
+      c.err = 1;
+      const uint32_t oldest = n > kRing ? n - kRing : 0;          // no copy is in flight when the block ends
+      for (uint32_t i = oldest; i < n; ++i) wait_all(&c.full[i % kRing], (i / kRing) & 1);
+    }
+  } else if (warp == kIssuer || warp == kIssuer + 1) {
+    // ------------------------------------------------------------------ products of warpgroup e
+    // The warp stays together and its values are the same in every lane (broadcast from lane 0 where they come from
+    // memory), so that descriptors stay in uniform registers; one elected lane issues. Both issuers pass every tile of
+    // the ring in order, whether they use it or not.
+    const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
+    constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys), idesc_o = idesc_bf16_f32(kRows, kHeadDim) | kBMn;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + 128 * e, to = tm + 256 + 128 * e;
+    struct Ring { uint32_t slot, phase; };                        // a tile's place; two tiles further
+    auto further = [](Ring& x) { x.slot += 2; if (x.slot >= kRing) { x.slot -= kRing; x.phase ^= 1; } };
+    Ring key = {0, 0}, value = {1, 0};
+    uint32_t looked = 0, par_p = 0, turns = e ^ 1;                // parities; the first warpgroup begins
+    bool ok = true;
+    for (uint32_t un = 0; ok; ++un) {
+      ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
+      if (!ok) break;
+      const Unit* x = &c.unit[un & 1];
+      const int valid = __shfl_sync(0xffffffffu, x->valid, 0), t0 = __shfl_sync(0xffffffffu, x->t0, 0);
+      const int nt = __shfl_sync(0xffffffffu, x->t1, 0) - t0, n_first = __shfl_sync(0xffffffffu, x->e0, 0) - t0;
+      const int both = __shfl_sync(0xffffffffu, x->both, 0), from = __shfl_sync(0xffffffffu, x->values_from, 0) - t0;
+      if (!valid) break;
+      if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
+      ok = wait_all(&c.q_full[e], un & 1);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive(&c.q_seen[e]);
+      auto mine = [&](int i) { return both ? (i & 1) == e : e || i < n_first; };
+      auto scores = [&]() {                                       // issued by the elected lane
+        const uint64_t a = sdesc_sw128(q_addr + e * kTileBytes), b = sdesc_sw128(ring + key.slot * kTileBytes);
+#pragma unroll
+        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+          const uint64_t o = (uint64_t)((ks >> 2) * (kRows * 128) + (ks & 3) * 32) / 16;
+          tc_mma_bf16(ts, a + o, b + o, idesc_s, ks != 0);
+        }
+        tc_commit(&c.s_full[e]);
+        tc_commit(&c.empty[key.slot]);
+      };
+      auto pass = [&](Ring& x) {                                  // a tile that the other issuer uses alone
+        if (!wait_all(&c.full[x.slot], x.phase)) return false;
+        if (elect_one()) mbar_arrive(&c.empty[x.slot]);
+        __syncwarp();
+        further(x);
+        return true;
+      };
+      auto next_scores = [&]() {                                  // by themselves, once the keys are there
+        if (!wait_all(&c.full[key.slot], key.phase)) return false;
+        tc_fence_after();
+        if (elect_one()) scores();
+        __syncwarp();
+        further(key);
+        return true;
+      };
+      // The keys of the first own tile; then per own tile its values, and the keys of the next one. Where both warpgroups
+      // use a tile the products are queued behind one another, as a wait between them would hold them up; a decode step
+      // waits for memory, and gives values back before it waits for keys.
+      const int step = both ? 2 : 1;
+      int ahead = 0;                                              // tiles whose keys are done
+      for (; ok && ahead < nt && ahead < step && !mine(ahead); ++ahead) ok = pass(key);
+      if (ok && ahead < nt && ahead < step) { ok = next_scores(); ++ahead; }
+      uint32_t accumulate = 0;                                    // the accumulator holds products of this unit
+      for (int i = 0; i < nt && ok; ++i) {
+        const uint32_t slot = value.slot;
+        if (!mine(i)) {
+          if (!both && ahead == i) { ok = pass(key); ++ahead; }
+          ok = ok && pass(value);
+        } else {
+          const bool queued = !both && ahead < nt && mine(ahead);
+          ok = wait_all(&c.full[slot], value.phase);
+          if (ok && i >= from) ok = wait_all(&c.looked[slot], (looked >> slot) & 1);
+          if (ok && queued) ok = wait_all(&c.full[key.slot], key.phase);
+          ok = ok && wait_all(&c.turn[e], turns & 1) && wait_all(&c.p_half[e], par_p);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t b = sdesc_sw128_mn(ring + slot * kTileBytes, kKeys * 128);
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = 0; ks < kKeys / 32; ++ks)
+              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, ks ? 1 : accumulate);
+            tc_commit(&c.o_half[e]);
+          }
+          __syncwarp();
+          ok = wait_all(&c.p_full[e], par_p);
+          if (!ok) break;
+          par_p ^= 1;
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int ks = kKeys / 32; ks < kKeys / 16; ++ks)
+              tc_mma_bf16_ts(to, ts + 8 * ks, b + ks * (2048 / 16), idesc_o, 1);
+            tc_commit(&c.o_full[e]);
+            tc_commit(&c.empty[slot]);
+            if (queued) scores();
+            mbar_arrive(&c.turn[e ^ 1]);
+          }
+          __syncwarp();
+          accumulate = 1;
+          ++turns;
+          further(value);
+          if (queued) { further(key); ++ahead; }
+          if (both) {
+            for (; ok && ahead < nt && ahead < i + step; ++ahead) ok = pass(key);
+            if (ok && ahead < nt) { ok = next_scores(); ++ahead; }
+          }
+        }
+        if (i >= from) looked ^= 1u << slot;
+      }
+      // both issuers take as many turns in a unit
+      const int all = both ? (nt + 1) / 2 : nt, own = both ? (nt + 1 - e) / 2 : e ? nt : min(n_first, nt);
+      for (int i = own; i < all && ok; ++i, ++turns) {
+        ok = wait_all(&c.turn[e], turns & 1);
+        if (ok && elect_one()) mbar_arrive(&c.turn[e ^ 1]);
+        __syncwarp();
+      }
+    }
+    if (!ok) {                                                    // the products in flight end before TMEM is freed
+      c.err = 1;
+      if (elect_one()) tc_commit(&c.drain[e]);
+      wait_all(&c.drain[e], 0);
+    }
+    __syncwarp();
+  } else if (warp == kValues) {
+    // ------------------------------------------------------------------ values that no row, or not every row, sees
+    if (blockIdx.x == 0) {
+      for (int s = lane; s < p.S; s += 32) {
+        SeqRange r;
+        if (!seq_range(p, s, r)) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      }
+    }
+    // a lane looks at eight columns (chunk) of every second key
+    const int panel = (lane >> 3) & 1, chunk = lane & 7, odd_key = lane >> 4;
+    uint32_t n0 = 0, par = 0;
+    bool ok = true;
+    for (uint32_t un = 0; ok; ++un) {
+      ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
+      if (!ok) break;
+      const Unit x = c.unit[un & 1];
+      __syncwarp();
+      if (!x.valid) break;
+      int16_t first[8][3];
+      bool any = false;
+      const int end = x.pos0 + x.ntok;
+      for (int t = x.values_from; t < x.t1; ++t) {
+        const uint32_t n = n0 + 2 * (t - x.t0) + 1, slot = n % kRing;
+        ok = wait_all(&c.look[slot], (par >> slot) & 1) && wait_all(&c.full[slot], (n / kRing) & 1);
+        if (!ok) break;
+        par ^= 1u << slot;
+        const int lo = min(kKeys, max(0, x.pos0 + 1 - t * kKeys)), hi = min(kKeys, end - t * kKeys);
+        unsigned char* v = smem + (2 + slot) * kTileBytes + panel * (kKeys * 128);
+        auto at = [&](int key) { return reinterpret_cast<uint4*>(v + key * 128 + ((chunk ^ (key & 7)) << 4)); };
+        // an exponent of all ones: infinity or NaN
+        auto odd = [](uint32_t a) { return __vcmpeq2(a & 0x7f807f80u, 0x7f807f80u); };
+        uint32_t found = 0;
+#pragma unroll 4
+        for (int key = lo + odd_key; key < hi; key += 2) {
+          const uint4 w = *at(key);
+          found |= odd(w.x) | odd(w.y) | odd(w.z) | odd(w.w);
+        }
+        if (__any_sync(0xffffffffu, found != 0)) {                // rare: element by element
+          if (!any) {
+#pragma unroll
+            for (int i = 0; i < 24; ++i) first[i / 3][i % 3] = kNone;
+          }
+          any = true;
+#pragma unroll 1
           for (int key = lo + odd_key; key < hi; key += 2) {
             const uint4 w = *at(key);
-            found |= odd(w.x) | odd(w.y) | odd(w.z) | odd(w.w);
-          }
-          if (__any_sync(0xffffffffu, found != 0)) {                // rare: element by element
-            if (!any) {
-  #pragma unroll
-              for (int i = 0; i < 8 * kKinds; ++i) first[i / kKinds][i % kKinds] = kNone;
+            uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t h = (a[j >> 1] >> (16 * (j & 1))) & 0xffffu;
+              if ((h & 0x7f80u) != 0x7f80u) continue;
+              a[j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+              const int16_t pos = (int16_t)(t * kKeys + key - x.values_from * kKeys);
+              if (h & 0x7f) first[j][2] = min(first[j][2], pos);
+              else if (h >> 15) first[j][1] = min(first[j][1], pos);
+              else first[j][0] = min(first[j][0], pos);
             }
-            any = true;
-  #pragma unroll 1
-            for (int key = lo + odd_key; key < hi; key += 2) {
-              const uint4 w = *at(key);
-              uint32_t a[4] = {w.x, w.y, w.z, w.w};
-  #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const uint32_t h = (a[j >> 1] >> (16 * (j & 1))) & 0xffffu;
-                if ((h & 0x7f80u) != 0x7f80u) continue;
-                a[j >> 1] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
-                const int16_t pos = (int16_t)(t * kKeys + key - x.values_from * kKeys);
-                if (kKinds == 1 || h & 0x7f) first[j][kKinds - 1] = min(first[j][kKinds - 1], pos);
-                else if (h >> 15) first[j][1 % kKinds] = min(first[j][1 % kKinds], pos);
-                else first[j][0] = min(first[j][0], pos);
-              }
-              *at(key) = make_uint4(a[0], a[1], a[2], a[3]);
-            }
-            __syncwarp();
+            *at(key) = make_uint4(a[0], a[1], a[2], a[3]);
           }
-  #pragma unroll 4
-          for (int key = hi + odd_key; key < kKeys; key += 2) *at(key) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&c.looked[slot]);
         }
-        if (!ok) break;
-        if (any) {                                                  // (the same in all lanes)
-  #pragma unroll
-          for (int i = 0; i < 8 * kKinds; ++i) {
-            const int other = __shfl_xor_sync(0xffffffffu, (int)first[i / kKinds][i % kKinds], 16);
-            if (!odd_key) c.special[un & 1][i % kKinds][64 * panel + 8 * chunk + i / kKinds] = min(first[i / kKinds][i % kKinds], (int16_t)other);
-          }
-        }
-        if (lane == 0) c.any_special[un & 1] = any;
+#pragma unroll 4
+        for (int key = hi + odd_key; key < kKeys; key += 2) *at(key) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&c.u_looked[un & 1]);
-          mbar_arrive(&c.u_empty[un & 1]);
-        }
-        n0 += 2 * (uint32_t)(x.t1 - x.t0);
+        if (lane == 0) mbar_arrive(&c.looked[slot]);
       }
-      if (!ok) c.err = 1;
-    } else if constexpr (kCoded) {
-      // ------------------------------------------------------------------ codes to bf16: one key per thread
-      const int key_in = tid - 32 * kExpand;
-      uint32_t n = 0, n_k = 0;
-      bool ok = true;
-      for (uint32_t un = 0; ok; ++un) {
-        ok = wait_all(&c.u_full[un & 1], (un >> 1) & 1);
-        if (!ok) break;
-        const Unit& x = c.unit[un & 1];
-        const int valid = x.valid, t0 = x.t0, t1 = x.t1, end = x.pos0 + x.ntok, g = x.g;
-        const int32_t* table = p.table + (int64_t)x.seq * p.max_pages;
-        __syncwarp();
-        if (!valid) break;
-        if (lane == 0) mbar_arrive(&c.u_empty[un & 1]);
-        auto page_at = [&](int t) {
-          const int key = t * kKeys + key_in;
-          return t < t1 && key < end ? __ldg(table + (key >> p.page_log2)) : -1;
-        };
-        auto scales_at = [&](int t, int page, uint32_t& k, uint32_t& v) {   // (a page out of range: the producer raises the status)
-          k = v = 0;
-          if (page < 0 || page >= p.n_pages) return;
-          const int64_t row = page_row(p, page, 0, g, (t * kKeys + key_in) & ((1 << p.page_log2) - 1));
-          k = __ldg(scale + scale_at(row));
-          v = __ldg(scale + scale_at(row + ((int64_t)p.G << p.page_log2)));
-        };
-        uint32_t sk, sv, sk1 = 0, sv1 = 0;
-        scales_at(t0, page_at(t0), sk, sv);
-        int page1 = page_at(t0 + 1);
-        for (int t = t0; t < t1 && ok; ++t) {
-          scales_at(t + 1, page1, sk1, sv1);
-          page1 = page_at(t + 2);
-          const bool there = t * kKeys + key_in < end;
-  #pragma unroll
-          for (int kv = 0; kv < 2; ++kv, ++n) {
-            const uint32_t slot = n % kRing;
-            ok = ok && wait_all(&c.raw[slot], (n / kRing) & 1);
-            if (!ok) break;
-              if (kv) {
-              expand_row<true>(smem + (2 + slot) * kTileBytes, kKeys, key_in, there, sv);
-            } else {
-              expand_row<false>(smem + (2 + slot) * kTileBytes, kKeys, key_in, there, 0);
-              if ((key_in & (kBlock - 1)) == 0) c.key_scale[n_k & 3][key_in >> kBlockLog2] = __uint_as_float(sk << 23);
-              ++n_k;
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&c.full[slot]);
-          }
-          sk = sk1;
-          sv = sv1;
+      if (!ok) break;
+      if (any) {                                                  // (the same in all lanes)
+#pragma unroll
+        for (int i = 0; i < 24; ++i) {
+          const int other = __shfl_xor_sync(0xffffffffu, (int)first[i / 3][i % 3], 16);
+          if (!odd_key) c.special[un & 1][i % 3][64 * panel + 8 * chunk + i / 3] = min(first[i / 3][i % 3], (int16_t)other);
         }
       }
-      if (!ok) c.err = 1;
+      if (lane == 0) c.any_special[un & 1] = any;
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&c.u_looked[un & 1]);
+        mbar_arrive(&c.u_empty[un & 1]);
+      }
+      n0 += 2 * (uint32_t)(x.t1 - x.t0);
     }
+    if (!ok) c.err = 1;
   } else {
     // ------------------------------------------------------------------ softmax: one row per thread
-    if constexpr (kCoded) more_registers<kSoftRegs>();
     const int e = warp >> 2, r = tid & 127, wrow = (warp & 3) * 32;
     const int tok_of = r / grp;                                   // of the query tile, and the row's place from its first one
     const int row_off = (tok_of * H + r % grp) * kHeadDim;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + 128 * e + lanes, to = tmem + 256 + 128 * e + lanes;
-    [[maybe_unused]] uint32_t n_k = 0;                            // key tiles of the units before
     uint32_t n_s = 0, n_o = 0, n_both = 0, n_q = 0;               // score tiles, value products, merged units, query tiles so far
     bool ok = true;
     float ref = -INFINITY, l = 0.f;                               // reference, sum
@@ -555,11 +434,11 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       }
       if (valid && wrow == 0 && lane == 0) {
         const Unit& x = c.unit[nu & 1];
-        mbar_arrive_expect_tx(query_bar(e), (uint32_t)(tq * grp) * 256);
+        mbar_arrive_expect_tx(&c.q_full[e], (uint32_t)(tq * grp) * 256);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
           tma_load_3d(q_addr + e * kTileBytes + half * (kRows * 128), &tmap_q, half * 64, x.g * grp,
-                      x.row0 + (x.both ? 0 : e * tq), query_bar(e));
+                      x.row0 + (x.both ? 0 : e * tq), &c.q_full[e]);
       }
       __syncwarp();
       if (nu > 0) {
@@ -623,9 +502,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
               for (int k = 0; k < 32; ++k) {
                 const int col = cb + k;
                 float y = 0.f;
-                if (!kCoded && c.special[un & 1][0][col] < at) y += INFINITY;
-                if (!kCoded && c.special[un & 1][1 % Ctl<kCoded>::kKinds][col] < at) y -= INFINITY;
-                if (c.special[un & 1][Ctl<kCoded>::kKinds - 1][col] < at) y = NAN;
+                if (c.special[un & 1][0][col] < at) y += INFINITY;
+                if (c.special[un & 1][1][col] < at) y -= INFINITY;
+                if (c.special[un & 1][2][col] < at) y = NAN;
                 add_at(v, k, y);
               }
             }
@@ -659,10 +538,6 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
               }
             }
           }
-          if constexpr (kCoded) {
-            if (mine && whole && lse)
-              lse[(int64_t)(x.row0 + tok0 + tok_of) * H + x.g * grp + r % grp] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718f;
-          }
           if (mine && !whole && begun) {
             float* ml = part + (int64_t)max_parts * part_rows * kHeadDim;
             *reinterpret_cast<float2*>(ml + ((int64_t)x.slot * part_rows + tok0 * grp + r) * 2) = make_float2(ref, l);
@@ -683,20 +558,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
       const int sees = x.pos0 + tok0 + tok_of + 1;                // keys that this row sees
       const int first_sees = __shfl_sync(0xffffffffu, sees, 0);   // the least of the warp
       const int step = both ? 2 : 1, last = both || e ? x.t1 : x.e0;
-      [[maybe_unused]] const int t_first = x.t0, tiles = x.t1 - x.t0;
       ref = -INFINITY;
       l = 0.f;
       unset = true;
       begun = false;
-      [[maybe_unused]] float row_scale = scale_log2;
-      if constexpr (kCoded) {                                     // the queries in fp16, and what that takes off their size
-        ok = wait_all(&c.q_raw[e], (n_q - 1) & 1);
-        if (!ok) break;
-        row_scale *= row_to_f16(smem + e * kTileBytes, kRows, r);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&c.q_full[e]);
-      }
       for (int t = x.t0 + (both ? e : 0); t < last; t += step) {
         ok = wait_all(&c.s_full[e], n_s & 1);
         if (!ok) break;
@@ -715,24 +580,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
           // number below kMost with them: the maximum of the scores first, then the weights again.
           float x[32];
           uint32_t pk[32];
-          // coded: what a score of a block of keys is multiplied by (neither an infinity, for scores of 0, nor 0, for hidden ones)
-          [[maybe_unused]] auto block_scale = [&](int b) {
-            if constexpr (kCoded) return fminf(fmaxf(row_scale * c.key_scale[(n_k + (t - t_first)) & 3][b], FLT_MIN), FLT_MAX);
-            else return scale_log2;
-          };
-          [[maybe_unused]] auto block_scales = [&](int b, float (&y)[4]) {
-            if constexpr (kCoded) {
-              const float4 k = *reinterpret_cast<const float4*>(&c.key_scale[(n_k + (t - t_first)) & 3][b]);
-              const float z[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) y[i] = fminf(fmaxf(row_scale * z[i], FLT_MIN), FLT_MAX);
-            }
-          };
           auto weights = [&](int cb0) {
             const float off1 = ref == -INFINITY ? 0.f : -ref;
-            const float2 off = make_float2(off1, off1);
-            float sc1[4] = {scale_log2, scale_log2, scale_log2, scale_log2};   // by 16 keys
-            if constexpr (kCoded) block_scales(cb0 / kBlock, sc1);
+            const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(off1, off1);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             float s[64];
             tmem_ld64(ts + cb0, s);
@@ -742,7 +592,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             }
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
-              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), make_float2(sc1[k / 8], sc1[k / 8]), off);
+              const float2 a = fma2(make_float2(s[2 * k], s[2 * k + 1]), sc, off);
               s[2 * k] = fast_exp2(a.x);
               s[2 * k + 1] = fast_exp2(a.y);
             }
@@ -762,32 +612,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
             for (bool first = true; cb < kKeys && (first || !some || __any_sync(0xffffffffu, mine && mx == -INFINITY)); cb += 32, first = false) {
               tmem_ld32(ts + cb, x);
               hide(cb, x);
-              if constexpr (kCoded) {
-                const float b0 = block_scale(cb / kBlock), b1 = block_scale(cb / kBlock + 1);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) x[k] *= k < 16 ? b0 : b1;
-              }
               float top[4] = {mx, x[0], x[1], x[2]};
 #pragma unroll
               for (int k = 3; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], x[k]);
               mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             }
-            if constexpr (!kCoded) mx *= scale_log2;
+            mx *= scale_log2;
             const float up = (l < 0.5f * kMost ? mx : fmaxf(mx, ref)) + kRoom;   // a sum that has grown makes room too
             float f = 1.f;
-            if (mine && up > ref) {
-              f = ref == -INFINITY ? 0.f : fast_exp2(ref - up);
-              ref = up;
-              if constexpr (kCoded) {
-                // So large that a rounding of the reference is not small beside kRoom: the row's scores are taken at 2^24 from here on.
-                // They are not known to a unit, the largest decides alone, and does so as well where they are smaller.
-                if (fabsf(ref) > 0x1p24f && fabsf(ref) < INFINITY) {
-                  const float down = __uint_as_float((uint32_t)(127 + 127 + 23 - (int)(__float_as_uint(fabsf(ref)) >> 23)) << 23);
-                  row_scale *= down;
-                  ref = fmaf(ref, down, kRoom);
-                }
-              }
-            }
+            if (mine && up > ref) { f = ref == -INFINITY ? 0.f : fast_exp2(ref - up); ref = up; }
             return f;
           };
           auto rescale = [&](float f) {                           // the accumulator, whose products have ended
@@ -839,11 +672,10 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_cons
         unset = __any_sync(0xffffffffu, mine && ref == -INFINITY);
       }
       if (!ok) break;
-      n_k += tiles;
     }
     if (!ok) {
       c.err = 1;
-      if (n_q > 0) wait_all(query_bar(e), (n_q - 1) & 1);   // no copy is in flight when the block ends
+      if (n_q > 0) wait_all(&c.q_full[e], (n_q - 1) & 1);         // no copy is in flight when the block ends
     }
   }
   __syncthreads();
@@ -860,47 +692,29 @@ size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms) {
   return paged_part_bytes(p, group, 2 * (kRows / group), num_sms);
 }
 
-namespace {
-
-// One of the two forms; scale and lse are null without codes.
-template <bool kCoded>
-int launch_tc(const Paged& p, int layer, int group, const void* q, const unsigned char* scale, void* out, float* lse,
-              int32_t* dev_status, void* ws, int num_sms, cudaStream_t st) {
+int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
+                         int num_sms, cudaStream_t st) {
   static std::atomic<int> smem_set[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || smem_set[dev].load(std::memory_order_acquire) == 0) {
-    if (cudaFuncSetAttribute(paged_attn_tc_kernel<kCoded>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes<kCoded>) != cudaSuccess)
+    if (cudaFuncSetAttribute(paged_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes) != cudaSuccess)
       return -1;
     if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
   }
   CUtensorMap tmap, tmap_q;
-  const int ps = 1 << p.page_log2, box = ps < kKeys ? ps : kKeys;
-  const unsigned char* pool = p.pool + (int64_t)layer * p.layer_rows * kHeadDim * (kCoded ? 1 : 2);
-  if (!(kCoded ? make_tmap_rows_u8(&tmap, pool, (uint64_t)p.layer_rows, box) : make_tmap_rows_bf16(&tmap, pool, (uint64_t)p.layer_rows, box)))
+  const int ps = 1 << p.page_log2;
+  if (!make_tmap_rows_bf16(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim * 2, (uint64_t)p.layer_rows, ps < kKeys ? ps : kKeys))
     return -1;
   if (!make_tmap_heads_bf16(&tmap_q, q, (uint32_t)(p.G * group), (uint64_t)p.T, (uint32_t)group, (uint32_t)(kRows / group))) return -1;
   unsigned char* w = static_cast<unsigned char*>(ws);
-  return launch_pdl(paged_attn_tc_kernel<kCoded>, dim3(num_sms), kThreads<kCoded>, kSmemBytes<kCoded>, st, tmap, tmap_q, p, scale,
-                    (__nv_bfloat16*)out, lse, dev_status, reinterpret_cast<Header*>(w), reinterpret_cast<float*>(w + kHeaderBytes),
-                    paged_part_rows(p, group, 2 * (kRows / group)), paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim))
-             ? 1 : -1;
-}
-
-}  // namespace
-
-int launch_paged_attn_tc(const Paged& p, int layer, int group, const void* q, void* out, int32_t* dev_status, void* ws,
-                         int num_sms, cudaStream_t st) {
-  if (launch_tc<false>(p, layer, group, q, nullptr, out, nullptr, dev_status, ws, num_sms, st) < 0) return -1;
-  unsigned char* w = static_cast<unsigned char*>(ws);
+  Header* header = reinterpret_cast<Header*>(w);
+  float* part = reinterpret_cast<float*>(w + kHeaderBytes);
   const int tq = kRows / group;
-  return launch_paged_merge(p, group, out, dev_status, reinterpret_cast<Header*>(w), reinterpret_cast<float*>(w + kHeaderBytes), tq,
-                            2 * tq, num_sms, st) < 0 ? -1 : 2;
-}
-
-int launch_paged8_attn_tc(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
-                          void* ws, int num_sms, cudaStream_t st) {
-  return launch_tc<true>(c.p, layer, group, q, c.scale + (int64_t)layer * (c.p.layer_rows >> kBlockLog2), out, lse, dev_status, ws,
-                         num_sms, st);
+  if (!launch_pdl(paged_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p, (__nv_bfloat16*)out, dev_status,
+                  header, part, paged_part_rows(p, group, 2 * tq), paged_max_parts(num_sms), group,
+                  kLog2e / sqrtf((float)kHeadDim)))
+    return -1;
+  return launch_paged_merge(p, group, out, dev_status, header, part, tq, 2 * tq, num_sms, st) < 0 ? -1 : 2;
 }
 
 }  // namespace vr

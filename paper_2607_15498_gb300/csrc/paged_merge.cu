@@ -15,46 +15,29 @@ __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<f
 // A warp per (row, query head); a lane has four columns. A run of a block counts for a row only where the row's query tile
 // reaches it. Eight runs are read at once, merged with the running reference and sum.
 // Bound by latency: what a row needs is read in two steps, first header and tables, then its partials.
-// kTwo: of two kernels' partials, each with its own plan.
-template <typename T, bool kTwo>
+template <typename T>
 __global__ void __launch_bounds__(256)
 paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Header* header, const float* __restrict__ part,
-                        int part_rows, int max_parts, int grp, int tq, int bq, MergeTwo two, int part_rows2) {
+                        int part_rows, int max_parts, int grp, int tq, int bq) {
   constexpr int kBatch = 8, kKeys = sizeof(T) == 4 ? kKeysF32 : kKeysBf16;
   const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
   pdl_trigger();
   pdl_wait();
-  const Header first = *header;
-  Header h = first, h2 = {};
-  if (kTwo && two.second) h2 = *reinterpret_cast<Header*>(two.second);
+  const Header h = *header;
   const float2* ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
-  [[maybe_unused]] const float* const part1 = part;
-  [[maybe_unused]] const int part_rows1 = part_rows, tq1 = tq, bq1 = bq;
   const unsigned total = (unsigned)p.T * H;                       // rows of 128 elements: below 2^31
-  const bool any = !kTwo || h.parts != 0 || h2.parts != 0;
-  for (unsigned i = blockIdx.x * 8 + warp; any && i < total; i += gridDim.x * 8) {
+  for (unsigned i = blockIdx.x * 8 + warp; i < total; i += gridDim.x * 8) {
     const int t = (int)(i / H), hq = (int)(i - (unsigned)t * H);
     const int s = count_le(p.row_start, p.S + 1, t, (int)lane) - 1;
     SeqRange r;
     if (s < 0 || s >= p.S || !seq_range(p, s, r) || t < r.row0 || t >= r.row0 + r.n) continue;
-    if (kTwo) {
-      const bool few = r.n <= two.few;
-      h = few ? first : h2;
-      part = few ? part1 : reinterpret_cast<const float*>(two.second + kHeaderBytes);
-      part_rows = few ? part_rows1 : part_rows2;
-      tq = few ? tq1 : two.tq;
-      bq = few ? bq1 : two.bq;
-      ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
-      if (h.parts == 0) continue;
-    } else if (h.parts == 0) {
-      break;
-    }
+    if (h.parts == 0) break;
     const SeqPlan f = seq_plan<kKeys>(r, bq, h.run);
     if (f.cuts < 2) continue;
     int before = 0;                                               // partials of the sequences before this one
     for (int s0 = 0; s0 < s; s0 += 32) {
       SeqRange r1;
-      if (s0 + (int)lane < s && seq_range(p, s0 + lane, r1) && (!kTwo || (r1.n <= two.few) == (r.n <= two.few))) {
+      if (s0 + (int)lane < s && seq_range(p, s0 + lane, r1)) {
         const SeqPlan f1 = seq_plan<kKeys>(r1, bq, h.run);
         before += f1.cuts > 1 ? p.G * f1.nb * f1.cuts : 0;
       }
@@ -106,30 +89,23 @@ paged_attn_merge_kernel(Paged p, T* __restrict__ out, int32_t* dev_status, Heade
     }
     const float f1 = l == 0.f ? 0.f : 1.f / l;
     store4(out + (int64_t)i * kHeadDim + lane * 4, make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1));
-    if (kTwo && two.lse && lane == 0)                             // (less what makes room)
-      two.lse[i] = l == 0.f ? -INFINITY : (m + log2f(l) + (float)(32 - __clz(runs - 1))) * 0.69314718f;
   }
-  auto close = [&](Header* header, const Header& h) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     if ((h.taken != (unsigned)h.units || h.first != h.units) && !h.gave_up) raise_status(dev_status, VARRATE_ERR_CORRUPT);
     header->taken = 0;
     header->gave_up = 0;
     header->first = 0;
     header->open = 0;
-  };
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    close(header, first);
-    if (kTwo && two.second) close(reinterpret_cast<Header*>(two.second), h2);
   }
 }
 
-template <typename T, bool kTwo>
+template <typename T>
 int launch(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq, int bq,
-           const MergeTwo& two, int num_sms, cudaStream_t st) {
+           int num_sms, cudaStream_t st) {
   const int64_t warps = (int64_t)p.T * p.G * group;
   const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
-  return launch_pdl(paged_attn_merge_kernel<T, kTwo>, dim3(grid), 256, 0, st, p, (T*)out, dev_status, header, part,
-                    paged_part_rows(p, group, bq), paged_max_parts(num_sms), group, tq, bq, two,
-                    kTwo ? paged_part_rows(p, group, two.bq) : 0)
+  return launch_pdl(paged_attn_merge_kernel<T>, dim3(grid), 256, 0, st, p, (T*)out, dev_status, header, part,
+                    paged_part_rows(p, group, bq), paged_max_parts(num_sms), group, tq, bq)
              ? 1 : -1;
 }
 
@@ -137,14 +113,8 @@ int launch(const Paged& p, int group, void* out, int32_t* dev_status, Header* he
 
 int launch_paged_merge(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
                        int bq, int num_sms, cudaStream_t st) {
-  const MergeTwo none = {};
-  return p.dtype == VARRATE_F32 ? launch<float, false>(p, group, out, dev_status, header, part, tq, bq, none, num_sms, st)
-                                : launch<__nv_bfloat16, false>(p, group, out, dev_status, header, part, tq, bq, none, num_sms, st);
-}
-
-int launch_paged_merge_two(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
-                           int bq, const MergeTwo& two, int num_sms, cudaStream_t st) {
-  return launch<__nv_bfloat16, true>(p, group, out, dev_status, header, part, tq, bq, two, num_sms, st);
+  return p.dtype == VARRATE_F32 ? launch<float>(p, group, out, dev_status, header, part, tq, bq, num_sms, st)
+                                : launch<__nv_bfloat16>(p, group, out, dev_status, header, part, tq, bq, num_sms, st);
 }
 
 }  // namespace vr

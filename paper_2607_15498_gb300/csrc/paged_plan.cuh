@@ -38,17 +38,25 @@ __device__ __forceinline__ int take_unit(Header* h, int ctas, int units) {
 }
 
 struct Unit {
-  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from, seq;
+  int valid, g, row0, ntok, pos0, t0, t1, e0, both, slot, values_from;
   // g: KV head; row0: row of the block's first token; pos0: its position; key tiles t0 .. t1 - 1, of which the first
   // warpgroup's query tile sees those before e0; both: one query tile for both; slot: partial, or -1; values_from: first
-  // tile whose values have to be looked at; seq: its sequence, where a kernel has set it
+  // tile whose values have to be looked at
+};
+struct SeqUnit : Unit {     // where a kernel needs its sequence as well
+  int seq;
 };
 
-// A sequence as a kernel's plan has it; kSome: without new tokens where it is another kernel's.
-template <bool kSome>
-__device__ __forceinline__ bool plan_range(const Paged& p, int s, SeqRange& r) {
+// The sequences whose number of new tokens is in n_min .. n_max, of a batch that two kernels share.
+struct PagedSome : Paged {
+  int n_min, n_max;
+};
+
+// A sequence as a kernel's plan has it: without new tokens where it is another kernel's.
+__device__ __forceinline__ bool plan_range(const Paged& p, int s, SeqRange& r) { return seq_range(p, s, r); }
+__device__ __forceinline__ bool plan_range(const PagedSome& p, int s, SeqRange& r) {
   if (!seq_range(p, s, r)) return false;
-  if (kSome && (r.n < p.n_min || r.n > p.n_max)) r.n = 0;
+  if (r.n < p.n_min || r.n > p.n_max) r.n = 0;
   return true;
 }
 
@@ -80,13 +88,13 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
 // not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the
 // warps share the sequences and add up in plan_add, one warp decides in plan_choose.
-template <int kKeys, bool kSome = false>
-__device__ __forceinline__ float plan_weight(const Paged& p, int bq, int lane, int& longest) {
+template <int kKeys, typename P>
+__device__ __forceinline__ float plan_weight(const P& p, int bq, int lane, int& longest) {
   float w = 0.f;
   int most = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
-    if (!plan_range<kSome>(p, s, r) || r.n == 0) continue;
+    if (!plan_range(p, s, r) || r.n == 0) continue;
     const int last = tiles_of<kKeys>(r.len), first = tiles_of<kKeys>(r.len - r.n + min(bq, r.n));
     w += (float)((unsigned)(r.n + bq - 1) / (unsigned)bq) * (0.5f * (float)(first + last));
     most = max(most, last);
@@ -104,12 +112,12 @@ __device__ __forceinline__ int plan_candidate(float W, int longest, int C, int l
   const float k = ceilf(W * (float)(16 + (lane & 3)) / (16.f * (float)(1 + (lane >> 2)) * (float)C));
   return min(max(1, (int)fminf(k, 1e9f)), longest + 1);
 }
-template <int kKeys, bool kSome = false>
-__device__ __forceinline__ void plan_add(const Paged& p, PlanSums& c, int bq, int cand, int warp, int warps, int lane) {
+template <int kKeys, typename P>
+__device__ __forceinline__ void plan_add(const P& p, PlanSums& c, int bq, int cand, int warp, int warps, int lane) {
   int u = 0, split = 0, chunk = 0;
   for (int s = warp; s < p.S; s += warps) {
     SeqRange r;
-    if (!plan_range<kSome>(p, s, r)) continue;
+    if (!plan_range(p, s, r)) continue;
     const SeqPlan q = seq_plan<kKeys>(r, bq, cand);
     const int n = p.G * q.nb * q.cuts;
     u += n;
@@ -139,16 +147,16 @@ __device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand
 }
 
 // Walks the units in increasing order; one warp. The lanes hold 32 sequences at a time.
-template <int kKeys, bool kSome = false>
+template <int kKeys, typename P = Paged>
 struct Walk {
   int s0 = 0, before = 0, parts_before = 0;     // first sequence held; units and partials before it
   int incl, parts_incl, total, parts;           // scans over the sequences held, and their sums
   SeqPlan q;
 
-  __device__ __forceinline__ void load(const Paged& p, int bq, int run, int lane) {
+  __device__ __forceinline__ void load(const P& p, int bq, int run, int lane) {
     SeqRange r;
     r.n = 0; r.len = 0; r.row0 = 0;
-    if (s0 + lane < p.S && !plan_range<kSome>(p, s0 + lane, r)) r.n = 0;
+    if (s0 + lane < p.S && !plan_range(p, s0 + lane, r)) r.n = 0;
     if (r.n == 0) r.len = 0;
     q = seq_plan<kKeys>(r, bq, run);
     incl = p.G * q.nb * q.cuts;
@@ -161,14 +169,14 @@ struct Walk {
     total = __shfl_sync(0xffffffffu, incl, 31);
     parts = __shfl_sync(0xffffffffu, parts_incl, 31);
   }
-  __device__ __forceinline__ void next(const Paged& p, int bq, int run, int lane) {
+  __device__ __forceinline__ void next(const P& p, int bq, int run, int lane) {
     before += total;
     parts_before += parts;
     s0 += 32;
     load(p, bq, run, lane);
   }
   // unit u (at or after the last one asked for, below the number of units): its sequence and what it is
-  __device__ __forceinline__ int find(const Paged& p, int bq, int tq, int run, int u, int lane, Unit& x) {
+  __device__ __forceinline__ int find(const P& p, int bq, int tq, int run, int u, int lane, Unit& x) {
     while (u >= before + total && s0 < p.S) next(p, bq, run, lane);
     const int l = __ffs(__ballot_sync(0xffffffffu, u < before + incl)) - 1;
     if (l < 0) { x.valid = 0; x.t0 = 0; x.t1 = 0; return 0; }
@@ -209,15 +217,5 @@ inline size_t paged_part_bytes(const Paged& p, int group, int bq, int num_sms) {
 // one or two.
 int launch_paged_merge(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
                        int bq, int num_sms, cudaStream_t st);
-// The same where one kernel took the sequences of at most `few` new tokens and another the rest, each with header and partials of
-// its own: of the second one from `second` on, or null where it was not launched. bf16. lse: [T][H], or null: the logarithm
-// of a row's sum as well.
-struct MergeTwo {
-  unsigned char* second;
-  float* lse;
-  int few, tq, bq;          // tq, bq: of the second
-};
-int launch_paged_merge_two(const Paged& p, int group, void* out, int32_t* dev_status, Header* header, const float* part, int tq,
-                           int bq, const MergeTwo& two, int num_sms, cudaStream_t st);
 
 }  // namespace vr

@@ -27,6 +27,14 @@ While a prompt is prefilled its keys and values stand in the pages of a PagedCac
     check(varrate_paged_attn(pages, seqs, layer, group, q_out, out, status, ws))
     check(varrate_paged_gather(pages, seqs, 0, n_layers, None, n, k, v, status))   # for varrate_encode
 
+or, in 8 bits and cut to a budget of tokens, in those of a Paged8Cache::
+
+    pages, ws = Paged8Cache.allocate(n_layers, n_pages, n_kv_heads, 64), paged8_attn_workspace(pages, seqs, group)
+    check(varrate_paged8_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, gone, q_out, status))
+    check(varrate_paged8_attn(pages, seqs, layer, group, q_out, out, lse, status, ws))
+    check(varrate_paged8_mass(pages, seqs, layer, group, q_out, lse, status))
+    check(varrate_paged8_evict(pages, seqs, 0, n_layers, budget, n_first, n_last, kept, new_len, gone, status))
+
 Shapes: q_win [B][L][w][H][d], k and v [B][L][G][N][d], bases [L][G][d][d] (row j = basis vector
 j), q and out [B][H][d]; every tensor contiguous on the GPU and 16-byte aligned.
 """
@@ -342,9 +350,12 @@ def _on_device(pages, call, *args) -> int:
         return call(*args)
 
 
-def _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out):
-    """(group, q, q_stride, k, k_stride, v, v_stride, freq, q_out) as an append's C call takes them, or None where a tensor is
-    not of the cache's type, shape or device."""
+def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
+                         dev_status, stream=None) -> int:
+    """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
+    ERR_ARG where a tensor is not of the cache's type, shape or device."""
+    if not pages.works_with(seqs, dev_status):
+        return ERR_ARG
     G, T = pages.heads, seqs.n_rows
     k_row, v_row = pages.row_stride(k, T, G), pages.row_stride(v, T, G)
     if q is None:
@@ -353,33 +364,22 @@ def _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out):
         H = q.shape[1] if q.dim() == 3 else 0
         q_row = pages.row_stride(q, T, H)
         if q_row < 0 or H % G or not pages.takes(q_out, (T, H, 128)):
-            return None
+            return ERR_ARG
         q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
     if k_row < 0 or v_row < 0:
-        return None
+        return ERR_ARG
     if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
-        return None
+        return ERR_ARG
     freq_ptr = None
     if rot_dim and freq is not None:
         freq_ptr = freq.data_ptr()
         if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
                 and freq.get_device() == pages.device):
-            return None
-    return H // G, q_ptr, q_row, k.data_ptr(), k_row, v.data_ptr(), v_row, freq_ptr, out_ptr
-
-
-def varrate_paged_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, q_out,
-                         dev_status, stream=None) -> int:
-    """q [T][H][d] or None, k, v [T][G][d]: rows may be apart (parts of one joint projection), heads not.
-    ERR_ARG where a tensor is not of the cache's type, shape or device."""
-    if not pages.works_with(seqs, dev_status):
-        return ERR_ARG
-    a = _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out)
-    if a is None:
-        return ERR_ARG
+            return ERR_ARG
     return _on_device(
-        pages, (_lib or lib()).varrate_paged_append, pages.ref, seqs.ref, layer, *a[:7], _ptr(q_norm), _ptr(k_norm), eps, a[7],
-        rot_dim, a[8], _ptr(dev_status), pages.stream(stream))
+        pages, (_lib or lib()).varrate_paged_append, pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row,
+        v.data_ptr(), v_row, _ptr(q_norm), _ptr(k_norm), eps, freq_ptr, rot_dim, out_ptr, _ptr(dev_status),
+        pages.stream(stream))
 
 
 def varrate_paged_attn_ws_bytes(pages, seqs, group) -> int:
@@ -420,14 +420,32 @@ def _i32(pages, t, shape) -> bool:
 def varrate_paged8_append(pages, seqs, layer, q, k, v, q_norm, k_norm, eps, freq, rot_dim, gone, q_out,
                           dev_status, stream=None) -> int:
     """As varrate_paged_append, on a Paged8Cache and bf16 rows; gone [S] int32 or None."""
-    if not pages.works_with(seqs, dev_status) or not _i32(pages, gone, (seqs.n_seqs,)):
+    if not pages.works_with(seqs, dev_status) or (gone is not None and not _i32(pages, gone, (seqs.n_seqs,))):
         return ERR_ARG
-    a = _append_args(pages, seqs, q, k, v, q_norm, k_norm, freq, rot_dim, q_out)
-    if a is None:
+    G, T = pages.heads, seqs.n_rows
+    k_row, v_row = pages.row_stride(k, T, G), pages.row_stride(v, T, G)
+    if q is None:
+        H, q_row, q_ptr, out_ptr = G, 0, None, None
+    else:
+        H = q.shape[1] if q.dim() == 3 else 0
+        q_row = pages.row_stride(q, T, H)
+        if q_row < 0 or H % G or not pages.takes(q_out, (T, H, 128)):
+            return ERR_ARG
+        q_ptr, out_ptr = q.data_ptr(), q_out.data_ptr()
+    if k_row < 0 or v_row < 0:
         return ERR_ARG
+    if (q_norm is not None and not pages.takes(q_norm, (128,))) or (k_norm is not None and not pages.takes(k_norm, (128,))):
+        return ERR_ARG
+    freq_ptr = None
+    if rot_dim and freq is not None:
+        freq_ptr = freq.data_ptr()
+        if not (freq.dtype is torch.float64 and freq.is_contiguous() and 2 * freq.numel() >= rot_dim
+                and freq.get_device() == pages.device):
+            return ERR_ARG
     return _on_device(
-        pages, (_lib or lib()).varrate_paged8_append, pages.ref, seqs.ref, layer, *a[:7], _ptr(q_norm), _ptr(k_norm), eps, a[7],
-        rot_dim, _ptr(gone), a[8], _ptr(dev_status), pages.stream(stream))
+        pages, (_lib or lib()).varrate_paged8_append, pages.ref, seqs.ref, layer, H // G, q_ptr, q_row, k.data_ptr(), k_row,
+        v.data_ptr(), v_row, _ptr(q_norm), _ptr(k_norm), eps, freq_ptr, rot_dim, _ptr(gone), out_ptr,
+        _ptr(dev_status), pages.stream(stream))
 
 
 def varrate_paged8_attn_ws_bytes(pages, seqs, group) -> int:
