@@ -7,14 +7,16 @@
 // and the older codes of the block times 2^(their byte - byte).
 // A unit is a block of 16 places of one sequence that gets new tokens; a warp takes the 16 tokens of one of its H + 2 G heads:
 // eight lanes a token, sixteen elements each (eight first members of pairs and their partners), four tokens at a time, so
-// that a block's largest element is found by one warp. Sines and cosines of the 16 tokens are made once for the CTA's heads.
+// that a block's largest element is found by one warp. Sines and cosines of the 16 tokens are made once for the CTA's heads: those of every
+// fourth token, and of the three behind it by a product with those of one, two and three positions (in units of 2^-24, off by 9 at most: the
+// angles 1.6 each, their cosines and sines 1 each, times sqrt 2, and the product 1.2).
 // Rows wait in shared memory as they came (cp.async), so that a thread holds no row that it does not work on and four CTAs fit
 // an SM: with rows in registers and two CTAs the prompt below took 43 us.
 //
-// Bound by instructions and memory alike for prompts: 8192 tokens of 32 + 8 + 8 heads 38 us, 185 MB at 4.9 TB/s (0.71 of a
-// copy); 16-byte loads and stores of a row are whole lines, what is left is norm, sines, turn, the largest element and two
-// conversions a pair. 23 chunks of 30 to 900 tokens with norms, older tokens in their first blocks: 34 us, 104 MB at 0.45 of a
-// copy. One token of eight sequences: 5 us, a launch and one chain of loads.
+// Bound by instructions and memory alike for prompts: 8192 tokens of 32 + 8 + 8 heads 36.7 us, 185 MB at 5.0 TB/s (0.74 of a
+// copy); what is left is norm, turn, the largest element and two roundings a pair. 23 chunks of 30 to 900 tokens with norms, older
+// tokens in their first blocks: 33.7 us, 104 MB at 0.45 of a copy. One token of eight sequences: 4.7 us, a launch and one chain of loads.
+// On the way: sines and cosines of every token by themselves 38.7 us on that prompt (made once a CTA they would take it to 35.6).
 #include "common.cuh"
 #include "paged.h"
 #include "paged8.h"
@@ -69,6 +71,12 @@ __device__ __forceinline__ uint2 codes8(const float2 (&x)[4], float f) {
   return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
 
+// Cosine and sine of a position times a frequency in turns, of which the upper 32 bits are kept: 2^-32 of a turn.
+__device__ __forceinline__ void sine(unsigned long long turn, uint32_t pos, float& c, float& s) {
+  const uint32_t at = (uint32_t)(turn >> 32) * pos + __umulhi((uint32_t)turn, pos);
+  sincospif(__int2float_rn((int)at) * 0x1p-31f, &s, &c);
+}
+
 // Units of the sequences before s: more than there are, found without a sum over the sequences (n new tokens lie in at most
 // (n + 14) / 16 + 1 <= n / 16 + 2 blocks).
 __device__ __forceinline__ int first_unit(const int32_t* row_start, int s) { return (__ldg(row_start + s) >> kBlockLog2) + 2 * s; }
@@ -89,6 +97,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
   __shared__ unsigned long long turn[kHeadDim / 2];   // freq / 2 pi modulo 1, times 2^64
   __shared__ __align__(16) float weight[2][kHeadDim];
   __shared__ __align__(16) float angle[kBlock][2][kHeadDim / 2];   // of the item's tokens: cosines, sines
+  __shared__ float step[3][2][kHeadDim / 2];           // of one, two and three positions
   __shared__ uint4 raw[kWarps][kSteps][2][32];                     // a warp's rows as they come, a lane's own
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = lane & 7;
   pdl_trigger();
@@ -105,6 +114,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
   const bool turns = sub < h8;
   const int e0 = 8 * (turns ? sub : sub + h8), e1 = 8 * (turns ? sub + h8 : sub + 8);
 
+  bool stepped = false;                               // `step` is there
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int u = (int)(it / chunks), lo = (int)(it % chunks) * a.per, hi = min(lo + a.per, tasks);
     const int s = seq_of_unit(p, u, lane);
@@ -149,11 +159,26 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
       cp_async_commit();
       if (!made) {                                    // behind the first loads
         __syncthreads();                              // (the last item's have been read)
-        for (int i = tid; i < kBlock * (a.rot / 2); i += kThreads) {
-          const int row = i / (a.rot / 2), j = i % (a.rot / 2);
-          if (row < old || row >= end) continue;
-          const unsigned long long pos = (unsigned long long)base + row + gone;
-          sincospif(__ll2float_rn((long long)(turn[j] * pos)) * 0x1p-63f, &angle[row][1][j], &angle[row][0][j]);
+        const int half = a.rot / 2;
+        const bool single = end - old <= 4;           // each row by itself
+        if (!single && !stepped) {
+          for (int i = tid; i < 3 * half; i += kThreads) sine(turn[i % half], i / half + 1, step[i / half][0][i % half], step[i / half][1][i % half]);
+          stepped = true;
+          __syncthreads();
+        }
+        for (int i = tid; i < (single ? end - old : kBlock / 4) * half; i += kThreads) {
+          const int j = i % half, row = single ? old + i / half : i / half * 4;
+          float c0, s0;
+          sine(turn[j], (uint32_t)base + row + gone, c0, s0);
+          angle[row][0][j] = c0;
+          angle[row][1][j] = s0;
+          if (single) continue;
+#pragma unroll
+          for (int k = 1; k < 4; ++k) {
+            const float c1 = step[k - 1][0][j], s1 = step[k - 1][1][j];
+            angle[row + k][0][j] = fmaf(-s0, s1, c0 * c1);
+            angle[row + k][1][j] = fmaf(c0, s1, s0 * c1);
+          }
         }
         __syncthreads();
         made = true;
@@ -190,7 +215,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) paged8_append_kernel(Paged p,
           load_pairs(angle[row][1] + e0, sn);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 z = fma2(make_float2(-y1[j].x, -y1[j].y), sn[j], mul2(y0[j], c[j]));
+            float2 z = mul2(y0[j], c[j]);               // (a product of pairs has no sign to turn)
+            z = make_float2(fmaf(-y1[j].x, sn[j].x, z.x), fmaf(-y1[j].y, sn[j].y, z.y));
             y1[j] = fma2(y0[j], sn[j], mul2(y1[j], c[j]));
             y0[j] = z;
           }

@@ -99,10 +99,12 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
   const float weight = plan_weight<kKeys>(p, tq, lane, longest);
-  const int cand = plan_candidate(weight, longest, C, lane);
-  plan_add<kKeys>(p, c.plan, tq, cand, warp, kWarps, lane);
-  __syncthreads();
-  plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
+  if (weight > 0.f) {                                               // (the same for the CTA) else every sequence is the other kernel's
+    const int cand = plan_candidate(weight, longest, C, lane);
+    plan_add<kKeys>(p, c.plan, tq, cand, warp, kWarps, lane);
+    __syncthreads();
+    plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
+  }
   if (blockIdx.x == 0) {
     if (tid == 0) {
       if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);   // by a call whose merge did not run, or runs still
@@ -114,7 +116,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
     }
   }
   Walk<kKeys, PagedSome> w;
-  if (warp == 0) w.load(p, tq, run, lane);
+  if (warp == 0 && units > 0) w.load(p, tq, run, lane);
   int next = blockIdx.x;                                            // of warp 0
   uint32_t stage = 0, phase = 0;                                    // of the warp's next step
   bool ok = true;

@@ -57,8 +57,9 @@ constexpr int kExpand = 12, kExpandWarps = 4, kThreads = 32 * (kExpand + kExpand
 // Registers a thread by warpgroup, softmax 0 and 1 and the others: 2 * 184 + 2 * 72 = 4 * 128 of the launch.
 constexpr int kSoftRegs = 184, kOtherRegs = 72;
 constexpr int kRows = 128, kKeys = kKeysBf16;
-constexpr float kOverhead = 2.f;                            // of a unit, in key tiles, as the plan counts it: geometric mean over
-                                                            // 19 cases 42.0 us, at 3 and 4 41.8, at 6 42.1, at 8 42.5
+// As the plan counts them, in key tiles: a unit's start and output; the merge, with a partial's share. Against 2, 0 and 0: 23 chunks of 30 to 900
+// tokens 159 us for 205, a prompt of 512 27.3 for 38.3 (not cut), eleven other batches within 1 %; 3 to 6, 2 to 8 and 0 to 4 are as good.
+constexpr float kOverhead = 4.f, kMerge = 4.f, kPart = 1.f;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // The weights of a row sum to less than kMost, so that neither an accumulator nor the sum of the two warpgroups' overflows,
@@ -139,7 +140,7 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       // ------------------------------------------------------------------ units, and their keys and values
       bool ok = wait_all(&c.planned, 0);
       int run = 1, units = 0, parts = 0;
-      if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts);
+      if (ok) plan_choose(c.plan, weight, cand, C, max_parts, kOverhead, lane, run, units, parts, kMerge, kPart);
       if (blockIdx.x == 0 && lane == 0) {
         if (open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
         header->run = run; header->units = units; header->parts = parts; header->open = 1;

@@ -9,14 +9,16 @@ namespace vr {
 namespace {
 
 // A warp per (row, query head); a lane has four columns. A run of a block counts for a row only where the row's query tile
-// reaches it. Eight runs are read at once, merged with the running reference and sum. Which of the two kernels took a row's
+// reaches it. kBatch runs are read at once, merged with the running reference and sum: eight where every row has a warp of its own at two CTAs an
+// SM (single tokens), else four at four CTAs: a chunk of 383 tokens 44.2 us for 47.4, eight single tokens on 32768 91.1 for 90.6, one on 8000 17.2 for 14.9. Which of the two kernels took a row's
 // sequence, and so which plan and partials are its own, follows from the number of the sequence's new tokens.
 // Bound by latency: what a row needs is read in two steps, first headers and tables, then its partials. 2.5 us of the 10.5 of a
 // step over 900 tokens. Where nothing was cut (a prompt) it ends after the headers.
-__global__ void __launch_bounds__(256)
+template <int kBatch, int kCtas>
+__global__ void __launch_bounds__(256, kCtas)
 paged8_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_status, unsigned char* first, int tq1, int part_rows1,
                     Merge8 two, int part_rows2, int max_parts, int grp) {
-  constexpr int kBatch = 8, kKeys = kKeysBf16;
+  constexpr int kKeys = kKeysBf16;
   const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.G * grp;
   pdl_trigger();
   pdl_wait();
@@ -116,7 +118,7 @@ int launch_paged8_merge(const Paged& p, int group, void* out, int32_t* dev_statu
                         int num_sms, cudaStream_t st) {
   const int64_t warps = (int64_t)p.T * p.G * group;
   const unsigned grid = (unsigned)(warps < (int64_t)num_sms * 32 ? (warps + 7) / 8 : (int64_t)num_sms * 4);
-  return launch_pdl(paged8_merge_kernel, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, (unsigned char*)ws, tq,
+  return launch_pdl(warps <= (int64_t)num_sms * 16 ? paged8_merge_kernel<8, 1> : paged8_merge_kernel<4, 4>, dim3(grid), 256, 0, st, p, (__nv_bfloat16*)out, dev_status, (unsigned char*)ws, tq,
                     paged_part_rows(p, group, tq), two, paged_part_rows(p, group, 2 * two.tq2), paged_max_parts(num_sms), group)
              ? 1 : -1;
 }

@@ -86,7 +86,7 @@ struct PlanSums {           // in shared memory, zero before plan_add
 // The length of a run of key tiles and the number of units. Weight W in tiles, C CTAs. A run of W (1 + i / 16) / (j C),
 // j = 1..8, i = 0..3, or no cut: the shortest of what the last CTA takes, estimated as whole rounds of
 // mean units and as an even share plus half of what the longest unit is above the mean; cuts that the workspace does
-// not hold are left out. `overhead`: of a unit (start, output), in key tiles. Same for every CTA. Lane = candidate; the
+// not hold are left out. `overhead`: of a unit (start, output), in key tiles; `merge`, `part`: what merging takes, with a partial's share. Same for every CTA. Lane = candidate; the
 // warps share the sequences and add up in plan_add, one warp decides in plan_choose.
 template <int kKeys, typename P>
 __device__ __forceinline__ float plan_weight(const P& p, int bq, int lane, int& longest) {
@@ -127,12 +127,13 @@ __device__ __forceinline__ void plan_add(const P& p, PlanSums& c, int bq, int ca
   if (u) { atomicAdd(&c.units[lane], u); atomicAdd(&c.split[lane], split); atomicMax(&c.chunk[lane], chunk); }
 }
 __device__ __forceinline__ void plan_choose(const PlanSums& c, float W, int cand, int C, int max_parts, float overhead, int lane,
-                                            int& run, int& units, int& parts) {
+                                            int& run, int& units, int& parts, float merge = 0.f, float part = 0.f) {
   const int u = c.units[lane];
   float est = INFINITY;
   if (c.split[lane] <= max_parts) {
     const float total = W + overhead * (float)u, mean = total / fmaxf((float)u, 1.f);
     est = fmaxf(ceilf((float)u / C) * mean, total / C + 0.5f * fmaxf(0.f, (float)c.chunk[lane] + overhead - mean));
+    if (merge > 0.f && c.split[lane]) est += merge + part * (float)c.split[lane] / C;
   }
   int best = lane;
 #pragma unroll
