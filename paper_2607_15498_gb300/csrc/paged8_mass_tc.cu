@@ -329,32 +329,31 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
         const int page = __ldg(p.table + (int64_t)x.seq * p.max_pages + (key >> p.page_log2));
         if (page >= 0 && page < p.n_pages) byte[e] = __ldg(scale + scale_at(page_row(p, page, 0, x.g, key & ((1 << p.page_log2) - 1))));
       }
-#pragma unroll
+#pragma unroll 1
       for (int e = 0; e < 2; ++e) {
-        ok = ok && warp_wait(&c.raw[un & 1][e], (un >> 1) & 1) && warp_wait(&c.k_empty[e], (un & 1) ^ 1);
+        ok = ok && warp_wait(&c.raw[un & 1][e], (un >> 1) & 1);
+        if (!ok) break;
+        const unsigned char* row = c.codes[un & 1][e] + key_in * 128;
+        const uint32_t scale2 = (e ? byte[1] : byte[0]) * 0x00800080u, to = tmem + kScores * kTile + 64 * e + ((uint32_t)((warp & 3) * 32) << 16);
+        const bool there = x.key0 + e * kTile + key_in < x.len;
+        uint4 y[4][4];                                            // expanded while the last unit's products run
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint4 w = *reinterpret_cast<const uint4*>(row + ((i ^ (key_in & 7)) << 4));
+          if (!there) w = make_uint4(0, 0, 0, 0);
+          expand16(w, scale2, y[i >> 1][2 * (i & 1)], y[i >> 1][2 * (i & 1) + 1]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&c.raw_empty[un & 1][e]);
+        ok = warp_wait(&c.k_empty[e], (un & 1) ^ 1);
         if (!ok) break;
         tc_fence_after();
-        const unsigned char* row = c.codes[un & 1][e] + key_in * 128;
-        const uint32_t scale2 = byte[e] * 0x00800080u, to = tmem + kScores * kTile + 64 * e + ((uint32_t)((warp & 3) * 32) << 16);
-        const bool there = x.key0 + e * kTile + key_in < x.len;
-#pragma unroll 1
-        for (int h = 0; h < 4; ++h) {                             // 32 elements, 16 columns
-          uint4 y[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint4 w = *reinterpret_cast<const uint4*>(row + (((2 * h + i) ^ (key_in & 7)) << 4));
-            if (!there) w = make_uint4(0, 0, 0, 0);
-            expand16(w, scale2, y[2 * i], y[2 * i + 1]);
-          }
-          tmem_st16(to + 16 * h, reinterpret_cast<const uint32_t(&)[16]>(y));
-        }
+        for (int h = 0; h < 4; ++h) tmem_st16(to + 16 * h, reinterpret_cast<const uint32_t(&)[16]>(y[h]));   // 32 elements
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&c.raw_empty[un & 1][e]);
-          mbar_arrive(&c.k_full[e]);
-        }
+        if (lane == 0) mbar_arrive(&c.k_full[e]);
       }
     }
     if (!ok) c.err = 1;
