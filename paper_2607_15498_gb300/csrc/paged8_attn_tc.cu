@@ -88,10 +88,6 @@ struct Ctl {
 constexpr size_t kSmemBytes = 2 * kTileBytes + kRing * kTileBytes + sizeof(Ctl);
 static_assert(kSmemBytes <= 232448, "shared memory of a block");
 
-
-template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
-template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
-
 __global__ void __launch_bounds__(kThreads, 1)
 paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_q, PagedSome p,
                      const unsigned char* __restrict__ scale, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,

@@ -10,11 +10,13 @@
 //
 // Warps: 0-3, 4-7 sums of a key tile each over the first 64 rows, 8-11, 12-15 over the others; 16 TMA producer; 17, 18 issue the
 // products of a key tile each; 19 fetches log2 e lse; 20-23 expand keys, a thread a key.
-// Bound by the exponentials and the additions beside the products: 512 tokens on 130560, 32 heads over 8: 400 us, 550 GFLOP at 1370 TFLOP/s
-// (0.71 of the measured bf16 rate). 2.15 10^9 exponentials take 230 us of the special function units if nothing waits, the
-// adding and scaling instructions as long again beside them, TMEM is read once.
+// Bound by the exponentials and the additions beside the products: 512 tokens on 130560, 32 heads over 8: 376 us, 550 GFLOP at 1460 TFLOP/s
+// (0.76 of the measured bf16 rate). 2.15 10^9 exponentials take 230 us of the special function units if nothing waits, the
+// adding and scaling instructions nearly as long beside them; a unit's start and end take 1.6 us of its 14.
 // On the way: keys in shared memory 606 us, in TMEM 573; the lse of a query tile fetched one tile ahead instead of when it is needed
-// 418, two ahead and its place found without divisions 396.
+// 418, two ahead and its place found without divisions 396; keys expanded before the last unit is done, both barriers of a tile
+// looked at together and the registers split 376. With the scores' place given back before they are added it is 385 to 426: the two
+// key tiles' warps then take the special function units at the same time.
 //
 // Units are dealt out in turns, back and forth, the first of a sequence (which most rows see) first. Every wait is bounded; one
 // that gives up raises VARRATE_ERR_TIMEOUT and its CTA ends after its copies and products in flight have.
@@ -41,6 +43,8 @@ namespace {
 
 constexpr int kThreads = 768;
 constexpr int kSumWarps = 16, kProducer = 16, kIssuer = 17, kRowsWarp = 19, kExpand = 20;   // issuers: 17 and 18
+// Registers a thread by warpgroup, four of sums, producer to lse, expansion: 4 * 88 + 56 + 72 = 6 * 80 of the launch.
+constexpr int kSumRegs = 88, kOtherRegs = 56, kExpandRegs = 72;
 constexpr int kTile = 128, kPair = 2 * kTile;               // keys of a tile, of a unit
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kCodeBytes = kTile * kHeadDim;
@@ -65,6 +69,14 @@ struct Shared {
 };
 static_assert(sizeof(Shared) <= 232448, "shared memory of a block");
 
+// Both at once: a wait for what is there already takes as long as it takes to look.
+__device__ __forceinline__ bool warp_wait_both(uint64_t* a, uint32_t pa, uint64_t* b, uint32_t pb) {
+  for (uint32_t i = 0; i < kWaitTries; ++i) {
+    const bool x = mbar_try_wait(a, pa), y = mbar_try_wait(b, pb);
+    if (__all_sync(0xffffffffu, x & y)) return true;
+  }
+  return false;
+}
 __device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};\n" ::"r"(taddr), "f"(v) : "memory");
 }
@@ -107,210 +119,8 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   pdl_wait();
   pdl_trigger();                                              // the kernel of few rows goes by it: not before
 
-  if (warp == kProducer) {
-    // ------------------------------------------------------------------ units, keys and queries
-    // Units of the 32 sequences from s0 on: [sequence][pair of tiles][head].
-    int s0 = 0, k = 0;
-    int64_t before = 0, incl = 0, total = 0;
-    SeqRange r;
-    auto scan = [&]() {
-      incl = 0;
-      if (s0 + lane < p.S && seq_range(p, s0 + lane, r) && r.n > few) incl = (int64_t)((r.len + kPair - 1) / kPair) * p.G;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-      }
-      total = __shfl_sync(0xffffffffu, incl, 31);
-    };
-    scan();
-    auto next_unit = [&]() {                                      // the CTA's k-th
-      const int64_t u = (int64_t)k * C + (k & 1 ? C - 1 - (int)blockIdx.x : (int)blockIdx.x);
-      ++k;
-      MassUnit x = {};
-      while (u >= before + total && s0 < p.S) {
-        before += total;
-        s0 += 32;
-        scan();
-      }
-      if (u >= before + total) return x;
-      const int l = __ffs(__ballot_sync(0xffffffffu, u < before + incl)) - 1;
-      x.len = __shfl_sync(0xffffffffu, r.len, l);
-      x.n = __shfl_sync(0xffffffffu, r.n, l);
-      x.row0 = __shfl_sync(0xffffffffu, r.row0, l);
-      const int64_t units = (int64_t)((x.len + kPair - 1) / kPair) * p.G, at = u - (before + __shfl_sync(0xffffffffu, incl, l) - units);
-      const int pair = (int)(at / p.G);
-      x.g = (int)(at - (int64_t)pair * p.G);
-      x.key0 = pair * kPair;
-      x.seq = s0 + l;
-      x.q0 = max(0, x.key0 - (x.len - x.n)) / tq;
-      x.q1 = (int)((unsigned)(x.n + tq - 1) / (unsigned)tq);
-      x.valid = 1;
-      return x;
-    };
-    const int page_keys = min(1 << p.page_log2, kTile), per_tile = kTile / page_keys;
-    uint32_t nu = 0, nq = 0, nk = 0;                              // units published, query tiles and pairs of key tiles asked for
-    bool ok = true;
-    auto publish = [&](const MassUnit& x) {
-      if (!warp_wait(&c.u_empty[nu % kUnits], ((nu / kUnits) & 1) ^ 1)) return false;
-      if (lane == 0) {
-        c.unit[nu % kUnits] = x;
-        mbar_arrive(&c.u_full[nu % kUnits]);
-      }
-      ++nu;
-      return true;
-    };
-    auto keys = [&](const MassUnit& x) {
-      const uint32_t slot = nk & 1, fill = nk >> 1;
-      for (int e = 0; e < 2; ++e)
-        if (!warp_wait(&c.raw_empty[slot][e], (fill & 1) ^ 1)) return false;
-      ++nk;
-      for (int e = 0; e < 2; ++e) {
-        const int base = x.key0 + e * kTile, key = base + lane * page_keys;
-        const int boxes = max(0, min(per_tile, (x.len - base + page_keys - 1) / page_keys));
-        if (lane == 0) mbar_arrive_expect_tx(&c.raw[slot][e], (uint32_t)boxes * page_keys * 128);
-        __syncwarp();
-        if (lane < boxes) {
-          int page = __ldg(p.table + (int64_t)x.seq * p.max_pages + (key >> p.page_log2));
-          if (page < 0 || page >= p.n_pages) {
-            raise_status(dev_status, VARRATE_ERR_CORRUPT);
-            page = 0;
-          }
-          tma_load_2d(smem_addr(c.codes[slot][e]) + lane * page_keys * 128, &tmap, 0,
-                      (int)page_row(p, page, 0, x.g, key & ((1 << p.page_log2) - 1)), &c.raw[slot][e]);
-        }
-      }
-      __syncwarp();
-      return true;
-    };
-    MassUnit x = next_unit();
-    ok = publish(x) && (!x.valid || keys(x));
-    while (ok && x.valid) {
-      MassUnit y = {};
-      for (int t = x.q0; t < x.q1 && ok; ++t) {
-        if (t == min(x.q0 + kQueries, x.q1 - 1)) {                // the next unit's keys, behind the first queries
-          y = next_unit();
-          ok = publish(y) && (!y.valid || keys(y));
-          if (!ok) break;
-        }
-        const uint32_t slot = nq % kQueries;
-        ok = warp_wait(&c.q_empty[slot], ((nq / kQueries) & 1) ^ 1);
-        if (!ok) break;
-        ++nq;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&c.q_full[slot], (uint32_t)(tq * grp) * 256);
-          for (int half = 0; half < 2; ++half)
-            tma_load_3d(smem_addr(c.query[slot]) + half * (kTile * 128), &tmap_q, half * 64, x.g * grp, x.row0 + t * tq, &c.q_full[slot]);
-        }
-        __syncwarp();
-      }
-      x = y;
-    }
-    if (!ok) {                                                    // no copy is in flight when the block ends
-      c.err = 1;
-      for (uint32_t i = nq > kQueries ? nq - kQueries : 0; i < nq; ++i) warp_wait(&c.q_full[i % kQueries], (i / kQueries) & 1);
-      for (uint32_t i = nk > 2 ? nk - 2 : 0; i < nk; ++i)
-        for (int e = 0; e < 2; ++e) warp_wait(&c.raw[i & 1][e], (i >> 1) & 1);
-    }
-  } else if (warp == kIssuer || warp == kIssuer + 1) {
-    // ------------------------------------------------------------------ products of key tile e
-    // (values that are the same in every lane, broadcast from lane 0 where they come from memory, stay in uniform registers)
-    constexpr uint32_t idesc = idesc_bf16_f32(kTile, kTile);
-    const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + kScores * kTile + 64 * e;
-    const uint64_t queries = sdesc_sw128(smem_addr(c.query));
-    uint32_t slot = 0, q_phase = 0, at = e, n = 0;                // of the next query tile; where its scores go; its number
-    bool ok = true;
-    for (uint32_t un = 0; ok; ++un) {
-      ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
-      if (!ok) break;
-      const MassUnit* x = &c.unit[un % kUnits];
-      const int valid = __shfl_sync(0xffffffffu, x->valid, 0), tiles = __shfl_sync(0xffffffffu, x->q1 - x->q0, 0);
-      if (!valid) break;
-      if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
-      ok = warp_wait(&c.k_full[e], un & 1);
-      for (int t = 0; t < tiles && ok; ++t) {
-        ok = warp_wait(&c.q_full[slot], q_phase);
-        // the scores' place: of the two key tiles' products, taken in turn, it was that of the third before this one, of the other tile
-        const uint32_t m = n + e - 2;
-        if (ok && n + e >= 2) ok = warp_wait(&c.s_done[e ^ 1][m & 3], (m >> 2) & 1);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t q = queries + slot * (kTileBytes / 16);
-#pragma unroll
-          for (int ks = 0; ks < kHeadDim / 16; ++ks)
-            tc_mma_bf16_ts(tm + at * kTile, keys + 8 * ks, q + ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) / 16, idesc, ks != 0);
-          tc_commit(&c.s_full[e][n & 3]);
-          tc_commit(&c.q_empty[slot]);
-          if (t == tiles - 1) tc_commit(&c.k_empty[e]);
-        }
-        __syncwarp();
-        if (++slot == kQueries) { slot = 0; q_phase ^= 1; }
-        at = at + 2 >= kScores ? at + 2 - kScores : at + 2;
-        ++n;
-      }
-    }
-    if (!ok) {                                                    // the products in flight end before TMEM is freed
-      c.err = 1;
-      if (elect_one()) tc_commit(&c.drain[e]);
-      warp_wait(&c.drain[e], 0);
-    }
-    __syncwarp();
-  } else if (warp == kRowsWarp) {
-    // ------------------------------------------------------------------ log2 e lse of the rows
-    uint32_t n = 0;
-    bool ok = true;
-    int token[4], off[4];                                         // of this lane's rows of a tile: past every tile's where there is none
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = lane + 32 * i;
-      token[i] = row < tq * grp ? row / grp : INT32_MAX / 2;
-      off[i] = row / grp * H + row % grp;
-    }
-    for (uint32_t un = 0; ok; ++un) {
-      ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
-      if (!ok) break;
-      const MassUnit x = c.unit[un % kUnits];
-      __syncwarp();
-      if (!x.valid) break;
-      if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
-      float z[2][4];                                              // lse of the next two tiles' rows
-      auto fetch = [&](int t, float (&z)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          z[i] = t < x.q1 && token[i] < x.n - t * tq ? __ldg(lse + (int64_t)(x.row0 + t * tq) * H + x.g * grp + off[i]) : 0.f;
-      };
-      fetch(x.q0, z[0]);
-      fetch(x.q0 + 1, z[1]);
-      for (int t0 = x.q0; t0 < x.q1 && ok; t0 += 2) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int t = t0 + h;
-          if (t >= x.q1 || !ok) break;
-          float y[4];
-          bool dead = false;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool there = token[i] < x.n - t * tq, finite = fabsf(z[h][i]) < INFINITY;
-            y[i] = there && finite ? -z[h][i] * kLog2e : -INFINITY;
-            dead |= there && !finite;
-          }
-          dead = __any_sync(0xffffffffu, dead);
-          fetch(t + 2, z[h]);
-          ok = warp_wait(&c.e_empty[n % kLse], ((n / kLse) & 1) ^ 1);
-          if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) c.lse[n % kLse][lane + 32 * i] = y[i];
-          if (lane == 0) c.dead[n % kLse] = dead;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&c.e_full[n % kLse]);
-          ++n;
-        }
-      }
-    }
-    if (!ok) c.err = 1;
-  } else if (warp >= kExpand) {
+  if (warp >= kExpand) {
+    fewer_registers<kExpandRegs>();
     // ------------------------------------------------------------------ codes to bf16: one key per thread
     const int key_in = tid - 32 * kExpand;
     bool ok = true;
@@ -357,7 +167,214 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       }
     }
     if (!ok) c.err = 1;
-  } else if (warp < kSumWarps) {
+  } else if (warp >= kSumWarps) {
+    fewer_registers<kOtherRegs>();
+    if (warp == kProducer) {
+      // ------------------------------------------------------------------ units, keys and queries
+      // Units of the 32 sequences from s0 on: [sequence][pair of tiles][head].
+      int s0 = 0, k = 0;
+      int64_t before = 0, incl = 0, total = 0;
+      SeqRange r;
+      auto scan = [&]() {
+        incl = 0;
+        if (s0 + lane < p.S && seq_range(p, s0 + lane, r) && r.n > few) incl = (int64_t)((r.len + kPair - 1) / kPair) * p.G;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += y;
+        }
+        total = __shfl_sync(0xffffffffu, incl, 31);
+      };
+      scan();
+      auto next_unit = [&]() {                                      // the CTA's k-th
+        const int64_t u = (int64_t)k * C + (k & 1 ? C - 1 - (int)blockIdx.x : (int)blockIdx.x);
+        ++k;
+        MassUnit x = {};
+        while (u >= before + total && s0 < p.S) {
+          before += total;
+          s0 += 32;
+          scan();
+        }
+        if (u >= before + total) return x;
+        const int l = __ffs(__ballot_sync(0xffffffffu, u < before + incl)) - 1;
+        x.len = __shfl_sync(0xffffffffu, r.len, l);
+        x.n = __shfl_sync(0xffffffffu, r.n, l);
+        x.row0 = __shfl_sync(0xffffffffu, r.row0, l);
+        const int64_t units = (int64_t)((x.len + kPair - 1) / kPair) * p.G, at = u - (before + __shfl_sync(0xffffffffu, incl, l) - units);
+        const int pair = (int)(at / p.G);
+        x.g = (int)(at - (int64_t)pair * p.G);
+        x.key0 = pair * kPair;
+        x.seq = s0 + l;
+        x.q0 = max(0, x.key0 - (x.len - x.n)) / tq;
+        x.q1 = (int)((unsigned)(x.n + tq - 1) / (unsigned)tq);
+        x.valid = 1;
+        return x;
+      };
+      const int page_keys = min(1 << p.page_log2, kTile), per_tile = kTile / page_keys;
+      uint32_t nu = 0, nq = 0, nk = 0;                              // units published, query tiles and pairs of key tiles asked for
+      bool ok = true;
+      auto publish = [&](const MassUnit& x) {
+        if (!warp_wait(&c.u_empty[nu % kUnits], ((nu / kUnits) & 1) ^ 1)) return false;
+        if (lane == 0) {
+          c.unit[nu % kUnits] = x;
+          mbar_arrive(&c.u_full[nu % kUnits]);
+        }
+        ++nu;
+        return true;
+      };
+      auto keys = [&](const MassUnit& x) {
+        const uint32_t slot = nk & 1, fill = nk >> 1;
+        for (int e = 0; e < 2; ++e)
+          if (!warp_wait(&c.raw_empty[slot][e], (fill & 1) ^ 1)) return false;
+        ++nk;
+        for (int e = 0; e < 2; ++e) {
+          const int base = x.key0 + e * kTile, key = base + lane * page_keys;
+          const int boxes = max(0, min(per_tile, (x.len - base + page_keys - 1) / page_keys));
+          if (lane == 0) mbar_arrive_expect_tx(&c.raw[slot][e], (uint32_t)boxes * page_keys * 128);
+          __syncwarp();
+          if (lane < boxes) {
+            int page = __ldg(p.table + (int64_t)x.seq * p.max_pages + (key >> p.page_log2));
+            if (page < 0 || page >= p.n_pages) {
+              raise_status(dev_status, VARRATE_ERR_CORRUPT);
+              page = 0;
+            }
+            tma_load_2d(smem_addr(c.codes[slot][e]) + lane * page_keys * 128, &tmap, 0,
+                        (int)page_row(p, page, 0, x.g, key & ((1 << p.page_log2) - 1)), &c.raw[slot][e]);
+          }
+        }
+        __syncwarp();
+        return true;
+      };
+      MassUnit x = next_unit();
+      ok = publish(x) && (!x.valid || keys(x));
+      while (ok && x.valid) {
+        MassUnit y = {};
+        for (int t = x.q0; t < x.q1 && ok; ++t) {
+          if (t == min(x.q0 + kQueries, x.q1 - 1)) {                // the next unit's keys, behind the first queries
+            y = next_unit();
+            ok = publish(y) && (!y.valid || keys(y));
+            if (!ok) break;
+          }
+          const uint32_t slot = nq % kQueries;
+          ok = warp_wait(&c.q_empty[slot], ((nq / kQueries) & 1) ^ 1);
+          if (!ok) break;
+          ++nq;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(&c.q_full[slot], (uint32_t)(tq * grp) * 256);
+            for (int half = 0; half < 2; ++half)
+              tma_load_3d(smem_addr(c.query[slot]) + half * (kTile * 128), &tmap_q, half * 64, x.g * grp, x.row0 + t * tq, &c.q_full[slot]);
+          }
+          __syncwarp();
+        }
+        x = y;
+      }
+      if (!ok) {                                                    // no copy is in flight when the block ends
+        c.err = 1;
+        for (uint32_t i = nq > kQueries ? nq - kQueries : 0; i < nq; ++i) warp_wait(&c.q_full[i % kQueries], (i / kQueries) & 1);
+        for (uint32_t i = nk > 2 ? nk - 2 : 0; i < nk; ++i)
+          for (int e = 0; e < 2; ++e) warp_wait(&c.raw[i & 1][e], (i >> 1) & 1);
+      }
+    } else if (warp == kIssuer || warp == kIssuer + 1) {
+      // ------------------------------------------------------------------ products of key tile e
+      // (values that are the same in every lane, broadcast from lane 0 where they come from memory, stay in uniform registers)
+      constexpr uint32_t idesc = idesc_bf16_f32(kTile, kTile);
+      const int e = __shfl_sync(0xffffffffu, warp - kIssuer, 0);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), keys = tm + kScores * kTile + 64 * e;
+      const uint64_t queries = sdesc_sw128(smem_addr(c.query));
+      uint32_t slot = 0, q_phase = 0, at = e, n = 0;                // of the next query tile; where its scores go; its number
+      bool ok = true;
+      for (uint32_t un = 0; ok; ++un) {
+        ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
+        if (!ok) break;
+        const MassUnit* x = &c.unit[un % kUnits];
+        const int valid = __shfl_sync(0xffffffffu, x->valid, 0), tiles = __shfl_sync(0xffffffffu, x->q1 - x->q0, 0);
+        if (!valid) break;
+        if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
+        ok = warp_wait(&c.k_full[e], un & 1);
+        for (int t = 0; t < tiles && ok; ++t) {
+          ok = warp_wait(&c.q_full[slot], q_phase);
+          // the scores' place: of the two key tiles' products, taken in turn, it was that of the third before this one, of the other tile
+          const uint32_t m = n + e - 2;
+          if (ok && n + e >= 2) ok = warp_wait(&c.s_done[e ^ 1][m & 3], (m >> 2) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t q = queries + slot * (kTileBytes / 16);
+#pragma unroll
+            for (int ks = 0; ks < kHeadDim / 16; ++ks)
+              tc_mma_bf16_ts(tm + at * kTile, keys + 8 * ks, q + ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) / 16, idesc, ks != 0);
+            tc_commit(&c.s_full[e][n & 3]);
+            tc_commit(&c.q_empty[slot]);
+            if (t == tiles - 1) tc_commit(&c.k_empty[e]);
+          }
+          __syncwarp();
+          if (++slot == kQueries) { slot = 0; q_phase ^= 1; }
+          at = at + 2 >= kScores ? at + 2 - kScores : at + 2;
+          ++n;
+        }
+      }
+      if (!ok) {                                                    // the products in flight end before TMEM is freed
+        c.err = 1;
+        if (elect_one()) tc_commit(&c.drain[e]);
+        warp_wait(&c.drain[e], 0);
+      }
+      __syncwarp();
+    } else if (warp == kRowsWarp) {
+      // ------------------------------------------------------------------ log2 e lse of the rows
+      uint32_t n = 0;
+      bool ok = true;
+      int token[4], off[4];                                         // of this lane's rows of a tile: past every tile's where there is none
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = lane + 32 * i;
+        token[i] = row < tq * grp ? row / grp : INT32_MAX / 2;
+        off[i] = row / grp * H + row % grp;
+      }
+      for (uint32_t un = 0; ok; ++un) {
+        ok = warp_wait(&c.u_full[un % kUnits], (un / kUnits) & 1);
+        if (!ok) break;
+        const MassUnit x = c.unit[un % kUnits];
+        __syncwarp();
+        if (!x.valid) break;
+        if (lane == 0) mbar_arrive(&c.u_empty[un % kUnits]);
+        float z[2][4];                                              // lse of the next two tiles' rows
+        auto fetch = [&](int t, float (&z)[4]) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            z[i] = t < x.q1 && token[i] < x.n - t * tq ? __ldg(lse + (int64_t)(x.row0 + t * tq) * H + x.g * grp + off[i]) : 0.f;
+        };
+        fetch(x.q0, z[0]);
+        fetch(x.q0 + 1, z[1]);
+        for (int t0 = x.q0; t0 < x.q1 && ok; t0 += 2) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int t = t0 + h;
+            if (t >= x.q1 || !ok) break;
+            float y[4];
+            bool dead = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const bool there = token[i] < x.n - t * tq, finite = fabsf(z[h][i]) < INFINITY;
+              y[i] = there && finite ? -z[h][i] * kLog2e : -INFINITY;
+              dead |= there && !finite;
+            }
+            dead = __any_sync(0xffffffffu, dead);
+            fetch(t + 2, z[h]);
+            ok = warp_wait(&c.e_empty[n % kLse], ((n / kLse) & 1) ^ 1);
+            if (!ok) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c.lse[n % kLse][lane + 32 * i] = y[i];
+            if (lane == 0) c.dead[n % kLse] = dead;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&c.e_full[n % kLse]);
+            ++n;
+          }
+        }
+      }
+      if (!ok) c.err = 1;
+    }
+  } else {
+    more_registers<kSumRegs>();
     // ------------------------------------------------------------------ sums: one key per thread
     const int e = warp >> 2 & 1, half = warp >> 3, r = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -377,7 +394,7 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       float total = 0.f;
       for (int t = x.q0; t < x.q1; ++t, ++n) {
         const uint32_t at = (2 * n + e) % kScores, slot = n % kLse, ts = tmem + at * kTile + lanes;
-        ok = warp_wait(&c.e_full[slot], (n / kLse) & 1) && warp_wait(&c.s_full[e][n & 3], (n >> 2) & 1);
+        ok = warp_wait_both(&c.e_full[slot], (n / kLse) & 1, &c.s_full[e][n & 3], (n >> 2) & 1);
         if (!ok) break;
         tc_fence_after();
         // some key of the warp is behind some row of the tile, or the tile has rows that add nothing

@@ -6,6 +6,10 @@
 
 namespace vr {
 
+// Registers a thread of a warpgroup from here on. At the head of the branch that the warpgroup takes: elsewhere the compiler spills.
+template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
+
 // 32 columns on their way; they are there after the wait, which waits for all that the thread has asked for.
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[32]) {
   asm volatile(
