@@ -16,8 +16,8 @@
 // Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh). Codes come by TMA into
 // a ring of each warp's own, two steps of keys and values in flight a warp and sixteen warps an SM: 128 KB.
 //
-// Bound by memory for batches: eight sequences of 32768 tokens 90 us with the merge, 538 MB at 5.9 TB/s (0.87 of a copy). By latency for
-// short ones: one sequence of 900 tokens 10.5 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
+// Bound by memory for batches: eight sequences of 32768 tokens 91 us with the merge, 538 MB at 5.9 TB/s (0.87 of a copy). By latency for
+// short ones: one sequence of 900 tokens 10.0 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
 // On the way, that batch: three stages of one CTA an SM 95 us, the next step's codes in registers 133, sixteen warps in one CTA 100.
 // Where other sequences of the batch have many new tokens, the kernel on tcgen05 is launched first and this one beside it
 // (`follows`): its CTAs come to the SMs as those end.

@@ -22,11 +22,11 @@
 // (setmaxnreg stands at the head of the two sides, or the compiler spills as if all had 128). Waits are bounded as in the
 // bf16 kernel.
 //
-// Bound by the widening and the softmax side by side: 8192 tokens, 32 heads over 8, 451 us, 1220 TFLOP/s (0.64 of the
-// measured bf16 rate; the bf16 cache, which has no widening, 337). Of the difference 40 us are the conversions (414 without
+// Bound by the widening and the softmax side by side: 8192 tokens, 32 heads over 8, 445 us, 1240 TFLOP/s (0.64 of the
+// measured bf16 rate; the bf16 cache, which has no widening, 336). Of the difference 40 us are the conversions (414 without
 // them, on zeros), 25 the block of 512 threads, 20 the hop from the copy over the widening to the product, 20 the
-// queries' scales and the block scales. 120 new tokens on 4096 and six others like it: 63 us, latency of the ramp (8 us before the
-// first scores) and of two waves of units.
+// queries' scales and the block scales. A chunk of 383 tokens on 4000: 44 us with the merge, latency of the start (8 us before the
+// first scores), three runs a block and partials of 252 rows.
 // On the way, same prompt: keys to bf16 with their scale, and loops of the widening unrolled in full (the softmax's instructions
 // are then fetched anew every tile), 528 us; registers not split, 1231 (spills).
 #include <float.h>

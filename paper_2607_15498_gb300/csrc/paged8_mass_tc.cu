@@ -10,12 +10,12 @@
 //
 // Warps: 0-3, 4-7 sums of a key tile each over the first 64 rows, 8-11, 12-15 over the others; 16 TMA producer; 17, 18 issue the
 // products of a key tile each; 19 fetches log2 e lse; 20-23 expand keys, a thread a key.
-// Bound by the exponentials and the additions beside the products: 512 tokens on 130560, 32 heads over 8: 376 us, 550 GFLOP at 1460 TFLOP/s
+// Bound by the exponentials and the additions beside the products: 512 tokens on 130560, 32 heads over 8: 379 us, 550 GFLOP at 1450 TFLOP/s
 // (0.76 of the measured bf16 rate). 2.15 10^9 exponentials take 230 us of the special function units if nothing waits, the
 // adding and scaling instructions nearly as long beside them; a unit's start and end take 1.6 us of its 14.
 // On the way: keys in shared memory 606 us, in TMEM 573; the lse of a query tile fetched one tile ahead instead of when it is needed
 // 418, two ahead and its place found without divisions 396; keys expanded before the last unit is done, both barriers of a tile
-// looked at together and the registers split 376. With the scores' place given back before they are added it is 385 to 426: the two
+// looked at together and the registers split 379. With the scores' place given back before they are added it is 385 to 426: the two
 // key tiles' warps then take the special function units at the same time.
 //
 // Units are dealt out in turns, back and forth, the first of a sequence (which most rows see) first. Every wait is bounded; one
