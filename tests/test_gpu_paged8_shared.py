@@ -56,3 +56,60 @@ def test_many_ragged_chunks(n):
     """More units than CTAs, cut or not, and single tokens beside them."""
     lens = [(1 + (i * 7919 + n) % n, (i * 104729) % 700) for i in range(12)] + [(1, 900), (1, 5)]
     run(Batch8(lens, G=4, grp=7, ps=16))
+
+
+def set_new(b, new):
+    """The same sequences with other numbers of new tokens, in place."""
+    b.lens = [(n, k - n) for n, k in zip(new, b.len)]
+    b.start = [0]
+    for n in new:
+        b.start.append(b.start[-1] + n)
+    b.total = b.start[-1]
+    b.row_start.copy_(torch.tensor(b.start, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("rows", [3, 64])
+def test_nothing_new(rows):
+    """Rows that belong to no sequence only."""
+    b = Batch8([(0, 40), (0, 3), (0, 0), (0, 700)], G=2, grp=4, pad=rows)
+    b.mass.copy_(b.mass.nan_to_num(0.5))
+    before = b.mass.clone()
+    q = b.rows(b.H).contiguous()
+    out, lse, ws = torch.full_like(q, 7.0), torch.full((b.T, b.H), 7.0, device="cuda"), b.workspace()
+    for _ in range(2):
+        V.check(V.varrate_paged8_attn(b.pages, b.seqs, 0, b.grp, q, out, lse, b.status, ws))
+        V.check(V.varrate_paged8_mass(b.pages, b.seqs, 0, b.grp, q, lse, b.status))
+    assert b.status.item() == 0 and (out == 7).all() and (lse == 7).all() and torch.equal(before, b.mass)
+
+
+def test_a_captured_step_takes_every_mixture():
+    """One graph for 64 rows: a chunk, single tokens, nothing, both, in any order; rows of no sequence are left alone."""
+    b = Batch8([(1, 99), (1, 299), (1, 63), (1, 4), (0, 0), (1, 699)], G=2, grp=4, ps=32, pad=59)
+    assert b.T == 64
+    q = b.rows(b.H).contiguous()
+    out, lse, ws = torch.empty_like(q), torch.empty((64, b.H), device="cuda"), b.workspace()
+    mass0 = b.mass.nan_to_num(0.5)
+
+    def step():
+        V.check(V.varrate_paged8_attn(b.pages, b.seqs, 0, b.grp, q, out, lse, b.status, ws))
+        V.check(V.varrate_paged8_mass(b.pages, b.seqs, 0, b.grp, q, lse, b.status))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for new in ([0, 64, 0, 0, 0, 0], [1, 1, 1, 1, 0, 1], [0] * 6, [2, 30, 0, 5, 0, 1], [0, 0, 0, 0, 0, 64], [0, 0, 0, 1, 0, 0],
+                [10, 10, 10, 5, 0, 10]):
+        set_new(b, new)
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        b.mass.copy_(mass0)
+        graph.replay()
+        assert b.status.item() == 0, new
+        want, tol, want_lse, tol_lse = attn8_ref(b, q)
+        close(out, want, tol)
+        close(lse, want_lse, tol_lse)
+        assert (out[b.total:] == 7).all() and (lse[b.total:] == 7).all()
+        w, allowed = mass8_ref(b, q, lse, mass0)
+        close(b.mass, w, allowed)
