@@ -784,6 +784,7 @@ int launch_paged8_attn_tc(const Paged8& c, int layer, int group, int n_min, cons
   static std::atomic<int> smem_set[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || smem_set[dev].load(std::memory_order_acquire) == 0) {
+    if (!registers_for(paged8_attn_tc_kernel, kThreads, 128 * (2 * kSoftRegs + 2 * kOtherRegs))) return -1;
     if (cudaFuncSetAttribute(paged8_attn_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes) != cudaSuccess) return -1;
     if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
   }

@@ -9,6 +9,12 @@ namespace vr {
 // Registers a thread of a warpgroup from here on. At the head of the branch that the warpgroup takes: elsewhere the compiler spills.
 template <int kRegs> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
 template <int kRegs> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegs)); }
+// Whether a kernel was compiled to as many registers a thread as its warpgroups share out in sum (a wait for more would not end).
+template <typename F>
+inline bool registers_for(F* kernel, int threads, int shared_out) {
+  cudaFuncAttributes a;
+  return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs * threads >= shared_out;
+}
 
 // 32 columns on their way; they are there after the wait, which waits for all that the thread has asked for.
 __device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[32]) {
