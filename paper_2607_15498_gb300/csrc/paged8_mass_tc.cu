@@ -60,8 +60,9 @@ struct Shared {
   unsigned char query[kQueries][kTileBytes];
   float lse[kLse][kTile];                                   // -log2 e lse of a query tile's rows; -infinity where one adds nothing
   uint64_t raw[2][2], raw_empty[2][2], k_full[2], k_empty[2], q_full[kQueries], q_empty[kQueries], e_full[kLse], e_empty[kLse];
-  uint64_t s_full[2][4], s_done[2][4], half_full[2],          // of a key tile's score tiles, by their number
-  u_full[kUnits], u_empty[kUnits], drain[2];
+  uint64_t s_full[2][4], s_done[2][4];                      // of a key tile's score tiles, by their number
+  uint64_t half_full[2][kUnits];                            // by the unit: the second half's warps may be two ahead of the first's
+  uint64_t u_full[kUnits], u_empty[kUnits], drain[2];
   MassUnit unit[kUnits];
   int dead[kLse];                                           // some row of the tile adds nothing
   int err;
@@ -96,14 +97,17 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   const int tq = kTile / grp, H = p.G * grp, C = gridDim.x;
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&c.k_full[i], 4); mbar_init(&c.k_empty[i], 1); mbar_init(&c.half_full[i], 4);
+      mbar_init(&c.k_full[i], 4); mbar_init(&c.k_empty[i], 1);
       for (int j = 0; j < 2; ++j) { mbar_init(&c.raw[i][j], 1); mbar_init(&c.raw_empty[i][j], 4); }
     }
     for (int i = 0; i < 4; ++i)
       for (int j = 0; j < 2; ++j) { mbar_init(&c.s_full[j][i], 1); mbar_init(&c.s_done[j][i], 8); }
     for (int i = 0; i < kQueries; ++i) { mbar_init(&c.q_full[i], 1); mbar_init(&c.q_empty[i], 2); }
     for (int i = 0; i < kLse; ++i) { mbar_init(&c.e_full[i], 1); mbar_init(&c.e_empty[i], kSumWarps); }
-    for (int i = 0; i < kUnits; ++i) { mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSumWarps + 3 + 4); }
+    for (int i = 0; i < kUnits; ++i) {
+      mbar_init(&c.u_full[i], 1); mbar_init(&c.u_empty[i], kSumWarps + 3 + 4);
+      for (int j = 0; j < 2; ++j) mbar_init(&c.half_full[j][i], 4);
+    }
     for (int i = 0; i < 2; ++i) mbar_init(&c.drain[i], 1);
     c.err = 0;
     fence_mbar_init();
@@ -447,9 +451,9 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&c.half_full[e]);
+            if (lane == 0) mbar_arrive(&c.half_full[e][un % kUnits]);
           } else {
-            ok = warp_wait(&c.half_full[e], un & 1);
+            ok = warp_wait(&c.half_full[e][un % kUnits], (un / kUnits) & 1);
             if (!ok) break;
             tc_fence_after();
             total += tmem_ld1(ts + 64);
