@@ -71,14 +71,13 @@ int launch_paged8_append(const Paged8& c, int layer, int group, const void* q, i
 size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms);
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
                        void* ws, int num_sms, cudaStream_t st);
-// The sequences of n_min new tokens and more, on tcgen05; partials are not merged. Its workspace is of the bf16 cache's size.
-size_t paged_attn_tc_ws_bytes(const Paged& p, int group, int num_sms);
+// The sequences of n_min new tokens and more, on tcgen05: the second header of workspace `ws`, partials to `part`, not merged.
 int launch_paged8_attn_tc(const Paged8& c, int layer, int group, int n_min, const void* q, void* out, float* lse,
-                          int32_t* dev_status, void* ws, int num_sms, cudaStream_t st);
+                          int32_t* dev_status, void* ws, float* part, int num_sms, cudaStream_t st);
 // Merges the partials of both, and writes lse of the rows that were cut: the first kernel took the sequences of at most `few`
-// new tokens, with tq tokens a block; the second the others, from workspace `second` on (null: not launched) with blocks of 2 tq2.
+// new tokens, with tq tokens a block; the second the others, with partials from `second` on (null: not launched) and blocks of 2 tq2.
 struct Merge8 {
-  unsigned char* second;
+  float* second;
   float* lse;               // [T][H], or null
   int few, tq2;
 };

@@ -342,8 +342,10 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
 }  // namespace
 
 size_t paged8_attn_ws_bytes(const Paged8& c, int group, int num_sms) {
+  // The headers, both kernels' partials one after the other. By the rows alone, not by the sequences: a smaller batch never asks for
+  // more, and may have chunks where a larger one of as many sequences as rows has none.
   const size_t mine = paged_part_bytes(c.p, group, kRows / group, num_sms);
-  return c.p.T <= few_tokens(c.p, group) ? mine : mine + paged_attn_tc_ws_bytes(c.p, group, num_sms);
+  return c.p.T <= 2 * (8 / group) ? mine : mine + paged_part_bytes(c.p, group, 2 * (128 / group), num_sms) - kHeaderBytes;
 }
 
 int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, void* out, float* lse, int32_t* dev_status,
@@ -356,8 +358,8 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   Merge8 two = {};
   two.lse = lse; two.few = few; two.tq2 = 128 / group;
   if (p.T > few) {                                                  // else no sequence can have more
-    two.second = w + paged_part_bytes(p, group, tq, num_sms);
-    if (launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, two.second, num_sms, st) < 0) return -1;
+    two.second = reinterpret_cast<float*>(w + paged_part_bytes(p, group, tq, num_sms));
+    if (launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, ws, two.second, num_sms, st) < 0) return -1;
   }
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;

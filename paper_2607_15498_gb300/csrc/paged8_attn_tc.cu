@@ -779,7 +779,7 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
 }  // namespace
 
 int launch_paged8_attn_tc(const Paged8& c, int layer, int group, int n_min, const void* q, void* out, float* lse,
-                          int32_t* dev_status, void* ws, int num_sms, cudaStream_t st) {
+                          int32_t* dev_status, void* ws, float* part, int num_sms, cudaStream_t st) {
   const PagedSome p{c.p, n_min, INT32_MAX};
   static std::atomic<int> smem_set[64];
   int dev = 0;
@@ -792,10 +792,9 @@ int launch_paged8_attn_tc(const Paged8& c, int layer, int group, int n_min, cons
   const int ps = 1 << p.page_log2, tq = kRows / group;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, ps < kKeys ? ps : kKeys)) return -1;
   if (!make_tmap_heads_bf16(&tmap_q, q, (uint32_t)(p.G * group), (uint64_t)p.T, (uint32_t)group, (uint32_t)tq)) return -1;
-  unsigned char* w = static_cast<unsigned char*>(ws);
   return launch_pdl(paged8_attn_tc_kernel, dim3(num_sms), kThreads, kSmemBytes, st, tmap, tmap_q, p,
                     c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2), (__nv_bfloat16*)out, lse, dev_status,
-                    reinterpret_cast<Header*>(w), reinterpret_cast<float*>(w + kHeaderBytes), paged_part_rows(p, group, 2 * tq),
+                    reinterpret_cast<Header*>(static_cast<unsigned char*>(ws) + kSecondHeader), part, paged_part_rows(p, group, 2 * tq),
                     paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim))
              ? 1 : -1;
 }

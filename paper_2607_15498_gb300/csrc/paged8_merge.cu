@@ -25,7 +25,7 @@ paged8_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_statu
   pdl_wait();
   const Header h1 = *reinterpret_cast<Header*>(first);
   Header h2 = {};
-  if (two.second) h2 = *reinterpret_cast<Header*>(two.second);
+  if (two.second) h2 = *reinterpret_cast<Header*>(first + kSecondHeader);
   const unsigned total = (unsigned)p.T * H;                       // rows of 128 elements: below 2^31
   const bool any = h1.parts != 0 || h2.parts != 0;
   for (unsigned i = blockIdx.x * 8 + warp; any && i < total; i += gridDim.x * 8) {
@@ -36,7 +36,7 @@ paged8_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_statu
     const bool few = r.n <= two.few;
     const Header h = few ? h1 : h2;
     if (h.parts == 0) continue;
-    const float* const part = reinterpret_cast<const float*>((few ? first : two.second) + kHeaderBytes);
+    const float* const part = few ? reinterpret_cast<const float*>(first + kHeaderBytes) : two.second;
     const int part_rows = few ? part_rows1 : part_rows2, tq = few ? tq1 : two.tq2, bq = few ? tq1 : 2 * two.tq2;
     const float2* const ml = reinterpret_cast<const float2*>(part + (int64_t)max_parts * part_rows * kHeadDim);
     const SeqPlan f = seq_plan<kKeys>(r, bq, h.run);
@@ -109,7 +109,7 @@ paged8_merge_kernel(Paged p, __nv_bfloat16* __restrict__ out, int32_t* dev_statu
   };
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     close(first, h1);
-    if (two.second) close(two.second, h2);
+    if (two.second) close(first + kSecondHeader, h2);
   }
 }
 

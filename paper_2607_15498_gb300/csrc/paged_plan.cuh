@@ -27,6 +27,9 @@ struct Header {
   int open;                 // a call is between its start and the end of its merge; zero between calls
 };
 constexpr size_t kHeaderBytes = 256;
+// Of a call that is two kernels: the second one's header, before the partials of any call on the same workspace.
+constexpr size_t kSecondHeader = 128;
+static_assert(sizeof(Header) <= kSecondHeader && kSecondHeader + sizeof(Header) <= kHeaderBytes, "two headers before the partials");
 
 // A CTA's next unit, after its first one, which has its own number. At or past `units`: none, also where the counter was not
 // zero before the call and is out of range. A counter found at c with 0 < c <= units - ctas ends at `units` like one found at

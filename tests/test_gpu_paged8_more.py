@@ -2,8 +2,8 @@
 import pytest
 import torch
 
-from paged8_helpers import Batch8, mass8_ref
-from paged_helpers import close
+from paged8_helpers import Batch8, attn8_ref, mass8_ref
+from paged_helpers import Batch, close
 from paper_2607_15498_gb300 import varrate as V
 
 pytestmark = pytest.mark.gpu
@@ -32,3 +32,33 @@ def test_weights_of_many_chunks_of_one_query_tile(lens, grp):
     assert b.status.item() == 0 and torch.equal(first, b.mass)
     want, tol = mass8_ref(b, q, lse, before)
     close(b.mass, want, tol)
+
+
+def test_one_workspace_for_every_group_and_cache():
+    """A workspace that is large enough serves calls of any shape, also of the uncompressed cache, one after another."""
+    kinds = [([(1, 3000)] * 3 + [(40, 700)], 4), ([(150, 3000), (1, 900), (0, 4), (9, 2000)], 3), ([(1, 4000)] * 8, 1),
+             ([(200, 900), (2, 3000)], 5), ([(64, 2000), (1, 700)], 8), ([(20, 1500)] + [(0, 5)] * 30, 6), ([(90, 3000)], 2)]
+    batches = [Batch8(lens, G=2, grp=grp, ps=64, seed=i) for i, (lens, grp) in enumerate(kinds)]
+    plain = [Batch([(1, 3000), (33, 2000)], "bf16", 2, grp, seed=grp) for grp in (4, 3)]
+    q = [b.rows(b.H) for b in batches]
+    want = [attn(b, x) for b, x in zip(batches, q)]
+    for b, x, (out, lse) in zip(batches, q, want):
+        o, tol, y, tol_lse = attn8_ref(b, x)
+        close(out, o, tol)
+        close(lse, y, tol_lse)
+    q_plain = [b.rows(b.H) for b in plain]
+    ws = torch.zeros(max(b.workspace().numel() for b in batches + plain), dtype=torch.uint8, device="cuda")
+    out_plain = [torch.empty_like(x) for x in q_plain]
+    want_plain = []
+    for b, x, o in zip(plain, q_plain, out_plain):
+        V.check(V.varrate_paged_attn(b.pages, b.seqs, 0, b.grp, x, o, b.status, b.workspace()))
+        want_plain.append(o.clone())
+    for order in (range(len(batches)), [3, 0, 1, 4, 0, 3, 6, 2, 5, 1, 0, 4]):
+        for n, i in enumerate(order):
+            out, lse = attn(batches[i], q[i], ws)
+            assert batches[i].status.item() == 0, (i, n)
+            assert torch.equal(out.view(torch.int16), want[i][0].view(torch.int16)) and torch.equal(lse, want[i][1]), (i, n)
+            j = n % len(plain)
+            V.check(V.varrate_paged_attn(plain[j].pages, plain[j].seqs, 0, plain[j].grp, q_plain[j], out_plain[j], plain[j].status, ws))
+            assert plain[j].status.item() == 0 and torch.equal(out_plain[j].view(torch.int16), want_plain[j].view(torch.int16))
+
