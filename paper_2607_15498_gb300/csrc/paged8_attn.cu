@@ -12,7 +12,8 @@
 //   weights  p x 2^(4 + b - u) in fp16, b the scale byte of the step's values and u that of the accumulator, which is
 //            in units of 2^(u - 127): u rises where b is more than 3 above it. A step more than 10 below goes in bf16, where the weight
 //            has the range of fp32 (and values below 2^-100 or so of the largest block's are lost at the end of that range).
-// The reference of a row moves only when a score is 8 (log2) above it.
+// The reference of a row moves only when a score is more than 8 (log2) above it, by their difference: the sum of a large reference and
+// 8 may round up to 16 above it, and the weight would pass what fp16 holds.
 // Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh). Codes come by TMA into
 // a ring of each warp's own, two steps of keys and values in flight a warp and sixteen warps an SM: 128 KB.
 //
@@ -192,7 +193,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
         if (b >= sees0) x2 = -INFINITY;
         if (b >= sees1) x3 = -INFINITY;
       }
-      if (__any_sync(0xffffffffu, fmaxf(x0, x2) > m0 + kSlack || fmaxf(x1, x3) > m1 + kSlack)) {
+      if (__any_sync(0xffffffffu, fmaxf(x0, x2) - m0 > kSlack || fmaxf(x1, x3) - m1 > kSlack)) {
         float a = fmaxf(x0, x2), b = fmaxf(x1, x3);
 #pragma unroll
         for (int i = 4; i < 32; i <<= 1) {
@@ -200,8 +201,8 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
           b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, i));
         }
         float fa = 1.f, fb = 1.f;
-        if (a > m0 + kSlack) { fa = fast_exp2(m0 - a); m0 = a; }
-        if (b > m1 + kSlack) { fb = fast_exp2(m1 - b); m1 = b; }
+        if (a - m0 > kSlack) { fa = fast_exp2(m0 - a); m0 = a; }
+        if (b - m1 > kSlack) { fb = fast_exp2(m1 - b); m1 = b; }
         l0 *= fa;
         l1 *= fb;
 #pragma unroll

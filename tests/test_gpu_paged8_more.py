@@ -62,3 +62,59 @@ def test_one_workspace_for_every_group_and_cache():
             V.check(V.varrate_paged_attn(plain[j].pages, plain[j].seqs, 0, plain[j].grp, q_plain[j], out_plain[j], plain[j].status, ws))
             assert plain[j].status.item() == 0 and torch.equal(out_plain[j].view(torch.int16), want_plain[j].view(torch.int16))
 
+
+def set_codes(b, s, u, c, codes):
+    """Codes of places u of a sequence (keys 0, values 1; the same for every head): numbers that e4m3 holds."""
+    p, i = b.place(s, u)
+    b.codes[0, p, c, :, i] = codes[:, None].to(torch.float8_e4m3fn).view(torch.uint8).expand(-1, b.G, -1)
+
+
+def set_bytes(b, s, u, c, byte):
+    p, i = b.place(s, u)
+    b.scale[0, p, c, :, i // 16] = byte
+
+
+# sequences enough that each of their blocks is one unit, and a warp has one step of 16 keys after the other
+MANY = 40
+
+
+@pytest.mark.parametrize("fraction", [0, 1, 2, 3, 5, 8, 13])
+def test_scores_a_place_apart_at_2_27(fraction):
+    """Scores of 2^27 log2 units and more, where neighbouring numbers of fp32 are 16 apart: each run of 128 keys is a place above
+    the one before, so the last 128 keys have all the weight."""
+    ctx = 1023
+    b = Batch8([(1, ctx)] * MANY, G=16, grp=1, ps=128)
+    u = torch.arange(ctx + 1, device="cuda")
+    k = torch.zeros((ctx + 1, 128), device="cuda")
+    k[:, 0], k[:, 1], k[:, 2] = 448.0, u // 128, fraction
+    for s in range(MANY):
+        set_codes(b, s, u, 0, k)
+        set_bytes(b, s, u, 0, 127)
+    q = torch.zeros((MANY, b.H, 128), device="cuda")
+    # in the kernel's units 448 * 1.5 * 2^14, 1 a step and 2^-3 a `fraction`, times 16.3: all of it exact but for the last product
+    q[..., 0], q[..., 1], q[..., 2] = 1.5 * 2.0 ** 21, 2.0 ** 7, 2.0 ** 4
+    out, lse = attn(b, q.bfloat16())
+    assert b.status.item() == 0
+    top = (448 * 1.5 * 2.0 ** 21 + 7 * 2.0 ** 7 + fraction * 2.0 ** 4) / 128 ** 0.5
+    # sum 1, log2 e / sqrt(d) 1.5, product 1, log2 of the sum 1, product 1 half step of 2^-24; log 128 is below one
+    assert ((lse.double() - top).abs() <= 8 * 2.0 ** -24 * top).all()
+    pool = b.values()
+    for s in range(MANY):
+        v = b.tokens(s, 1, pool=pool)
+        want = v[:, 896:].mean(1)
+        # the keys of the run before are at least 16 - 1 below in exact arithmetic and, two roundings apart, no less than a place in
+        # fp32: 2^-16 of the weight; the average's sums and the output's rounding
+        tol = 2.0 ** -8 * want.abs() + (2.0 ** -15 + 200 * 2.0 ** -24) * v.abs().amax()
+        assert ((out[s].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("size", [8.0, 30.0, 300.0])
+def test_values_for_large_queries(size):
+    """Rows that few tokens decide, for both kernels."""
+    b = Batch8([(1, 200), (9, 50), (1, 3000), (70, 300)], G=2, grp=4)
+    q = (size * b.rows(b.H).double()).bfloat16()
+    out, lse = attn(b, q)
+    want, tol, want_lse, tol_lse = attn8_ref(b, q)
+    assert b.status.item() == 0
+    close(out, want, tol)
+    close(lse, want_lse, tol_lse)
