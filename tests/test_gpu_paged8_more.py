@@ -116,5 +116,7 @@ def test_values_for_large_queries(size):
     out, lse = attn(b, q)
     want, tol, want_lse, tol_lse = attn8_ref(b, q)
     assert b.status.item() == 0
-    close(out, want, tol)
+    # fp32 ends at 2^-126, and the reference of many rows stands up to 2^40 above the largest weight: what is lighter than 2^-86 of it
+    # counts as nothing, less than that of the largest value for each token
+    close(out, want, tol + max(b.len) * 2.0 ** -86 * b.values().nan_to_num(0).abs().amax())
     close(lse, want_lse, tol_lse)
