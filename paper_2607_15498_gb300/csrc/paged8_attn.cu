@@ -9,17 +9,22 @@
 // free as long as both operands agree, so that a lane takes 16 bytes of a key (or of four keys' values) as they stand in the page.
 //   queries  x 2^n with the largest element of a row in [2^14, 2^15): exact in fp16 down to 2^-38 of it;
 //   scores   x (scale of the block) x (2^-n log2 e / sqrt(d)) in fp32;
-//   weights  p x 2^(4 + b - u) in fp16, b the scale byte of the step's values and u that of the accumulator, which is
-//            in units of 2^(u - 127): u rises where b is more than 3 above it. A step more than 10 below goes in bf16, where the weight
-//            has the range of fp32 (and values below 2^-100 or so of the largest block's are lost at the end of that range).
-// The reference of a row moves only when a score is more than 8 (log2) above it, by their difference: the sum of a large reference and
-// 8 may round up to 16 above it, and the weight would pass what fp16 holds.
+//   weights  p x 2^(7 + b - u) in fp16, b the scale byte of the step's values and u that of the accumulator, which is
+//            in units of 2^(u - 127), u the largest b so far.
+// A row's reference is a whole number (log2) that stands where fp16 has its places for the weights of most keys: those between 2^-24
+// and 2^8 of it go in one product a step (2^-17 to 2^15 as stored: half a step of fp16 is 2^-8 of the smallest, no more than bf16's
+// would be). A step with others moves the reference where that takes them in, and gives what is left products of its own, times the
+// power of two that brings the largest to fp16's end, as often as it takes: what a heavy token without a value leaves to the others
+// is not lost. The sums, in fp32, may grow to 2^72 and their range below; what goes is values below 2^-100 or so of the largest block's.
+// How far a score is from the reference is their difference: the sum of a large reference and 8 may round up to 16 above it.
 // Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh). Codes come by TMA into
 // a ring of each warp's own, two steps of keys and values in flight a warp and sixteen warps an SM: 128 KB.
 //
-// Bound by memory for batches: eight sequences of 32768 tokens 91 us with the merge, 538 MB at 5.9 TB/s (0.87 of a copy). By latency for
-// short ones: one sequence of 900 tokens 10.0 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
+// Bound by memory for batches: eight sequences of 32768 tokens 93 us with the merge, 538 MB at 5.8 TB/s (0.85 of a copy), 98 where one key
+// in 200 is four times as long as the others and one step in twelve so takes products in several bands. By latency for
+// short ones: one sequence of 900 tokens 10.6 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
 // On the way, that batch: three stages of one CTA an SM 95 us, the next step's codes in registers 133, sixteen warps in one CTA 100.
+// One product a step from the largest score on, light weights lost, 91.5; those in bf16 products beside it 116; every step in bands 112.
 // Where other sequences of the batch have many new tokens, the kernel on tcgen05 is launched first and this one beside it
 // (`follows`): its CTAs come to the SMs as those end.
 #include <float.h>
@@ -44,8 +49,11 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32, kCtas = 2;
 constexpr int kRows = 8, kKeys = kKeysBf16;
 constexpr float kOverhead = 8.f;             // of a unit, in key tiles, as the plan counts it
-constexpr float kSlack = 8.f;                // what scores may rise above the reference before it moves (log2)
-constexpr int kUp = 4;                       // weights are stored times 2^kUp
+constexpr int kUp = 7;                       // weights are stored times 2^kUp
+constexpr float kSlack = 8.f, kLow = 17.f + kUp;   // what scores may be above and below the reference for one product a step (log2)
+constexpr float kMost = 0x1p15f, kLeast = 0x1p-17f;   // the same of a weight as it is stored
+constexpr float kFar = 72.f;                 // how far weights and sums of a row may grow (log2)
+constexpr int kBands = 10;                   // bands of 2^31 that hold all weights of fp32
 
 constexpr int kStages = 2, kStepBytes = 16 * kHeadDim * 2;           // a warp's steps in flight: keys, then values
 struct Shared {
@@ -74,6 +82,43 @@ __device__ __forceinline__ bool take_nan(uint4& v, uint32_t& bits) {
     bits |= ((n & 1) | (n >> 7 & 2) | (n >> 14 & 4) | (n >> 21 & 8)) << (4 * i);
   }
   return bits != 0;
+}
+
+// A row's reference m after a step whose weights fp16 has not the places for as it stands: the factor for what the row has added up, a
+// power of two. x, y: the lane's two scores of the row, whose others are in the lanes of the same four; l: the lane's sum. low: what
+// scores may be below the reference, less where the block's values are smaller than the accumulator's unit.
+__device__ __forceinline__ float move_reference(float& m, float l, float x, float y, float low) {
+  float a = fmaxf(x, y), b = fminf(x == -INFINITY ? INFINITY : x, y == -INFINITY ? INFINITY : y);   // of the scores that count
+#pragma unroll
+  for (int i = 4; i < 32; i <<= 1) {
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, i));
+    b = fminf(b, __shfl_xor_sync(0xffffffffu, b, i));
+    l = fmaxf(l, __shfl_xor_sync(0xffffffffu, l, i));
+  }
+  if (a == -INFINITY) return 1.f;
+  // the step's scores in the middle of what there is room for where they fit in, else the largest near its end
+  const bool narrow = a - b <= kSlack + kLow - 2.f;
+  const float to = floorf(narrow ? a - 0.5f * (a - b - (kLow - kSlack)) : a - (kSlack - 1.f)), was = m;
+  if (l == 0.f) {                                                   // nothing added up yet
+    m = to;
+    return 1.f;
+  }
+  if (a - m > kFar) m = floorf(a - (kFar - kSlack));                // sums would come near fp32's end
+  else if (a - m > kSlack ? narrow : b - m < low) m = fmaxf(narrow ? to : fminf(to, m), ceilf(m - fmaxf(kFar - __log2f(l), 0.f)));
+  return fast_exp2(was - m);
+}
+
+// At the end of a unit: the sum l of a row to [1, 2), its reference m up by as much where that is exact, as the references of warps and
+// units are compared; the factor for the row's values, which are times 2^kUp.
+__device__ __forceinline__ float settle(float& m, float& l) {
+  if (l == 0.f) m = -INFINITY;                                      // no score: no say in a merge
+  const int e = (int)(__float_as_uint(l) >> 23) - 127;
+  const float up = m + (float)e;
+  if (!(l > 0.f && e <= 126 && up - m == (float)e)) return 1.f / (1 << kUp);
+  const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+  m = up;
+  l *= f;
+  return f * (1.f / (1 << kUp));
 }
 
 __global__ void __launch_bounds__(kThreads, kCtas)
@@ -161,12 +206,13 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
       ahead = ahead + 1 == kStages ? 0 : ahead + 1;
     }
     QueryFrags qf;
-    qf.load(q + ((int64_t)(x.row0 + g8 / grp) * H + x.g * grp + g8 % grp) * kHeadDim, g8 < rows, scale_log2, lane);
-    const int sees0 = x.pos0 + 2 * t4 / grp + 1, sees1 = x.pos0 + (2 * t4 + 1) / grp + 1;   // keys that rows 2 t4, 2 t4 + 1 see
+    const int gr = min(g8, rows - 1);                               // rows past the last one are it again, and not written
+    qf.load(q + ((int64_t)(x.row0 + gr / grp) * H + x.g * grp + gr % grp) * kHeadDim, true, scale_log2, lane);
+    const int sees0 = x.pos0 + min(2 * t4, rows - 1) / grp + 1, sees1 = x.pos0 + min(2 * t4 + 1, rows - 1) / grp + 1;   // keys that rows 2 t4, 2 t4 + 1 see
     float o[8][4];
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float m0 = 0.f, m1 = 0.f, l0 = 0.f, l1 = 0.f;                   // references, sums
     int unit = -1;                                                  // scale byte of the accumulator's unit, none yet
 
     int i = 0;
@@ -193,27 +239,6 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
         if (b >= sees0) x2 = -INFINITY;
         if (b >= sees1) x3 = -INFINITY;
       }
-      if (__any_sync(0xffffffffu, fmaxf(x0, x2) - m0 > kSlack || fmaxf(x1, x3) - m1 > kSlack)) {
-        float a = fmaxf(x0, x2), b = fmaxf(x1, x3);
-#pragma unroll
-        for (int i = 4; i < 32; i <<= 1) {
-          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, i));
-          b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, i));
-        }
-        float fa = 1.f, fb = 1.f;
-        if (a - m0 > kSlack) { fa = fast_exp2(m0 - a); m0 = a; }
-        if (b - m1 > kSlack) { fb = fast_exp2(m1 - b); m1 = b; }
-        l0 *= fa;
-        l1 *= fb;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { o[j][0] *= fa; o[j][2] *= fa; o[j][1] *= fb; o[j][3] *= fb; }
-      }
-      const float r0 = m0 == -INFINITY ? 0.f : m0, r1 = m1 == -INFINITY ? 0.f : m1;
-      x0 = fast_exp2(x0 - r0); x2 = fast_exp2(x2 - r0);
-      x1 = fast_exp2(x1 - r1); x3 = fast_exp2(x3 - r1);
-      l0 += x0 + x2;
-      l1 += x1 + x3;
-
       uint32_t nan[4];
       bool odd = false;
       if (edge) {
@@ -226,7 +251,7 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
         }
         odd = __any_sync(0xffffffffu, odd);
       }
-      if (unit < 0 || bv > unit + 3) {                              // (the same for the warp)
+      if (bv > unit) {                                              // (the same for the warp)
         if (unit >= 0) {
           const float down = exp2f((float)(unit - bv));
 #pragma unroll
@@ -234,24 +259,61 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
         }
         unit = bv;
       }
-      const int d = bv ? bv - unit : 0;
-      if (d >= -10) {
-        const float up = __uint_as_float((uint32_t)(127 + kUp + d) << 23);
-        const uint32_t b0 = movmatrix_trans(pack_f16(x0 * up, x1 * up)), b1 = movmatrix_trans(pack_f16(x2 * up, x3 * up));
+      const float up = __uint_as_float((uint32_t)max(bv ? 127 + kUp + bv - unit : 127 + kUp, 0) << 23);
+      const float low = bv ? __int_as_float(0x4b000000 + unit - bv) - (0x1p23f + kLow) : -kLow;   // (unit - bv >= 0 as a float, in two steps)
+      // scores from the reference, and whether fp16 has its places for all of the step's weights (hidden ones are none)
+      float y0, y1, y2, y3;
+      auto fits = [&]() {
+        y0 = x0 - m0; y1 = x1 - m1; y2 = x2 - m0; y3 = x3 - m1;
+        float least = fminf(fminf(y0, y1), fminf(y2, y3));
+        if (edge) least = fminf(fminf(y0 == -INFINITY ? 0.f : y0, y1 == -INFINITY ? 0.f : y1), fminf(y2 == -INFINITY ? 0.f : y2, y3 == -INFINITY ? 0.f : y3));
+        return !__any_sync(0xffffffffu, fmaxf(fmaxf(y0, y1), fmaxf(y2, y3)) > kSlack || least < low);
+      };
+      bool direct = fits();
+      if (!direct) {
+        const float fa = move_reference(m0, l0, x0, x2, low), fb = move_reference(m1, l1, x1, x3, low);
+        l0 *= fa;
+        l1 *= fb;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
-          const uint32_t a[4] = {f16_codes(lo), f16_codes(lo >> 16), f16_codes(hi), f16_codes(hi >> 16)};
-          mma_f16_16816(o[j], a, b0, b1);
-        }
-      } else {
-        const float up = exp2f((float)(kUp + d));
-        const uint32_t b0 = movmatrix_trans(pack_bf16(x0 * up, x1 * up)), b1 = movmatrix_trans(pack_bf16(x2 * up, x3 * up));
+        for (int j = 0; j < 8; ++j) { o[j][0] *= fa; o[j][2] *= fa; o[j][1] *= fb; o[j][3] *= fb; }
+        direct = fits();
+      }
+      y0 = fast_exp2(y0); y1 = fast_exp2(y1); y2 = fast_exp2(y2); y3 = fast_exp2(y3);
+      l0 += y0 + y2;
+      l1 += y1 + y3;
+      y0 *= up; y1 *= up; y2 *= up; y3 *= up;
+      float z0 = y0, z1 = y1, z2 = y2, z3 = y3;
+      if (!direct) {                                                // the others in bands of their own, below
+        auto inside = [](float y) { return y >= kLeast && y <= kMost ? y : 0.f; };
+        z0 = inside(y0); z1 = inside(y1); z2 = inside(y2); z3 = inside(y3);
+        y0 -= z0; y1 -= z1; y2 -= z2; y3 -= z3;
+      }
+      uint32_t b0 = movmatrix_trans(pack_f16(z0, z1)), b1 = movmatrix_trans(pack_f16(z2, z3));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
-          const uint32_t a[4] = {bf16_codes(lo), bf16_codes(lo >> 16), bf16_codes(hi), bf16_codes(hi >> 16)};
-          mma_bf16_16816(o[j], a, b0, b1);
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
+        const uint32_t a[4] = {f16_codes(lo), f16_codes(lo >> 16), f16_codes(hi), f16_codes(hi >> 16)};
+        mma_f16_16816(o[j], a, b0, b1);
+      }
+      if (!direct) {                                                // the largest weight of each band in [2^14, 2^15)
+#pragma unroll 1
+        for (int band = 0; band < kBands; ++band) {
+          const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fmaxf(fmaxf(y0, y1), fmaxf(y2, y3)), 0.f)));
+          if (most == 0) break;
+          const int e = min(max((int)(most >> 23), 15), 254);
+          const float to = __uint_as_float((uint32_t)(268 - e) << 23), back = __uint_as_float((uint32_t)(e - 14) << 23);
+          auto inside = [&](float& y) { const float z = y * to; if (z >= kLeast) { y = 0.f; return z; } return 0.f; };
+          z0 = inside(y0); z1 = inside(y1); z2 = inside(y2); z3 = inside(y3);
+          b0 = movmatrix_trans(pack_f16(z0, z1)); b1 = movmatrix_trans(pack_f16(z2, z3));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t lo = value_bytes(vq[0], vq[1], j), hi = value_bytes(vq[2], vq[3], j);
+            const uint32_t a[4] = {f16_codes(lo), f16_codes(lo >> 16), f16_codes(hi), f16_codes(hi >> 16)};
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+            mma_f16_16816(d, a, b0, b1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[j][i] = fmaf(d[i], back, o[j][i]);
+          }
         }
       }
       if (odd) {                                                    // rare: NaN of keys that a part of the rows sees
@@ -289,17 +351,17 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
       l0 += __shfl_xor_sync(0xffffffffu, l0, i);
       l1 += __shfl_xor_sync(0xffffffffu, l1, i);
     }
+    const float down0 = settle(m0, l0), down1 = settle(m1, l1);
     if (lane < 4) {
       c.m[warp][2 * lane] = m0; c.m[warp][2 * lane + 1] = m1;
       c.l[warp][2 * lane] = l0; c.l[warp][2 * lane + 1] = l1;
       if (lane == 0) c.u[warp] = max(unit, 0);
     }
     {                                                               // (a step that timed out leaves no part of its unit)
-      const float down = 1.f / (1 << kUp);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        *reinterpret_cast<float2*>(&c.o[warp][2 * t4][16 * g8 + 2 * j]) = make_float2(o[j][0] * down, o[j][2] * down);
-        *reinterpret_cast<float2*>(&c.o[warp][2 * t4 + 1][16 * g8 + 2 * j]) = make_float2(o[j][1] * down, o[j][3] * down);
+        *reinterpret_cast<float2*>(&c.o[warp][2 * t4][16 * g8 + 2 * j]) = make_float2(o[j][0] * down0, o[j][2] * down0);
+        *reinterpret_cast<float2*>(&c.o[warp][2 * t4 + 1][16 * g8 + 2 * j]) = make_float2(o[j][1] * down1, o[j][3] * down1);
       }
     }
     __syncthreads();

@@ -120,3 +120,80 @@ def test_values_for_large_queries(size):
     # counts as nothing, less than that of the largest value for each token
     close(out, want, tol + max(b.len) * 2.0 ** -86 * b.values().nan_to_num(0).abs().amax())
     close(lse, want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("new, ctx, n", [(1, 1200, MANY), (2, 30, 1), (1, 15, 1), (4, 1000, MANY)])
+@pytest.mark.parametrize("lighter, up", [(5, 0), (18, 0), (24, 0), (35, 0), (60, 0), (80, 0), (5, 10), (20, 10), (20, 3), (30, 11), (30, 40)])
+def test_a_heavy_token_without_a_value(new, ctx, n, lighter, up):
+    """As attention sinks have it: the first token has all the weight and a value of zeros, the others 2^-lighter of it; its block's
+    scale is 2^up times theirs. What there is comes from the light ones, each with its weight rounded to 16 bits at worst."""
+    b = Batch8([(new, ctx)] * n, G=8, grp=4, ps=64, spread=0.0)
+    u = torch.arange(new + ctx, device="cuda")
+    for s in range(n):
+        set_bytes(b, s, u, 0, 120)
+        set_bytes(b, s, u, 1, 120)
+        p, i = b.place(s, u)
+        b.codes[0, p, 0, :, i, 0] = 0                   # no other key has an element 0
+        b.codes[0, p[0], 0, :, i[0]] = 0
+        b.codes[0, p[0], 0, :, i[0], 0] = 0x7E          # 448
+        if n > 1:
+            b.codes[0, p[:16], 1, :, i[:16]] = 0        # the first block's values
+            b.scale[0, p[0], 1, :, i[0] // 16] = 120 + up
+        else:                                           # other tokens of the first step have values as well
+            b.codes[0, p[0], 1, :, i[0]] = 0
+    q = 0.5 * b.rows(b.H).float()
+    q[..., 0] = lighter * 0.6931472 * 128 ** 0.5 / (448 * 2.0 ** -7)
+    q = q.bfloat16()
+    out, lse = attn(b, q)
+    assert b.status.item() == 0
+    want, tol, want_lse, tol_lse = attn8_ref(b, q)
+    assert (want.abs() > 2.0 ** -(lighter + 30)).any()
+    close(out, want, tol)
+    close(lse, want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("byte", [1, 2, 3, 4, 9])
+@pytest.mark.parametrize("new", [1, 3])
+def test_values_of_the_smallest_scales_behind_zeros(new, byte):
+    """The first 128 tokens' values are zeros, of scale byte 0; the others' have the smallest scales there are."""
+    b = Batch8([(new, 300)] * MANY, G=8, grp=4, ps=64)
+    u = torch.arange(300 + new, device="cuda")
+    for s in range(MANY):
+        set_bytes(b, s, u, 1, byte)
+        p, i = b.place(s, u[:128])
+        b.codes[0, p, 1, :, i] = 0
+        b.scale[0, p, 1, :, i // 16] = 0
+    q = b.rows(b.H)
+    out, lse = attn(b, q)
+    want, tol, _, _ = attn8_ref(b, q)
+    assert (want.abs() > 2.0 ** -130).any()
+    # half a step of bf16's numbers below 2^-126, and the kernel's sums below it, a rounding a warp
+    close(out, want, tol + 2.0 ** -134 + 20 * 2.0 ** -150)
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "jumps"])
+@pytest.mark.parametrize("size", [20.0, 60.0, 300.0])
+def test_scores_that_drift(order, size):
+    """Scores that rise or fall by `size` log2 units over the context, or jump by as much from key to key."""
+    ctx = 1100
+    b = Batch8([(1, ctx)] * MANY + [(2, ctx)], G=8, grp=4, ps=64)
+    ramp = torch.linspace(-1, 1, ctx + 2, device="cuda")
+    if order == "falling":
+        ramp = -ramp
+    if order == "jumps":
+        ramp = ramp[torch.randperm(ctx + 2, generator=b.gen).cuda()]
+    for s in range(MANY + 1):
+        u = torch.arange(b.len[s], device="cuda")
+        set_bytes(b, s, u, 0, 121)
+        p, i = b.place(s, u)
+        codes = (448 * ramp[:len(u)]).to(torch.float8_e4m3fn).view(torch.uint8)
+        b.codes[0, p, 0, :, i, 0] = codes[:, None].expand(-1, b.G)
+    q = 0.5 * b.rows(b.H).float()
+    q[..., 0] = 0.5 * size * 0.6931472 * 128 ** 0.5 / (448 * 2.0 ** -6)
+    q = q.bfloat16()
+    out, lse = attn(b, q)
+    assert b.status.item() == 0
+    want, tol, want_lse, tol_lse = attn8_ref(b, q)
+    # weights that fp32 does not hold beside the largest count as nothing (as in the test of large queries)
+    close(out, want, tol + max(b.len) * 2.0 ** -86 * b.values().nan_to_num(0).abs().amax())
+    close(lse, want_lse, tol_lse)
