@@ -12,8 +12,9 @@
 //           but for elements below 2^-31 of it, which are off by 2^-39 of it at most; the factor is in the row's scale as well.
 // Scores and outputs are sums of exact products in fp32, and weights are rounded to bf16 as for the bf16 cache.
 //
-// A row whose reference is past 2^24 in size has its scores scaled down so that it is 2^24 (raise): then an ulp of it is 2 of log2
-// units at most, not more than kRoom, and the weights stay below kMost.
+// A row whose largest score is past 2^24 in size has its scores scaled down so that it is 2^24 (raise): then an ulp of it is 2 of log2
+// units at most, not more than kRoom, and the weights stay below kMost. Where a later maximum is smaller in size (the scores before were
+// far below 0) they are taken as they are again; references leave a unit as those of the scores themselves.
 //
 // Values come to be infinite only by a scale byte above 246, which append does not write; a code that is NaN counts as one
 // where it is seen and as nothing elsewhere (warp 11, as in the bf16 kernel).
@@ -475,6 +476,7 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
     uint32_t n_s = 0, n_o = 0, n_both = 0, n_q = 0;               // score tiles, value products, merged units, query tiles so far
     bool ok = true;
     float ref = -INFINITY, l = 0.f;                               // reference, sum
+    float down = 1.f;                                             // what a row's scores are multiplied by, and its reference is of
     bool unset = true;                                            // some row of the warp has no reference yet
     bool begun = false;                                           // the accumulator holds something of this unit
     // Pass nu: the queries of unit nu on their way, the output of unit nu - 1, the tiles of nu. (The code between the tiles
@@ -509,6 +511,7 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
         if (!ok) break;
         tc_fence_after();
         if (l == 0.f) ref = -INFINITY;                              // nothing with a weight: no say in a merge
+        if (down != 1.f) ref = (ref - kRoom) / down + kRoom;        // of the scores as they are, for lse and the merges
         float w0 = 1.f, w1 = 0.f;                                   // weights of the two warpgroups' values
         bool second = false;
         if (x.both) {
@@ -617,6 +620,7 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
       const int t_first = x.t0, tiles = x.t1 - x.t0;
       ref = -INFINITY;
       l = 0.f;
+      down = 1.f;
       unset = true;
       begun = false;
       float row_scale = scale_log2;
@@ -702,12 +706,15 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
             if (mine && up > ref) {
               f = ref == -INFINITY ? 0.f : fast_exp2(ref - up);
               ref = up;
-              // So large that a rounding of the reference is not small beside kRoom: the row's scores are taken at 2^24 from here on.
-              // They are not known to a unit, the largest decides alone, and does so as well where they are smaller.
-              if (fabsf(ref) > 0x1p24f && fabsf(ref) < INFINITY) {
-                const float down = __uint_as_float((uint32_t)(127 + 127 + 23 - (int)(__float_as_uint(fabsf(ref)) >> 23)) << 23);
-                row_scale *= down;
-                ref = fmaf(ref, down, kRoom);
+              // So large that a rounding of the reference is not small beside kRoom: the row's scores are taken at 2^24 from here on,
+              // as long as the maximum is of that size. They are not known to a unit, the largest decides alone, and does so as well
+              // where they are smaller.
+              const float whole = mx / down, size = fabsf(whole);   // (exact: a power of two)
+              const float to = size > 0x1p24f ? __uint_as_float((uint32_t)(127 + 127 + 23 - (int)(__float_as_uint(size) >> 23)) << 23) : 1.f;
+              if (up == mx + kRoom && size < INFINITY && to != down) {
+                row_scale *= to / down;
+                down = to;
+                ref = fmaf(whole, to, kRoom);
               }
             }
             return f;

@@ -197,3 +197,60 @@ def test_scores_that_drift(order, size):
     # weights that fp32 does not hold beside the largest count as nothing (as in the test of large queries)
     close(out, want, tol + max(b.len) * 2.0 ** -86 * b.values().nan_to_num(0).abs().amax())
     close(lse, want_lse, tol_lse)
+
+
+@pytest.mark.parametrize("new, ctx, at", [(20, 300, 200), (40, 300, 200), (40, 9000, 6000), (20, 9000, 6000), (12, 700, 3), (100, 3000, 2900)])
+@pytest.mark.parametrize("first", [True, False])
+def test_scores_past_2_24_of_many_rows(new, ctx, at, first):
+    """One key has a score of 2^30 log2 units, one far from it 2^23.5: the first has all the weight, wherever the two stand, and is lse."""
+    b = Batch8([(new, ctx)], G=1, grp=4, ps=64)
+    u = torch.arange(new + ctx, device="cuda")
+    k = torch.zeros((new + ctx, 128), device="cuda")
+    big, small = (1, at) if first else (at, 1)
+    k[big, 0], k[small, 0] = 448.0, 5.0
+    set_codes(b, 0, u, 0, k)
+    set_bytes(b, 0, u, 0, 127)
+    q = torch.zeros((new, 4, 128), device="cuda")
+    q[..., 0] = 1.02 * 2.0 ** 30 * 0.6931472 * 128 ** 0.5 / 448
+    q = q.bfloat16()
+    out, lse = attn(b, q)
+    assert b.status.item() == 0
+    v = b.tokens(0, 1)[0][big].expand_as(out)
+    assert ((out.double() - v).abs() <= (2 * 2.0 ** -8 + 2.0 ** -16) * v.abs()).all()   # the weight and the output in bf16
+    top = q[..., 0].double() * 448 / 128 ** 0.5
+    # log2 e / sqrt(d) 1.5, product 1, the reference's distance on and off 2, log2 of the sum 1, product 1 half step of 2^-24
+    assert ((lse.double() - top).abs() <= 8 * 2.0 ** -24 * top).all()
+
+
+@pytest.mark.parametrize("new, ctx", [(40, 600), (20, 900), (3, 900)])
+@pytest.mark.parametrize("low", [-2.0 ** 30, -2.0 ** 25])
+def test_scores_far_below_the_others(new, ctx, low):
+    """The first 200 keys' scores are -2^25 or -2^30 log2 units, the others' ordinary: those decide as if they stood alone."""
+    b = Batch8([(new, ctx)], G=1, grp=4, ps=64)
+    u = torch.arange(new + ctx, device="cuda")
+    set_bytes(b, 0, u, 0, 121)
+    p, i = b.place(0, u)
+    b.codes[0, p, 0, :, i, 0] = 0
+    b.codes[0, p[:200], 0, :, i[:200]] = 0
+    b.codes[0, p[:200], 0, :, i[:200], 0] = 0xFE        # -448
+    q = b.rows(4).float()
+    q[..., 0] = -low * 0.6931472 * 128 ** 0.5 / (448 * 2.0 ** -6)
+    q = q.bfloat16()
+    out, lse = attn(b, q)
+    assert b.status.item() == 0
+    # the same without the first keys: what is left has the same keys and values, positions do not matter to it
+    x = q.clone()
+    x[..., 0] = 0
+    pool = b.values()
+    k, v = (b.tokens(0, c, pool=pool)[0][200:] for c in (0, 1))
+    w = torch.einsum("ihd,td->iht", x.double(), k) / 128 ** 0.5
+    size = torch.einsum("ihd,td->iht", x.double().abs(), k.abs()) / 128 ** 0.5
+    seen = torch.arange(200, new + ctx, device="cuda")[None] <= torch.arange(ctx, ctx + new, device="cuda")[:, None]
+    w = w.masked_fill(~seen[:, None], -float("inf"))
+    a, y = torch.softmax(w, -1), torch.logsumexp(w, -1)
+    # as attn8_ref; the elements beside the large one are fp16 times a power of two, off by 2^-39 of it
+    ds = (132 * 2.0 ** -23 * size + 2.0 ** -39 * q[..., :1].abs().double() * k.abs().sum(-1) / 128 ** 0.5).amax(-1, keepdim=True)
+    rel = 2 * ds + 2.0 ** -20 + 2 * (new + ctx + 8) * 2.0 ** -24 + 2.0 ** -8
+    mass, o = torch.einsum("iht,td->ihd", a, v.abs()), torch.einsum("iht,td->ihd", a, v)
+    close(out, o, rel * mass + 2.0 ** -8 * (o.abs() + rel * mass))
+    close(lse, y, ds[..., 0] + 2.0 ** -20 + (new + ctx + 8) * 2.0 ** -24 + 4 * 2.0 ** -24 * (1 + y.abs()))
