@@ -25,8 +25,10 @@
 // short ones: one sequence of 900 tokens 10.6 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
 // On the way, that batch: three stages of one CTA an SM 95 us, the next step's codes in registers 133, sixteen warps in one CTA 100.
 // One product a step from the largest score on, light weights lost, 91.5; those in bf16 products beside it 116; every step in bands 112.
-// Where other sequences of the batch have many new tokens, the kernel on tcgen05 is launched first and this one beside it
-// (`follows`): its CTAs come to the SMs as those end.
+// Where sequences of the batch may have many new tokens, the kernel on tcgen05 is launched behind this one and waits for it as any kernel
+// for the one before: its barriers and TMEM are set up by then. (The other order, this one beginning on the SMs that the other
+// has left, is not one that a kernel may have without a wait of its own; it took 64.2 us for 67.2 on a chunk beside 23 single tokens, 148
+// for 138 on one beside 32.)
 #include <float.h>
 #include <math.h>
 
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const unsigned char* __restrict__ scale,
                    const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                    int32_t* __restrict__ dev_status, Header* header, float* __restrict__ part, int part_rows, int max_parts,
-                   int grp, int follows, float scale_log2) {
+                   int grp, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
@@ -137,11 +139,8 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
   }
   if (tid == 0) c.err = 0;
   __syncthreads();
-  // The kernel before this one takes other sequences, and lets this one start when what comes before both has ended. So this one fills
-  // the SMs that the other has no unit for, or is done with.
-  if (follows) __threadfence();
-  else pdl_wait();
   pdl_trigger();
+  pdl_wait();
   const int open = blockIdx.x == 0 && tid == 0 ? header->open : 0;
   int longest, run = 1, units = 0, parts = 0;
   const float weight = plan_weight<kKeys>(p, tq, lane, longest);
@@ -399,7 +398,6 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
     raise_status(dev_status, VARRATE_ERR_TIMEOUT);
     atomicExch(&header->gave_up, 1u);
   }
-  if (follows) pdl_wait();                                          // so that what waits for this kernel waits for both
 }
 
 }  // namespace
@@ -420,10 +418,7 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   const int tq = kRows / group, few = few_tokens(p, group);
   Merge8 two = {};
   two.lse = lse; two.few = few; two.tq2 = 128 / group;
-  if (p.T > few) {                                                  // else no sequence can have more
-    two.second = reinterpret_cast<float*>(w + paged_part_bytes(p, group, tq, num_sms));
-    if (launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, ws, two.second, num_sms, st) < 0) return -1;
-  }
+  if (p.T > few) two.second = reinterpret_cast<float*>(w + paged_part_bytes(p, group, tq, num_sms));   // else no sequence can have more
   CUtensorMap tmap;
   if (!make_tmap_rows_u8(&tmap, p.pool + (int64_t)layer * p.layer_rows * kHeadDim, (uint64_t)p.layer_rows, 16)) return -1;
   static std::atomic<int> smem_set[64];
@@ -435,8 +430,9 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
   if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, PagedSome{p, 0, few},
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
                   (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
-                  paged_max_parts(num_sms), group, (int)(two.second != nullptr), kLog2e / sqrtf((float)kHeadDim)))
+                  paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim)))
     return -1;
+  if (two.second && launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, ws, two.second, num_sms, st) < 0) return -1;
   return launch_paged8_merge(p, group, out, dev_status, ws, tq, two, num_sms, st) < 0 ? -1 : 2;
 }
 

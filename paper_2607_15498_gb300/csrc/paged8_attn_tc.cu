@@ -121,8 +121,8 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
+  pdl_trigger();
   pdl_wait();
-  pdl_trigger();                        // the kernel of few rows goes by it: not before
   // by a call whose merge did not run, or runs still
   const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;

@@ -42,7 +42,7 @@ __device__ __forceinline__ int64_t steps_of(const Paged& p, int s, int few, SeqR
 __global__ void __launch_bounds__(kThreads, kCtas)
 paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsigned char* __restrict__ scale,
                    float* __restrict__ mass, const __nv_bfloat16* __restrict__ q, const float* __restrict__ lse,
-                   int32_t* __restrict__ dev_status, int grp, int few, int follows, float scale_log2) {
+                   int32_t* __restrict__ dev_status, int grp, int few, float scale_log2) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared& c = *reinterpret_cast<Shared*>(smem);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3, H = p.G * grp, tq = kRows / grp;
@@ -51,9 +51,8 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     fence_mbar_init();
   }
   __syncwarp();
-  if (follows) __threadfence();                                     // (as in the attention of few rows)
-  else pdl_wait();
   pdl_trigger();
+  pdl_wait();
   int64_t total = 0;
   for (int s = lane; s < p.S; s += 32) {
     SeqRange r;
@@ -65,10 +64,7 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
   const int64_t warps = (int64_t)gridDim.x * kWarps, id = (int64_t)blockIdx.x * kWarps + warp;
   int64_t at = total * id / warps;
   const int64_t stop = total * (id + 1) / warps;
-  if (at >= stop) {
-    if (follows) pdl_wait();
-    return;
-  }
+  if (at >= stop) return;
   uint32_t stage = 0, phase = 0;
   bool ok = true;
 
@@ -181,7 +177,6 @@ paged8_mass_kernel(const __grid_constant__ CUtensorMap tmap, Paged p, const unsi
     }
     at += st1 - st0;
   }
-  if (follows) pdl_wait();                                          // so that what waits for this kernel waits for both
 }
 
 }  // namespace
@@ -201,7 +196,7 @@ int launch_paged8_mass(const Paged8& c, int layer, int group, const void* q, con
   }
   if (!launch_pdl(paged8_mass_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, p,
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2), c.mass + (int64_t)layer * (p.layer_rows / 2),
-                  (const __nv_bfloat16*)q, lse, dev_status, group, few_tokens(p, group), (int)many, kLog2e / sqrtf((float)kHeadDim)))
+                  (const __nv_bfloat16*)q, lse, dev_status, group, few_tokens(p, group), kLog2e / sqrtf((float)kHeadDim)))
     return -1;
   return many ? 2 : 1;
 }

@@ -120,8 +120,8 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = c.tmem;
+  pdl_trigger();
   pdl_wait();
-  pdl_trigger();                                              // the kernel of few rows goes by it: not before
 
   if (warp >= kExpand) {
     fewer_registers<kExpandRegs>();

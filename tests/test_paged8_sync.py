@@ -6,6 +6,7 @@ import re
 import pytest
 
 from paper_2607_15498_gb300 import build
+from test_source_order import kernel_body
 
 
 def source(file):
@@ -61,3 +62,18 @@ def test_half_sums_are_told_apart(held):
     index = {f"[un % {declared}]", f"[un & {n - 1}]"} if n > 1 else {""}
     assert uses[0][1] == uses[1][1] and uses[0][1] in index
     assert uses[1][2] in (f"(un / {declared}) & 1", f"(un >> {n.bit_length() - 1}) & 1")
+
+
+@pytest.mark.parametrize("file, kernel", [("paged8_append.cu", "paged8_append_kernel"), ("paged8_attn.cu", "paged8_attn_kernel"),
+                                          ("paged8_attn_tc.cu", "paged8_attn_tc_kernel"), ("paged8_merge.cu", "paged8_merge_kernel"),
+                                          ("paged8_mass.cu", "paged8_mass_kernel"), ("paged8_mass_tc.cu", "paged8_mass_tc_kernel"),
+                                          ("paged8_evict.cu", "paged8_evict_kernel")])
+def test_every_kernel_waits_before_it_reads(file, kernel):
+    """Kernels are launched while the one before still runs: each waits for it whatever its arguments, before anything in memory that
+    another kernel may have written is looked at. That the one before has waited in its turn is not enough."""
+    body = kernel_body(file, kernel)
+    wait = body.index("pdl_wait()")
+    before = body[:wait]
+    assert before.count("{") == before.count("}") and re.search(r"[;}]\s*$", before) and not re.search(r"\belse\s*$", before)
+    assert not re.search(r"__ldg|header->|table\[|seq_range|plan_\w+<|\bkv_len\b|row_start|tma_load|\bscale\[|\bmass\[", before)
+    assert body.count("pdl_wait()") == 1
