@@ -503,6 +503,8 @@ varrate_status varrate_paged8_append(const varrate_pages8* pages, const varrate_
  *   lse   [T][H] fp32, or NULL: log sum_{u <= p} exp(<q, k_u> / sqrt(d)) of every row; -infinity where the scores all are
  *   ws    as for varrate_paged_attn, of varrate_paged8_attn_ws_bytes(pages, seqs, group) bytes: by n_rows, group and the current
  *         device, never less for more rows. One workspace may serve calls of both caches, of any group.
+ * A batch of as many rows as sequences is taken for one of single tokens: a chunk in it is attended to, and weighed, as well, but in a
+ * time that grows with its tokens times the cached ones (n_rows may be larger than the rows that sequences have).
  * Finite values of any size give finite results, as there; parts of a result whose blocks' scales are 2^85 and more below the largest
  * one's may be lost. Scores of a row past 2^24 in size are compared to 2^-23 of it. */
 size_t varrate_paged8_attn_ws_bytes(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t group);

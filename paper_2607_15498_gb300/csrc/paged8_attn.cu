@@ -427,12 +427,13 @@ int launch_paged8_attn(const Paged8& c, int layer, int group, const void* q, voi
     if (cudaFuncSetAttribute(paged8_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)) != cudaSuccess) return -1;
     if (dev >= 0 && dev < 64) smem_set[dev].store(1, std::memory_order_release);
   }
+  auto many = [&]() { return launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, ws, two.second, num_sms, st); };
   if (!launch_pdl(paged8_attn_kernel, dim3(kCtas * num_sms), kThreads, sizeof(Shared), st, tmap, PagedSome{p, 0, few},
                   c.scale + (int64_t)layer * (p.layer_rows >> kBlockLog2),
                   (const __nv_bfloat16*)q, (__nv_bfloat16*)out, lse, dev_status, header, part, paged_part_rows(p, group, tq),
                   paged_max_parts(num_sms), group, kLog2e / sqrtf((float)kHeadDim)))
     return -1;
-  if (two.second && launch_paged8_attn_tc(c, layer, group, few + 1, q, out, lse, dev_status, ws, two.second, num_sms, st) < 0) return -1;
+  if (two.second && many() < 0) return -1;
   return launch_paged8_merge(p, group, out, dev_status, ws, tq, two, num_sms, st) < 0 ? -1 : 2;
 }
 

@@ -123,6 +123,19 @@ paged8_attn_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   const uint32_t tmem = c.tmem;
   pdl_trigger();
   pdl_wait();
+  bool some = false;                                                // a sequence for this kernel, or it ends here
+  for (int s = tid; s < p.S; s += kThreads) {
+    SeqRange r;
+    some |= plan_range(p, s, r) && r.n > 0;
+  }
+  if (!__syncthreads_or(some)) {
+    if (blockIdx.x == 0 && tid == 0) {
+      if (header->open) raise_status(dev_status, VARRATE_ERR_CORRUPT);
+      header->run = 1; header->units = 0; header->parts = 0; header->open = 1;
+    }
+    if (warp == kIssuer) tmem_dealloc(tmem, 512);
+    return;
+  }
   // by a call whose merge did not run, or runs still
   const int open = blockIdx.x == 0 && warp == kProducer && lane == 0 ? header->open : 0;
   int longest;

@@ -122,6 +122,15 @@ paged8_mass_tc_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
   const uint32_t tmem = c.tmem;
   pdl_trigger();
   pdl_wait();
+  bool some = false;                                          // a sequence for this kernel, or it ends here
+  for (int s = tid; s < p.S; s += kThreads) {
+    SeqRange r;
+    some |= seq_range(p, s, r) && r.n > few;
+  }
+  if (!__syncthreads_or(some)) {
+    if (warp == kIssuer) tmem_dealloc(tmem, 512);
+    return;
+  }
 
   if (warp >= kExpand) {
     fewer_registers<kExpandRegs>();

@@ -126,10 +126,16 @@ struct Steps {
   }
 };
 
-// Sequences of at most this many new tokens are taken by mma.sync: one or two blocks of eight rows; more by tcgen05. A batch with no
-// more rows than sequences is one of single tokens, or nearly so: mma.sync takes all of it, and the other kernel, which would look for
-// work for 8 us, is not launched.
-inline int few_tokens(const Paged& p, int group) { return p.T <= p.S ? p.T : 2 * (8 / group); }
+// Sequences of at most this many new tokens are taken by mma.sync: one or two blocks of eight rows; more by tcgen05, whose kernel is
+// launched where a sequence can have more (which ones do is known on the device only) and ends at once where none does. A batch of as many
+// rows as sequences is taken for one of single tokens, all for mma.sync: 64 on 1000 tokens take 38.7 us with that kernel alone, 45.4
+// with the other one launched as well. One with fewer rows than sequences has empty slots, and may have a chunk beside them: 60 tokens on
+// 32768 and 63 empty slots take 297 us by mma.sync and 48 by tcgen05 (weights 268 and 37), 8 tokens 48 and 42, so up to four blocks of
+// rows the one kernel does.
+inline int few_tokens(const Paged& p, int group) {
+  const int block = 8 / group;
+  return p.T == p.S || (p.T < p.S && p.T <= 4 * block) ? p.T : 2 * block;
+}
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
   for (uint32_t i = 0; i < kWaitTries; ++i)

@@ -254,3 +254,43 @@ def test_scores_far_below_the_others(new, ctx, low):
     mass, o = torch.einsum("iht,td->ihd", a, v.abs()), torch.einsum("iht,td->ihd", a, v)
     close(out, o, rel * mass + 2.0 ** -8 * (o.abs() + rel * mass))
     close(lse, y, ds[..., 0] + 2.0 ** -20 + (new + ctx + 8) * 2.0 ** -24 + 4 * 2.0 ** -24 * (1 + y.abs()))
+
+
+@pytest.mark.parametrize("call", ["attn", "mass"])
+def test_a_chunk_among_empty_slots_takes_no_longer(call):
+    """60 new tokens on 32768 of one sequence beside 63 that have nothing new: the time of the chunk alone, or a little more."""
+    times, outs = [], []
+    for slots in (1, 64):
+        b = Batch8([(60, 300)] + [(0, 40)] * (slots - 1), G=8, grp=4, ps=64)
+        n, pages = 32768, 32768 // 64
+        gen = torch.Generator(device="cuda").manual_seed(3)
+        codes = torch.randint(0, 0x60, (1, pages, 2, 8, 64, 128), generator=gen, dtype=torch.uint8, device="cuda")
+        scale = torch.full((1, pages, 2, 8, 4), 122, dtype=torch.uint8, device="cuda")
+        table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(slots, pages).contiguous()
+        length = torch.tensor([n] + [40] * (slots - 1), dtype=torch.int32, device="cuda")
+        cache = V.Paged8Cache.of(codes, scale, torch.zeros((1, pages, 8, 64), device="cuda"))
+        seqs = V.SeqBatch.of(b.row_start, length, table, 60)
+        q = torch.randn((60, 32, 128), generator=gen, device="cuda").bfloat16()
+        out, lse, ws = torch.empty_like(q), torch.empty((60, 32), device="cuda"), V.paged8_attn_workspace(cache, seqs, 4)
+
+        def run():
+            if call == "attn":
+                V.check(V.varrate_paged8_attn(cache, seqs, 0, 4, q, out, lse, b.status, ws))
+            else:
+                V.check(V.varrate_paged8_mass(cache, seqs, 0, 4, q, lse, b.status))
+
+        V.check(V.varrate_paged8_attn(cache, seqs, 0, 4, q, out, lse, b.status, ws))
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        best = float("inf")
+        for _ in range(8):
+            start.record()
+            for _ in range(10):
+                run()
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        assert b.status.item() == 0
+        times.append(best)
+        outs.append((out, lse))
+    assert times[1] < 2 * times[0], times               # (6 to 7 times where every row is one of the kernel of few)
+    assert (outs[0][0].float() - outs[1][0].float()).abs().max() <= 2.0 ** -6 * outs[0][0].abs().max()
