@@ -468,7 +468,7 @@ varrate_status varrate_paged_gather(const varrate_pages* pages, const varrate_se
 typedef struct {
   void* codes;           /* [n_layers][n_pages][2][n_kv_heads][page_size][d] e4m3; 0 is K, 1 is V */
   void* scale;           /* [n_layers][n_pages][2][n_kv_heads][page_size / 16] bytes: b stands for 2^(b - 127), b <= 246;
-                            0 only where every code of the block's tokens is a zero */
+                            0 only where every code of the block's tokens is a zero or NaN */
   float* mass;           /* [n_layers][n_pages][n_kv_heads][page_size], or NULL: no weights are kept */
   int32_t n_layers;
   int32_t n_pages;
@@ -506,7 +506,8 @@ varrate_status varrate_paged8_append(const varrate_pages8* pages, const varrate_
  * A batch of as many rows as sequences is taken for one of single tokens: a chunk in it is attended to, and weighed, as well, but in a
  * time that grows with its tokens times the cached ones (n_rows may be larger than the rows that sequences have).
  * Finite values of any size give finite results, as there; parts of a result whose blocks' scales are 2^85 and more below the largest
- * one's may be lost. Scores of a row past 2^24 in size are compared to 2^-23 of it. */
+ * one's may be lost. Scores of a row whose largest is past 2^24 in size are compared to 2^-23 of it. An element of a query that is below
+ * 2^-31 of its row's largest counts to 2^-39 of that. */
 size_t varrate_paged8_attn_ws_bytes(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t group);
 varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
                                    int32_t group, const void* q, void* out, float* lse, int32_t* dev_status,
@@ -515,7 +516,8 @@ varrate_status varrate_paged8_attn(const varrate_pages8* pages, const varrate_se
 /* Attention weights: for every sequence with new tokens, every KV head g and place u,
  *   mass[u] += sum over the new tokens (rows t) that see u, and the query heads h of g, of exp(<q_th, k_u> / sqrt(d) - lse[t][h]),
  * in fp32, in an order that does not change from call to call. lse as varrate_paged8_attn gives it for these queries; a row
- * whose lse is not finite adds nothing. A page that two sequences share gets the weights of both, in either order.
+ * whose lse is not finite adds nothing. A weight is off by up to 2^-22 |lse| relative to it, as scores and lse are known to
+ * that. A page that two sequences share gets the weights of both, in either order, so that its last places may differ.
  * pages->mass must not be NULL. No workspace. */
 varrate_status varrate_paged8_mass(const varrate_pages8* pages, const varrate_seqs* seqs, int32_t layer,
                                    int32_t group, const void* q, const float* lse, int32_t* dev_status,

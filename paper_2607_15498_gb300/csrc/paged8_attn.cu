@@ -22,7 +22,7 @@
 //
 // Bound by memory for batches: eight sequences of 32768 tokens 93 us with the merge, 538 MB at 5.8 TB/s (0.85 of a copy), 98 where one key
 // in 200 is four times as long as the others and one step in twelve so takes products in several bands. By latency for
-// short ones: one sequence of 900 tokens 10.6 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
+// short ones: one sequence of 900 tokens 10.4 us, of which the plan is 2.5, the first step 2 and the merge 2.5.
 // On the way, that batch: three stages of one CTA an SM 95 us, the next step's codes in registers 133, sixteen warps in one CTA 100.
 // One product a step from the largest score on, light weights lost, 91.5; those in bf16 products beside it 116; every step in bands 112.
 // Where sequences of the batch may have many new tokens, the kernel on tcgen05 is launched behind this one and waits for it as any kernel

@@ -23,10 +23,10 @@
 // (setmaxnreg stands at the head of the two sides, or the compiler spills as if all had 128). Waits are bounded as in the
 // bf16 kernel.
 //
-// Bound by the widening and the softmax side by side: 8192 tokens, 32 heads over 8, 445 us, 1240 TFLOP/s (0.64 of the
-// measured bf16 rate; the bf16 cache, which has no widening, 336). Of the difference 40 us are the conversions (414 without
-// them, on zeros), 25 the block of 512 threads, 20 the hop from the copy over the widening to the product, 20 the
-// queries' scales and the block scales. A chunk of 383 tokens on 4000: 44 us with the merge, latency of the start (8 us before the
+// Bound by the widening and the softmax side by side: 8192 tokens, 32 heads over 8, 441 us, 1250 TFLOP/s (0.65 of the
+// measured bf16 rate; the bf16 cache, which has no widening, 336). Of the difference 40 us are the conversions (one instruction for
+// two codes of a key; five for two of a value, which goes over fp32 to bf16 and meets its scale; without them, on zeros, it is 30 less), 25 the block of 512 threads, 20 the hop from the copy over the widening to the product, 20 the
+// queries' scales and the block scales. A chunk of 383 tokens on 4000: 49.5 us with the kernel before and the merge, latency of the start (8 us before the
 // first scores), three runs a block and partials of 252 rows.
 // On the way, same prompt: keys to bf16 with their scale, and loops of the widening unrolled in full (the softmax's instructions
 // are then fetched anew every tile), 528 us; registers not split, 1231 (spills). Without the
@@ -60,14 +60,13 @@ constexpr int kExpand = 12, kExpandWarps = 4, kThreads = 32 * (kExpand + kExpand
 constexpr int kSoftRegs = 184, kOtherRegs = 72;
 constexpr int kRows = 128, kKeys = kKeysBf16;
 // As the plan counts them, in key tiles: a unit's start and output; the merge, with a partial's share. Against 2, 0 and 0: 23 chunks of 30 to 900
-// tokens 159 us for 205, a prompt of 512 27.3 for 38.3 (not cut), eleven other batches within 1 %; 3 to 6, 2 to 8 and 0 to 4 are as good.
+// tokens 162 us for 196, a prompt of 512 23.1 for 33.5 (not cut), other batches within 1 %; 3 to 6, 2 to 8 and 0 to 4 are as good.
 constexpr float kOverhead = 4.f, kMerge = 4.f, kPart = 1.f;
 constexpr int kTileBytes = kRows * kHeadDim * 2;            // a query, key or value tile
 constexpr int kRing = 5;                                    // key and value tiles in flight, in turn
 // The weights of a row sum to less than kMost, so that neither an accumulator nor the sum of the two warpgroups' overflows,
 // whatever the values. kRoom (log2) is what scores may rise, and their number grow, before the reference moves: 8192 tokens,
-// one key in 200 four times as long as the others, take 411 us at 24, 392 at 28, 377 at 32, 366 at 36, 361 at 40 (357 with no bound on
-// the sum of a row, 2^40 for half a tile's). What it costs is the low end: products with values below 2^-90 or so leave the range
+// one key in 200 four times as long as the others, take 519 us at 24, 492 at 28, 468 at 32, 450 at 36, 441 at 40. What it costs is the low end: products with values below 2^-90 or so leave the range
 // of fp32.
 constexpr float kMost = 0.25f, kRoom = 40.f;
 

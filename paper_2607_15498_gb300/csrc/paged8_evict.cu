@@ -11,7 +11,9 @@
 // Bound by latency: a cluster barrier and the memory's latency a round, few bytes in flight beside what the memory takes. 131072 tokens of 8
 // heads cut to 65536: 100 us (277 MB, 0.41 of a copy); 4 layers of 8 sequences of 9000 to 32000 tokens to 12288: 264 us (0.81); four
 // sequences of 900 to 1500 tokens to 1024: 21 us, of which the passes of the select and one round each are latency alone. A head is a chain of rounds, and there are only as many
-// heads as the cache has: clusters are the largest that keep all SMs in one wave (at 131072 tokens clusters of 16 104 us, of 8 133, of 4 193).
+// heads as the cache has: clusters are the largest, up to 16, with no more than four times as many CTAs as the device holds (at 131072 tokens
+// clusters of 16 104 us, of 8 133, of 4 193; the 256 heads of 4 layers and 8 sequences 265 us with four times as many, in clusters of 4; with
+// one, two and eight times 369, 283 and 303).
 // On the way, at 131072 tokens: histograms of other CTAs read one after another 11000 cycles a pass, now by all lanes at once;
 // cluster barriers with release and acquire of everything 117 us, with only the shared memory's order needed 103; mbarriers in their place
 // 107; larger rounds, choice and move in two kernels, and warps that follow each other's progress by counters were not faster (103, 278

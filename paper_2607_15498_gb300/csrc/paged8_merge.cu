@@ -10,10 +10,10 @@ namespace {
 
 // A warp per (row, query head); a lane has four columns. A run of a block counts for a row only where the row's query tile
 // reaches it. kBatch runs are read at once, merged with the running reference and sum: eight where every row has a warp of its own
-// at two CTAs an SM (single tokens), else four at four CTAs. A chunk of 383 tokens, with its attention, 44.2 us for 47.4 with eight; one
+// at two CTAs an SM (single tokens), else four at four CTAs. A chunk of 383 tokens, with its attention, 49.5 us for 51.4 with eight; one
 // token on 8000 17.2 for 14.9. Which of the two kernels took a row's sequence, and so which plan and partials are its own, follows
 // from the number of the sequence's new tokens.
-// Bound by latency: what a row needs is read in two steps, first headers and tables, then its partials. 2.5 us of the 10 of a
+// Bound by latency: what a row needs is read in two steps, first headers and tables, then its partials. 2.5 us of the 10.4 of a
 // step over 900 tokens. Where nothing was cut (a prompt) it ends after the headers.
 template <int kBatch, int kCtas>
 __global__ void __launch_bounds__(256, kCtas)
