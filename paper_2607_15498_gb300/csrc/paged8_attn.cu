@@ -11,11 +11,12 @@
 //   scores   x (scale of the block) x (2^-n log2 e / sqrt(d)) in fp32;
 //   weights  p x 2^(7 + b - u) in fp16, b the scale byte of the step's values and u that of the accumulator, which is
 //            in units of 2^(u - 127), u the largest b so far.
-// A row's reference is a whole number (log2) that stands where fp16 has its places for the weights of most keys: those between 2^-24
+// A row's reference (log2) stands where fp16 has its places for the weights of most keys: those between 2^-24
 // and 2^8 of it go in one product a step (2^-17 to 2^15 as stored: half a step of fp16 is 2^-8 of the smallest, no more than bf16's
-// would be). A step with others moves the reference where that takes them in, and gives what is left products of its own, times the
-// power of two that brings the largest to fp16's end, as often as it takes: what a heavy token without a value leaves to the others
-// is not lost. The sums, in fp32, may grow to 2^72 and their range below; what goes is values below 2^-100 or so of the largest block's.
+// would be). A step with others moves the reference where that takes them in, and gives what is left products of its own, times what
+// brings the largest to 2^14, as often as it takes: what a heavy token without a value leaves to the others is not lost. The largest weight
+// of such a band, and of the step that sets a reference first, is a power of two as stored, not rounded: where one token has most of the
+// weight the output is its value to fp32 (0.0005 of its size from the plain form's for 0.0011 on the batch below). The sums, in fp32, may grow to 2^72 and their range below; what goes is values below 2^-100 or so of the largest block's.
 // How far a score is from the reference is their difference: the sum of a large reference and 8 may round up to 16 above it.
 // Units of work, partials and their merge are those of the uncompressed cache's attention (paged_plan.cuh). Codes come by TMA into
 // a ring of each warp's own, two steps of keys and values in flight a warp and sixteen warps an SM: 128 KB.
@@ -87,7 +88,7 @@ __device__ __forceinline__ bool take_nan(uint4& v, uint32_t& bits) {
 }
 
 // A row's reference m after a step whose weights fp16 has not the places for as it stands: the factor for what the row has added up, a
-// power of two. x, y: the lane's two scores of the row, whose others are in the lanes of the same four; l: the lane's sum. low: what
+// power of two but for a rounding of m. x, y: the lane's two scores of the row, whose others are in the lanes of the same four; l: the lane's sum. low: what
 // scores may be below the reference, less where the block's values are smaller than the accumulator's unit.
 __device__ __forceinline__ float move_reference(float& m, float l, float x, float y, float low) {
   float a = fmaxf(x, y), b = fminf(x == -INFINITY ? INFINITY : x, y == -INFINITY ? INFINITY : y);   // of the scores that count
@@ -100,23 +101,26 @@ __device__ __forceinline__ float move_reference(float& m, float l, float x, floa
   if (a == -INFINITY) return 1.f;
   // the step's scores in the middle of what there is room for where they fit in, else the largest near its end
   const bool narrow = a - b <= kSlack + kLow - 2.f;
-  const float to = floorf(narrow ? a - 0.5f * (a - b - (kLow - kSlack)) : a - (kSlack - 1.f)), was = m;
-  if (l == 0.f) {                                                   // nothing added up yet
-    m = to;
+  const float below = ceilf(narrow ? 0.5f * (a - b - (kLow - kSlack)) : kSlack - 1.f);   // of the largest: the new reference
+  if (l == 0.f) {                                                   // nothing added up yet: the largest weight is a power of two
+    m = a - below;
     return 1.f;
   }
-  if (a - m > kFar) m = floorf(a - (kFar - kSlack));                // sums would come near fp32's end
-  else if (a - m > kSlack ? narrow : b - m < low) m = fmaxf(narrow ? to : fminf(to, m), ceilf(m - fmaxf(kFar - __log2f(l), 0.f)));
+  float by = 0.f;
+  if (a - m > kFar) by = floorf(a - m - (kFar - kSlack));           // sums would come near fp32's end
+  else if (a - m > kSlack ? narrow : b - m < low) by = fmaxf(narrow ? floorf(a - m - below) : fminf(floorf(a - m - below), 0.f), -floorf(fmaxf(kFar - __log2f(l), 0.f)));
+  const float was = m;
+  m += by;
   return fast_exp2(was - m);
 }
 
-// At the end of a unit: the sum l of a row to [1, 2), its reference m up by as much where that is exact, as the references of warps and
-// units are compared; the factor for the row's values, which are times 2^kUp.
+// At the end of a unit: the sum l of a row to [1, 2), its reference m up by as much, as the references of warps and units are compared,
+// where a rounding of m is not more than one of its scores was (and stays small: scores past 2^12 may be exact and near each other); the factor for the row's values, which are times 2^kUp.
 __device__ __forceinline__ float settle(float& m, float& l) {
   if (l == 0.f) m = -INFINITY;                                      // no score: no say in a merge
   const int e = (int)(__float_as_uint(l) >> 23) - 127;
   const float up = m + (float)e;
-  if (!(l > 0.f && e <= 126 && up - m == (float)e)) return 1.f / (1 << kUp);
+  if (!(l > 0.f && e <= 126 && fabsf(up - m - (float)e) <= 0x1p-12f)) return 1.f / (1 << kUp);
   const float f = __uint_as_float((uint32_t)(127 - e) << 23);
   m = up;
   l *= f;
@@ -294,13 +298,12 @@ paged8_attn_kernel(const __grid_constant__ CUtensorMap tmap, PagedSome p, const 
         const uint32_t a[4] = {f16_codes(lo), f16_codes(lo >> 16), f16_codes(hi), f16_codes(hi >> 16)};
         mma_f16_16816(o[j], a, b0, b1);
       }
-      if (!direct) {                                                // the largest weight of each band in [2^14, 2^15)
+      if (!direct) {                                                // the largest weight of each band at 2^14
 #pragma unroll 1
         for (int band = 0; band < kBands; ++band) {
           const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fmaxf(fmaxf(y0, y1), fmaxf(y2, y3)), 0.f)));
           if (most == 0) break;
-          const int e = min(max((int)(most >> 23), 15), 254);
-          const float to = __uint_as_float((uint32_t)(268 - e) << 23), back = __uint_as_float((uint32_t)(e - 14) << 23);
+          const float top = fmaxf(__uint_as_float(most), 0x1p-112f), to = __fdividef(0x1p14f, top), back = top * 0x1p-14f;
           auto inside = [&](float& y) { const float z = y * to; if (z >= kLeast) { y = 0.f; return z; } return 0.f; };
           z0 = inside(y0); z1 = inside(y1); z2 = inside(y2); z3 = inside(y3);
           b0 = movmatrix_trans(pack_f16(z0, z1)); b1 = movmatrix_trans(pack_f16(z2, z3));
